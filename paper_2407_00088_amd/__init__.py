@@ -6,3 +6,5 @@ this package is its thin Python binding.
 from .binding import *  # noqa: F401,F403
 from .binding import lib, LIB_PATH, EXPORTS, TmacError  # noqa: F401
 from .runner import LinearLUT  # noqa: F401
+from . import attention  # noqa: F401
+from .attention import KVCache, attn_prompt, attn_weights  # noqa: F401

@@ -1,0 +1,807 @@
+// Attention over packed prompts and over shared prefixes and caches (tmac_attn.h): kernels on the core of tmac_attn_core.h,
+// the kernel that joins parts of a row, the kernel of the keys' weights, and their host entry points.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "tmac_attn.h"
+#include "tmac_attn_core.h"
+#include "tmac_attn_host.h"
+#include "tmac_internal.h"
+
+namespace tmac {
+namespace attn {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// --- epilogue ------------------------------------------------------------------------------------------------------------
+
+// Where a row's result goes: the finished row, or a part of it (sums against its own maximum, which ml holds in units of
+// log 2, with the sum of exponentials).
+struct Target {
+  char* out;     // the row's D elements; null: the lane's row does not exist
+  float* lse;    // or null
+  float* part;   // parts: the row's D sums
+  float* ml;     // parts: maximum and sum
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(char* to, f4 x) {
+  *reinterpret_cast<typename T::v4*>(to) = __builtin_convertvector(x, typename T::v4);
+}
+
+// m c, the maximum in units of log 2 (-inf stays).
+__device__ __forceinline__ float log2_units(float m, float c) { return m == -INFINITY ? m : m * c; }
+
+template <typename T, int DP, bool DMA, int RW>
+__device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, float c, char* lds) {
+  constexpr int ND = DP / 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  w.l = add_halves(w.l);
+  if constexpr (RW == 4) {
+    if (!to.out) return;
+    if (parts) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = d * 32 + r * 8 + half * 4;
+          if (at < D) *reinterpret_cast<f4*>(to.part + at) = f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]};
+        }
+      if (half == 0) *reinterpret_cast<f2*>(to.ml) = f2{log2_units(w.m, c), w.l};
+      return;
+    }
+    const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int at = d * 32 + r * 8 + half * 4;
+        if (at < D) store4<T>(to.out + at * 2, f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]} * inv);
+      }
+    if (half == 0 && to.lse) *to.lse = w.l == 0.0f ? -INFINITY : (log2_units(w.m, c) + __builtin_log2f(w.l)) * LN2;
+  } else {
+    // the wavefronts that share rows meet in LDS: [wave][32 rows][DP + 4] sums, then [wave][32] maximum and sum
+    constexpr int KW = 4 / RW, W = DP + 4;
+    float* sums = reinterpret_cast<float*>(lds);
+    f2* ml = reinterpret_cast<f2*>(lds + 4 * 32 * W * 4);
+    __syncthreads();
+    if (half == 0) ml[wave * 32 + lane] = f2{w.m, w.l};
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < KW; ++i) m = fmaxf(m, ml[(i * RW + wave % RW) * 32 + (lane & 31)][0]);
+    const float a = w.m == m ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
+    float* mine = sums + (wave * 32 + (lane & 31)) * W + half * 4;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f4*>(mine + d * 32 + r * 8) =
+            f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]} * a;
+    float l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < KW; ++i) {
+      const f2 x = ml[(i * RW + wave % RW) * 32 + (lane & 31)];
+      l += x[0] == m ? x[1] : x[1] * __builtin_amdgcn_exp2f((x[0] - m) * c);
+    }
+    // every lane keeps its row's scale and target for the lanes that store the row
+    __syncthreads();
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (to.out && half == 0 && wave < RW) {
+      if (parts) *reinterpret_cast<f2*>(to.ml) = f2{log2_units(m, c), l};
+      else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (log2_units(m, c) + __builtin_log2f(l)) * LN2;
+    }
+    // wave % RW's rows, dealt over the KW wavefronts that hold them: 16 lanes a row where D = 64, 32 where it is 128
+    constexpr int LPR = DP / 4, RPW = 64 / LPR, N = 32 / KW / RPW;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = ((wave / RW) * N + i) * RPW + lane / LPR, at = (lane % LPR) * 4;
+      f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < KW; ++j) x += *reinterpret_cast<const f4*>(sums + ((j * RW + wave % RW) * 32 + row) * W + at);
+      char* out = reinterpret_cast<char*>(__shfl((unsigned long long)to.out, row));
+      float* part = reinterpret_cast<float*>(__shfl((unsigned long long)to.part, row));
+      const float iv = __shfl(inv, row);
+      if (out && at < D) {
+        if (parts) *reinterpret_cast<f4*>(part + at) = x;
+        else store4<T>(out + at * 2, x * iv);
+      }
+    }
+  }
+}
+
+// The lane's row as the first product's operand; rows that do not exist and columns from D on are zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void load_q(Rows<T, DP>& w, const char* row, bool exists, int D, int lane) {
+  const int half = lane >> 5;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    u2 x[2] = {{0u, 0u}, {0u, 0u}};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = 16 * t + 8 * half + 4 * j;
+      if (exists && at < D) x[j] = *reinterpret_cast<const u2*>(row + at * 2);
+    }
+    w.q[t] = __builtin_bit_cast(typename T::v8, u4{x[0][0], x[0][1], x[1][0], x[1][1]});
+  }
+}
+
+// --- prompts --------------------------------------------------------------------------------------------------------------
+
+struct PromptArgs {
+  const char *q, *k, *v;
+  char* out;
+  const int32_t *cu_q, *cu_k;
+  float *lse, *part, *ml;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;  // bytes
+  int S, Tq, Tk, Hq, Hkv, G, D, causal, tiles, slices;
+  float scale;
+};
+
+__device__ __forceinline__ int clamp_to(int x, int most) { return x < 0 ? 0 : x > most ? most : x; }
+
+// Sequence and place in it of tile t of all sequences' tiles, those being ceil(n rows / per_tile) each; counted from the last
+// where `descending`.  False: there is no such tile.
+struct Place {
+  int seq, tile, q0, nq;
+};
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int S, int T, int G, int per_tile, int t, bool descending, Place& p) {
+  if (S == 1) {
+    p.seq = 0;
+    p.q0 = clamp_to(cu[0], T);
+    p.nq = max(0, clamp_to(cu[1], T) - p.q0);
+    const int n = (int)(((int64_t)p.nq * G + per_tile - 1) / per_tile);
+    p.tile = descending ? n - 1 - t : t;
+    return t < n;
+  }
+  const int lane = threadIdx.x & 63;
+  auto tiles = [&](int s, int& q0, int& nq) {
+    q0 = nq = 0;
+    if (s < S) {
+      q0 = clamp_to(cu[s], T);
+      nq = max(0, clamp_to(cu[s + 1], T) - q0);
+    }
+    return (int)(((int64_t)nq * G + per_tile - 1) / per_tile);
+  };
+  int q0, nq;
+  if (descending) {
+    int total = 0;
+    for (int s = 0; s < S; s += 64) {
+      int n = tiles(s + lane, q0, nq);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+      total += n;
+    }
+    if (t >= total) return false;
+    t = total - 1 - t;
+  }
+  for (int s = 0; s < S; s += 64) {
+    const int n = tiles(s + lane, q0, nq);
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(incl, o);
+      if (lane >= o) incl += x;
+    }
+    const int total = __shfl(incl, 63);
+    if (t < total) {
+      const int at = __builtin_ctzll(__ballot(t < incl));
+      p.seq = s + at;
+      p.tile = t - __shfl(incl - n, at);
+      p.q0 = __shfl(q0, at);
+      p.nq = __shfl(nq, at);
+      return true;
+    }
+    t -= total;
+  }
+  return false;
+}
+
+// Unit of a grid of `heads` x `units`: a head's units on one XCD, one head after the other, where the heads divide among the
+// eight (workgroups go round the XCDs by their number), so that a head's keys stay in that XCD's L2.
+__device__ __forceinline__ void head_and_unit(int id, int heads, int units, int& head, int& unit) {
+  if (heads % 8 == 0) {
+    const int j = id / 8;
+    head = id % 8 + 8 * (j / units);
+    unit = j % units;
+  } else {
+    head = id % heads;
+    unit = id / heads;
+  }
+}
+
+// One workgroup: 32 RW rows (query, head of the group) of one sequence and key head over the keys they see, or one slice of those.
+template <typename T, int DP, bool DMA, int RW>
+__global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
+  typedef Shape<DP, DMA, RW> Sh;
+  __shared__ __align__(1024) char lds[Sh::LDS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int h, unit;
+  head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
+  const int z = unit % a.slices;
+  Place p;
+  if (!find_tile(a.cu_q, a.S, a.Tq, a.G, 32 * RW, unit / a.slices, true, p)) return;
+  p.seq = __builtin_amdgcn_readfirstlane(p.seq);
+  p.tile = __builtin_amdgcn_readfirstlane(p.tile);
+  p.q0 = __builtin_amdgcn_readfirstlane(p.q0);
+  p.nq = __builtin_amdgcn_readfirstlane(p.nq);
+  const int k0 = clamp_to(a.cu_k[p.seq], a.Tk), nk = max(0, clamp_to(a.cu_k[p.seq + 1], a.Tk) - k0);
+  const int row0 = p.tile * 32 * RW, rows = p.nq * a.G, off = nk - p.nq;
+  const int r = row0 + (wave % RW) * 32 + (lane & 31);
+  const bool exists = r < rows;
+  const int i = exists ? r / a.G : 0, head = h * a.G + (exists ? r - i * a.G : 0);
+  // the keys that any row of the tile sees, and this slice of them
+  const int last = (min(row0 + 32 * RW, rows) - 1) / a.G;
+  const int seen = a.causal ? max(0, min(nk, last + off + 1)) : nk;
+  const int stages = (seen + Sh::SK - 1) / Sh::SK, per = (stages + a.slices - 1) / a.slices;
+  Keys keys;
+  keys.k_stride = a.k_token;
+  keys.v_stride = a.v_token;
+  keys.k = a.k + k0 * a.k_token + h * a.k_head;
+  keys.v = a.v + k0 * a.v_token + h * a.v_head;
+  keys.begin = min(seen, z * per * Sh::SK);
+  keys.end = min(seen, (z + 1) * per * Sh::SK);
+  const int lim = min(keys.end, exists && a.causal ? max(0, i + off + 1) : nk);
+  // rows ascend with the lane, so the wavefront's first row sees least
+  const int first_row = row0 + (wave % RW) * 32, last_row = min(first_row + 31, rows - 1);
+  const int least = first_row >= rows ? keys.end : min(keys.end, a.causal ? max(0, first_row / a.G + off + 1) : nk);
+  const int most = first_row >= rows ? 0 : min(keys.end, a.causal ? max(0, last_row / a.G + off + 1) : nk);
+  Rows<T, DP> w;
+  load_q<T, DP>(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane);
+  const float c = a.scale * LOG2E;
+  run_keys<T, DP, DMA, RW>(w, keys, a.D, c, lim, __builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most), lds, nullptr);
+  Target to = {};
+  if (exists) {
+    const int64_t token = p.q0 + i, slot = ((int64_t)z * a.Tq + token) * a.Hq + head;
+    to.out = a.out + token * a.o_token + head * a.o_head;
+    to.lse = a.lse ? a.lse + (int64_t)head * a.Tq + token : nullptr;
+    to.part = a.part + slot * a.D;
+    to.ml = a.ml + slot * 2;
+  }
+  finish<T, DP, DMA, RW>(w, to, a.slices > 1, a.D, c, lds);
+}
+
+// --- decode -----------------------------------------------------------------------------------------------------------------
+
+struct DecodeArgs {
+  const char *q, *k0, *v0, *k, *v;
+  char* out;
+  const int32_t* lens;
+  float *lse, *part, *ml, *scores, *weight;
+  int64_t q_seq, q_head, k0_token, k0_head, v0_token, v0_head, k_seq, k_token, k_head, v_seq, v_token, v_head, o_seq, o_head;  // bytes
+  int64_t score_stride;  // floats from row to row of the scores
+  int B, Hq, Hkv, G, D, P, C;
+  int prefix_tiles, prefix_slices, slice_keys;  // row tiles and slices of the prefix, keys of a slice
+  int chunks, chunk_keys, row_blocks;           // of the caches: chunks of a whole one, keys of a chunk, blocks of 32 heads of a group
+  int weight_blocks;                            // of the joining kernel: blocks of 1024 slots
+  float scale;
+};
+
+__device__ __forceinline__ int slots_in_use(const DecodeArgs& a, int b, int h) { return clamp_to(a.lens[b * a.Hkv + h], a.C); }
+
+// Workgroups of the prefix first (all rows of a key head, 32 RW at a time, over one slice of its keys), then those of the
+// caches (one sequence and key head, one chunk of its slots).  Every one leaves a part of its rows.
+template <typename T, int DP, bool DMA, int RW>
+__global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
+  typedef Shape<DP, DMA, RW> ShP;
+  typedef Shape<DP, DMA, 1> ShO;
+  __shared__ __align__(1024) char lds[ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float c = a.scale * LOG2E;
+  const int prefix = a.Hkv * a.prefix_tiles * a.prefix_slices;
+  Target to = {};
+  Keys keys;
+  if ((int)blockIdx.x < prefix) {
+    int h, unit;
+    head_and_unit(blockIdx.x, a.Hkv, a.prefix_tiles * a.prefix_slices, h, unit);
+    const int z = unit / a.prefix_tiles, tile = unit % a.prefix_tiles;  // (a slice's tiles side by side: the same keys)
+    const int rows = a.B * a.G, first_row = tile * 32 * RW + (wave % RW) * 32, r = first_row + (lane & 31);
+    const bool exists = r < rows;
+    const int b = exists ? r / a.G : 0, head = h * a.G + (exists ? r - b * a.G : 0);
+    keys.k_stride = a.k0_token;
+    keys.v_stride = a.v0_token;
+    keys.k = a.k0 + h * a.k0_head;
+    keys.v = a.v0 + h * a.v0_head;
+    keys.begin = z * a.slice_keys;
+    keys.end = min(a.P, keys.begin + a.slice_keys);
+    Rows<T, DP> w;
+    load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+    const int most = __builtin_amdgcn_readfirstlane(first_row >= rows ? 0 : keys.end);
+    run_keys<T, DP, DMA, RW>(w, keys, a.D, c, keys.end, keys.end, most, lds, nullptr);
+    if (exists) {
+      const int64_t row = (int64_t)b * a.Hq + head, slot = (int64_t)z * a.B * a.Hq + row;
+      to.out = a.out;
+      to.part = a.part + slot * a.D;
+      to.ml = a.ml + slot * 2;
+    }
+    finish<T, DP, DMA, RW>(w, to, true, a.D, c, lds);
+    return;
+  }
+  int id = blockIdx.x - prefix;
+  const int h = id % a.Hkv;
+  id /= a.Hkv;
+  const int b = id % a.B;
+  id /= a.B;
+  const int block = id % a.row_blocks, chunk = id / a.row_blocks;
+  const int n = slots_in_use(a, b, h);
+  keys.begin = chunk * a.chunk_keys;
+  keys.end = min(n, keys.begin + a.chunk_keys);
+  if (keys.begin >= keys.end) return;
+  keys.k_stride = a.k_token;
+  keys.v_stride = a.v_token;
+  keys.k = a.k + b * a.k_seq + h * a.k_head;
+  keys.v = a.v + b * a.v_seq + h * a.v_head;
+  const int g = block * 32 + (lane & 31);
+  const bool exists = g < a.G;
+  const int head = h * a.G + (exists ? g : 0);
+  const int64_t row = (int64_t)b * a.Hq + head;
+  Rows<T, DP> w;
+  load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+  float* scores = a.scores && exists ? a.scores + row * a.score_stride + keys.begin : nullptr;
+  run_keys<T, DP, DMA, 1>(w, keys, a.D, c, keys.end, keys.end, keys.end, lds, scores);
+  if (exists) {
+    const int64_t slot = (int64_t)(a.prefix_slices + chunk) * a.B * a.Hq + row;
+    to.out = a.out;
+    to.part = a.part + slot * a.D;
+    to.ml = a.ml + slot * 2;
+  }
+  finish<T, DP, DMA, 1>(w, to, true, a.D, c, lds);
+}
+
+// --- parts of rows ------------------------------------------------------------------------------------------------------------
+
+struct Joined {
+  float top, sum;  // maximum of the parts in units of log 2, sum of exponentials against it
+};
+
+// Of a row's n parts, one wavefront.
+__device__ __forceinline__ Joined join(const float* ml, int64_t stride, int n, int lane) {
+  float top = -INFINITY;
+  for (int i = lane; i < n; i += 64) top = fmaxf(top, ml[i * stride]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float sum = 0.0f;
+  for (int i = lane; i < n; i += 64) {
+    const f2 x = *reinterpret_cast<const f2*>(ml + i * stride);
+    sum += x[0] == top ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - top);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  return {top, sum};
+}
+
+template <typename T>
+__device__ __forceinline__ void join_row(const float* part, const float* ml, int64_t rows, int64_t row, int n, int D, char* out, float* lse,
+                                         int lane) {
+  const Joined j = join(ml + row * 2, rows * 2, n, lane);
+  f2 x = {0.0f, 0.0f};
+  const int at = lane * 2;
+  if (at < D) {
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float m = ml[(i * rows + row) * 2];
+      const float a = m == j.top ? 1.0f : __builtin_amdgcn_exp2f(m - j.top);
+      x += *reinterpret_cast<const f2*>(part + (i * rows + row) * D + at) * a;
+    }
+    const float inv = j.sum == 0.0f ? 0.0f : 1.0f / j.sum;
+    typedef typename T::elem e2 __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<e2*>(out + at * 2) = __builtin_convertvector(x * inv, e2);
+  }
+  if (lane == 0 && lse) *lse = j.sum == 0.0f ? -INFINITY : (j.top + __builtin_log2f(j.sum)) * LN2;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void join_prompt_kernel(const PromptArgs a) {
+  const int64_t rows = (int64_t)a.Tq * a.Hq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int64_t token = row / a.Hq, head = row % a.Hq;
+  join_row<T>(a.part, a.ml, rows, row, a.slices, a.D, a.out + token * a.o_token + head * a.o_head,
+              a.lse ? a.lse + head * a.Tq + token : nullptr, threadIdx.x & 63);
+}
+
+// Rows, then (where weights are wanted) 1024 slots of a sequence and key head a workgroup: the scores that the decode kernel
+// left become weights now that the rows' sums are known.
+template <typename T>
+__global__ __launch_bounds__(256) void join_decode_kernel(const DecodeArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows = (int64_t)a.B * a.Hq;
+  const int row_wgs = (int)((rows + 3) / 4);
+  if ((int)blockIdx.x < row_wgs) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+    if (row >= rows) return;
+    const int64_t b = row / a.Hq, head = row % a.Hq;
+    const int n = a.C ? (slots_in_use(a, (int)b, (int)head / a.G) + a.chunk_keys - 1) / a.chunk_keys : 0;
+    join_row<T>(a.part, a.ml, rows, row, a.prefix_slices + n, a.D, a.out + b * a.o_seq + head * a.o_head, a.lse ? a.lse + row : nullptr,
+                lane);
+    return;
+  }
+  const int id = blockIdx.x - row_wgs, bh = id % (a.B * a.Hkv), block = id / (a.B * a.Hkv);
+  const int b = bh / a.Hkv, h = bh % a.Hkv, n = slots_in_use(a, b, h);
+  if (block * 1024 >= n) return;
+  const float c = a.scale * LOG2E;
+  __shared__ float lse2[128];
+  const int at = block * 1024 + threadIdx.x * 4;
+  f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g0 = 0; g0 < a.G; g0 += 128) {
+    const int heads = min(128, a.G - g0);
+    if (g0) __syncthreads();
+    for (int g = wave; g < heads; g += 4) {
+      const int64_t row = (int64_t)b * a.Hq + h * a.G + g0 + g;
+      const Joined j = join(a.ml + row * 2, rows * 2, a.prefix_slices + (n + a.chunk_keys - 1) / a.chunk_keys, lane);
+      // (a row without a score above -inf gives no weights)
+      if (lane == 0) lse2[g] = j.sum == 0.0f ? INFINITY : j.top + __builtin_log2f(j.sum);
+    }
+    __syncthreads();
+    if (at >= n) continue;
+    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G + g0) * a.score_stride + at;
+#pragma unroll 4
+    for (int g = 0; g < heads; ++g) {
+      const f4 x = *reinterpret_cast<const f4*>(s + g * a.score_stride);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -lse2[g]));
+    }
+  }
+  float* w = a.weight + (int64_t)bh * a.C + at;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (at + j < n) w[j] += sum[j];
+}
+
+// --- weights of a prompt's keys -----------------------------------------------------------------------------------------------
+
+struct WeightArgs {
+  const char *q, *k;
+  const float* lse;
+  const int32_t *cu_q, *cu_k;
+  float *weight, *part;
+  int64_t q_token, q_head, k_token, k_head;  // bytes
+  int S, Tq, Tk, Hq, Hkv, G, D, causal, tiles, slices;
+  float scale;
+};
+
+// One workgroup: 128 keys of one sequence and key head, 32 a wavefront, which stay in registers as the second operand of
+// S = Q K^T; a lane owns a key and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
+template <typename T, int DP, bool DMA>
+__global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
+  constexpr int SQ = 64, TILE = SQ * DP * 2, NT = DP / 16;
+  __shared__ __align__(1024) char lds[2 * TILE];
+  __shared__ __align__(16) float lse2[2][SQ];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  int h, unit;
+  head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
+  const int z = unit % a.slices;
+  Place p;
+  if (!find_tile(a.cu_k, a.S, a.Tk, 1, 128, unit / a.slices, false, p)) return;
+  p.seq = __builtin_amdgcn_readfirstlane(p.seq);
+  p.tile = __builtin_amdgcn_readfirstlane(p.tile);
+  const int k0 = __builtin_amdgcn_readfirstlane(p.q0), nk = __builtin_amdgcn_readfirstlane(p.nq);
+  const int q0 = clamp_to(a.cu_q[p.seq], a.Tq), nq = max(0, clamp_to(a.cu_q[p.seq + 1], a.Tq) - q0);
+  const int off = nk - nq;                       // query i sees keys up to i + off
+  const int j = p.tile * 128 + wave * 32 + (lane & 31);
+  // queries that see the tile's first key, in stages of 64, head after head; this slice's share of the stages
+  const int first = a.causal ? min(nq, max(0, p.tile * 128 - off)) / SQ * SQ : 0;
+  const int stages = (nq - first + SQ - 1) / SQ;
+  const int total = stages * a.G, from = (int)((int64_t)total * z / a.slices), to = (int)((int64_t)total * (z + 1) / a.slices);
+  typename T::v8 kf[NT];
+  {
+    const bool there = j < nk;
+    const char* row = a.k + (int64_t)(k0 + (there ? j : 0)) * a.k_token + h * a.k_head;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      u2 x[2] = {{0u, 0u}, {0u, 0u}};
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int at = 16 * t + 8 * half + 4 * y;
+        if (there && at < a.D) x[y] = *reinterpret_cast<const u2*>(row + at * 2);
+      }
+      kf[t] = __builtin_bit_cast(typename T::v8, u4{x[0][0], x[0][1], x[1][0], x[1][1]});
+    }
+  }
+  const float c = a.scale * LOG2E;
+  float next_lse = 0.0f;
+  auto load = [&](int s, int buf) {
+    const int g = s / stages, i0 = first + (s - g * stages) * SQ, head = h * a.G + g;
+    const char* base = a.q + (int64_t)(q0 + i0) * a.q_token + head * a.q_head;
+    if constexpr (DMA) stage_dma<DP, SQ, false>(base, a.q_token, nq - i0, a.D, lds + buf * TILE, wave, lane);
+    else stage_copy<DP, SQ, false>(base, a.q_token, nq - i0, a.D, lds + buf * TILE, tid);
+    if (tid < SQ) next_lse = i0 + tid < nq ? a.lse[(int64_t)head * a.Tq + q0 + i0 + tid] : -INFINITY;
+  };
+  // rows that are not there, or see nothing, give exp(s - inf) = 0
+  auto keep_lse = [&](int buf) {
+    if (tid < SQ) lse2[buf][tid] = next_lse == -INFINITY ? INFINITY : next_lse * LOG2E;
+  };
+  float sum = 0.0f;
+  if (from < to) {
+    load(from, 0);
+    keep_lse(0);
+  }
+  for (int s = from; s < to; ++s) {
+    const int buf = (s - from) & 1;
+    wait_stage();
+    if (s + 1 < to) load(s + 1, buf ^ 1);
+    const int i0 = first + (s % stages) * SQ;
+    const char* tile = lds + buf * TILE;
+    const bool mask = a.causal && p.tile * 128 + wave * 32 + 31 > i0 + off;
+#pragma unroll
+    for (int b = 0; b < SQ / 32; ++b) {
+      f16x x = (f16x)(0.0f);
+      const char* row = tile + (b * 32 + (lane & 31)) * DP * 2;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const auto f = *reinterpret_cast<const typename T::v8*>(row + ((2 * t + half) ^ k_swizzle<DP>(lane & 31)) * 16);
+        x = T::mfma(f, kf[t], x);
+      }
+      f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f4 l = *reinterpret_cast<const f4*>(&lse2[buf][b * 32 + r * 8 + half * 4]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * r + y], c, -l[y]));
+          if (mask) e = j <= i0 + b * 32 + r * 8 + half * 4 + y + off ? e : 0.0f;
+          part[y] += e;
+        }
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+    }
+    if (s + 1 < to) keep_lse(buf ^ 1);
+  }
+  sum = add_halves(sum);
+  if (half == 0 && j < nk) (a.slices > 1 ? a.part + ((int64_t)z * a.Hkv + h) * a.Tk : a.weight + (int64_t)h * a.Tk)[k0 + j] = sum;
+}
+
+__global__ __launch_bounds__(256) void sum_weights_kernel(const float* part, float* weight, int64_t n, int slices) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float x = 0.0f;
+  for (int z = 0; z < slices; ++z) x += part[z * n + i];
+  weight[i] = x;
+}
+
+// --- host -----------------------------------------------------------------------------------------------------------------------
+
+static bool desc_ok(const tmac_attn_desc* d) {
+  return d && d->Hq > 0 && d->Hkv > 0 && d->Hq % d->Hkv == 0 && d->D > 0 && d->D % 4 == 0 && std::isfinite(d->scale) && d->scale > 0.0f &&
+         (d->elem == TMAC_ELEM_F16 || d->elem == TMAC_ELEM_BF16) && (d->causal == 0 || d->causal == 1) && !d->reserved[0] && !d->reserved[1];
+}
+
+constexpr int WGS = 512;  // workgroups that the chip holds at once, two on a CU
+
+// Rows of a workgroup and slices of the keys.  Rows: 128 share each key read from LDS by four wavefronts, 32 let the
+// wavefronts share the keys instead.  Slices: as many as it takes to fill the chip, none shorter than 256 keys.
+struct PromptPlan {
+  int rw, tiles, slices;
+  size_t part, ml, bytes;
+};
+static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
+  PromptPlan p;
+  const int64_t G = d->Hq / d->Hkv, rows = Tq * G;
+  auto tiles_of = [&](int per) { return (int)std::min<int64_t>(rows / per + S, rows); };
+  p.rw = rows / S <= 64 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
+  p.tiles = tiles_of(32 * p.rw);
+  const int64_t wgs = (int64_t)p.tiles * d->Hkv;
+  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WGS / wgs, (Tk / S) / 256, 64}));
+  p.part = p.slices > 1 ? (size_t)p.slices * Tq * d->Hq * d->D * 4 : 0;
+  p.ml = p.slices > 1 ? (size_t)p.slices * Tq * d->Hq * 8 : 0;
+  p.bytes = p.part + p.ml;
+  return p;
+}
+
+struct WeightsPlan {
+  int tiles, slices;
+  size_t bytes;
+};
+static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
+  WeightsPlan p;
+  p.tiles = (int)std::min<int64_t>(Tk / 128 + S, Tk);
+  const int64_t wgs = (int64_t)p.tiles * d->Hkv, stages = (int64_t)(Tq / S + 63) / 64 * (d->Hq / d->Hkv);
+  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({4 * WGS / wgs, stages / 4, 64}));
+  p.bytes = p.slices > 1 ? (size_t)p.slices * d->Hkv * Tk * 4 : 0;
+  return p;
+}
+
+struct DecodePlan {
+  int rw, tiles, slices, slice_keys, chunks, chunk_keys, row_blocks;
+  int64_t score_stride;
+  size_t part, ml, scores, bytes;
+};
+static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool accumulate) {
+  DecodePlan p = {};
+  const int64_t G = d->Hq / d->Hkv, rows = B * G;
+  p.row_blocks = (int)((G + 31) / 32);
+  if (C) {
+    // chunks of at most 1024 slots: a long cache beside short ones is then shared by many workgroups
+    const int64_t units = (int64_t)B * d->Hkv * p.row_blocks, want = units * C / WGS;
+    p.chunk_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(128, (want + 127) / 128 * 128));
+    p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
+  }
+  p.rw = rows <= 32 ? 1 : 4;
+  if (P) {
+    p.tiles = (int)((rows + 32 * p.rw - 1) / (32 * p.rw));
+    const int64_t slices = std::max<int64_t>(1, std::min<int64_t>({WGS / ((int64_t)p.tiles * d->Hkv), P / 256, 64}));
+    p.slice_keys = (int)((P + slices - 1) / slices + 127) / 128 * 128;
+    p.slices = (P + p.slice_keys - 1) / p.slice_keys;
+  }
+  const size_t R = (size_t)B * d->Hq, parts = (size_t)p.slices + p.chunks;
+  p.part = parts * R * d->D * 4;
+  p.ml = parts * R * 8;
+  p.score_stride = (int64_t)p.chunks * p.chunk_keys;
+  p.scores = accumulate ? R * p.score_stride * 4 : 0;
+  p.bytes = p.part + p.ml + p.scores + 32;
+  return p;
+}
+
+template <typename Args>
+static tmac_status launch(const void* kernel, int64_t grid, const Args& args, void* stream) {
+  if (grid <= 0) return TMAC_OK;
+  if (grid > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  Args a = args;
+  void* ptrs[] = {&a};
+  const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3(256), ptrs, 0, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) return TMAC_OK;
+  note_hip_error((int)e);
+  return TMAC_EHIP;
+}
+
+template <typename T, int DP>
+static const void* prompt_kernel(bool dma, int rw) {
+  if (dma) return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, true, 4> : (const void*)attn_prompt_kernel<T, DP, true, 1>;
+  return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, false, 4> : (const void*)attn_prompt_kernel<T, DP, false, 1>;
+}
+template <typename T, int DP>
+static const void* decode_kernel(bool dma, int rw) {
+  if (dma) return rw == 4 ? (const void*)attn_decode_kernel<T, DP, true, 4> : (const void*)attn_decode_kernel<T, DP, true, 1>;
+  return rw == 4 ? (const void*)attn_decode_kernel<T, DP, false, 4> : (const void*)attn_decode_kernel<T, DP, false, 1>;
+}
+template <typename T, int DP>
+static const void* weights_kernel(bool dma, int) {
+  return dma ? (const void*)attn_weights_kernel<T, DP, true> : (const void*)attn_weights_kernel<T, DP, false>;
+}
+// Kernel for the types and sizes of a call: PICK(T, DP) of the above.
+#define TMAC_PICK(f, d, dma, rw)                                                                         \
+  ((d)->elem == TMAC_ELEM_F16 ? ((d)->D <= 64 ? f<F16, 64>(dma, rw) : f<F16, 128>(dma, rw))             \
+                              : ((d)->D <= 64 ? f<BF16, 64>(dma, rw) : f<BF16, 128>(dma, rw)))
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace attn
+}  // namespace tmac
+
+using namespace tmac;
+using namespace tmac::attn;
+
+extern "C" size_t tmac_attn_prompt_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk) {
+  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0) return 0;
+  return prompt_plan(desc, S, Tq, Tk).bytes;
+}
+
+extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k, const tmac_view* v, int32_t S,
+                                        int32_t Tq, int32_t Tk, const int32_t* cu_q_dev, const int32_t* cu_k_dev, const tmac_view* out,
+                                        float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  if (!desc_ok(desc) || S < 0 || Tq < 0 || Tk < 0) return TMAC_EINVAL;
+  if (S == 0 || Tq == 0) return TMAC_OK;
+  if (!rows_ok(q, false, true, true) || !rows_ok(out, false, true, true) || !cu_q_dev || !cu_k_dev) return TMAC_EINVAL;
+  if (Tk > 0 && (!rows_ok(k, false, true, true) || !rows_ok(v, false, true, true))) return TMAC_EINVAL;
+  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  const tmac_view none = {};
+  if (Tk == 0) k = v = &none;
+  if (far_rows(k) || far_rows(v)) return TMAC_EUNSUPPORTED;
+  PromptPlan p = prompt_plan(desc, S, Tq, std::max(Tk, 1));
+  if (p.bytes) {
+    if (!workspace_dev || !aligned16(workspace_dev)) return TMAC_EINVAL;
+    if (workspace_bytes < p.bytes) return TMAC_ESIZE;
+  }
+  PromptArgs a = {};
+  a.q = static_cast<const char*>(q->data), a.k = static_cast<const char*>(k->data), a.v = static_cast<const char*>(v->data);
+  a.out = static_cast<char*>(out->data);
+  a.cu_q = cu_q_dev, a.cu_k = cu_k_dev, a.lse = lse_dev;
+  a.part = static_cast<float*>(workspace_dev);
+  a.ml = a.part ? a.part + p.part / 4 : nullptr;
+  a.q_token = q->token * 2, a.q_head = q->head * 2, a.k_token = k->token * 2, a.k_head = k->head * 2;
+  a.v_token = v->token * 2, a.v_head = v->head * 2, a.o_token = out->token * 2, a.o_head = out->head * 2;
+  a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
+  a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
+  const bool dma = direct_ok(k, desc->D) && direct_ok(v, desc->D);
+  const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, dma, p.rw), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+  if (st != TMAC_OK || p.slices == 1) return st;
+  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>,
+                ((int64_t)Tq * desc->Hq + 3) / 4, a, stream);
+}
+
+extern "C" size_t tmac_attn_weights_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk) {
+  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0) return 0;
+  return weights_plan(desc, S, Tq, Tk).bytes;
+}
+
+extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k, const float* lse_dev,
+                                         int32_t S, int32_t Tq, int32_t Tk, const int32_t* cu_q_dev, const int32_t* cu_k_dev,
+                                         float* weight_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  if (!desc_ok(desc) || S < 0 || Tq < 0 || Tk < 0) return TMAC_EINVAL;
+  if (S == 0 || Tk == 0) return TMAC_OK;
+  if (!rows_ok(k, false, true, true) || !cu_q_dev || !cu_k_dev || !weight_dev) return TMAC_EINVAL;
+  if (Tq > 0 && (!rows_ok(q, false, true, true) || !lse_dev)) return TMAC_EINVAL;
+  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  const tmac_view none = {};
+  if (Tq == 0) q = &none;
+  if (far_rows(q)) return TMAC_EUNSUPPORTED;
+  const WeightsPlan p = weights_plan(desc, S, Tq, Tk);
+  if (p.bytes) {
+    if (!workspace_dev || !aligned16(workspace_dev)) return TMAC_EINVAL;
+    if (workspace_bytes < p.bytes) return TMAC_ESIZE;
+  }
+  WeightArgs a = {};
+  a.q = static_cast<const char*>(q->data), a.k = static_cast<const char*>(k->data);
+  a.lse = lse_dev, a.cu_q = cu_q_dev, a.cu_k = cu_k_dev, a.weight = weight_dev, a.part = static_cast<float*>(workspace_dev);
+  a.q_token = q->token * 2, a.q_head = q->head * 2, a.k_token = k->token * 2, a.k_head = k->head * 2;
+  a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
+  a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
+  const tmac_status st =
+      launch(TMAC_PICK(weights_kernel, desc, direct_ok(q, desc->D), 0), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+  if (st != TMAC_OK || p.slices == 1) return st;
+  const int64_t n = (int64_t)desc->Hkv * Tk;
+  int64_t n_arg = n;
+  int slices = p.slices;
+  void* ptrs[] = {&a.part, &a.weight, &n_arg, &slices};
+  const hipError_t e = hipLaunchKernel((const void*)sum_weights_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), ptrs, 0,
+                                       static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) return TMAC_OK;
+  note_hip_error((int)e);
+  return TMAC_EHIP;
+}
+
+static bool decode_sizes_ok(const tmac_attn_desc* d, const tmac_cache* c, int32_t P, int32_t accumulate) {
+  return desc_ok(d) && c && c->B >= 0 && c->capacity >= 0 && P >= 0 && (accumulate == 0 || accumulate == 1) && c->Hkv == d->Hkv &&
+         c->D == d->D && c->elem == d->elem;
+}
+
+extern "C" size_t tmac_attn_decode_workspace_bytes(const tmac_attn_desc* desc, const tmac_cache* cache, int32_t P, int32_t accumulate) {
+  if (!decode_sizes_ok(desc, cache, P, accumulate) || desc->D > 128 || cache->B == 0) return 0;
+  return decode_plan(desc, cache->B, cache->capacity, P, accumulate).bytes;
+}
+
+extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k0, const tmac_view* v0, int32_t P,
+                                        const tmac_cache* cache, int32_t accumulate, const tmac_view* out, float* lse_dev,
+                                        void* workspace_dev, size_t workspace_bytes, void* stream) {
+  if (!decode_sizes_ok(desc, cache, P, accumulate)) return TMAC_EINVAL;
+  const int B = cache->B, C = cache->capacity;
+  if (B == 0) return TMAC_OK;
+  if (!rows_ok(q, true, false, true) || !rows_ok(out, true, false, true)) return TMAC_EINVAL;
+  if (P > 0 && (!rows_ok(k0, false, true, true) || !rows_ok(v0, false, true, true))) return TMAC_EINVAL;
+  if (C > 0 && (!rows_ok(&cache->k, true, true, true) || !rows_ok(&cache->v, true, true, true) || !cache->lens_dev)) return TMAC_EINVAL;
+  if (C > 0 && accumulate && !cache->weight_dev) return TMAC_EINVAL;
+  if (desc->D > 128 || (int64_t)B * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  const tmac_view none = {};
+  if (P == 0) k0 = v0 = &none;
+  const tmac_view* k = C ? &cache->k : &none;
+  const tmac_view* v = C ? &cache->v : &none;
+  if (far_rows(k0) || far_rows(v0) || far_rows(k) || far_rows(v)) return TMAC_EUNSUPPORTED;
+  const DecodePlan p = decode_plan(desc, B, C, P, accumulate);
+  if (!workspace_dev || !aligned16(workspace_dev)) return TMAC_EINVAL;
+  if (workspace_bytes < p.bytes) return TMAC_ESIZE;
+  DecodeArgs a = {};
+  a.q = static_cast<const char*>(q->data), a.k0 = static_cast<const char*>(k0->data), a.v0 = static_cast<const char*>(v0->data);
+  a.k = static_cast<const char*>(k->data), a.v = static_cast<const char*>(v->data), a.out = static_cast<char*>(out->data);
+  a.lens = cache->lens_dev, a.lse = lse_dev, a.weight = cache->weight_dev;
+  a.scores = accumulate && C ? static_cast<float*>(workspace_dev) : nullptr;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.scores);
+  a.ml = a.part + p.part / 4;
+  a.q_seq = q->seq * 2, a.q_head = q->head * 2, a.o_seq = out->seq * 2, a.o_head = out->head * 2;
+  a.k0_token = k0->token * 2, a.k0_head = k0->head * 2, a.v0_token = v0->token * 2, a.v0_head = v0->head * 2;
+  a.k_seq = k->seq * 2, a.k_token = k->token * 2, a.k_head = k->head * 2;
+  a.v_seq = v->seq * 2, a.v_token = v->token * 2, a.v_head = v->head * 2;
+  a.score_stride = p.score_stride;
+  a.B = B, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D, a.P = P, a.C = C;
+  a.prefix_tiles = p.tiles, a.prefix_slices = p.slices, a.slice_keys = p.slice_keys;
+  a.chunks = p.chunks, a.chunk_keys = std::max(1, p.chunk_keys), a.row_blocks = p.row_blocks;
+  a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
+  a.scale = desc->scale;
+  const bool dma = direct_ok(k0, desc->D) && direct_ok(v0, desc->D) && direct_ok(k, desc->D) && direct_ok(v, desc->D);
+  const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
+  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, dma, p.rw), grid, a, stream);
+  if (st != TMAC_OK) return st;
+  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
+                ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);
+}

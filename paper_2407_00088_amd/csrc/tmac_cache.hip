@@ -1,0 +1,306 @@
+// Caches that keep the heaviest keys (tmac_attn.h): filling one from prompts or from another cache, and taking in one token.
+//
+// Eviction orders tokens by (recent or not, weight, slot).  As whole numbers: a weight's bits, mapped so that they ascend with
+// its value (NaN as -inf), all ones for a recent token, which is above +inf; equal keys go by the slot.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "tmac_attn.h"
+#include "tmac_attn_host.h"
+#include "tmac_internal.h"
+
+namespace tmac {
+namespace cache {
+
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t order_key(float weight, bool recent) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, weight != weight ? -INFINITY : weight + 0.0f);  // (-0 becomes 0)
+  return recent ? 0xffffffffu : (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ int clamp_to(int x, int most) { return x < 0 ? 0 : x > most ? most : x; }
+
+struct FillArgs {
+  const char *k_src, *v_src;
+  const float* w_src;
+  const int32_t *pos_src, *cu, *src_lens, *src_seen;
+  char *k, *v;
+  float* weight;
+  int32_t *pos, *lens, *seen, *index;
+  int64_t ks_seq, ks_token, ks_head, vs_seq, vs_token, vs_head;  // bytes
+  int64_t ws_seq, ws_token, ws_head, ps_seq, ps_token, ps_head;  // elements
+  int64_t k_seq, k_token, k_head, v_seq, v_token, v_head;        // bytes
+  int B, Hkv, D, C, recent, total, blocks;
+};
+
+// Tokens of a sequence and head in the source: how many, and the first one's token index.
+__device__ __forceinline__ int source_tokens(const FillArgs& a, int b, int h, int& first) {
+  if (!a.cu) {
+    first = 0;
+    return clamp_to(a.src_lens[b * a.Hkv + h], a.total);
+  }
+  first = clamp_to(a.cu[b], a.total);
+  return max(0, clamp_to(a.cu[b + 1], a.total) - first);
+}
+
+constexpr int WAVES = 16, DIGIT = 2048, HELD = 32768;  // keys that LDS holds
+
+// Number of set bits of `mask` below the lane.
+__device__ __forceinline__ int below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Which tokens of one sequence and head stay: the (n - C)-th smallest key is found digit by digit (11, 11 and 10 bits, counted
+// in LDS), then every wavefront numbers the staying tokens of its run.  Writes weights, positions and the tokens' places in
+// the source for the copy.
+__global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs a) {
+  __shared__ uint32_t held[HELD];
+  __shared__ uint32_t count[DIGIT];
+  __shared__ uint32_t wave_sum[WAVES];
+  __shared__ uint32_t chosen[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
+  int first;
+  const int n = source_tokens(a, b, h, first), keep = min(n, a.C);
+  const int seen = a.src_seen ? a.src_seen[bh] : n;
+  const float* w = a.w_src + b * a.ws_seq + h * a.ws_head + first * a.ws_token;
+  const int32_t* p = a.pos_src ? a.pos_src + b * a.ps_seq + h * a.ps_head + first * a.ps_token : nullptr;
+  auto position = [&](int i) { return p ? p[i * a.ps_token] : i; };
+  int32_t* index = a.index + (int64_t)bh * a.C;
+  float* weight = a.weight + (int64_t)bh * a.C;
+  int32_t* pos = a.pos + (int64_t)bh * a.C;
+  if (tid == 0) {
+    a.lens[bh] = keep;
+    a.seen[bh] = seen;
+  }
+  if (n <= a.C) {
+    for (int i = tid; i < n; i += 64 * WAVES) {
+      weight[i] = w[i * a.ws_token];
+      pos[i] = position(i);
+      index[i] = i;
+    }
+    return;
+  }
+  auto read_key = [&](int i) { return order_key(w[i * a.ws_token], (int64_t)position(i) >= (int64_t)seen - a.recent); };
+  const bool holds = n <= HELD;
+  auto key = [&](int i) { return holds ? held[i] : read_key(i); };
+  if (holds) {
+#pragma unroll 4
+    for (int i = tid; i < n; i += 64 * WAVES) held[i] = read_key(i);
+  }
+  // the rank-th smallest key (from zero): what is left of `rank` counts equal keys
+  uint32_t prefix = 0, rank = n - a.C - 1;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, above = shift + bits;
+    for (int i = tid; i < DIGIT; i += 64 * WAVES) count[i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < n; i += 64 * WAVES) {
+      const uint32_t x = key(i);
+      if (above == 32 || x >> above == prefix >> above) atomicAdd(&count[(x >> shift) & ((1u << bits) - 1)], 1u);
+    }
+    __syncthreads();
+    // two digits a thread
+    const uint32_t c0 = count[2 * tid], c1 = count[2 * tid + 1];
+    uint32_t incl = c0 + c1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t x = __shfl_up(incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - c0 - c1;
+    for (int i = 0; i < wave; ++i) before += wave_sum[i];
+    if (rank >= before && rank < before + c0) chosen[0] = 2 * tid, chosen[1] = before;
+    if (rank >= before + c0 && rank < before + c0 + c1) chosen[0] = 2 * tid + 1, chosen[1] = before + c0;
+    __syncthreads();
+    prefix |= chosen[0] << shift;
+    rank -= chosen[1];
+    __syncthreads();
+  }
+  // of the tokens whose key is `prefix`, the first rank + 1 leave
+  const uint32_t leave = rank + 1;
+  const int run = ((n + WAVES - 1) / WAVES + 63) / 64 * 64, lo = min(n, wave * run), hi = min(n, lo + run);
+  uint32_t greater = 0, equal = 0;
+  for (int i = lo; i < hi; i += 64) {
+    const uint32_t x = i + lane < hi ? key(i + lane) : 0;
+    greater += __builtin_popcountll(__ballot(i + lane < hi && x > prefix));
+    equal += __builtin_popcountll(__ballot(i + lane < hi && x == prefix));
+  }
+  if (lane == 0) count[wave] = greater, count[64 + wave] = equal;
+  __syncthreads();
+  greater = equal = 0;
+  for (int i = 0; i < wave; ++i) greater += count[i], equal += count[64 + i];
+  uint32_t at = greater + (equal > leave ? equal - leave : 0);
+  for (int i = lo; i < hi; i += 64) {
+    const bool there = i + lane < hi;
+    const uint32_t x = there ? key(i + lane) : 0;
+    const uint64_t same = __ballot(there && x == prefix);
+    const bool stays = there && (x > prefix || (x == prefix && equal + below(same) >= leave));
+    const uint64_t mask = __ballot(stays);
+    if (stays) {
+      const int to = at + below(mask);
+      weight[to] = w[(i + lane) * a.ws_token];
+      pos[to] = position(i + lane);
+      index[to] = i + lane;
+    }
+    equal += __builtin_popcountll(same);
+    at += __builtin_popcountll(mask);
+  }
+}
+
+// Rows of keys and values into their slots: 64 slots of a sequence and head a workgroup, 8 bytes a lane.
+__global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
+  const int bh = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, b = bh / a.Hkv, h = bh % a.Hkv;
+  const int n = clamp_to(a.lens[bh], a.C), per_row = a.D / 4;
+  const int lo = block * 64, rows = min(64, n - lo);
+  if (rows <= 0) return;
+  int first;
+  source_tokens(a, b, h, first);
+  const int32_t* index = a.index + (int64_t)bh * a.C + lo;
+  const char* ks = a.k_src + b * a.ks_seq + h * a.ks_head + first * a.ks_token;
+  const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
+  char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
+  char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
+#pragma unroll 4
+  for (int x = threadIdx.x; x < rows * per_row; x += 256) {
+    const int row = x / per_row, at = (x - row * per_row) * 8;
+    const int64_t i = index[row];
+    *reinterpret_cast<u2*>(kd + row * a.k_token + at) = *reinterpret_cast<const u2*>(ks + i * a.ks_token + at);
+    *reinterpret_cast<u2*>(vd + row * a.v_token + at) = *reinterpret_cast<const u2*>(vs + i * a.vs_token + at);
+  }
+}
+
+struct AppendArgs {
+  const char *k_new, *v_new;
+  char *k, *v;
+  float* weight;
+  int32_t *pos, *lens, *seen;
+  int64_t kn_seq, kn_head, vn_seq, vn_head, k_seq, k_token, k_head, v_seq, v_token, v_head;  // bytes
+  int Hkv, D, C, recent;
+};
+
+// One workgroup a sequence and key head.
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
+  __shared__ uint64_t least[4];
+  const int tid = threadIdx.x, bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
+  const int n = clamp_to(a.lens[bh], a.C), seen = a.seen[bh];
+  float* weight = a.weight + (int64_t)bh * a.C;
+  int32_t* pos = a.pos + (int64_t)bh * a.C;
+  int slot = n;
+  if (n == a.C) {
+    const int64_t recent_from = (int64_t)seen + 1 - a.recent;
+    uint64_t best = ~0ull;
+#pragma unroll 8
+    for (int i = tid; i < n; i += 256) {
+      const uint64_t x = (uint64_t)order_key(weight[i], pos[i] >= recent_from) << 32 | (uint32_t)i;
+      best = x < best ? x : best;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const uint64_t x = __shfl_xor((unsigned long long)best, o);
+      best = x < best ? x : best;
+    }
+    if ((tid & 63) == 0) least[tid >> 6] = best;
+    __syncthreads();
+    for (int i = 0; i < 4; ++i) best = least[i] < best ? least[i] : best;
+    slot = (int)(uint32_t)best;
+  }
+  // (every thread has read the lengths and the slot before any of them is changed)
+  __syncthreads();
+  if (tid == 0) {
+    weight[slot] = 0.0f;
+    pos[slot] = seen;
+    a.seen[bh] = seen + 1;
+    if (n < a.C) a.lens[bh] = n + 1;
+  }
+  const int at = (tid & 127) * 8;
+  if (at < a.D * 2) {
+    if (tid < 128) *reinterpret_cast<u2*>(a.k + b * a.k_seq + h * a.k_head + slot * a.k_token + at) = *reinterpret_cast<const u2*>(a.k_new + b * a.kn_seq + h * a.kn_head + at);
+    else *reinterpret_cast<u2*>(a.v + b * a.v_seq + h * a.v_head + slot * a.v_token + at) = *reinterpret_cast<const u2*>(a.v_new + b * a.vn_seq + h * a.vn_head + at);
+  }
+}
+
+static bool cache_ok(const tmac_cache* c) {
+  return c && c->B >= 0 && c->Hkv > 0 && c->D > 0 && c->D % 4 == 0 && c->capacity > 0 && c->recent >= 0 && c->recent <= c->capacity &&
+         (c->elem == TMAC_ELEM_F16 || c->elem == TMAC_ELEM_BF16) && !c->reserved[0] && !c->reserved[1];
+}
+static bool cache_set(const tmac_cache* c) {
+  return attn::rows_ok(&c->k, true, true, true) && attn::rows_ok(&c->v, true, true, true) && c->weight_dev && c->pos_dev && c->lens_dev &&
+         c->seen_dev;
+}
+static tmac_status launch(const void* kernel, int64_t grid, int threads, void* args, void* stream) {
+  if (grid > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  void* ptrs[] = {args};
+  const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), ptrs, 0, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) return TMAC_OK;
+  note_hip_error((int)e);
+  return TMAC_EHIP;
+}
+
+}  // namespace cache
+}  // namespace tmac
+
+using namespace tmac;
+using namespace tmac::cache;
+
+extern "C" size_t tmac_cache_fill_workspace_bytes(const tmac_cache* cache) {
+  return cache_ok(cache) ? (size_t)cache->B * cache->Hkv * cache->capacity * 4 : 0;
+}
+
+extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache_source* src, void* workspace_dev, size_t workspace_bytes,
+                                       void* stream) {
+  if (!cache_ok(cache) || !src || src->total < 0 || src->reserved) return TMAC_EINVAL;
+  const int B = cache->B;
+  if (B == 0) return TMAC_OK;
+  if (!cache_set(cache) || !!src->cu_dev == !!src->lens_dev) return TMAC_EINVAL;
+  const bool packed = src->cu_dev != nullptr;
+  if (src->total > 0) {
+    if (!attn::rows_ok(&src->k, !packed, true, true) || !attn::rows_ok(&src->v, !packed, true, true) || !src->weight.data) return TMAC_EINVAL;
+    for (const tmac_view* x : {&src->weight, &src->pos})
+      if (x->data && ((!packed && x->seq < 0) || x->token < 0 || x->head < 0 || (reinterpret_cast<uintptr_t>(x->data) & 3))) return TMAC_EINVAL;
+  }
+  if (cache->D > 128 || (int64_t)B * cache->Hkv > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return TMAC_EINVAL;
+  if (workspace_bytes < tmac_cache_fill_workspace_bytes(cache)) return TMAC_ESIZE;
+  FillArgs a = {};
+  a.k_src = static_cast<const char*>(src->k.data), a.v_src = static_cast<const char*>(src->v.data);
+  a.w_src = static_cast<const float*>(src->weight.data), a.pos_src = static_cast<const int32_t*>(src->pos.data);
+  a.cu = src->cu_dev, a.src_lens = src->lens_dev, a.src_seen = src->seen_dev;
+  a.k = static_cast<char*>(cache->k.data), a.v = static_cast<char*>(cache->v.data);
+  a.weight = cache->weight_dev, a.pos = cache->pos_dev, a.lens = cache->lens_dev, a.seen = cache->seen_dev;
+  a.index = static_cast<int32_t*>(workspace_dev);
+  a.ks_seq = packed ? 0 : src->k.seq * 2, a.ks_token = src->k.token * 2, a.ks_head = src->k.head * 2;
+  a.vs_seq = packed ? 0 : src->v.seq * 2, a.vs_token = src->v.token * 2, a.vs_head = src->v.head * 2;
+  a.ws_seq = packed ? 0 : src->weight.seq, a.ws_token = src->weight.token, a.ws_head = src->weight.head;
+  a.ps_seq = packed ? 0 : src->pos.seq, a.ps_token = src->pos.token, a.ps_head = src->pos.head;
+  a.k_seq = cache->k.seq * 2, a.k_token = cache->k.token * 2, a.k_head = cache->k.head * 2;
+  a.v_seq = cache->v.seq * 2, a.v_token = cache->v.token * 2, a.v_head = cache->v.head * 2;
+  a.B = B, a.Hkv = cache->Hkv, a.D = cache->D, a.C = cache->capacity, a.recent = cache->recent, a.total = src->total;
+  a.blocks = (cache->capacity + 63) / 64;
+  const int64_t bh = (int64_t)B * cache->Hkv;
+  if (bh * a.blocks > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  const tmac_status st = cache::launch((const void*)cache_select_kernel, bh, 64 * WAVES, &a, stream);
+  return st != TMAC_OK ? st : cache::launch((const void*)cache_copy_kernel, bh * a.blocks, 256, &a, stream);
+}
+
+extern "C" tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_view* k, const tmac_view* v, void* stream) {
+  if (!cache_ok(cache)) return TMAC_EINVAL;
+  if (cache->B == 0) return TMAC_OK;
+  if (!cache_set(cache) || !attn::rows_ok(k, true, false, true) || !attn::rows_ok(v, true, false, true)) return TMAC_EINVAL;
+  if (cache->D > 128 || (int64_t)cache->B * cache->Hkv > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  AppendArgs a = {};
+  a.k_new = static_cast<const char*>(k->data), a.v_new = static_cast<const char*>(v->data);
+  a.k = static_cast<char*>(cache->k.data), a.v = static_cast<char*>(cache->v.data);
+  a.weight = cache->weight_dev, a.pos = cache->pos_dev, a.lens = cache->lens_dev, a.seen = cache->seen_dev;
+  a.kn_seq = k->seq * 2, a.kn_head = k->head * 2, a.vn_seq = v->seq * 2, a.vn_head = v->head * 2;
+  a.k_seq = cache->k.seq * 2, a.k_token = cache->k.token * 2, a.k_head = cache->k.head * 2;
+  a.v_seq = cache->v.seq * 2, a.v_token = cache->v.token * 2, a.v_head = cache->v.head * 2;
+  a.Hkv = cache->Hkv, a.D = cache->D, a.C = cache->capacity, a.recent = cache->recent;
+  return cache::launch((const void*)cache_append_kernel, (int64_t)cache->B * cache->Hkv, 256, &a, stream);
+}
