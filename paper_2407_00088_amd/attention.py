@@ -8,6 +8,7 @@ library's HIP kernels), functions that allocate results and workspace, and a hol
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 from typing import Optional
@@ -63,6 +64,10 @@ def _declare(lib):
 
 
 lib = _declare(B.lib)
+# the ordinary calls go through the native side of the binding, which answers None for all others; those are checked, worded
+# and made here
+calls = B.calls
+calls.bind_attention(tmac_attn_desc, tmac_cache, *(C.cast(getattr(lib, f), C.c_void_p).value for f in EXPORTS))
 
 
 def attn_desc(Hq: int, Hkv: int, D: int, dtype, scale: Optional[float] = None, causal: bool = True) -> tmac_attn_desc:
@@ -108,6 +113,12 @@ def _workspace(n: int, device):
     return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
 
 
+def _on(stream):
+    """Results and workspaces of a call on a stream of the caller's belong to that stream: memory of another one could be handed
+    out again there while the call still runs."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _packed(q, k, cu_q, cu_k):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q is [Tq, Hq, D], k is [Tk, Hkv, D]")
@@ -129,20 +140,25 @@ def attn_prompt(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optional[f
     """Attention over packed sequences: q [Tq, Hq, D], k and v [Tk, Hkv, D], cu_q and cu_k int32 [S + 1] (cu_k None: the queries' own).
     Returns (out [Tq, Hq, D], lse fp32 [Hq, Tq])."""
     cu_k = cu_q if cu_k is None else cu_k
+    if out is None and lse is None and stream is None:
+        got = calls.attn_prompt(q, k, v, cu_q, cu_k, causal, scale)
+        if got is not None:
+            return got
     S, Tq, Tk, Hq, Hkv, D = _packed(q, k, cu_q, cu_k)
     _dims("v", v, "Tk, Hkv, D", (Tk, Hkv, D), q.dtype)
     _rows("v", v)
     desc = attn_desc(Hq, Hkv, D, q.dtype, scale, causal)
-    if out is None:
-        out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device)
-    if lse is None:
-        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
+    n = lib.tmac_attn_prompt_workspace_bytes(desc, S, Tq, Tk)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
+        ws = _workspace(n, q.device) if n else None
     _dims("out", out, "Tq, Hq, D", (Tq, Hq, D), q.dtype)
     _rows("out", out)
     _plain("lse", lse, (Hq, Tq), torch.float32)
     _same_device(q, k, v, cu_q, cu_k, out, lse)
-    n = lib.tmac_attn_prompt_workspace_bytes(desc, S, Tq, Tk)
-    ws = _workspace(n, q.device) if n else None
     B._check(lib.tmac_attn_prompt(desc, _view(q, None, 0, 1), _view(k, None, 0, 1), _view(v, None, 0, 1), S, Tq, Tk, cu_q.data_ptr(),
                                   cu_k.data_ptr(), _view(out, None, 0, 1), lse.data_ptr(), ws.data_ptr() if n else None, n,
                                   B._stream_ptr(stream)), "tmac_attn_prompt")
@@ -153,15 +169,20 @@ def attn_weights(q, k, lse, cu_q, cu_k=None, causal: bool = True, scale: Optiona
     """Weight [Hkv, Tk] (fp32) that each key received: exp(s - lse) summed over the queries that see it and the heads of its group;
     lse as attn_prompt returns it."""
     cu_k = cu_q if cu_k is None else cu_k
+    if out is None and stream is None:
+        got = calls.attn_weights(q, k, lse, cu_q, cu_k, causal, scale)
+        if got is not None:
+            return got
     S, Tq, Tk, Hq, Hkv, D = _packed(q, k, cu_q, cu_k)
     _plain("lse", lse, (Hq, Tq), torch.float32)
     desc = attn_desc(Hq, Hkv, D, q.dtype, scale, causal)
-    if out is None:
-        out = torch.empty((Hkv, Tk), dtype=torch.float32, device=q.device)
+    n = lib.tmac_attn_weights_workspace_bytes(desc, S, Tq, Tk)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((Hkv, Tk), dtype=torch.float32, device=q.device)
+        ws = _workspace(n, q.device) if n else None
     _plain("out", out, (Hkv, Tk), torch.float32)
     _same_device(q, k, lse, cu_q, cu_k, out)
-    n = lib.tmac_attn_weights_workspace_bytes(desc, S, Tq, Tk)
-    ws = _workspace(n, q.device) if n else None
     B._check(lib.tmac_attn_weights(desc, _view(q, None, 0, 1), _view(k, None, 0, 1), lse.data_ptr(), S, Tq, Tk, cu_q.data_ptr(),
                                    cu_k.data_ptr(), out.data_ptr(), ws.data_ptr() if n else None, n, B._stream_ptr(stream)),
              "tmac_attn_weights")
@@ -174,6 +195,8 @@ class KVCache:
 
       k, v    [batch, Hkv, capacity, D]          weight  fp32 [batch, Hkv, capacity]
       pos     int32 [batch, Hkv, capacity]       lens, seen  int32 [batch, Hkv]
+
+    The tensors may be written to, not replaced.  Calls of one cache share its workspaces: on several streams they must not overlap.
     """
 
     def __init__(self, batch: int, Hkv: int, D: int, capacity: int, recent: int = 0, dtype=torch.float16, Hq: Optional[int] = None,
@@ -194,16 +217,25 @@ class KVCache:
         self.fill_ws = None
         self.attend_ws = None
 
-    def _grown(self, ws, n: int):
-        return ws if ws is not None and ws.numel() >= n else _workspace(n, self.k.device)
+    def _grown(self, ws, n: int, stream):
+        """A workspace of n bytes at least.  (One that is too small may still be in use by an earlier call: its memory is not handed out
+        again before that stream gets there.)"""
+        if ws is not None and ws.numel() >= n:
+            return ws
+        with _on(stream):
+            if ws is not None:
+                ws.record_stream(torch.cuda.current_stream())
+            return _workspace(n, self.k.device)
 
     def _fill(self, source: tmac_cache_source, stream) -> None:
         n = lib.tmac_cache_fill_workspace_bytes(self.cache)
-        self.fill_ws = self._grown(self.fill_ws, n)
+        self.fill_ws = self._grown(self.fill_ws, n, stream)
         B._check(lib.tmac_cache_fill(self.cache, source, self.fill_ws.data_ptr(), n, B._stream_ptr(stream)), "tmac_cache_fill")
 
     def fill(self, k, v, weight, cu, stream=None) -> None:
         """From packed prompts: k, v [T, Hkv, D], weight fp32 [Hkv, T] (attn_weights), cu int32 [batch + 1]."""
+        if stream is None and self.fill_ws is not None and calls.cache_fill(self.cache, self.k, k, v, weight, cu, self.fill_ws):
+            return
         T = k.shape[0]
         _dims("k", k, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
         _dims("v", v, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
@@ -224,6 +256,8 @@ class KVCache:
 
     def append(self, k, v, stream=None) -> None:
         """One token for every sequence: k, v [batch, Hkv, D]."""
+        if stream is None and calls.cache_append(self.cache, self.k, k, v):
+            return
         for name, t in (("k", k), ("v", v)):
             _dims(name, t, "batch, Hkv, D", (self.B, self.Hkv, self.D), self.k.dtype)
             _rows(name, t)
@@ -233,6 +267,10 @@ class KVCache:
     def attend(self, q, prefix_k=None, prefix_v=None, weigh: bool = True, out=None, lse=None, stream=None):
         """One decode step: q [batch, Hq, D] over the prefix (k and v [P, Hkv, D], shared by all sequences), if there is one, and the
         slots in use; `weigh` adds the step's weights to the slots'.  Returns (out [batch, Hq, D], lse fp32 [batch, Hq])."""
+        if out is None and lse is None and stream is None and self.attend_ws is not None:
+            got = calls.attend(self.cache, self.k, self.desc, q, prefix_k, prefix_v, weigh, self.attend_ws)
+            if got is not None:
+                return got
         dt = self.k.dtype
         _dims("q", q, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
         _rows("q", q)
@@ -245,16 +283,17 @@ class KVCache:
                 _dims(name, t, "P, Hkv, D", (P, self.Hkv, self.D), dt)
                 _rows(name, t)
             v0, v1 = _view(prefix_k, None, 0, 1), _view(prefix_v, None, 0, 1)
-        if out is None:
-            out = torch.empty((self.B, self.Hq, self.D), dtype=dt, device=q.device)
-        if lse is None:
-            lse = torch.empty((self.B, self.Hq), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            if out is None:
+                out = torch.empty((self.B, self.Hq, self.D), dtype=dt, device=q.device)
+            if lse is None:
+                lse = torch.empty((self.B, self.Hq), dtype=torch.float32, device=q.device)
         _dims("out", out, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
         _rows("out", out)
         _plain("lse", lse, (self.B, self.Hq), torch.float32)
         _same_device(self.k, q, prefix_k, prefix_v, out, lse)
         n = lib.tmac_attn_decode_workspace_bytes(self.desc, self.cache, P, int(weigh))
-        self.attend_ws = self._grown(self.attend_ws, n)
+        self.attend_ws = self._grown(self.attend_ws, n, stream)
         B._check(lib.tmac_attn_decode(self.desc, _view(q, 0, None, 1), v0, v1, P, self.cache, int(weigh), _view(out, 0, None, 1),
                                       lse.data_ptr(), self.attend_ws.data_ptr(), n, B._stream_ptr(stream)), "tmac_attn_decode")
         return out, lse

@@ -124,6 +124,7 @@ class _NoCalls:
     def _refuse(*args):
         return None
     forward_fused = forward = forward_one_call = multi = _refuse
+    attn_prompt = attn_weights = cache_fill = cache_append = attend = bind_attention = _refuse
 
 
 def _load_calls():

@@ -35,7 +35,7 @@ __device__ __forceinline__ void store4(char* to, f4 x) {
 // m c, the maximum in units of log 2 (-inf stays).
 __device__ __forceinline__ float log2_units(float m, float c) { return m == -INFINITY ? m : m * c; }
 
-template <typename T, int DP, bool DMA, int RW>
+template <typename T, int DP, int RW>
 __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, float c, char* lds) {
   constexpr int ND = DP / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
@@ -214,9 +214,9 @@ __device__ __forceinline__ void head_and_unit(int id, int heads, int units, int&
 }
 
 // One workgroup: 32 RW rows (query, head of the group) of one sequence and key head over the keys they see, or one slice of those.
-template <typename T, int DP, bool DMA, int RW>
+template <typename T, int DP, int RW>
 __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
-  typedef Shape<DP, DMA, RW> Sh;
+  typedef Shape<DP, RW> Sh;
   __shared__ __align__(1024) char lds[Sh::LDS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int h, unit;
@@ -252,7 +252,9 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
   Rows<T, DP> w;
   load_q<T, DP>(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane);
   const float c = a.scale * LOG2E;
-  run_keys<T, DP, DMA, RW>(w, keys, a.D, c, lim, __builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most), lds, nullptr);
+  const int least_wg = min(keys.end, a.causal ? max(0, row0 / a.G + off + 1) : nk);
+  run_keys<T, DP, RW, false>(w, keys, a.D, c, Limits{lim, least_wg, __builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most)}, lds,
+                             nullptr);
   Target to = {};
   if (exists) {
     const int64_t token = p.q0 + i, slot = ((int64_t)z * a.Tq + token) * a.Hq + head;
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, DMA, RW>(w, to, a.slices > 1, a.D, c, lds);
+  finish<T, DP, RW>(w, to, a.slices > 1, a.D, c, lds);
 }
 
 // --- decode -----------------------------------------------------------------------------------------------------------------
@@ -284,10 +286,10 @@ __device__ __forceinline__ int slots_in_use(const DecodeArgs& a, int b, int h) {
 
 // Workgroups of the prefix first (all rows of a key head, 32 RW at a time, over one slice of its keys), then those of the
 // caches (one sequence and key head, one chunk of its slots).  Every one leaves a part of its rows.
-template <typename T, int DP, bool DMA, int RW>
+template <typename T, int DP, int RW>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
-  typedef Shape<DP, DMA, RW> ShP;
-  typedef Shape<DP, DMA, 1> ShO;
+  typedef Shape<DP, RW> ShP;
+  typedef Shape<DP, 1> ShO;
   __shared__ __align__(1024) char lds[ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float c = a.scale * LOG2E;
@@ -310,14 +312,14 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     Rows<T, DP> w;
     load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
     const int most = __builtin_amdgcn_readfirstlane(first_row >= rows ? 0 : keys.end);
-    run_keys<T, DP, DMA, RW>(w, keys, a.D, c, keys.end, keys.end, most, lds, nullptr);
+    run_keys<T, DP, RW, false>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, most}, lds, nullptr);
     if (exists) {
       const int64_t row = (int64_t)b * a.Hq + head, slot = (int64_t)z * a.B * a.Hq + row;
       to.out = a.out;
       to.part = a.part + slot * a.D;
       to.ml = a.ml + slot * 2;
     }
-    finish<T, DP, DMA, RW>(w, to, true, a.D, c, lds);
+    finish<T, DP, RW>(w, to, true, a.D, c, lds);
     return;
   }
   int id = blockIdx.x - prefix;
@@ -341,14 +343,14 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   Rows<T, DP> w;
   load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
   float* scores = a.scores && exists ? a.scores + row * a.score_stride + keys.begin : nullptr;
-  run_keys<T, DP, DMA, 1>(w, keys, a.D, c, keys.end, keys.end, keys.end, lds, scores);
+  run_keys<T, DP, 1, true>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
   if (exists) {
     const int64_t slot = (int64_t)(a.prefix_slices + chunk) * a.B * a.Hq + row;
     to.out = a.out;
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, DMA, 1>(w, to, true, a.D, c, lds);
+  finish<T, DP, 1>(w, to, true, a.D, c, lds);
 }
 
 // --- parts of rows ------------------------------------------------------------------------------------------------------------
@@ -464,7 +466,7 @@ struct WeightArgs {
 
 // One workgroup: 128 keys of one sequence and key head, 32 a wavefront, which stay in registers as the second operand of
 // S = Q K^T; a lane owns a key and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
-template <typename T, int DP, bool DMA>
+template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
   constexpr int SQ = 64, TILE = SQ * DP * 2, NT = DP / 16;
   __shared__ __align__(1024) char lds[2 * TILE];
@@ -501,16 +503,22 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
     }
   }
   const float c = a.scale * LOG2E;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(TMAC_LDS char*)lds;
+  clear_pads<DP>(a.D, lds0, 2 * TILE, tid);
+  const Stage<DP, SQ, false> qs(a.q_token, a.D, wave, lane);
+  const Reads<DP> reads(lds0, 0, lane);
   float next_lse = 0.0f;
+  u2 next_tail = {0u, 0u};
   auto load = [&](int s, int buf) {
     const int g = s / stages, i0 = first + (s - g * stages) * SQ, head = h * a.G + g;
     const char* base = a.q + (int64_t)(q0 + i0) * a.q_token + head * a.q_head;
-    if constexpr (DMA) stage_dma<DP, SQ, false>(base, a.q_token, nq - i0, a.D, lds + buf * TILE, wave, lane);
-    else stage_copy<DP, SQ, false>(base, a.q_token, nq - i0, a.D, lds + buf * TILE, tid);
+    qs.load(base, a.q_token, nq - i0, a.D, lds0 + buf * TILE, wave);
+    next_tail = load_tail<SQ>(base, a.q_token, nq - i0, a.D, tid);
     if (tid < SQ) next_lse = i0 + tid < nq ? a.lse[(int64_t)head * a.Tq + q0 + i0 + tid] : -INFINITY;
   };
   // rows that are not there, or see nothing, give exp(s - inf) = 0
   auto keep_lse = [&](int buf) {
+    store_tail<DP, SQ>(next_tail, a.D, lds0 + buf * TILE, tid);
     if (tid < SQ) lse2[buf][tid] = next_lse == -INFINITY ? INFINITY : next_lse * LOG2E;
   };
   float sum = 0.0f;
@@ -523,17 +531,12 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
     wait_stage();
     if (s + 1 < to) load(s + 1, buf ^ 1);
     const int i0 = first + (s % stages) * SQ;
-    const char* tile = lds + buf * TILE;
     const bool mask = a.causal && p.tile * 128 + wave * 32 + 31 > i0 + off;
 #pragma unroll
     for (int b = 0; b < SQ / 32; ++b) {
       f16x x = (f16x)(0.0f);
-      const char* row = tile + (b * 32 + (lane & 31)) * DP * 2;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const auto f = *reinterpret_cast<const typename T::v8*>(row + ((2 * t + half) ^ k_swizzle<DP>(lane & 31)) * 16);
-        x = T::mfma(f, kf[t], x);
-      }
+      for (int t = 0; t < NT; ++t) x = T::mfma(read_k<T>(reads.k[t] + buf * TILE + b * 32 * DP * 2), kf[t], x);
       f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -647,23 +650,21 @@ static tmac_status launch(const void* kernel, int64_t grid, const Args& args, vo
 }
 
 template <typename T, int DP>
-static const void* prompt_kernel(bool dma, int rw) {
-  if (dma) return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, true, 4> : (const void*)attn_prompt_kernel<T, DP, true, 1>;
-  return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, false, 4> : (const void*)attn_prompt_kernel<T, DP, false, 1>;
+static const void* prompt_kernel(int rw) {
+  return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, 4> : (const void*)attn_prompt_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
-static const void* decode_kernel(bool dma, int rw) {
-  if (dma) return rw == 4 ? (const void*)attn_decode_kernel<T, DP, true, 4> : (const void*)attn_decode_kernel<T, DP, true, 1>;
-  return rw == 4 ? (const void*)attn_decode_kernel<T, DP, false, 4> : (const void*)attn_decode_kernel<T, DP, false, 1>;
+static const void* decode_kernel(int rw) {
+  return rw == 4 ? (const void*)attn_decode_kernel<T, DP, 4> : (const void*)attn_decode_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
-static const void* weights_kernel(bool dma, int) {
-  return dma ? (const void*)attn_weights_kernel<T, DP, true> : (const void*)attn_weights_kernel<T, DP, false>;
+static const void* weights_kernel(int) {
+  return (const void*)attn_weights_kernel<T, DP>;
 }
-// Kernel for the types and sizes of a call: PICK(T, DP) of the above.
-#define TMAC_PICK(f, d, dma, rw)                                                                         \
-  ((d)->elem == TMAC_ELEM_F16 ? ((d)->D <= 64 ? f<F16, 64>(dma, rw) : f<F16, 128>(dma, rw))             \
-                              : ((d)->D <= 64 ? f<BF16, 64>(dma, rw) : f<BF16, 128>(dma, rw)))
+// Kernel for the type and the row length of a call, rows being padded to 64 or 128 elements in LDS.
+#define TMAC_PICK(f, d, rw)                                                              \
+  ((d)->elem == TMAC_ELEM_F16 ? ((d)->D <= 64 ? f<F16, 64>(rw) : f<F16, 128>(rw))       \
+                              : ((d)->D <= 64 ? f<BF16, 64>(rw) : f<BF16, 128>(rw)))
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -704,8 +705,7 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
   a.v_token = v->token * 2, a.v_head = v->head * 2, a.o_token = out->token * 2, a.o_head = out->head * 2;
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
-  const bool dma = direct_ok(k, desc->D) && direct_ok(v, desc->D);
-  const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, dma, p.rw), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+  const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, p.rw), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>,
                 ((int64_t)Tq * desc->Hq + 3) / 4, a, stream);
@@ -739,7 +739,7 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
   const tmac_status st =
-      launch(TMAC_PICK(weights_kernel, desc, direct_ok(q, desc->D), 0), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+      launch(TMAC_PICK(weights_kernel, desc, 0), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
   const int64_t n = (int64_t)desc->Hkv * Tk;
   int64_t n_arg = n;
@@ -798,9 +798,8 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.chunks = p.chunks, a.chunk_keys = std::max(1, p.chunk_keys), a.row_blocks = p.row_blocks;
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
-  const bool dma = direct_ok(k0, desc->D) && direct_ok(v0, desc->D) && direct_ok(k, desc->D) && direct_ok(v, desc->D);
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
-  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, dma, p.rw), grid, a, stream);
+  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.rw), grid, a, stream);
   if (st != TMAC_OK) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
                 ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);
