@@ -126,7 +126,9 @@ tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_view* k, const
  *   cache      B, Hkv, D and elem as in desc; k, v, lens_dev are read.  capacity 0 with no pointers set: prefix only
  *   lse_dev    fp32 [B, Hq], or NULL
  *   accumulate 1: weight[b, h, j] += sum over the group's heads of exp(s - lse) for the slots in use
- *   workspace  tmac_attn_decode_workspace_bytes(desc, cache, P, accumulate) */
+ *   workspace  tmac_attn_decode_workspace_bytes(desc, cache, P, accumulate), 16-byte aligned, contents arbitrary
+ * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; a stride of 128 rows beyond 2^30 elements; accumulate with the lesser of the group and 32
+ * times the capacity beyond 5e8), TMAC_ESIZE, TMAC_EHIP. */
 size_t tmac_attn_decode_workspace_bytes(const tmac_attn_desc* desc, const tmac_cache* cache, int32_t P, int32_t accumulate);
 tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k0, const tmac_view* v0, int32_t P,
                              const tmac_cache* cache, int32_t accumulate, const tmac_view* out, float* lse_dev, void* workspace_dev,

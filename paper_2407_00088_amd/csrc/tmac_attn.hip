@@ -32,39 +32,30 @@ __device__ __forceinline__ void store4(char* to, f4 x) {
   *reinterpret_cast<typename T::v4*>(to) = __builtin_convertvector(x, typename T::v4);
 }
 
-// m c, the maximum in units of log 2 (-inf stays).
-__device__ __forceinline__ float log2_units(float m, float c) { return m == -INFINITY ? m : m * c; }
-
-template <typename T, int DP, int RW>
-__device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, float c, char* lds) {
+template <typename T, int DP, int BLOCKS>
+__device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, char* lds) {
   constexpr int ND = DP / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   w.l = add_halves(w.l);
-  if constexpr (RW == 4) {
+  if constexpr (BLOCKS != 1) {
     if (!to.out) return;
-    if (parts) {
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int at = d * 32 + r * 8 + half * 4;
-          if (at < D) *reinterpret_cast<f4*>(to.part + at) = f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]};
-        }
-      if (half == 0) *reinterpret_cast<f2*>(to.ml) = f2{log2_units(w.m, c), w.l};
-      return;
-    }
-    const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
+    const float scale = parts ? 1.0f : w.l == 0.0f ? 0.0f : 1.0f / w.l;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int at = d * 32 + r * 8 + half * 4;
-        if (at < D) store4<T>(to.out + at * 2, f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]} * inv);
+        if (at >= D) continue;
+        const f4 x = f4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]};
+        if (parts) *reinterpret_cast<f4*>(to.part + at) = x;
+        else store4<T>(to.out + at * 2, x * scale);
       }
-    if (half == 0 && to.lse) *to.lse = w.l == 0.0f ? -INFINITY : (log2_units(w.m, c) + __builtin_log2f(w.l)) * LN2;
+    if (half != 0) return;
+    if (parts) *reinterpret_cast<f2*>(to.ml) = f2{w.m, w.l};
+    else if (to.lse) *to.lse = w.l == 0.0f ? -INFINITY : (w.m + __builtin_log2f(w.l)) * LN2;
   } else {
     // the wavefronts that share rows meet in LDS: [wave][32 rows][DP + 4] sums, then [wave][32] maximum and sum
-    constexpr int KW = 4 / RW, W = DP + 4;
+    constexpr int KW = 4, W = DP + 4;
     float* sums = reinterpret_cast<float*>(lds);
     f2* ml = reinterpret_cast<f2*>(lds + 4 * 32 * W * 4);
     __syncthreads();
@@ -72,8 +63,8 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
     __syncthreads();
     float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < KW; ++i) m = fmaxf(m, ml[(i * RW + wave % RW) * 32 + (lane & 31)][0]);
-    const float a = w.m == m ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
+    for (int i = 0; i < KW; ++i) m = fmaxf(m, ml[i * 32 + (lane & 31)][0]);
+    const float a = w.m == m ? 1.0f : __builtin_amdgcn_exp2f(w.m - m);
     float* mine = sums + (wave * 32 + (lane & 31)) * W + half * 4;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -84,24 +75,24 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
     float l = 0.0f;
 #pragma unroll
     for (int i = 0; i < KW; ++i) {
-      const f2 x = ml[(i * RW + wave % RW) * 32 + (lane & 31)];
-      l += x[0] == m ? x[1] : x[1] * __builtin_amdgcn_exp2f((x[0] - m) * c);
+      const f2 x = ml[i * 32 + (lane & 31)];
+      l += x[0] == m ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - m);
     }
     // every lane keeps its row's scale and target for the lanes that store the row
     __syncthreads();
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (to.out && half == 0 && wave < RW) {
-      if (parts) *reinterpret_cast<f2*>(to.ml) = f2{log2_units(m, c), l};
-      else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (log2_units(m, c) + __builtin_log2f(l)) * LN2;
+    if (to.out && half == 0 && wave == 0) {
+      if (parts) *reinterpret_cast<f2*>(to.ml) = f2{m, l};
+      else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * LN2;
     }
-    // wave % RW's rows, dealt over the KW wavefronts that hold them: 16 lanes a row where D = 64, 32 where it is 128
+    // the rows, dealt over the wavefronts: 16 lanes a row where DP = 64, 32 where it is 128
     constexpr int LPR = DP / 4, RPW = 64 / LPR, N = 32 / KW / RPW;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = ((wave / RW) * N + i) * RPW + lane / LPR, at = (lane % LPR) * 4;
+      const int row = (wave * N + i) * RPW + lane / LPR, at = (lane % LPR) * 4;
       f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < KW; ++j) x += *reinterpret_cast<const f4*>(sums + ((j * RW + wave % RW) * 32 + row) * W + at);
+      for (int j = 0; j < KW; ++j) x += *reinterpret_cast<const f4*>(sums + (j * 32 + row) * W + at);
       char* out = reinterpret_cast<char*>(__shfl((unsigned long long)to.out, row));
       float* part = reinterpret_cast<float*>(__shfl((unsigned long long)to.part, row));
       const float iv = __shfl(inv, row);
@@ -213,49 +204,57 @@ __device__ __forceinline__ void head_and_unit(int id, int heads, int units, int&
   }
 }
 
-// One workgroup: 32 RW rows (query, head of the group) of one sequence and key head over the keys they see, or one slice of those.
-template <typename T, int DP, int RW>
+// A wavefront's rows of a workgroup's tile, (query, head of the group) in that order, so that the keys they see do not fall with the
+// row: 32 side by side (BLOCKS = 1: all wavefronts have the same).
+struct Tile {
+  int first, last;  // first > last: none
+  int row;          // the lane's, or -1
+  __device__ __forceinline__ Tile(int tile, int blocks, int wave, int lane, int rows) {
+    first = tile * 32 * blocks + (blocks == 1 ? 0 : wave * 32);
+    last = min(first + 32, rows) - 1;
+    row = first + (lane & 31) < rows ? first + (lane & 31) : -1;
+  }
+};
+
+// One workgroup: 32 BLOCKS rows of one sequence and key head over the keys they see, or one slice of those.
+template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
-  typedef Shape<DP, RW> Sh;
+  typedef Shape<DP, BLOCKS> Sh;
   __shared__ __align__(1024) char lds[Sh::LDS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int h, unit;
   head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
   const int z = unit % a.slices;
   Place p;
-  if (!find_tile(a.cu_q, a.S, a.Tq, a.G, 32 * RW, unit / a.slices, true, p)) return;
+  if (!find_tile(a.cu_q, a.S, a.Tq, a.G, 32 * BLOCKS, unit / a.slices, true, p)) return;
   p.seq = __builtin_amdgcn_readfirstlane(p.seq);
   p.tile = __builtin_amdgcn_readfirstlane(p.tile);
   p.q0 = __builtin_amdgcn_readfirstlane(p.q0);
   p.nq = __builtin_amdgcn_readfirstlane(p.nq);
   const int k0 = clamp_to(a.cu_k[p.seq], a.Tk), nk = max(0, clamp_to(a.cu_k[p.seq + 1], a.Tk) - k0);
-  const int row0 = p.tile * 32 * RW, rows = p.nq * a.G, off = nk - p.nq;
-  const int r = row0 + (wave % RW) * 32 + (lane & 31);
-  const bool exists = r < rows;
-  const int i = exists ? r / a.G : 0, head = h * a.G + (exists ? r - i * a.G : 0);
+  const int row0 = p.tile * 32 * BLOCKS, rows = p.nq * a.G, off = nk - p.nq;
+  const Tile tile(p.tile, BLOCKS, wave, lane, rows);
   // the keys that any row of the tile sees, and this slice of them
-  const int last = (min(row0 + 32 * RW, rows) - 1) / a.G;
-  const int seen = a.causal ? max(0, min(nk, last + off + 1)) : nk;
-  const int stages = (seen + Sh::SK - 1) / Sh::SK, per = (stages + a.slices - 1) / a.slices;
+  auto sees = [&](int row) { return a.causal ? max(0, min(nk, row / a.G + off + 1)) : nk; };
+  constexpr int SK = BLOCKS == 1 ? 128 : 32 * Sh::KB;
+  const int seen = sees(min(row0 + 32 * BLOCKS, rows) - 1), stages = (seen + SK - 1) / SK, per = (stages + a.slices - 1) / a.slices;
   Keys keys;
   keys.k_stride = a.k_token;
   keys.v_stride = a.v_token;
   keys.k = a.k + k0 * a.k_token + h * a.k_head;
   keys.v = a.v + k0 * a.v_token + h * a.v_head;
-  keys.begin = min(seen, z * per * Sh::SK);
-  keys.end = min(seen, (z + 1) * per * Sh::SK);
-  const int lim = min(keys.end, exists && a.causal ? max(0, i + off + 1) : nk);
-  // rows ascend with the lane, so the wavefront's first row sees least
-  const int first_row = row0 + (wave % RW) * 32, last_row = min(first_row + 31, rows - 1);
-  const int least = first_row >= rows ? keys.end : min(keys.end, a.causal ? max(0, first_row / a.G + off + 1) : nk);
-  const int most = first_row >= rows ? 0 : min(keys.end, a.causal ? max(0, last_row / a.G + off + 1) : nk);
+  keys.begin = min(seen, z * per * SK);
+  keys.end = min(seen, (z + 1) * per * SK);
   Rows<T, DP> w;
-  load_q<T, DP>(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane);
-  const float c = a.scale * LOG2E;
-  const int least_wg = min(keys.end, a.causal ? max(0, row0 / a.G + off + 1) : nk);
-  run_keys<T, DP, RW, false>(w, keys, a.D, c, Limits{lim, least_wg, __builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most)}, lds,
-                             nullptr);
   Target to = {};
+  Limits lim;
+  const bool any = tile.first <= tile.last, exists = tile.row >= 0;
+  lim.least_wg = min(keys.end, sees(row0));
+  lim.least = any ? min(keys.end, sees(tile.first)) : keys.end;
+  lim.most = any ? min(keys.end, sees(tile.last)) : 0;
+  lim.row = exists ? min(keys.end, sees(tile.row)) : keys.end;
+  const int i = exists ? tile.row / a.G : 0, head = h * a.G + (exists ? tile.row - i * a.G : 0);
+  load_q(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane);
   if (exists) {
     const int64_t token = p.q0 + i, slot = ((int64_t)z * a.Tq + token) * a.Hq + head;
     to.out = a.out + token * a.o_token + head * a.o_head;
@@ -263,7 +262,15 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, RW>(w, to, a.slices > 1, a.D, c, lds);
+  const float c = a.scale * LOG2E;
+  if constexpr (BLOCKS == 1) {
+    run_streams<T, DP, false, false>(w, keys, a.D, c, lim, lds, Scores{});
+    if (a.causal && has_odd_sums(w)) run_streams<T, DP, false, true>(w, keys, a.D, c, lim, lds, Scores{});
+  } else {
+    run_shared<T, DP, Sh::KB, false>(w, keys, a.D, c, lim, lds);
+    if (a.causal && __syncthreads_or(has_odd_sums(w))) run_shared<T, DP, Sh::KB, true>(w, keys, a.D, c, lim, lds);
+  }
+  finish<T, DP, BLOCKS>(w, to, a.slices > 1, a.D, lds);
 }
 
 // --- decode -----------------------------------------------------------------------------------------------------------------
@@ -284,25 +291,25 @@ struct DecodeArgs {
 
 __device__ __forceinline__ int slots_in_use(const DecodeArgs& a, int b, int h) { return clamp_to(a.lens[b * a.Hkv + h], a.C); }
 
-// Workgroups of the prefix first (all rows of a key head, 32 RW at a time, over one slice of its keys), then those of the
+// Workgroups of the prefix first (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys), then those of the
 // caches (one sequence and key head, one chunk of its slots).  Every one leaves a part of its rows.
-template <typename T, int DP, int RW>
+template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
-  typedef Shape<DP, RW> ShP;
+  typedef Shape<DP, BLOCKS> ShP;
   typedef Shape<DP, 1> ShO;
   __shared__ __align__(1024) char lds[ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = a.scale * LOG2E;
   const int prefix = a.Hkv * a.prefix_tiles * a.prefix_slices;
-  Target to = {};
   Keys keys;
   if ((int)blockIdx.x < prefix) {
     int h, unit;
     head_and_unit(blockIdx.x, a.Hkv, a.prefix_tiles * a.prefix_slices, h, unit);
-    const int z = unit / a.prefix_tiles, tile = unit % a.prefix_tiles;  // (a slice's tiles side by side: the same keys)
-    const int rows = a.B * a.G, first_row = tile * 32 * RW + (wave % RW) * 32, r = first_row + (lane & 31);
-    const bool exists = r < rows;
-    const int b = exists ? r / a.G : 0, head = h * a.G + (exists ? r - b * a.G : 0);
+    const int z = unit / a.prefix_tiles;  // (a slice's tiles side by side: the same keys)
+    const int rows = a.B * a.G;
+    const Tile tile(unit % a.prefix_tiles, BLOCKS, wave, lane, rows);
+    const bool exists = tile.row >= 0;
+    const int b = exists ? tile.row / a.G : 0, head = h * a.G + (exists ? tile.row - b * a.G : 0);
     keys.k_stride = a.k0_token;
     keys.v_stride = a.v0_token;
     keys.k = a.k0 + h * a.k0_head;
@@ -310,16 +317,18 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     keys.begin = z * a.slice_keys;
     keys.end = min(a.P, keys.begin + a.slice_keys);
     Rows<T, DP> w;
-    load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
-    const int most = __builtin_amdgcn_readfirstlane(first_row >= rows ? 0 : keys.end);
-    run_keys<T, DP, RW, false>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, most}, lds, nullptr);
+    load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+    Target to = {};
     if (exists) {
       const int64_t row = (int64_t)b * a.Hq + head, slot = (int64_t)z * a.B * a.Hq + row;
       to.out = a.out;
       to.part = a.part + slot * a.D;
       to.ml = a.ml + slot * 2;
     }
-    finish<T, DP, RW>(w, to, true, a.D, c, lds);
+    const Limits lim{keys.end, keys.end, keys.end, tile.first <= tile.last ? keys.end : 0};
+    if constexpr (BLOCKS == 1) run_streams<T, DP, false, false>(w, keys, a.D, c, lim, lds, Scores{});
+    else run_shared<T, DP, ShP::KB, false>(w, keys, a.D, c, lim, lds);
+    finish<T, DP, BLOCKS>(w, to, true, a.D, lds);
     return;
   }
   int id = blockIdx.x - prefix;
@@ -341,16 +350,25 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   const int head = h * a.G + (exists ? g : 0);
   const int64_t row = (int64_t)b * a.Hq + head;
   Rows<T, DP> w;
-  load_q<T, DP>(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
-  float* scores = a.scores && exists ? a.scores + row * a.score_stride + keys.begin : nullptr;
-  run_keys<T, DP, 1, true>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
+  load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+  // the group's rows of scores from this chunk on, in one range (the entry point keeps it below 2^31 bytes)
+  Scores scores{};
+  if (a.scores) {
+    const int64_t from = ((int64_t)b * a.Hq + h * a.G + block * 32) * a.score_stride + keys.begin;
+    const int rows = min(32, a.G - block * 32);
+    scores.base = a.scores + from;
+    scores.range = (int)(((rows - 1) * a.score_stride + a.chunk_keys) * 4);
+    scores.offset = exists ? (uint32_t)((lane & 31) * a.score_stride * 4) : 0x7fff0000u;
+  }
+  run_streams<T, DP, true, false>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
+  Target to = {};
   if (exists) {
     const int64_t slot = (int64_t)(a.prefix_slices + chunk) * a.B * a.Hq + row;
     to.out = a.out;
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, 1>(w, to, true, a.D, c, lds);
+  finish<T, DP, 1>(w, to, true, a.D, lds);
 }
 
 // --- parts of rows ------------------------------------------------------------------------------------------------------------
@@ -468,7 +486,7 @@ struct WeightArgs {
 // S = Q K^T; a lane owns a key and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
-  constexpr int SQ = 64, TILE = SQ * DP * 2, NT = DP / 16;
+  constexpr int SQ = 64, TILE = Layout<DP>::k_bytes(SQ), NT = DP / 16;
   __shared__ __align__(1024) char lds[2 * TILE];
   __shared__ __align__(16) float lse2[2][SQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
@@ -505,7 +523,7 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   const float c = a.scale * LOG2E;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(TMAC_LDS char*)lds;
   clear_pads<DP>(a.D, lds0, 2 * TILE, tid);
-  const Stage<DP, SQ, false> qs(a.q_token, a.D, wave, lane);
+  const Stage<DP, SQ, 4, false> qs(a.q_token, a.D, wave, lane);
   const Reads<DP> reads(lds0, 0, lane);
   float next_lse = 0.0f;
   u2 next_tail = {0u, 0u};
@@ -536,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
     for (int b = 0; b < SQ / 32; ++b) {
       f16x x = (f16x)(0.0f);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) x = T::mfma(read_k<T>(reads.k[t] + buf * TILE + b * 32 * DP * 2), kf[t], x);
+      for (int t = 0; t < NT; ++t) x = T::mfma(read_k<T>(reads.k_at(t) + buf * TILE + b * (TILE / 2)), kf[t], x);
       f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -576,15 +594,15 @@ constexpr int WGS = 512;  // workgroups that the chip holds at once, two on a CU
 // Rows of a workgroup and slices of the keys.  Rows: 128 share each key read from LDS by four wavefronts, 32 let the
 // wavefronts share the keys instead.  Slices: as many as it takes to fill the chip, none shorter than 256 keys.
 struct PromptPlan {
-  int rw, tiles, slices;
+  int blocks, tiles, slices;
   size_t part, ml, bytes;
 };
 static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   PromptPlan p;
   const int64_t G = d->Hq / d->Hkv, rows = Tq * G;
   auto tiles_of = [&](int per) { return (int)std::min<int64_t>(rows / per + S, rows); };
-  p.rw = rows / S <= 64 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
-  p.tiles = tiles_of(32 * p.rw);
+  p.blocks = rows / S <= 64 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
+  p.tiles = tiles_of(32 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
   p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WGS / wgs, (Tk / S) / 256, 64}));
   p.part = p.slices > 1 ? (size_t)p.slices * Tq * d->Hq * d->D * 4 : 0;
@@ -607,7 +625,7 @@ static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) 
 }
 
 struct DecodePlan {
-  int rw, tiles, slices, slice_keys, chunks, chunk_keys, row_blocks;
+  int blocks, tiles, slices, slice_keys, chunks, chunk_keys, row_blocks;
   int64_t score_stride;
   size_t part, ml, scores, bytes;
 };
@@ -621,9 +639,9 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
     p.chunk_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(128, (want + 127) / 128 * 128));
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }
-  p.rw = rows <= 32 ? 1 : 4;
+  p.blocks = rows <= 32 ? 1 : 4;
   if (P) {
-    p.tiles = (int)((rows + 32 * p.rw - 1) / (32 * p.rw));
+    p.tiles = (int)((rows + 32 * p.blocks - 1) / (32 * p.blocks));
     const int64_t slices = std::max<int64_t>(1, std::min<int64_t>({WGS / ((int64_t)p.tiles * d->Hkv), P / 256, 64}));
     p.slice_keys = (int)((P + slices - 1) / slices + 127) / 128 * 128;
     p.slices = (P + p.slice_keys - 1) / p.slice_keys;
@@ -650,21 +668,21 @@ static tmac_status launch(const void* kernel, int64_t grid, const Args& args, vo
 }
 
 template <typename T, int DP>
-static const void* prompt_kernel(int rw) {
-  return rw == 4 ? (const void*)attn_prompt_kernel<T, DP, 4> : (const void*)attn_prompt_kernel<T, DP, 1>;
+static const void* prompt_kernel(int blocks) {
+  return blocks == 4 ? (const void*)attn_prompt_kernel<T, DP, 4> : (const void*)attn_prompt_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
-static const void* decode_kernel(int rw) {
-  return rw == 4 ? (const void*)attn_decode_kernel<T, DP, 4> : (const void*)attn_decode_kernel<T, DP, 1>;
+static const void* decode_kernel(int blocks) {
+  return blocks == 4 ? (const void*)attn_decode_kernel<T, DP, 4> : (const void*)attn_decode_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
 static const void* weights_kernel(int) {
   return (const void*)attn_weights_kernel<T, DP>;
 }
 // Kernel for the type and the row length of a call, rows being padded to 64 or 128 elements in LDS.
-#define TMAC_PICK(f, d, rw)                                                              \
-  ((d)->elem == TMAC_ELEM_F16 ? ((d)->D <= 64 ? f<F16, 64>(rw) : f<F16, 128>(rw))       \
-                              : ((d)->D <= 64 ? f<BF16, 64>(rw) : f<BF16, 128>(rw)))
+#define TMAC_PICK(f, d, blocks)                                                              \
+  ((d)->elem == TMAC_ELEM_F16 ? ((d)->D <= 64 ? f<F16, 64>(blocks) : f<F16, 128>(blocks))       \
+                              : ((d)->D <= 64 ? f<BF16, 64>(blocks) : f<BF16, 128>(blocks)))
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -705,7 +723,7 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
   a.v_token = v->token * 2, a.v_head = v->head * 2, a.o_token = out->token * 2, a.o_head = out->head * 2;
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
-  const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, p.rw), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+  const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, p.blocks), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>,
                 ((int64_t)Tq * desc->Hq + 3) / 4, a, stream);
@@ -779,6 +797,7 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   const tmac_view* v = C ? &cache->v : &none;
   if (far_rows(k0) || far_rows(v0) || far_rows(k) || far_rows(v)) return TMAC_EUNSUPPORTED;
   const DecodePlan p = decode_plan(desc, B, C, P, accumulate);
+  if (accumulate && std::min(32, desc->Hq / desc->Hkv) * p.score_stride >= 0x1fff0000) return TMAC_EUNSUPPORTED;
   if (!workspace_dev || !aligned16(workspace_dev)) return TMAC_EINVAL;
   if (workspace_bytes < p.bytes) return TMAC_ESIZE;
   DecodeArgs a = {};
@@ -799,7 +818,7 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
-  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.rw), grid, a, stream);
+  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.blocks), grid, a, stream);
   if (st != TMAC_OK) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
                 ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);

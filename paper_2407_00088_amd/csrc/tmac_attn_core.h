@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace tmac {
 namespace attn {
@@ -63,16 +64,20 @@ __device__ __forceinline__ float add_halves(float x) {
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
 
-// Tiles of 16-bit rows of DP elements in LDS, unpadded, their 16-byte chunks permuted by the row so that a wavefront's
-// reads meet all banks: K tiles are read 16 bytes of 32 rows at a time, V tiles 64 bytes of four rows.
+// Tiles of 16-bit rows, padded to DP elements, in LDS.  A load of one wavefront fills 1024 bytes, 16 a lane, in whole rows (pieces
+// of rows would come slower from memory), within which the lanes' order is free.  K (and q for the weights) is read 16 bytes of 32 rows
+// at a time: chunks of 16 bytes are permuted within fours by the row, and each 1024 bytes are followed by 64 unused ones; sixteen
+// rows' chunks then meet all banks, and the products' steps along a row differ by constants.  V is read 64 bytes of four rows at a
+// time: its 64-byte pieces are permuted by the row.
 template <int DP>
-__device__ __forceinline__ int k_swizzle(int row) {
-  return DP == 128 ? row & 15 : (row >> 1) & 7;
-}
-template <int DP>
-__device__ __forceinline__ int v_swizzle(int row) {
-  return DP == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
-}
+struct Layout {
+  static constexpr int CH = DP / 8, RPI = 64 / CH;  // chunks of a row, rows of a load
+  static constexpr int k_bytes(int rows) { return rows / RPI * 1088; }
+  static constexpr int v_bytes(int rows) { return rows * DP * 2; }
+  static __device__ __forceinline__ int k_swizzle(int row) { return (DP == 128 ? row : row >> 1) & 3; }
+  static __device__ __forceinline__ int v_swizzle(int row) { return (DP == 128 ? row & 3 : row >> 1 & 1) << 2; }
+  static __device__ __forceinline__ int k_row(int row) { return row / RPI * 1088 + row % RPI * DP * 2; }
+};
 
 // What a workgroup reads: keys [begin, end) of one sequence and key head.
 struct Keys {
@@ -93,39 +98,43 @@ struct Keys {
 __device__ __forceinline__ void load_to_lds(u4 rsrc, uint32_t lds, uint32_t offset, uint32_t scalar_offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
-               : "s"(lds), "v"(offset), "s"(rsrc), "s"(scalar_offset)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(scalar_offset))
                : "memory");
 }
 __device__ __forceinline__ u4 buffer_of(const char* base, int range) {
   const uint64_t at = (uint64_t)base;
-  return u4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)range, 0x00020000u};
+  return u4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xffffu,
+            (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x00020000u};
 }
-template <int DP, int ROWS, bool IS_V>
+// WAVES wavefronts share the ROWS rows, or each loads rows of its own (WAVES = 1).
+template <int DP, int ROWS, int WAVES, bool IS_V>
 struct Stage {
-  static constexpr int CH = DP / 8, RPI = 64 / CH, N = ROWS / (4 * RPI);
-  uint32_t offset;  // of the lane's chunk in the wavefront's first load
-  bool wanted;
+  typedef Layout<DP> L;
+  static constexpr int N = ROWS / (WAVES * L::RPI), APART = IS_V ? 1024 : 1088;
+  uint32_t at;   // bytes from the first row to the lane's chunk in the wavefront's first load
+  bool wanted;   // its elements lie within the row (K: all of them)
 
   __device__ __forceinline__ Stage(int64_t stride, int D, int wave, int lane) {
-    // (a lane's row modulo the swizzle's period is the same in all its loads)
-    const int row = wave * RPI + lane / CH, chunk = (lane % CH) ^ (IS_V ? v_swizzle<DP>(row) : k_swizzle<DP>(row));
-    offset = row * (uint32_t)stride + chunk * 16;
+    const int row = lane / L::CH, chunk = (lane % L::CH) ^ (IS_V ? L::v_swizzle(row) : L::k_swizzle(row));
+    at = (row + (WAVES == 1 ? 0 : wave * L::RPI)) * (uint32_t)stride + chunk * 16;
     wanted = IS_V ? chunk * 8 < D : chunk * 8 + 8 <= D;
   }
   // Rows from `rows` on read as zeros: the descriptor's range ends there.  (What a scalar register adds to the address is not
-  // checked against the range, so it is used for whole stages only.)
+  // checked against the range, so it is used for whole stages only.)  Unwanted chunks stay as they are where wavefronts share a
+  // stage, and become zeros where they do not: such a load is always issued, so that loads can be counted.
   __device__ __forceinline__ void load(const char* base, int64_t stride, int rows, int D, uint32_t lds, int wave) const {
-    const int step = 4 * RPI * (int)stride;
-    if (!wanted) return;
+    if (WAVES != 1 && !wanted) return;
+    const uint32_t offset = wanted ? at : 0x7fffff00u;
+    const int step = WAVES * L::RPI * (int)stride;
+    if (WAVES != 1) lds += wave * APART;
     if (rows >= ROWS) {
       const u4 rsrc = buffer_of(base, (ROWS - 1) * (int)stride + D * 2);
 #pragma unroll
-      for (int i = 0; i < N; ++i) load_to_lds(rsrc, lds + (i * 4 + wave) * 1024, offset, i * step);
+      for (int i = 0; i < N; ++i) load_to_lds(rsrc, lds + i * WAVES * APART, offset, i * step);
     } else {
       const int range = rows > 0 ? (rows - 1) * (int)stride + D * 2 : 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        load_to_lds(buffer_of(base + i * (int64_t)step, max(0, range - i * step)), lds + (i * 4 + wave) * 1024, offset, 0);
+      for (int i = 0; i < N; ++i) load_to_lds(buffer_of(base + i * (int64_t)step, max(0, range - i * step)), lds + i * WAVES * APART, offset, 0);
     }
   }
 };
@@ -138,8 +147,9 @@ __device__ __forceinline__ u2 load_tail(const char* base, int64_t stride, int ro
 template <int DP, int ROWS>
 __device__ __forceinline__ void store_tail(u2 x, int D, uint32_t lds, int tid) {
   if (D % 8 && tid < ROWS)
-    *in_lds<u4>(lds + tid * DP * 2 + (((D - 4) / 8) ^ k_swizzle<DP>(tid)) * 16) = u4{x[0], x[1], 0u, 0u};
+    *in_lds<u4>(lds + Layout<DP>::k_row(tid) + (((D - 4) / 8) ^ Layout<DP>::k_swizzle(tid)) * 16) = u4{x[0], x[1], 0u, 0u};
 }
+// (four wavefronts that share a stage)
 template <int DP>
 __device__ __forceinline__ void clear_pads(int D, uint32_t lds, int bytes, int tid) {
   if (D == DP) return;
@@ -147,15 +157,15 @@ __device__ __forceinline__ void clear_pads(int D, uint32_t lds, int bytes, int t
   __syncthreads();
 }
 
-// Shape of a workgroup: RW wavefronts side by side over the rows, 32 each, 4 / RW over the keys of a stage.
-template <int DP, int RW>
+// Shape of a workgroup, by the blocks of 32 rows that it serves.  4: its wavefronts have one each and share every stage of 32 KB
+// keys, of which there are two.  1: all have the same block and stream tiles of 32 keys of their own, every fourth; their sums meet in
+// LDS at the end.
+template <int DP, int BLOCKS>
 struct Shape {
-  static constexpr int KW = 4 / RW, KT = RW == 4 ? 64 : 32, SK = KW * KT;
-  static constexpr int TILE = SK * DP * 2, STAGE = 2 * TILE;
-  // two stages where they leave room for two workgroups on a CU
-  static constexpr int STAGES = 2 * STAGE <= 65536 ? 2 : 1;
-  static constexpr int MERGE = KW > 1 ? 4 * 32 * (DP + 4) * 4 + 4 * 32 * 8 : 0;
-  static constexpr int LDS = STAGES * STAGE > MERGE ? STAGES * STAGE : MERGE;
+  static constexpr int KB = 2;
+  static constexpr int MERGE = BLOCKS == 1 ? 4 * 32 * (DP + 4) * 4 + 4 * 32 * 8 : 0;
+  static constexpr int STAGES = (BLOCKS == 4 ? 2 * KB : 4) * (Layout<DP>::k_bytes(32) + Layout<DP>::v_bytes(32));
+  static constexpr int LDS = STAGES > MERGE ? STAGES : MERGE;
 };
 
 // The running softmax and sums of one wavefront's 32 rows.
@@ -163,21 +173,29 @@ template <typename T, int DP>
 struct Rows {
   typename T::v8 q[DP / 16];
   f16x o[DP / 32];
-  float m, l;      // largest score that the sums are taken against (as the product gives it), sum of this half's exponentials
+  float m, l;  // what the sums are taken against, in units of log 2, a whole number or infinite; sum of this half's exponentials
 };
 
-// Where a lane reads its operands, in the first stage.  K: row lane % 32, 16 bytes at 16 (2 t + its half).  V^T: lane i of sixteen
+// Where a lane reads its operands.  K: row lane % 32, for step t of the product the chunk 2 t + the lane's half.  V^T: lane i of sixteen
 // takes row i / 4, columns 4 (i % 4) .. +3 and gets column i, rows 0..3.
 template <int DP>
 struct Reads {
-  uint32_t k[DP / 16], v[DP / 32];
-  __device__ __forceinline__ Reads(uint32_t ktile, uint32_t vtile, int lane) {
+  uint32_t k[2], v[DP / 32], tile;  // tile: that of V itself
+  __device__ __forceinline__ Reads(uint32_t ktile, uint32_t vtile, int lane) : tile(vtile) {
     const int half = lane >> 5, row = lane & 31, i = lane & 15;
 #pragma unroll
-    for (int t = 0; t < DP / 16; ++t) k[t] = ktile + row * DP * 2 + ((2 * t + half) ^ k_swizzle<DP>(row)) * 16;
+    for (int y = 0; y < 2; ++y) k[y] = ktile + Layout<DP>::k_row(row) + ((2 * y + half) ^ Layout<DP>::k_swizzle(row)) * 16;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
-      v[d] = vtile + (4 * half + (i >> 2)) * DP * 2 + ((d * 4 + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ v_swizzle<DP>(i >> 2)) * 16 + (i & 1) * 8;
+      v[d] = vtile + (4 * half + (i >> 2)) * DP * 2 + ((d * 4 + 2 * (lane >> 4 & 1) + ((i & 3) >> 1)) ^ Layout<DP>::v_swizzle(i >> 2)) * 16 + (i & 1) * 8;
+  }
+  __device__ __forceinline__ uint32_t k_at(int t) const { return k[t & 1] + (t >> 1) * 64; }
+  __device__ __forceinline__ uint32_t v_at(int u, int d) const { return v[d] + u * DP * 32; }
+  __device__ __forceinline__ void turn_k(int by) { k[0] += by, k[1] += by; }
+  __device__ __forceinline__ void turn_v(int by) {
+    tile += by;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) v[d] += by;
   }
 };
 template <typename T>
@@ -187,15 +205,16 @@ __device__ __forceinline__ typename T::v8 read_k(uint32_t at) {
 template <typename T, int DP>
 __device__ __forceinline__ typename T::v8 read_v(uint32_t at) {
   const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s4>(at));
-  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s4>(at + 8 * DP * 2));
+  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s4>(at + DP * 16));
   return __builtin_bit_cast(typename T::v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // NaN and infinities of V in a tile some of whose places are hidden from some rows: a hidden place must not give 0 * NaN.  The finite
 // values are multiplied as ever, the others counted for the rows that see them: n1 +inf or NaN, n2 -inf or NaN, so that NaN comes
-// out as inf - inf.  Rare, and the only loop over it that is not unrolled.
+// out as inf - inf.  Rare, and the only loop over it that is not unrolled.  x: keys of the tile that the lane's row sees (less four
+// in the upper half).
 template <typename T, int DP, int KT>
-__device__ __forceinline__ void multiply_odd_values(Rows<T, DP>& w, typename T::v8 (&p)[KT / 16], const uint32_t (&v)[DP / 32], int x) {
+__device__ __forceinline__ void multiply_odd_values(Rows<T, DP>& w, typename T::v8 (&p)[KT / 16], const Reads<DP>& reads, int x) {
 #pragma unroll 1
   for (int u = 0; u < KT / 16; ++u) {
     // which of the sixteen keys the lane's row sees, as ones and zeros
@@ -211,7 +230,7 @@ __device__ __forceinline__ void multiply_odd_values(Rows<T, DP>& w, typename T::
     for (int j = 1; j < KT / 16; ++j) p[j - 1] = p[j];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-      const u4 a = __builtin_bit_cast(u4, read_v<T, DP>(v[d] + 16 * u * DP * 2));
+      const u4 a = __builtin_bit_cast(u4, read_v<T, DP>(reads.v_at(u, d)));
       u4 fin, up, down;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -227,19 +246,24 @@ __device__ __forceinline__ void multiply_odd_values(Rows<T, DP>& w, typename T::
         fin[j] = f, up[j] = p1, down[j] = p2;
       }
       w.o[d] = T::mfma(__builtin_bit_cast(typename T::v8, fin), pu, w.o[d]);
+      __builtin_amdgcn_sched_barrier(0);  // (one count at a time in registers)
       const f16x n1 = T::mfma(__builtin_bit_cast(typename T::v8, up), sees, (f16x)(0.0f));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w.o[d][r] += n1[r] > 0.0f ? INFINITY : 0.0f;
+      __builtin_amdgcn_sched_barrier(0);
       const f16x n2 = T::mfma(__builtin_bit_cast(typename T::v8, down), sees, (f16x)(0.0f));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) w.o[d][r] += (n1[r] > 0.0f ? INFINITY : 0.0f) + (n2[r] > 0.0f ? -INFINITY : 0.0f);
+      for (int r = 0; r < 16; ++r) w.o[d][r] += n2[r] > 0.0f ? -INFINITY : 0.0f;
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
 
-// Whether a wavefront's tile of V, KT rows from `vtile`, has anything but finite values.
+// Whether a wavefront's tile of V has anything but finite values.
 template <typename T, int BYTES>
 __device__ __forceinline__ bool has_odd_values(uint32_t vtile, int lane) {
   bool found = false;
-#pragma unroll 4
+#pragma unroll 1
   for (int i = 0; i < BYTES / 1024; ++i) {
     const u4 q = *in_lds<const u4>(vtile + (i * 64 + lane) * 16);
 #pragma unroll
@@ -248,85 +272,78 @@ __device__ __forceinline__ bool has_odd_values(uint32_t vtile, int lane) {
   return __any(found);
 }
 
-// One tile of KT keys for one wavefront, `at` bytes after the places of `reads`.  MASKED: the lane's row sees x of the tile's
-// keys (less four in the upper half), and where `hidden`, some of those it does not see are there all the same.
-template <typename T, int DP, int KT, bool MASKED, bool SCORES>
-__device__ __forceinline__ void tile_step(Rows<T, DP>& w, const Reads<DP>& reads, uint32_t at, float c, bool hidden, int x, uint32_t vtile, int lane,
-                                          float* scores) {
-  constexpr int NT = DP / 16, ND = DP / 32, NB = KT / 32;
-  f16x s[NB];
+// Whether any row of the wavefront has sums that are not finite.
+template <typename T, int DP>
+__device__ __forceinline__ bool has_odd_sums(const Rows<T, DP>& w) {
+  float x = 0.0f;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) s[b] = (f16x)(0.0f);
+  for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+    for (int r = 0; r < 16; ++r) x = __builtin_fmaf(w.o[d][r], 0.0f, x);
+  return __any(x != x);
+}
+
+// Scores of 32 keys for the lane's row.
+template <typename T, int DP>
+__device__ __forceinline__ f16x scores_of(const Rows<T, DP>& w, const Reads<DP>& reads, int bytes) {
+  f16x s = (f16x)(0.0f);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] = T::mfma(read_k<T>(reads.k[t] + at + b * 32 * DP * 2), w.q[t], s[b]);
-  if constexpr (SCORES) {
-    // a decode step keeps its scores: the weights need the whole row's sum
-    if (scores) {
-      const int half = lane >> 5;
+  for (int t = 0; t < DP / 16; ++t) s = T::mfma(read_k<T>(reads.k_at(t) + bytes), w.q[t], s);
+  return s;
+}
+
+__device__ __forceinline__ float largest(const f16x& s) {
+  float mx = s[0];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+  for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+  return mx;
+}
+
+// Whether the row's sums have to be taken against a larger number.  They keep theirs until a score is 2^8 times larger:
+// exponentials up to 256 are as exact in 16 bits, and most tiles then need no rescaling.  (Row by row: a row's bits do not
+// depend on its neighbours.)  A whole number in units of log 2, so that what is rescaled keeps its bits.
+__device__ __forceinline__ bool outgrows(float mx, float c, float m) { return mx * c > m + 8.0f; }
+template <typename T, int DP>
+__device__ __forceinline__ void rescale(Rows<T, DP>& w, float mx, float c, bool grows) {
+  const float m = grows ? __builtin_ceilf(mx * c) : w.m;
+  const float alpha = grows ? __builtin_amdgcn_exp2f(w.m - m) : 1.0f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *reinterpret_cast<f4*>(scores + b * 32 + r * 8 + half * 4) = f4{s[b][4 * r], s[b][4 * r + 1], s[b][4 * r + 2], s[b][4 * r + 3]};
-    }
+  for (int d = 0; d < DP / 32; ++d) w.o[d] *= alpha;
+  w.l *= alpha;
+  w.m = m;
+}
+
+// exp(s - m) of 32 keys, rounded to the type for the second product; returns their sum before rounding.
+template <typename T>
+__device__ __forceinline__ float exponentials(const f16x& s, float c, float m, typename T::v8& p0, typename T::v8& p1) {
+  f16x e;
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -m));
+    sum[r & 1] += e[r];
   }
-  if constexpr (MASKED) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + (r >> 2) * 8 + (r & 3) < x ? s[b][r] : -INFINITY;
-  }
-  float mx = s[0][0];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-  mx = max_halves(mx);
-  // The sums keep the maximum they have until a row's is 2^8 times larger: exponentials up to 256 are as exact in 16
-  // bits, and most tiles then need no rescaling.  (Row by row: a row's bits do not depend on its neighbours.)
-  const bool grows = mx * c > w.m * c + 8.0f;
-  if (__any(grows)) {
-    const float m = grows ? mx : w.m;
-    const float alpha = grows ? __builtin_amdgcn_exp2f((w.m - m) * c) : 1.0f;
-#pragma unroll
-    for (int d = 0; d < ND; ++d) w.o[d] *= alpha;
-    w.l *= alpha;
-    w.m = m;
-  }
-  const float mc = w.m == -INFINITY ? 0.0f : w.m * c;
-  typename T::v8 p[KT / 16];
-  float sum = 0.0f;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    f16x e;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-      sum += e[r];
-    }
-    p[2 * b] = __builtin_convertvector(__builtin_shufflevector(e, e, 0, 1, 2, 3, 4, 5, 6, 7), typename T::v8);
-    p[2 * b + 1] = __builtin_convertvector(__builtin_shufflevector(e, e, 8, 9, 10, 11, 12, 13, 14, 15), typename T::v8);
-  }
-  w.l += sum;
-  if constexpr (MASKED) {
-    if (hidden && has_odd_values<T, KT * DP * 2>(vtile + at, lane)) {
-      uint32_t v[ND];
-#pragma unroll
-      for (int d = 0; d < ND; ++d) v[d] = reads.v[d] + at;
-      multiply_odd_values<T, DP, KT>(w, p, v, x);
-      return;
-    }
-  }
+  p0 = __builtin_convertvector(__builtin_shufflevector(e, e, 0, 1, 2, 3, 4, 5, 6, 7), typename T::v8);
+  p1 = __builtin_convertvector(__builtin_shufflevector(e, e, 8, 9, 10, 11, 12, 13, 14, 15), typename T::v8);
+  return sum[0] + sum[1];
+}
+
+// What exponents are taken against: a row without a score above -inf keeps exponentials of zero.
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+
+template <typename T, int DP, int KT>
+__device__ __forceinline__ void multiply_v(Rows<T, DP>& w, const Reads<DP>& reads, const typename T::v8 (&p)[KT / 16]) {
 #pragma unroll
   for (int u = 0; u < KT / 16; ++u)
 #pragma unroll
-    for (int d = 0; d < ND; ++d) w.o[d] = T::mfma(read_v<T, DP>(reads.v[d] + at + 16 * u * DP * 2), p[u], w.o[d]);
+    for (int d = 0; d < DP / 32; ++d) w.o[d] = T::mfma(read_v<T, DP>(reads.v_at(u, d)), p[u], w.o[d]);
 }
 
-// Whether a wavefront's loads into LDS have landed, then the workgroup's.
-__device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Scores beyond the x keys of 32 that the lane's row sees (less four in the upper half).
+__device__ __forceinline__ void hide(f16x& s, int x) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (r >> 2) * 8 + (r & 3) < x ? s[r] : -INFINITY;
+}
 
 // Keys that the rows see, counted from the sequence's start and at most keys.end: the lane's own row, the least of the
 // workgroup's and of the wavefront's rows, the most of the wavefront's.
@@ -334,80 +351,170 @@ struct Limits {
   int row, least_wg, least, most;
 };
 
-// All keys of a unit for the workgroup's rows.  scores: where the lane's row keeps its scores (index 0 = keys.begin), or null.
-template <typename T, int DP, int RW, bool SCORES>
-__device__ __forceinline__ void run_keys(Rows<T, DP>& w, const Keys& keys, int D, float c, const Limits& lim, char* shared, float* scores) {
-  typedef Shape<DP, RW> Sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kw = RW == 4 ? 0 : wave / RW;  // which part of a stage's keys
-  const uint32_t lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)shared;
+// Where a decode step keeps its scores (the weights need the whole row's sum): one row of floats per lane's row, index 0 =
+// keys.begin; rows that do not exist have an offset out of the range.
+struct Scores {
+  float* base;      // null: nowhere
+  int range;        // bytes
+  uint32_t offset;  // the lane's, in bytes
+};
+
+template <typename T, int DP>
+__device__ __forceinline__ void clear(Rows<T, DP>& w) {
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) w.o[d] = (f16x)(0.0f);
   w.m = -INFINITY;
   w.l = 0.0f;
+}
+
+// Whether a wavefront's loads into LDS have landed, then the workgroup's.
+__device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// All keys of a unit where four wavefronts share the stages, of 32 KB keys each.
+//
+// A hidden place has an exponential of zero, and 0 * NaN is NaN: values of V that are not finite would show in rows that do not
+// see them.  They are not looked for (that cost 15 % where sequences are short): the sums then hold something that is not finite
+// at the end, and the unit is run again, CAREFUL, with the same bits for the rows that such values do not concern.
+template <typename T, int DP, int KB, bool CAREFUL>
+__device__ __forceinline__ void run_shared(Rows<T, DP>& w, const Keys& keys, int D, float c, const Limits& lim, char* shared) {
+  constexpr int SK = 32 * KB, KS = Layout<DP>::k_bytes(SK), VS = Layout<DP>::v_bytes(SK);  // a stage's keys, its bytes
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)shared, lds_v = lds + 2 * KS;  // two stages of K, two of V
+  clear(w);
   if (keys.begin >= keys.end) return;
-  clear_pads<DP>(D, lds, Sh::STAGES * Sh::STAGE, tid);
-  const Stage<DP, Sh::SK, false> ks(keys.k_stride, D, wave, lane);
-  const Stage<DP, Sh::SK, true> vs(keys.v_stride, D, wave, lane);
-  const Reads<DP> reads(lds + kw * Sh::KT * DP * 2, lds + Sh::TILE + kw * Sh::KT * DP * 2, lane);
-  auto load = [&](int at, uint32_t to) {
-    const char* kb = keys.k + (int64_t)at * keys.k_stride;
-    ks.load(kb, keys.k_stride, keys.end - at, D, lds + to, wave);
-    vs.load(keys.v + (int64_t)at * keys.v_stride, keys.v_stride, keys.end - at, D, lds + to + Sh::TILE, wave);
-    return load_tail<Sh::SK>(kb, keys.k_stride, keys.end - at, D, tid);
+  clear_pads<DP>(D, lds, 2 * (KS + VS), tid);
+  const Stage<DP, SK, 4, false> ks(keys.k_stride, D, wave, lane);
+  const Stage<DP, SK, 4, true> vs(keys.v_stride, D, wave, lane);
+  Reads<DP> reads(lds, lds_v, lane);
+  // the stage from key `at` on goes to `place` (0 or 1); what a row's last half chunk needs of a register is stored after the
+  // computation that the load runs beside
+  auto load = [&](int at, int place) {
+    const char* base = keys.k + (int64_t)at * keys.k_stride;
+    ks.load(base, keys.k_stride, keys.end - at, D, lds + place * KS, wave);
+    vs.load(keys.v + (int64_t)at * keys.v_stride, keys.v_stride, keys.end - at, D, lds_v + place * VS, wave);
+    return load_tail<SK>(base, keys.k_stride, keys.end - at, D, tid);
   };
-  auto whole = [&](int at, uint32_t from) {
-    tile_step<T, DP, Sh::KT, false, SCORES>(w, reads, from, c, false, 0, 0, lane, SCORES && scores ? scores + (at + kw * Sh::KT - keys.begin) : nullptr);
+  store_tail<DP, SK>(load(keys.begin, 0), D, lds, tid);
+  int place = 0, at = keys.begin;
+  auto turn = [&](u2 tail) {
+    reads.turn_k(place ? -KS : KS);
+    reads.turn_v(place ? -VS : VS);
+    place ^= 1;
+    at += SK;
+    store_tail<DP, SK>(tail, D, lds + place * KS, tid);
   };
-  auto masked = [&](int at, uint32_t from) {
-    const int first = at + kw * Sh::KT;  // the wavefront's first key
-    if (first >= lim.most) return;
-    tile_step<T, DP, Sh::KT, true, SCORES>(w, reads, from, c, lim.least < min(keys.end, first + Sh::KT), lim.row - first - 4 * (lane >> 5),
-                                           lds + Sh::TILE + kw * Sh::KT * DP * 2, lane, SCORES && scores ? scores + (first - keys.begin) : nullptr);
-  };
-  int at = keys.begin;
-  if constexpr (Sh::STAGES == 2) {
-    store_tail<DP, Sh::SK>(load(at, 0), D, lds, tid);
-    // stages that every row sees whole, two at a time, so that their places are constants
-    while (at + 2 * Sh::SK <= lim.least_wg) {
-      wait_stage();
-      u2 tail = load(at + Sh::SK, Sh::STAGE);
-      whole(at, 0);
-      store_tail<DP, Sh::SK>(tail, D, lds + Sh::STAGE, tid);
-      at += Sh::SK;
-      wait_stage();
-      if (at + Sh::SK < keys.end) tail = load(at + Sh::SK, 0);
-      whole(at, Sh::STAGE);
-      store_tail<DP, Sh::SK>(tail, D, lds, tid);
-      at += Sh::SK;
+  auto step = [&](auto masked) {
+    f16x s[KB];
+    typename T::v8 p[2 * KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) s[b] = (f16x)(0.0f);
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+      for (int b = 0; b < KB; ++b) s[b] = T::mfma(read_k<T>(reads.k_at(t) + b * Layout<DP>::k_bytes(32)), w.q[t], s[b]);
+    const int x = lim.row - at - 4 * (lane >> 5);
+    if constexpr (masked) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b) hide(s[b], x - 32 * b);
     }
-    uint32_t from = 0;
+    float mx = largest(s[0]);
+#pragma unroll
+    for (int b = 1; b < KB; ++b) mx = fmaxf(mx, largest(s[b]));
+    mx = max_halves(mx);
+    const bool grows = outgrows(mx, c, w.m);
+    if (__any(grows)) rescale(w, mx, c, grows);
+    const float m = base_of(w.m);
+#pragma unroll
+    for (int b = 0; b < KB; ++b) w.l += exponentials<T>(s[b], c, m, p[2 * b], p[2 * b + 1]);
+    if constexpr (CAREFUL) {
+      if (has_odd_values<T, VS>(reads.tile, lane)) {
+        multiply_odd_values<T, DP, SK>(w, p, reads, x);
+        return;
+      }
+    }
+    multiply_v<T, DP, SK>(w, reads, p);
+  };
+  auto next_stage = [&] {
+    wait_stage();
+    return at + SK < keys.end ? load(at + SK, place ^ 1) : u2{0u, 0u};
+  };
+  if constexpr (!CAREFUL) {
+    while (at + SK <= lim.least_wg) {  // stages that every row sees whole
+      const u2 tail = next_stage();
+      step(std::false_type{});
+      turn(tail);
+    }
+  }
 #pragma unroll 1
-    for (; at < keys.end; at += Sh::SK) {
-      wait_stage();
-      u2 tail = {0u, 0u};
-      if (at + Sh::SK < keys.end) tail = load(at + Sh::SK, from ^ Sh::STAGE);
-      masked(at, from);
-      from ^= Sh::STAGE;
-      store_tail<DP, Sh::SK>(tail, D, lds + from, tid);
+  while (at < keys.end) {
+    const u2 tail = next_stage();
+    if (at < lim.most) step(std::true_type{});
+    turn(tail);
+  }
+}
+
+// All keys of a unit where every wavefront streams tiles of its own, 32 keys each, every fourth: a tile of K is requested as soon as
+// the one before has met q, one of V as soon as the one before has met the exponentials, and nobody waits for anybody.
+template <typename T, int DP, bool SCORES, bool CAREFUL>
+__device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, int D, float c, const Limits& lim, char* shared, const Scores& scores) {
+  constexpr int KT = 32, KB = Layout<DP>::k_bytes(KT), VB = Layout<DP>::v_bytes(KT);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)shared + wave * (KB + VB), lds_v = lds + KB;
+  clear(w);
+  const Stage<DP, KT, 1, false> ks(keys.k_stride, D, wave, lane);
+  const Stage<DP, KT, 1, true> vs(keys.v_stride, D, wave, lane);
+  constexpr int LOADS = Stage<DP, KT, 1, false>::N;
+  const Reads<DP> reads(lds, lds_v, lane);
+  const int end = min(keys.end, lim.most);
+  int at = keys.begin + wave * KT;
+  if (at >= end) return;
+  u2 tail;
+  auto load_k = [&](int i) {
+    const char* base = keys.k + (int64_t)i * keys.k_stride;
+    ks.load(base, keys.k_stride, keys.end - i, D, lds, wave);
+    tail = load_tail<KT>(base, keys.k_stride, keys.end - i, D, lane);
+  };
+  auto load_v = [&](int i) { vs.load(keys.v + (int64_t)i * keys.v_stride, keys.v_stride, keys.end - i, D, lds_v, wave); };
+  load_k(at);
+  load_v(at);
+  bool stored = false;  // the tile before left scores, four stores after V's loads
+  while (true) {
+    // K has landed: V's loads, and stores of scores, are younger
+    if (SCORES && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + 4) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    store_tail<DP, KT>(tail, D, lds, lane);
+    f16x s = scores_of(w, reads, 0);
+    const int next = at + 4 * KT;
+    // (the products have read all of K)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (next < end) load_k(next);
+    const f16x raw = s;
+    const int x = lim.row - at - 4 * (lane >> 5);
+    if (lim.least < at + KT) hide(s, x);
+    const float mx = max_halves(largest(s));
+    const bool grows = outgrows(mx, c, w.m);
+    if (__any(grows)) rescale(w, mx, c, grows);
+    typename T::v8 p[2];
+    w.l += exponentials<T>(s, c, base_of(w.m), p[0], p[1]);
+    if (next < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bool odd = false;
+    if constexpr (CAREFUL) odd = has_odd_values<T, VB>(lds_v, lane);
+    if (odd) multiply_odd_values<T, DP, 32>(w, p, reads, x);
+    else multiply_v<T, DP, 32>(w, reads, p);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (next < end) load_v(next);
+    if (SCORES && scores.base) {
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(scores.base, (short)0, scores.range, 0x00020000);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f4 x4 = {raw[4 * r], raw[4 * r + 1], raw[4 * r + 2], raw[4 * r + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x4), rsrc, (int)(scores.offset + (uint32_t)(at - keys.begin + r * 8 + (lane >> 5) * 4) * 4u), 0, 0);
+      }
+      stored = true;
     }
-  } else {
-    bool again = false;
-    for (; at + Sh::SK <= lim.least_wg; at += Sh::SK) {
-      if (again) __syncthreads();
-      again = true;
-      store_tail<DP, Sh::SK>(load(at, 0), D, lds, tid);
-      wait_stage();
-      whole(at, 0);
-    }
-#pragma unroll 1
-    for (; at < keys.end; at += Sh::SK) {
-      if (again) __syncthreads();
-      again = true;
-      store_tail<DP, Sh::SK>(load(at, 0), D, lds, tid);
-      wait_stage();
-      masked(at, 0);
-    }
+    if (next >= end) break;
+    at = next;
   }
 }
 
