@@ -32,8 +32,9 @@ __device__ __forceinline__ void store4(char* to, f4 x) {
   *reinterpret_cast<typename T::v4*>(to) = __builtin_convertvector(x, typename T::v4);
 }
 
+// row_lse (BLOCKS = 1 only, or null): 32 numbers in LDS beyond those that the sums meet in, the rows' lse in units of log 2.
 template <typename T, int DP, int BLOCKS>
-__device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, char* lds) {
+__device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, char* lds, float* row_lse = nullptr) {
   constexpr int ND = DP / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   w.l = add_halves(w.l);
@@ -81,6 +82,7 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
     // every lane keeps its row's scale and target for the lanes that store the row
     __syncthreads();
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (row_lse && half == 0 && wave == 0) row_lse[lane] = l == 0.0f ? INFINITY : m + __builtin_log2f(l);
     if (to.out && half == 0 && wave == 0) {
       if (parts) *reinterpret_cast<f2*>(to.ml) = f2{m, l};
       else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * LN2;
@@ -285,26 +287,56 @@ struct DecodeArgs {
   int B, Hq, Hkv, G, D, P, C;
   int prefix_tiles, prefix_slices, slice_keys;  // row tiles and slices of the prefix, keys of a slice
   int chunks, chunk_keys, row_blocks;           // of the caches: chunks of a whole one, keys of a chunk, blocks of 32 heads of a group
+  int whole_rows;                               // no prefix, and a whole cache in one chunk: nothing is joined
   int weight_blocks;                            // of the joining kernel: blocks of 1024 slots
   float scale;
 };
 
 __device__ __forceinline__ int slots_in_use(const DecodeArgs& a, int b, int h) { return clamp_to(a.lens[b * a.Hkv + h], a.C); }
 
-// Workgroups of the prefix first (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys), then those of the
-// caches (one sequence and key head, one chunk of its slots).  Every one leaves a part of its rows.
+// Weights of a workgroup's slots: what the scores of `heads` rows come to now that the rows' sums are known; 4 slots a thread.
+// x: the first rows' scores, requested before the sums were known.
+constexpr int AHEAD = 8;
+__device__ __forceinline__ void request_scores(const float* scores, int64_t stride, int heads, f4 (&x)[AHEAD]) {
+#pragma unroll
+  for (int g = 0; g < AHEAD; ++g) x[g] = g < heads ? *reinterpret_cast<const f4*>(scores + g * stride) : f4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+__device__ __forceinline__ f4 sum_weights(const float* scores, int64_t stride, int heads, const f4 (&x)[AHEAD], const float* row_lse, float c) {
+  f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int g = 0; g < AHEAD; ++g)
+    if (g < heads) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[g][j], c, -row_lse[g]));
+    }
+#pragma unroll 4
+  for (int g = AHEAD; g < heads; ++g) {
+    const f4 y = *reinterpret_cast<const f4*>(scores + g * stride);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], c, -row_lse[g]));
+  }
+  return sum;
+}
+
+// Workgroups of the prefix (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys) and of the caches (one sequence
+// and key head, one chunk of its slots), the former, longer ones first (mixed, 4 rows over 2047 keys took 13.9 instead of 11.7 us).  Every one
+// leaves a part of its rows; where a row has only one, finished rows and, with accumulate, the slots' weights.
 template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<DP, BLOCKS> ShP;
   typedef Shape<DP, 1> ShO;
-  __shared__ __align__(1024) char lds[ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS];
+  constexpr int LDS = ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS;
+  __shared__ __align__(1024) char lds[LDS];
+  __shared__ float row_lse[32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = a.scale * LOG2E;
-  const int prefix = a.Hkv * a.prefix_tiles * a.prefix_slices;
   Keys keys;
-  if ((int)blockIdx.x < prefix) {
+  const int prefix = a.Hkv * a.prefix_tiles * a.prefix_slices;
+  int id = (int)blockIdx.x - prefix;
+  if (id < 0) {
+    id += prefix;
     int h, unit;
-    head_and_unit(blockIdx.x, a.Hkv, a.prefix_tiles * a.prefix_slices, h, unit);
+    head_and_unit(id, a.Hkv, a.prefix_tiles * a.prefix_slices, h, unit);
     const int z = unit / a.prefix_tiles;  // (a slice's tiles side by side: the same keys)
     const int rows = a.B * a.G;
     const Tile tile(unit % a.prefix_tiles, BLOCKS, wave, lane, rows);
@@ -331,26 +363,25 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     finish<T, DP, BLOCKS>(w, to, true, a.D, lds);
     return;
   }
-  int id = blockIdx.x - prefix;
   const int h = id % a.Hkv;
   id /= a.Hkv;
   const int b = id % a.B;
   id /= a.B;
   const int block = id % a.row_blocks, chunk = id / a.row_blocks;
-  const int n = slots_in_use(a, b, h);
-  keys.begin = chunk * a.chunk_keys;
-  keys.end = min(n, keys.begin + a.chunk_keys);
-  if (keys.begin >= keys.end) return;
-  keys.k_stride = a.k_token;
-  keys.v_stride = a.v_token;
-  keys.k = a.k + b * a.k_seq + h * a.k_head;
-  keys.v = a.v + b * a.v_seq + h * a.v_head;
   const int g = block * 32 + (lane & 31);
   const bool exists = g < a.G;
   const int head = h * a.G + (exists ? g : 0);
   const int64_t row = (int64_t)b * a.Hq + head;
   Rows<T, DP> w;
-  load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+  load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);  // (on its way while the length is)
+  const int n = slots_in_use(a, b, h);
+  keys.begin = chunk * a.chunk_keys;
+  keys.end = min(n, keys.begin + a.chunk_keys);
+  if (keys.begin >= keys.end && !a.whole_rows) return;
+  keys.k_stride = a.k_token;
+  keys.v_stride = a.v_token;
+  keys.k = a.k + b * a.k_seq + h * a.k_head;
+  keys.v = a.v + b * a.v_seq + h * a.v_head;
   // the group's rows of scores from this chunk on, in one range (the entry point keeps it below 2^31 bytes)
   Scores scores{};
   if (a.scores) {
@@ -364,11 +395,24 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   Target to = {};
   if (exists) {
     const int64_t slot = (int64_t)(a.prefix_slices + chunk) * a.B * a.Hq + row;
-    to.out = a.out;
+    to.out = a.out + b * a.o_seq + head * a.o_head;
+    to.lse = a.lse ? a.lse + row : nullptr;
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, 1>(w, to, true, a.D, lds);
+  finish<T, DP, 1>(w, to, !a.whole_rows, a.D, lds, row_lse);
+  if (!a.whole_rows || !a.scores) return;
+  // (the scores have been written by this workgroup: all are past the barriers of `finish`)
+  for (int at = threadIdx.x * 4; at < n; at += 1024) {
+    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G) * a.score_stride + at;
+    f4 x[AHEAD];
+    request_scores(s, a.score_stride, a.G, x);
+    const f4 sum = sum_weights(s, a.score_stride, a.G, x, row_lse, c);
+    float* weight = a.weight + ((int64_t)b * a.Hkv + h) * a.C + at;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j < n) weight[j] += sum[j];
+  }
 }
 
 // --- parts of rows ------------------------------------------------------------------------------------------------------------
@@ -442,32 +486,31 @@ __global__ __launch_bounds__(256) void join_decode_kernel(const DecodeArgs a) {
   const int b = bh / a.Hkv, h = bh % a.Hkv, n = slots_in_use(a, b, h);
   if (block * 1024 >= n) return;
   const float c = a.scale * LOG2E;
-  __shared__ float lse2[128];
+  __shared__ float row_lse[128];
   const int at = block * 1024 + threadIdx.x * 4;
+  float* weight = a.weight + (int64_t)bh * a.C + at;
+  float old[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) old[j] = at + j < n ? weight[j] : 0.0f;
   f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int g0 = 0; g0 < a.G; g0 += 128) {
     const int heads = min(128, a.G - g0);
+    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G + g0) * a.score_stride + at;
+    f4 x[AHEAD];
+    request_scores(s, a.score_stride, at < n ? heads : 0, x);
     if (g0) __syncthreads();
     for (int g = wave; g < heads; g += 4) {
       const int64_t row = (int64_t)b * a.Hq + h * a.G + g0 + g;
       const Joined j = join(a.ml + row * 2, rows * 2, a.prefix_slices + (n + a.chunk_keys - 1) / a.chunk_keys, lane);
       // (a row without a score above -inf gives no weights)
-      if (lane == 0) lse2[g] = j.sum == 0.0f ? INFINITY : j.top + __builtin_log2f(j.sum);
+      if (lane == 0) row_lse[g] = j.sum == 0.0f ? INFINITY : j.top + __builtin_log2f(j.sum);
     }
     __syncthreads();
-    if (at >= n) continue;
-    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G + g0) * a.score_stride + at;
-#pragma unroll 4
-    for (int g = 0; g < heads; ++g) {
-      const f4 x = *reinterpret_cast<const f4*>(s + g * a.score_stride);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -lse2[g]));
-    }
+    if (at < n) sum += sum_weights(s, a.score_stride, heads, x, row_lse, c);
   }
-  float* w = a.weight + (int64_t)bh * a.C + at;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (at + j < n) w[j] += sum[j];
+    if (at + j < n) weight[j] = old[j] + sum[j];
 }
 
 // --- weights of a prompt's keys -----------------------------------------------------------------------------------------------
@@ -626,6 +669,7 @@ static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) 
 
 struct DecodePlan {
   int blocks, tiles, slices, slice_keys, chunks, chunk_keys, row_blocks;
+  bool whole_rows;
   int64_t score_stride;
   size_t part, ml, scores, bytes;
 };
@@ -634,9 +678,17 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
   const int64_t G = d->Hq / d->Hkv, rows = B * G;
   p.row_blocks = (int)((G + 31) / 32);
   if (C) {
-    // chunks of at most 1024 slots: a long cache beside short ones is then shared by many workgroups
-    const int64_t units = (int64_t)B * d->Hkv * p.row_blocks, want = units * C / WGS;
-    p.chunk_keys = (int)std::min<int64_t>(1024, std::max<int64_t>(128, (want + 127) / 128 * 128));
+    // Chunks of 128 to 512 slots, so that a long cache beside short ones is shared by many workgroups, by the rounds that full
+    // caches take times what a round costs: its slots and about 96 more for the start, the meeting and the parts.
+    const int64_t units = (int64_t)B * d->Hkv * p.row_blocks;
+    int64_t best = INT64_MAX;
+    for (int keys = 128; keys <= 512; keys += 128) {
+      const int64_t cost = (units * ((C + keys - 1) / keys) + WGS - 1) / WGS * (keys + 96);
+      if (cost < best) best = cost, p.chunk_keys = keys;
+    }
+    // a short cache in one chunk has nothing to join, which saves a launch (about 4 us; another 128 slots cost 0.6)
+    p.whole_rows = !P && C <= 512 && p.row_blocks == 1;
+    if (p.whole_rows) p.chunk_keys = 512;
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }
   p.blocks = rows <= 32 ? 1 : 4;
@@ -815,11 +867,12 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.B = B, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D, a.P = P, a.C = C;
   a.prefix_tiles = p.tiles, a.prefix_slices = p.slices, a.slice_keys = p.slice_keys;
   a.chunks = p.chunks, a.chunk_keys = std::max(1, p.chunk_keys), a.row_blocks = p.row_blocks;
+  a.whole_rows = p.whole_rows;
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
   const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.blocks), grid, a, stream);
-  if (st != TMAC_OK) return st;
+  if (st != TMAC_OK || p.whole_rows) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
                 ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);
 }

@@ -154,26 +154,32 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
   }
 }
 
-// Rows of keys and values into their slots: 64 slots of a sequence and head a workgroup, 8 bytes a lane.
-__global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
-  const int bh = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, b = bh / a.Hkv, h = bh % a.Hkv;
-  const int n = clamp_to(a.lens[bh], a.C), per_row = a.D / 4;
-  const int lo = block * 64, rows = min(64, n - lo);
-  if (rows <= 0) return;
-  int first;
-  source_tokens(a, b, h, first);
-  const int32_t* index = a.index + (int64_t)bh * a.C + lo;
+// Rows of keys and values into slots [lo, lo + rows), 8 bytes a lane; index: their tokens.
+template <int THREADS>
+__device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int first, const int32_t* index, int lo, int rows) {
+  const int per_row = a.D / 4;
   const char* ks = a.k_src + b * a.ks_seq + h * a.ks_head + first * a.ks_token;
   const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
   char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
   char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
 #pragma unroll 4
-  for (int x = threadIdx.x; x < rows * per_row; x += 256) {
+  for (int x = threadIdx.x; x < rows * per_row; x += THREADS) {
     const int row = x / per_row, at = (x - row * per_row) * 8;
     const int64_t i = index[row];
-    *reinterpret_cast<u2*>(kd + row * a.k_token + at) = *reinterpret_cast<const u2*>(ks + i * a.ks_token + at);
-    *reinterpret_cast<u2*>(vd + row * a.v_token + at) = *reinterpret_cast<const u2*>(vs + i * a.vs_token + at);
+    const u2 k = *reinterpret_cast<const u2*>(ks + i * a.ks_token + at), v = *reinterpret_cast<const u2*>(vs + i * a.vs_token + at);
+    *reinterpret_cast<u2*>(kd + row * a.k_token + at) = k;
+    *reinterpret_cast<u2*>(vd + row * a.v_token + at) = v;
   }
+}
+
+// 64 slots of a sequence and key head a workgroup.
+__global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
+  const int bh = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, b = bh / a.Hkv, h = bh % a.Hkv;
+  const int n = clamp_to(a.lens[bh], a.C), lo = block * 64, rows = min(64, n - lo);
+  if (rows <= 0) return;
+  int first;
+  source_tokens(a, b, h, first);
+  copy_rows<256>(a, b, h, first, a.index + (int64_t)bh * a.C + lo, lo, rows);
 }
 
 struct AppendArgs {
@@ -185,22 +191,41 @@ struct AppendArgs {
   int Hkv, D, C, recent;
 };
 
-// One workgroup a sequence and key head.
-__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
-  __shared__ uint64_t least[4];
+// One workgroup a sequence and key head, of 256 threads or, for more than 1024 slots, 1024 (4095 slots: 14.3 us with 256, most of it
+// waiting for one load after another).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs a) {
+  __shared__ uint64_t least[THREADS / 64];
   const int tid = threadIdx.x, bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
   const int n = clamp_to(a.lens[bh], a.C), seen = a.seen[bh];
   float* weight = a.weight + (int64_t)bh * a.C;
   int32_t* pos = a.pos + (int64_t)bh * a.C;
+  // the new rows, 8 bytes a thread: keys, then values
+  const int per_row = a.D / 4, at = (tid < per_row ? tid : tid - per_row) * 8;
+  u2 row = {0u, 0u};
+  if (tid < 2 * per_row)
+    row = *reinterpret_cast<const u2*>((tid < per_row ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head) + at);
+  // four slots a thread are on their way before it is known whether the cache is full
+  float w4[4];
+  int32_t p4[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = min(tid + j * THREADS, a.C - 1);
+    w4[j] = weight[i], p4[j] = pos[i];
+  }
   int slot = n;
   if (n == a.C) {
     const int64_t recent_from = (int64_t)seen + 1 - a.recent;
     uint64_t best = ~0ull;
-#pragma unroll 8
-    for (int i = tid; i < n; i += 256) {
-      const uint64_t x = (uint64_t)order_key(weight[i], pos[i] >= recent_from) << 32 | (uint32_t)i;
+    auto consider = [&](int i, float w, int32_t p) {
+      const uint64_t x = (uint64_t)order_key(w, p >= recent_from) << 32 | (uint32_t)i;
       best = x < best ? x : best;
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (tid + j * THREADS < n) consider(tid + j * THREADS, w4[j], p4[j]);
+#pragma unroll 4
+    for (int i = tid + 4 * THREADS; i < n; i += THREADS) consider(i, weight[i], pos[i]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       const uint64_t x = __shfl_xor((unsigned long long)best, o);
@@ -208,10 +233,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
     }
     if ((tid & 63) == 0) least[tid >> 6] = best;
     __syncthreads();
-    for (int i = 0; i < 4; ++i) best = least[i] < best ? least[i] : best;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) best = least[i] < best ? least[i] : best;
     slot = (int)(uint32_t)best;
   }
-  // (every thread has read the lengths and the slot before any of them is changed)
+  // (every thread has read the lengths and the slots before any of them is changed)
   __syncthreads();
   if (tid == 0) {
     weight[slot] = 0.0f;
@@ -219,11 +245,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
     a.seen[bh] = seen + 1;
     if (n < a.C) a.lens[bh] = n + 1;
   }
-  const int at = (tid & 127) * 8;
-  if (at < a.D * 2) {
-    if (tid < 128) *reinterpret_cast<u2*>(a.k + b * a.k_seq + h * a.k_head + slot * a.k_token + at) = *reinterpret_cast<const u2*>(a.k_new + b * a.kn_seq + h * a.kn_head + at);
-    else *reinterpret_cast<u2*>(a.v + b * a.v_seq + h * a.v_head + slot * a.v_token + at) = *reinterpret_cast<const u2*>(a.v_new + b * a.vn_seq + h * a.vn_head + at);
-  }
+  if (tid < 2 * per_row)
+    *reinterpret_cast<u2*>((tid < per_row ? a.k + b * a.k_seq + h * a.k_head + slot * a.k_token : a.v + b * a.v_seq + h * a.v_head + slot * a.v_token) + at) = row;
 }
 
 static bool cache_ok(const tmac_cache* c) {
@@ -302,5 +325,7 @@ extern "C" tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_vie
   a.k_seq = cache->k.seq * 2, a.k_token = cache->k.token * 2, a.k_head = cache->k.head * 2;
   a.v_seq = cache->v.seq * 2, a.v_token = cache->v.token * 2, a.v_head = cache->v.head * 2;
   a.Hkv = cache->Hkv, a.D = cache->D, a.C = cache->capacity, a.recent = cache->recent;
-  return cache::launch((const void*)cache_append_kernel, (int64_t)cache->B * cache->Hkv, 256, &a, stream);
+  const bool many = cache->capacity > 1024;
+  return cache::launch(many ? (const void*)cache_append_kernel<1024> : (const void*)cache_append_kernel<256>, (int64_t)cache->B * cache->Hkv,
+                       many ? 1024 : 256, &a, stream);
 }
