@@ -40,7 +40,7 @@ typedef struct {
 
 /* A tensor of rows of D consecutive elements, with strides in elements from sequence to sequence, token to token and head to
  * head (those that a call does not speak of are not read).  Data 8-byte aligned, strides multiples of 4 and not negative;
- * k and v are read fastest where data are 16-byte aligned and strides and D multiples of 8. */
+ * tmac_cache_fill moves rows fastest where data are 16-byte aligned and strides and D multiples of 8. */
 typedef struct {
   void*   data;
   int64_t seq, token, head;

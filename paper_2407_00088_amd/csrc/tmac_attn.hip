@@ -136,59 +136,73 @@ struct PromptArgs {
 
 __device__ __forceinline__ int clamp_to(int x, int most) { return x < 0 ? 0 : x > most ? most : x; }
 
-// Sequence and place in it of tile t of all sequences' tiles, those being ceil(n rows / per_tile) each; counted from the last
-// where `descending`.  False: there is no such tile.
+// Sum, and largest, of a number over the wavefront, in all lanes.
+template <bool MAX>
+__device__ __forceinline__ int over_wave(int x) {
+  auto with = [](int a, int b) { return MAX ? max(a, b) : a + b; };
+  // (lanes without a source keep 0, so the largest is of numbers that are not negative)
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // from 1, 2, 4, 8 lanes below in the row of 16
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // the last lane of the row below
+  x = with(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // lane 31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Sequence, and place in it, of unit t of all sequences' tiles, heaviest first: sequence s has as many tiles as its rows (`n` rows of `cu`,
+// G times) fill, tile i of which weighs i + (its keys before the first row) / (rows of a tile) / G or so.  Workgroups start in the order of their
+// units, and a heavy one that starts last is what all others wait for.
+// by_keys: the tiles are of keys, of which the first are the heaviest.  False: there is no such tile.
 struct Place {
-  int seq, tile, q0, nq;
+  int seq, tile, q0, nq, k0, nk;
 };
-__device__ __forceinline__ bool find_tile(const int32_t* cu, int S, int T, int G, int per_tile, int t, bool descending, Place& p) {
+__device__ __forceinline__ bool find_tile(const int32_t* cu_q, const int32_t* cu_k, int S, int Tq, int Tk, bool by_keys, int G, int per_tile, int t,
+                                          Place& p) {
+  auto extent = [](const int32_t* cu, int s, int T, int& at) {
+    at = clamp_to(cu[s], T);
+    return max(0, clamp_to(cu[s + 1], T) - at);
+  };
+  auto tiles_of = [&](int nq, int nk) { return (int)(((int64_t)(by_keys ? nk : nq) * G + per_tile - 1) / per_tile); };
   if (S == 1) {
     p.seq = 0;
-    p.q0 = clamp_to(cu[0], T);
-    p.nq = max(0, clamp_to(cu[1], T) - p.q0);
-    const int n = (int)(((int64_t)p.nq * G + per_tile - 1) / per_tile);
-    p.tile = descending ? n - 1 - t : t;
+    p.nq = extent(cu_q, 0, Tq, p.q0);
+    p.nk = extent(cu_k, 0, Tk, p.k0);
+    const int n = tiles_of(p.nq, p.nk);
+    p.tile = by_keys ? t : n - 1 - t;
     return t < n;
   }
   const int lane = threadIdx.x & 63;
-  auto tiles = [&](int s, int& q0, int& nq) {
-    q0 = nq = 0;
-    if (s < S) {
-      q0 = clamp_to(cu[s], T);
-      nq = max(0, clamp_to(cu[s + 1], T) - q0);
+  for (int s0 = 0; s0 < S; s0 += 64) {  // (heaviest first among each 64 sequences)
+    int q0 = 0, nq = 0, k0 = 0, nk = 0;
+    if (s0 + lane < S) {
+      nq = extent(cu_q, s0 + lane, Tq, q0);
+      nk = extent(cu_k, s0 + lane, Tk, k0);
     }
-    return (int)(((int64_t)nq * G + per_tile - 1) / per_tile);
-  };
-  int q0, nq;
-  if (descending) {
-    int total = 0;
-    for (int s = 0; s < S; s += 64) {
-      int n = tiles(s + lane, q0, nq);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-      total += n;
+    const int n = tiles_of(nq, nk), base = by_keys ? 0 : (int)((int64_t)max(0, nk - nq) * G / per_tile);
+    const int total = over_wave<false>(n);
+    if (t >= total) {
+      t -= total;
+      continue;
     }
-    if (t >= total) return false;
-    t = total - 1 - t;
-  }
-  for (int s = 0; s < S; s += 64) {
-    const int n = tiles(s + lane, q0, nq);
-    int incl = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(incl, o);
-      if (lane >= o) incl += x;
+    // the least level x of which at most t tiles lie above: count(x) = tiles of level x or more
+    auto count = [&](int x) { return over_wave<false>(min(n, max(0, n + base - x))); };
+    int lo = 0, hi = over_wave<true>(n ? n + base : 0);  // count(lo) > t, count(hi) = 0 <= t
+    int above = 0;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2, c = count(mid);
+      if (c > t) lo = mid;
+      else hi = mid, above = c;
     }
-    const int total = __shfl(incl, 63);
-    if (t < total) {
-      const int at = __builtin_ctzll(__ballot(t < incl));
-      p.seq = s + at;
-      p.tile = t - __shfl(incl - n, at);
-      p.q0 = __shfl(q0, at);
-      p.nq = __shfl(nq, at);
-      return true;
-    }
-    t -= total;
+    const uint64_t there = __ballot(lo >= base && lo < n + base);
+    const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0));
+    const int at = __builtin_ctzll(__ballot((there >> lane & 1) && rank == t - above));
+    p.seq = s0 + at;
+    p.q0 = __builtin_amdgcn_readlane(q0, at), p.nq = __builtin_amdgcn_readlane(nq, at);
+    p.k0 = __builtin_amdgcn_readlane(k0, at), p.nk = __builtin_amdgcn_readlane(nk, at);
+    const int level = lo - __builtin_amdgcn_readlane(base, at);
+    p.tile = by_keys ? __builtin_amdgcn_readlane(n, at) - 1 - level : level;
+    return true;
   }
   return false;
 }
@@ -228,12 +242,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
   head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
   const int z = unit % a.slices;
   Place p;
-  if (!find_tile(a.cu_q, a.S, a.Tq, a.G, 32 * BLOCKS, unit / a.slices, true, p)) return;
-  p.seq = __builtin_amdgcn_readfirstlane(p.seq);
-  p.tile = __builtin_amdgcn_readfirstlane(p.tile);
-  p.q0 = __builtin_amdgcn_readfirstlane(p.q0);
-  p.nq = __builtin_amdgcn_readfirstlane(p.nq);
-  const int k0 = clamp_to(a.cu_k[p.seq], a.Tk), nk = max(0, clamp_to(a.cu_k[p.seq + 1], a.Tk) - k0);
+  if (!find_tile(a.cu_q, a.cu_k, a.S, a.Tq, a.Tk, false, a.G, 32 * BLOCKS, unit / a.slices, p)) return;
+  const int k0 = p.k0, nk = p.nk;
   const int row0 = p.tile * 32 * BLOCKS, rows = p.nq * a.G, off = nk - p.nq;
   const Tile tile(p.tile, BLOCKS, wave, lane, rows);
   // the keys that any row of the tile sees, and this slice of them
@@ -525,11 +535,13 @@ struct WeightArgs {
   float scale;
 };
 
-// One workgroup: 128 keys of one sequence and key head, 32 a wavefront, which stay in registers as the second operand of
-// S = Q K^T; a lane owns a key and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
-template <typename T, int DP>
+// One workgroup: 128 KB keys of one sequence and key head, 32 KB a wavefront, which stay in registers as the second operand of
+// S = Q K^T; a lane owns a key (of each 32) and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
+// The exponentials bind (16 a lane for 8 products of 32 x 32 x 16), so the rest is kept away from the vector ALUs: with two blocks of keys
+// a wavefront the reads of q and of lse serve twice.
+template <typename T, int DP, int KB>
 __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
-  constexpr int SQ = 64, TILE = Layout<DP>::k_bytes(SQ), NT = DP / 16;
+  constexpr int SQ = 64, TILE = Layout<DP>::k_bytes(SQ), NT = DP / 16, KEYS = 128 * KB;
   __shared__ __align__(1024) char lds[2 * TILE];
   __shared__ __align__(16) float lse2[2][SQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
@@ -537,30 +549,29 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
   const int z = unit % a.slices;
   Place p;
-  if (!find_tile(a.cu_k, a.S, a.Tk, 1, 128, unit / a.slices, false, p)) return;
-  p.seq = __builtin_amdgcn_readfirstlane(p.seq);
-  p.tile = __builtin_amdgcn_readfirstlane(p.tile);
-  const int k0 = __builtin_amdgcn_readfirstlane(p.q0), nk = __builtin_amdgcn_readfirstlane(p.nq);
-  const int q0 = clamp_to(a.cu_q[p.seq], a.Tq), nq = max(0, clamp_to(a.cu_q[p.seq + 1], a.Tq) - q0);
+  if (!find_tile(a.cu_q, a.cu_k, a.S, a.Tq, a.Tk, true, 1, KEYS, unit / a.slices, p)) return;
+  const int k0 = p.k0, nk = p.nk, q0 = p.q0, nq = p.nq;
   const int off = nk - nq;                       // query i sees keys up to i + off
-  const int j = p.tile * 128 + wave * 32 + (lane & 31);
+  const int j0 = p.tile * KEYS + wave * 32 * KB;  // the wavefront's first key
   // queries that see the tile's first key, in stages of 64, head after head; this slice's share of the stages
-  const int first = a.causal ? min(nq, max(0, p.tile * 128 - off)) / SQ * SQ : 0;
+  const int first = a.causal ? min(nq, max(0, p.tile * KEYS - off)) / SQ * SQ : 0;
   const int stages = (nq - first + SQ - 1) / SQ;
   const int total = stages * a.G, from = (int)((int64_t)total * z / a.slices), to = (int)((int64_t)total * (z + 1) / a.slices);
-  typename T::v8 kf[NT];
-  {
+  typename T::v8 kf[KB][NT];
+#pragma unroll
+  for (int y = 0; y < KB; ++y) {
+    const int j = j0 + y * 32 + (lane & 31);
     const bool there = j < nk;
     const char* row = a.k + (int64_t)(k0 + (there ? j : 0)) * a.k_token + h * a.k_head;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       u2 x[2] = {{0u, 0u}, {0u, 0u}};
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int at = 16 * t + 8 * half + 4 * y;
-        if (there && at < a.D) x[y] = *reinterpret_cast<const u2*>(row + at * 2);
+      for (int i = 0; i < 2; ++i) {
+        const int at = 16 * t + 8 * half + 4 * i;
+        if (there && at < a.D) x[i] = *reinterpret_cast<const u2*>(row + at * 2);
       }
-      kf[t] = __builtin_bit_cast(typename T::v8, u4{x[0][0], x[0][1], x[1][0], x[1][1]});
+      kf[y][t] = __builtin_bit_cast(typename T::v8, u4{x[0][0], x[0][1], x[1][0], x[1][1]});
     }
   }
   const float c = a.scale * LOG2E;
@@ -570,51 +581,76 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   const Reads<DP> reads(lds0, 0, lane);
   float next_lse = 0.0f;
   u2 next_tail = {0u, 0u};
-  auto load = [&](int s, int buf) {
-    const int g = s / stages, i0 = first + (s - g * stages) * SQ, head = h * a.G + g;
+  auto load = [&](int g, int i0, int buf) {
+    const int head = h * a.G + g;
     const char* base = a.q + (int64_t)(q0 + i0) * a.q_token + head * a.q_head;
     qs.load(base, a.q_token, nq - i0, a.D, lds0 + buf * TILE, wave);
     next_tail = load_tail<SQ>(base, a.q_token, nq - i0, a.D, tid);
     if (tid < SQ) next_lse = i0 + tid < nq ? a.lse[(int64_t)head * a.Tq + q0 + i0 + tid] : -INFINITY;
   };
   // rows that are not there, or see nothing, give exp(s - inf) = 0
-  auto keep_lse = [&](int buf) {
+  auto settle = [&](int buf) {
     store_tail<DP, SQ>(next_tail, a.D, lds0 + buf * TILE, tid);
     if (tid < SQ) lse2[buf][tid] = next_lse == -INFINITY ? INFINITY : next_lse * LOG2E;
   };
-  float sum = 0.0f;
+  float sum[KB];
+#pragma unroll
+  for (int y = 0; y < KB; ++y) sum[y] = 0.0f;
+  int g = 0, i0 = 0;  // head and first query of the stage
   if (from < to) {
-    load(from, 0);
-    keep_lse(0);
+    g = from / stages;
+    i0 = first + (from - g * stages) * SQ;
+    load(g, i0, 0);
+    settle(0);
   }
   for (int s = from; s < to; ++s) {
     const int buf = (s - from) & 1;
+    const int now = i0;
     wait_stage();
-    if (s + 1 < to) load(s + 1, buf ^ 1);
-    const int i0 = first + (s % stages) * SQ;
-    const bool mask = a.causal && p.tile * 128 + wave * 32 + 31 > i0 + off;
+    i0 += SQ;
+    if (i0 >= nq) i0 = first, ++g;
+    if (s + 1 < to) load(g, i0, buf ^ 1);
+    const bool mask = a.causal && j0 + 32 * KB - 1 > now + off;
+    if (!(a.causal && j0 > now + SQ - 1 + off)) {  // (else no query of the stage sees a key of the wavefront)
 #pragma unroll
-    for (int b = 0; b < SQ / 32; ++b) {
-      f16x x = (f16x)(0.0f);
+      for (int b = 0; b < SQ / 32; ++b) {
+        f16x x[KB];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) x = T::mfma(read_k<T>(reads.k_at(t) + buf * TILE + b * (TILE / 2)), kf[t], x);
-      f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int y = 0; y < KB; ++y) x[y] = (f16x)(0.0f);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const f4 l = *reinterpret_cast<const f4*>(&lse2[buf][b * 32 + r * 8 + half * 4]);
+        for (int t = 0; t < NT; ++t) {
+          const auto q = read_k<T>(reads.k_at(t) + buf * TILE + b * (TILE / 2));
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * r + y], c, -l[y]));
-          if (mask) e = j <= i0 + b * 32 + r * 8 + half * 4 + y + off ? e : 0.0f;
-          part[y] += e;
+          for (int y = 0; y < KB; ++y) x[y] = T::mfma(q, kf[y][t], x[y]);
+        }
+        f4 l[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l[r] = *reinterpret_cast<const f4*>(&lse2[buf][b * 32 + r * 8 + half * 4]);
+#pragma unroll
+        for (int y = 0; y < KB; ++y) {
+          f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+          // (the lane's key is seen by the queries from this row of the block on)
+          const int seen_from = j0 + y * 32 + (lane & 31) - off - now - b * 32 - half * 4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[y][4 * r + i], c, -l[r][i]));
+              if (mask) e = r * 8 + i >= seen_from ? e : 0.0f;
+              part[i] += e;
+            }
+          sum[y] += (part[0] + part[1]) + (part[2] + part[3]);
         }
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
     }
-    if (s + 1 < to) keep_lse(buf ^ 1);
+    if (s + 1 < to) settle(buf ^ 1);
   }
-  sum = add_halves(sum);
-  if (half == 0 && j < nk) (a.slices > 1 ? a.part + ((int64_t)z * a.Hkv + h) * a.Tk : a.weight + (int64_t)h * a.Tk)[k0 + j] = sum;
+#pragma unroll
+  for (int y = 0; y < KB; ++y) {
+    const int j = j0 + y * 32 + (lane & 31);
+    const float x = add_halves(sum[y]);
+    if (half == 0 && j < nk) (a.slices > 1 ? a.part + ((int64_t)z * a.Hkv + h) * a.Tk : a.weight + (int64_t)h * a.Tk)[k0 + j] = x;
+  }
 }
 
 __global__ __launch_bounds__(256) void sum_weights_kernel(const float* part, float* weight, int64_t n, int slices) {
@@ -654,15 +690,23 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   return p;
 }
 
+#ifndef WB
+#define WB 8192
+#define WT 4
+#define WS 2
+#endif
 struct WeightsPlan {
-  int tiles, slices;
+  int blocks, tiles, slices;
   size_t bytes;
 };
 static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   WeightsPlan p;
-  p.tiles = (int)std::min<int64_t>(Tk / 128 + S, Tk);
-  const int64_t wgs = (int64_t)p.tiles * d->Hkv, stages = (int64_t)(Tq / S + 63) / 64 * (d->Hq / d->Hkv);
-  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({4 * WGS / wgs, stages / 4, 64}));
+  const int64_t stages = (int64_t)(Tq / S + 63) / 64 * (d->Hq / d->Hkv);
+  auto tiles_of = [&](int per) { return (int)std::min<int64_t>(Tk / per + S, Tk); };
+  p.blocks = (int64_t)tiles_of(256) * d->Hkv * stages >= WB ? 2 : 1;
+  p.tiles = tiles_of(128 * p.blocks);
+  const int64_t wgs = (int64_t)p.tiles * d->Hkv;
+  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WT * WGS / wgs, stages / WS, 64}));
   p.bytes = p.slices > 1 ? (size_t)p.slices * d->Hkv * Tk * 4 : 0;
   return p;
 }
@@ -728,8 +772,8 @@ static const void* decode_kernel(int blocks) {
   return blocks == 4 ? (const void*)attn_decode_kernel<T, DP, 4> : (const void*)attn_decode_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
-static const void* weights_kernel(int) {
-  return (const void*)attn_weights_kernel<T, DP>;
+static const void* weights_kernel(int blocks) {
+  return blocks == 2 ? (const void*)attn_weights_kernel<T, DP, 2> : (const void*)attn_weights_kernel<T, DP, 1>;
 }
 // Kernel for the type and the row length of a call, rows being padded to 64 or 128 elements in LDS.
 #define TMAC_PICK(f, d, blocks)                                                              \
@@ -809,7 +853,7 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
   const tmac_status st =
-      launch(TMAC_PICK(weights_kernel, desc, 0), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
+      launch(TMAC_PICK(weights_kernel, desc, p.blocks), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
   const int64_t n = (int64_t)desc->Hkv * Tk;
   int64_t n_arg = n;

@@ -19,6 +19,11 @@ inline bool rows_ok(const tmac_view* v, bool seq, bool token, bool head) {
 // 128 rows span more than a buffer's range.
 inline bool far_rows(const tmac_view* v) { return v->token >= ((int64_t)1 << 22); }
 
+// Rows that can be moved 16 bytes at a time.
+inline bool wide_rows(const tmac_view* v, int D) {
+  return (reinterpret_cast<uintptr_t>(v->data) & 15) == 0 && D % 8 == 0 && v->seq % 8 == 0 && v->token % 8 == 0 && v->head % 8 == 0;
+}
+
 }  // namespace attn
 }  // namespace tmac
 #endif

@@ -15,6 +15,7 @@ namespace tmac {
 namespace cache {
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t order_key(float weight, bool recent) {
   const uint32_t u = __builtin_bit_cast(uint32_t, weight != weight ? -INFINITY : weight + 0.0f);  // (-0 becomes 0)
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
   const bool holds = n <= HELD;
   auto key = [&](int i) { return holds ? held[i] : read_key(i); };
   if (holds) {
-#pragma unroll 4
+#pragma unroll 16
     for (int i = tid; i < n; i += 64 * WAVES) held[i] = read_key(i);
   }
   // the rank-th smallest key (from zero): what is left of `rank` counts equal keys
@@ -137,49 +138,66 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
   greater = equal = 0;
   for (int i = 0; i < wave; ++i) greater += count[i], equal += count[64 + i];
   uint32_t at = greater + (equal > leave ? equal - leave : 0);
-  for (int i = lo; i < hi; i += 64) {
-    const bool there = i + lane < hi;
-    const uint32_t x = there ? key(i + lane) : 0;
-    const uint64_t same = __ballot(there && x == prefix);
-    const bool stays = there && (x > prefix || (x == prefix && equal + below(same) >= leave));
-    const uint64_t mask = __ballot(stays);
-    if (stays) {
-      const int to = at + below(mask);
-      weight[to] = w[(i + lane) * a.ws_token];
-      pos[to] = position(i + lane);
-      index[to] = i + lane;
+  // eight times 64 tokens a turn, whose weights and positions are all on their way before the first is stored
+  constexpr int TURN = 8;
+  for (int i0 = lo; i0 < hi; i0 += 64 * TURN) {
+    float wt[TURN];
+    int32_t ps[TURN];
+#pragma unroll
+    for (int y = 0; y < TURN; ++y) {
+      const int i = min(i0 + 64 * y + lane, n - 1);
+      wt[y] = w[i * a.ws_token];
+      ps[y] = position(i);
     }
-    equal += __builtin_popcountll(same);
-    at += __builtin_popcountll(mask);
+#pragma unroll
+    for (int y = 0; y < TURN; ++y) {
+      const int i = i0 + 64 * y + lane;
+      const bool there = i < hi;
+      const uint32_t x = there ? key(i) : 0;
+      const uint64_t same = __ballot(there && x == prefix);
+      const bool stays = there && (x > prefix || (x == prefix && equal + below(same) >= leave));
+      const uint64_t mask = __ballot(stays);
+      if (stays) {
+        const int to = at + below(mask);
+        weight[to] = wt[y];
+        pos[to] = ps[y];
+        index[to] = i;
+      }
+      equal += __builtin_popcountll(same);
+      at += __builtin_popcountll(mask);
+    }
   }
 }
 
-// Rows of keys and values into slots [lo, lo + rows), 8 bytes a lane; index: their tokens.
-template <int THREADS>
+// Rows of keys and values into slots [lo, lo + rows), Unit by Unit, past the caches: every byte is read once and written once.
+// index: their tokens.
+template <typename Unit>
 __device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int first, const int32_t* index, int lo, int rows) {
-  const int per_row = a.D / 4;
+  const int per_row = a.D * 2 / (int)sizeof(Unit);
   const char* ks = a.k_src + b * a.ks_seq + h * a.ks_head + first * a.ks_token;
   const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
   char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
   char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
 #pragma unroll 4
-  for (int x = threadIdx.x; x < rows * per_row; x += THREADS) {
-    const int row = x / per_row, at = (x - row * per_row) * 8;
+  for (int x = threadIdx.x; x < rows * per_row; x += 256) {
+    const int row = x / per_row, at = (x - row * per_row) * (int)sizeof(Unit);
     const int64_t i = index[row];
-    const u2 k = *reinterpret_cast<const u2*>(ks + i * a.ks_token + at), v = *reinterpret_cast<const u2*>(vs + i * a.vs_token + at);
-    *reinterpret_cast<u2*>(kd + row * a.k_token + at) = k;
-    *reinterpret_cast<u2*>(vd + row * a.v_token + at) = v;
+    const Unit k = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(ks + i * a.ks_token + at));
+    const Unit v = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(vs + i * a.vs_token + at));
+    __builtin_nontemporal_store(k, reinterpret_cast<Unit*>(kd + row * a.k_token + at));
+    __builtin_nontemporal_store(v, reinterpret_cast<Unit*>(vd + row * a.v_token + at));
   }
 }
 
 // 64 slots of a sequence and key head a workgroup.
+template <typename Unit>
 __global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
   const int bh = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, b = bh / a.Hkv, h = bh % a.Hkv;
   const int n = clamp_to(a.lens[bh], a.C), lo = block * 64, rows = min(64, n - lo);
   if (rows <= 0) return;
   int first;
   source_tokens(a, b, h, first);
-  copy_rows<256>(a, b, h, first, a.index + (int64_t)bh * a.C + lo, lo, rows);
+  copy_rows<Unit>(a, b, h, first, a.index + (int64_t)bh * a.C + lo, lo, rows);
 }
 
 struct AppendArgs {
@@ -309,7 +327,9 @@ extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache
   const int64_t bh = (int64_t)B * cache->Hkv;
   if (bh * a.blocks > 0x7fffffff) return TMAC_EUNSUPPORTED;
   const tmac_status st = cache::launch((const void*)cache_select_kernel, bh, 64 * WAVES, &a, stream);
-  return st != TMAC_OK ? st : cache::launch((const void*)cache_copy_kernel, bh * a.blocks, 256, &a, stream);
+  if (st != TMAC_OK) return st;
+  const bool wide = attn::wide_rows(&src->k, a.D) && attn::wide_rows(&src->v, a.D) && attn::wide_rows(&cache->k, a.D) && attn::wide_rows(&cache->v, a.D);
+  return cache::launch(wide ? (const void*)cache_copy_kernel<u4> : (const void*)cache_copy_kernel<u2>, bh * a.blocks, 256, &a, stream);
 }
 
 extern "C" tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_view* k, const tmac_view* v, void* stream) {
