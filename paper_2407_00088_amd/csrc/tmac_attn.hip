@@ -106,10 +106,20 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
   }
 }
 
-// The lane's row as the first product's operand; rows that do not exist and columns from D on are zeros.
+// The lane's row as the first product's operand; rows that do not exist and columns from D on are zeros.  wide: 16 bytes at a time.
 template <typename T, int DP>
-__device__ __forceinline__ void load_q(Rows<T, DP>& w, const char* row, bool exists, int D, int lane) {
+__device__ __forceinline__ void load_q(Rows<T, DP>& w, const char* row, bool exists, int D, int lane, bool wide) {
   const int half = lane >> 5;
+  if (wide) {
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) {
+      const int at = 16 * t + 8 * half;
+      u4 x = {0u, 0u, 0u, 0u};
+      if (exists && at < D) x = *reinterpret_cast<const u4*>(row + at * 2);
+      w.q[t] = __builtin_bit_cast(typename T::v8, x);
+    }
+    return;
+  }
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t) {
     u2 x[2] = {{0u, 0u}, {0u, 0u}};
@@ -131,6 +141,7 @@ struct PromptArgs {
   float *lse, *part, *ml;
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;  // bytes
   int S, Tq, Tk, Hq, Hkv, G, D, causal, tiles, slices;
+  int q_wide;  // rows of q that are read 16 bytes at a time
   float scale;
 };
 
@@ -266,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
   lim.most = any ? min(keys.end, sees(tile.last)) : 0;
   lim.row = exists ? min(keys.end, sees(tile.row)) : keys.end;
   const int i = exists ? tile.row / a.G : 0, head = h * a.G + (exists ? tile.row - i * a.G : 0);
-  load_q(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane);
+  load_q(w, a.q + (int64_t)(p.q0 + i) * a.q_token + head * a.q_head, exists, a.D, lane, a.q_wide);
   if (exists) {
     const int64_t token = p.q0 + i, slot = ((int64_t)z * a.Tq + token) * a.Hq + head;
     to.out = a.out + token * a.o_token + head * a.o_head;
@@ -297,6 +308,8 @@ struct DecodeArgs {
   int B, Hq, Hkv, G, D, P, C;
   int prefix_tiles, prefix_slices, slice_keys;  // row tiles and slices of the prefix, keys of a slice
   int chunks, chunk_keys, row_blocks;           // of the caches: chunks of a whole one, keys of a chunk, blocks of 32 heads of a group
+  int q_wide;                                   // rows of q that are read 16 bytes at a time
+  int once;                                     // the caches are more than the chip's own caches hold
   int whole_rows;                               // no prefix, and a whole cache in one chunk: nothing is joined
   int weight_blocks;                            // of the joining kernel: blocks of 1024 slots
   float scale;
@@ -359,7 +372,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     keys.begin = z * a.slice_keys;
     keys.end = min(a.P, keys.begin + a.slice_keys);
     Rows<T, DP> w;
-    load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);
+    load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane, a.q_wide);
     Target to = {};
     if (exists) {
       const int64_t row = (int64_t)b * a.Hq + head, slot = (int64_t)z * a.B * a.Hq + row;
@@ -383,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   const int head = h * a.G + (exists ? g : 0);
   const int64_t row = (int64_t)b * a.Hq + head;
   Rows<T, DP> w;
-  load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane);  // (on its way while the length is)
+  load_q(w, a.q + b * a.q_seq + head * a.q_head, exists, a.D, lane, a.q_wide);  // (on its way while the length is)
   const int n = slots_in_use(a, b, h);
   keys.begin = chunk * a.chunk_keys;
   keys.end = min(n, keys.begin + a.chunk_keys);
@@ -392,6 +405,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   keys.v_stride = a.v_token;
   keys.k = a.k + b * a.k_seq + h * a.k_head;
   keys.v = a.v + b * a.v_seq + h * a.v_head;
+  keys.once = a.once;
   // the group's rows of scores from this chunk on, in one range (the entry point keeps it below 2^31 bytes)
   Scores scores{};
   if (a.scores) {
@@ -557,25 +571,29 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   const int first = a.causal ? min(nq, max(0, p.tile * KEYS - off)) / SQ * SQ : 0;
   const int stages = (nq - first + SQ - 1) / SQ;
   const int total = stages * a.G, from = (int)((int64_t)total * z / a.slices), to = (int)((int64_t)total * (z + 1) / a.slices);
-  typename T::v8 kf[KB][NT];
-#pragma unroll
-  for (int y = 0; y < KB; ++y) {
-    const int j = j0 + y * 32 + (lane & 31);
-    const bool there = j < nk;
-    const char* row = a.k + (int64_t)(k0 + (there ? j : 0)) * a.k_token + h * a.k_head;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      u2 x[2] = {{0u, 0u}, {0u, 0u}};
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = 16 * t + 8 * half + 4 * i;
-        if (there && at < a.D) x[i] = *reinterpret_cast<const u2*>(row + at * 2);
-      }
-      kf[y][t] = __builtin_bit_cast(typename T::v8, u4{x[0][0], x[0][1], x[1][0], x[1][1]});
-    }
-  }
   const float c = a.scale * LOG2E;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(TMAC_LDS char*)lds;
+  // The keys pass through the room of the queries, a wavefront's 32 at a time in a quarter of it: as rows, which memory gives whole (read
+  // 8 bytes here and there by the lanes that need them they took 10 of a small call's 19 us).
+  typename T::v8 kf[KB][NT];
+  {
+    const Stage<DP, 32, 1, false> ks(a.k_token, a.D, wave, lane);
+    const uint32_t mine = lds0 + wave * Layout<DP>::k_bytes(32);
+    const Reads<DP> reads(mine, 0, lane);
+#pragma unroll
+    for (int y = 0; y < KB; ++y) {
+      const char* base = a.k + (int64_t)(k0 + min(nk, j0 + y * 32)) * a.k_token + h * a.k_head;
+      const int there = nk - j0 - y * 32;
+      ks.load(base, a.k_token, there, a.D, mine, wave);
+      const u2 tail = load_tail<32>(base, a.k_token, there, a.D, lane);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      store_tail<DP, 32>(tail, a.D, mine, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) kf[y][t] = read_k<T>(reads.k_at(t));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+  __syncthreads();
   clear_pads<DP>(a.D, lds0, 2 * TILE, tid);
   const Stage<DP, SQ, 4, false> qs(a.q_token, a.D, wave, lane);
   const Reads<DP> reads(lds0, 0, lane);
@@ -819,6 +837,7 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
   a.v_token = v->token * 2, a.v_head = v->head * 2, a.o_token = out->token * 2, a.o_head = out->head * 2;
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
+  a.q_wide = wide_rows(q, desc->D);
   const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, p.blocks), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>,
@@ -912,6 +931,9 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.prefix_tiles = p.tiles, a.prefix_slices = p.slices, a.slice_keys = p.slice_keys;
   a.chunks = p.chunks, a.chunk_keys = std::max(1, p.chunk_keys), a.row_blocks = p.row_blocks;
   a.whole_rows = p.whole_rows;
+  a.q_wide = wide_rows(q, desc->D);
+  // (24 caches of 4095 slots, 400 MB: 107 us a step where they are kept, 99.6 where they are not; a prefix of 42 MB 11.6 and 14.3)
+  a.once = (int64_t)B * desc->Hkv * C * desc->D * 4 > (256 << 20);
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;

@@ -85,6 +85,7 @@ struct Keys {
   const char* v;
   int64_t k_stride, v_stride;  // bytes from row to row
   int begin, end;
+  bool once;                   // read once, and more of them in a call than the caches hold (run_streams with SCORES only)
 };
 
 // Rows of 16-bit elements on their way from memory to LDS: 1024 bytes a load of one wavefront, lane after lane, without passing
@@ -95,19 +96,18 @@ struct Keys {
 //
 // The load is written out: of the builtin the compiler knows only that it writes LDS, and makes every transposed read wait
 // for it, although that is another stage.  It has no result register; wait_stage waits for it.
-// ONCE: nobody else reads these bytes, so they are not kept in L2 (a batch's caches of 400 MB: 107 us a step without, 99.6 with).
-template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(u4 rsrc, uint32_t lds, uint32_t offset, uint32_t scalar_offset) {
-  if constexpr (ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
-                 :
-                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(scalar_offset))
-                 : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :
-                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(scalar_offset))
-                 : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(scalar_offset))
+               : "memory");
+}
+// The same for bytes that nobody reads again soon.
+__device__ __forceinline__ void load_to_lds_once(u4 rsrc, uint32_t lds, uint32_t offset, uint32_t scalar_offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(scalar_offset))
+               : "memory");
 }
 __device__ __forceinline__ u4 buffer_of(const char* base, int range) {
   const uint64_t at = (uint64_t)base;
@@ -115,7 +115,7 @@ __device__ __forceinline__ u4 buffer_of(const char* base, int range) {
             (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x00020000u};
 }
 // WAVES wavefronts share the ROWS rows, or each loads rows of its own (WAVES = 1).
-template <int DP, int ROWS, int WAVES, bool IS_V, bool ONCE = false>
+template <int DP, int ROWS, int WAVES, bool IS_V>
 struct Stage {
   typedef Layout<DP> L;
   static constexpr int N = ROWS / (WAVES * L::RPI), APART = IS_V ? 1024 : 1088;
@@ -130,19 +130,24 @@ struct Stage {
   // Rows from `rows` on read as zeros: the descriptor's range ends there.  (What a scalar register adds to the address is not
   // checked against the range, so it is used for whole stages only.)  Unwanted chunks stay as they are where wavefronts share a
   // stage, and become zeros where they do not: such a load is always issued, so that loads can be counted.
-  __device__ __forceinline__ void load(const char* base, int64_t stride, int rows, int D, uint32_t lds, int wave) const {
+  __device__ __forceinline__ void load(const char* base, int64_t stride, int rows, int D, uint32_t lds, int wave, bool once = false) const {
     if (WAVES != 1 && !wanted) return;
     const uint32_t offset = wanted ? at : 0x7fffff00u;
     const int step = WAVES * L::RPI * (int)stride;
     if (WAVES != 1) lds += wave * APART;
     if (rows >= ROWS) {
       const u4 rsrc = buffer_of(base, (ROWS - 1) * (int)stride + D * 2);
+      if (once) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) load_to_lds<ONCE>(rsrc, lds + i * WAVES * APART, offset, i * step);
+        for (int i = 0; i < N; ++i) load_to_lds_once(rsrc, lds + i * WAVES * APART, offset, i * step);
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_to_lds(rsrc, lds + i * WAVES * APART, offset, i * step);
     } else {
       const int range = rows > 0 ? (rows - 1) * (int)stride + D * 2 : 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) load_to_lds<ONCE>(buffer_of(base + i * (int64_t)step, max(0, range - i * step)), lds + i * WAVES * APART, offset, 0);
+      for (int i = 0; i < N; ++i) load_to_lds(buffer_of(base + i * (int64_t)step, max(0, range - i * step)), lds + i * WAVES * APART, offset, 0);
     }
   }
 };
@@ -463,15 +468,15 @@ __device__ __forceinline__ void run_shared(Rows<T, DP>& w, const Keys& keys, int
 
 // All keys of a unit where every wavefront streams tiles of its own, 32 keys each, every fourth: a tile of K is requested as soon as
 // the one before has met q, one of V as soon as the one before has met the exponentials, and nobody waits for anybody.
-// OWN: a cache, which only this unit reads, and which keeps its scores where `scores` says.
-template <typename T, int DP, bool OWN, bool CAREFUL>
+// SCORES: a cache, which keeps its scores where `scores` says.
+template <typename T, int DP, bool SCORES, bool CAREFUL>
 __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, int D, float c, const Limits& lim, char* shared, const Scores& scores) {
   constexpr int KT = 32, KB = Layout<DP>::k_bytes(KT), VB = Layout<DP>::v_bytes(KT);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)shared + wave * (KB + VB), lds_v = lds + KB;
   clear(w);
-  const Stage<DP, KT, 1, false, OWN> ks(keys.k_stride, D, wave, lane);
-  const Stage<DP, KT, 1, true, OWN> vs(keys.v_stride, D, wave, lane);
+  const Stage<DP, KT, 1, false> ks(keys.k_stride, D, wave, lane);
+  const Stage<DP, KT, 1, true> vs(keys.v_stride, D, wave, lane);
   constexpr int LOADS = Stage<DP, KT, 1, false>::N;
   const Reads<DP> reads(lds, lds_v, lane);
   const int end = min(keys.end, lim.most);
@@ -480,16 +485,16 @@ __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, in
   u2 tail;
   auto load_k = [&](int i) {
     const char* base = keys.k + (int64_t)i * keys.k_stride;
-    ks.load(base, keys.k_stride, keys.end - i, D, lds, wave);
+    ks.load(base, keys.k_stride, keys.end - i, D, lds, wave, SCORES && keys.once);
     tail = load_tail<KT>(base, keys.k_stride, keys.end - i, D, lane);
   };
-  auto load_v = [&](int i) { vs.load(keys.v + (int64_t)i * keys.v_stride, keys.v_stride, keys.end - i, D, lds_v, wave); };
+  auto load_v = [&](int i) { vs.load(keys.v + (int64_t)i * keys.v_stride, keys.v_stride, keys.end - i, D, lds_v, wave, SCORES && keys.once); };
   load_k(at);
   load_v(at);
   bool stored = false;  // the tile before left scores, four stores after V's loads
   while (true) {
     // K has landed: V's loads, and stores of scores, are younger
-    if (OWN && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + 4) : "memory");
+    if (SCORES && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + 4) : "memory");
     else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
     store_tail<DP, KT>(tail, D, lds, lane);
     f16x s = scores_of(w, reads, 0);
@@ -513,7 +518,7 @@ __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, in
     else multiply_v<T, DP, 32>(w, reads, p);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (next < end) load_v(next);
-    if (OWN && scores.base) {
+    if (SCORES && scores.base) {
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(scores.base, (short)0, scores.range, 0x00020000);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {

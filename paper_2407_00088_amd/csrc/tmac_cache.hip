@@ -48,15 +48,37 @@ __device__ __forceinline__ int source_tokens(const FillArgs& a, int b, int h, in
 }
 
 constexpr int WAVES = 16, DIGIT = 2048, HELD = 32768;  // keys that LDS holds
+constexpr int COPIED = 1024;                           // slots whose rows the selecting workgroup copies itself
 
 // Number of set bits of `mask` below the lane.
 __device__ __forceinline__ int below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
+// Rows of keys and values into slots [lo, lo + rows), Unit by Unit, past the caches: every byte is read once and written once.
+// index: their tokens.
+template <typename Unit, int THREADS>
+__device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int first, const int32_t* index, int lo, int rows) {
+  const int per_row = a.D * 2 / (int)sizeof(Unit);
+  const char* ks = a.k_src + b * a.ks_seq + h * a.ks_head + first * a.ks_token;
+  const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
+  char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
+  char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
+#pragma unroll 4
+  for (int x = threadIdx.x; x < rows * per_row; x += THREADS) {
+    const int row = x / per_row, at = (x - row * per_row) * (int)sizeof(Unit);
+    const int64_t i = index[row];
+    const Unit k = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(ks + i * a.ks_token + at));
+    const Unit v = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(vs + i * a.vs_token + at));
+    __builtin_nontemporal_store(k, reinterpret_cast<Unit*>(kd + row * a.k_token + at));
+    __builtin_nontemporal_store(v, reinterpret_cast<Unit*>(vd + row * a.v_token + at));
+  }
+}
+
 // Which tokens of one sequence and head stay: the (n - C)-th smallest key is found digit by digit (11, 11 and 10 bits, counted
 // in LDS), then every wavefront numbers the staying tokens of its run.  Writes weights, positions and the tokens' places in
 // the source for the copy.
+template <bool COPIES, typename Unit>
 __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs a) {
   __shared__ uint32_t held[HELD];
   __shared__ uint32_t count[DIGIT];
@@ -70,19 +92,28 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
   const float* w = a.w_src + b * a.ws_seq + h * a.ws_head + first * a.ws_token;
   const int32_t* p = a.pos_src ? a.pos_src + b * a.ps_seq + h * a.ps_head + first * a.ps_token : nullptr;
   auto position = [&](int i) { return p ? p[i * a.ps_token] : i; };
-  int32_t* index = a.index + (int64_t)bh * a.C;
+  // the tokens' places: for the copying launch, or, where this workgroup copies its rows itself, in LDS
+  __shared__ int32_t kept[COPIES ? COPIED : 1];
+  int32_t* index = COPIES ? kept : a.index + (int64_t)bh * a.C;
   float* weight = a.weight + (int64_t)bh * a.C;
   int32_t* pos = a.pos + (int64_t)bh * a.C;
   if (tid == 0) {
     a.lens[bh] = keep;
     a.seen[bh] = seen;
   }
+  auto copy = [&] {
+    if constexpr (COPIES) {
+      __syncthreads();
+      copy_rows<Unit, 64 * WAVES>(a, b, h, first, kept, 0, keep);
+    }
+  };
   if (n <= a.C) {
     for (int i = tid; i < n; i += 64 * WAVES) {
       weight[i] = w[i * a.ws_token];
       pos[i] = position(i);
       index[i] = i;
     }
+    copy();
     return;
   }
   auto read_key = [&](int i) { return order_key(w[i * a.ws_token], (int64_t)position(i) >= (int64_t)seen - a.recent); };
@@ -145,12 +176,14 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
     int32_t ps[TURN];
 #pragma unroll
     for (int y = 0; y < TURN; ++y) {
+      if (i0 + 64 * y >= hi) break;
       const int i = min(i0 + 64 * y + lane, n - 1);
       wt[y] = w[i * a.ws_token];
       ps[y] = position(i);
     }
 #pragma unroll
     for (int y = 0; y < TURN; ++y) {
+      if (i0 + 64 * y >= hi) break;
       const int i = i0 + 64 * y + lane;
       const bool there = i < hi;
       const uint32_t x = there ? key(i) : 0;
@@ -167,26 +200,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
       at += __builtin_popcountll(mask);
     }
   }
-}
-
-// Rows of keys and values into slots [lo, lo + rows), Unit by Unit, past the caches: every byte is read once and written once.
-// index: their tokens.
-template <typename Unit>
-__device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int first, const int32_t* index, int lo, int rows) {
-  const int per_row = a.D * 2 / (int)sizeof(Unit);
-  const char* ks = a.k_src + b * a.ks_seq + h * a.ks_head + first * a.ks_token;
-  const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
-  char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
-  char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
-#pragma unroll 4
-  for (int x = threadIdx.x; x < rows * per_row; x += 256) {
-    const int row = x / per_row, at = (x - row * per_row) * (int)sizeof(Unit);
-    const int64_t i = index[row];
-    const Unit k = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(ks + i * a.ks_token + at));
-    const Unit v = __builtin_nontemporal_load(reinterpret_cast<const Unit*>(vs + i * a.vs_token + at));
-    __builtin_nontemporal_store(k, reinterpret_cast<Unit*>(kd + row * a.k_token + at));
-    __builtin_nontemporal_store(v, reinterpret_cast<Unit*>(vd + row * a.v_token + at));
-  }
+  copy();
 }
 
 // 64 slots of a sequence and key head a workgroup.
@@ -197,7 +211,7 @@ __global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
   if (rows <= 0) return;
   int first;
   source_tokens(a, b, h, first);
-  copy_rows<Unit>(a, b, h, first, a.index + (int64_t)bh * a.C + lo, lo, rows);
+  copy_rows<Unit, 256>(a, b, h, first, a.index + (int64_t)bh * a.C + lo, lo, rows);
 }
 
 struct AppendArgs {
@@ -326,9 +340,13 @@ extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache
   a.blocks = (cache->capacity + 63) / 64;
   const int64_t bh = (int64_t)B * cache->Hkv;
   if (bh * a.blocks > 0x7fffffff) return TMAC_EUNSUPPORTED;
-  const tmac_status st = cache::launch((const void*)cache_select_kernel, bh, 64 * WAVES, &a, stream);
-  if (st != TMAC_OK) return st;
   const bool wide = attn::wide_rows(&src->k, a.D) && attn::wide_rows(&src->v, a.D) && attn::wide_rows(&cache->k, a.D) && attn::wide_rows(&cache->v, a.D);
+  // Small caches are copied by the workgroup that selects, which saves a launch (96 caches of 256 slots of 100 elements: 16.3 -> FUSED us in all);
+  // beyond 256 KB of keys and values one workgroup's copy takes longer than that, the more so where there are few.
+  if (cache->capacity <= COPIED && (int64_t)cache->capacity * a.D * 4 <= 262144)
+    return cache::launch(wide ? (const void*)cache_select_kernel<true, u4> : (const void*)cache_select_kernel<true, u2>, bh, 64 * WAVES, &a, stream);
+  const tmac_status st = cache::launch((const void*)cache_select_kernel<false, u2>, bh, 64 * WAVES, &a, stream);
+  if (st != TMAC_OK) return st;
   return cache::launch(wide ? (const void*)cache_copy_kernel<u4> : (const void*)cache_copy_kernel<u2>, bh * a.blocks, 256, &a, stream);
 }
 
