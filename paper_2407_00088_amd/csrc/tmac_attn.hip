@@ -750,7 +750,7 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
     }
     // a short cache in one chunk has nothing to join, which saves a launch (about 4 us; another 128 slots cost 0.6)
     p.whole_rows = !P && C <= 512 && p.row_blocks == 1;
-    if (p.whole_rows) p.chunk_keys = 512;
+    if (p.whole_rows) p.chunk_keys = (C + 127) / 128 * 128;
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }
   p.blocks = rows <= 32 ? 1 : 4;
