@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "tmac_attn.h"
 #include "tmac_attn_core.h"
@@ -628,8 +629,10 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
     i0 += SQ;
     if (i0 >= nq) i0 = first, ++g;
     if (s + 1 < to) load(g, i0, buf ^ 1);
-    const bool mask = a.causal && j0 + 32 * KB - 1 > now + off;
-    if (!(a.causal && j0 > now + SQ - 1 + off)) {  // (else no query of the stage sees a key of the wavefront)
+    // some query does not see some key, or is not there (zeros times an infinite key would be NaN)
+    const bool mask = (a.causal && j0 + 32 * KB - 1 > now + off) || now + SQ > nq;
+    // the stage's part of the sums; masked: as a stage of its own, which the others are not to pay for
+    auto add = [&](auto masked) {
 #pragma unroll
       for (int b = 0; b < SQ / 32; ++b) {
         f16x x[KB];
@@ -647,19 +650,24 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
 #pragma unroll
         for (int y = 0; y < KB; ++y) {
           f4 part = {0.0f, 0.0f, 0.0f, 0.0f};
-          // (the lane's key is seen by the queries from this row of the block on)
-          const int seen_from = j0 + y * 32 + (lane & 31) - off - now - b * 32 - half * 4;
+          // (the lane's key is seen by the queries from one row of the block on, up to the last)
+          const int row0 = now + b * 32 + half * 4, seen_from = a.causal ? j0 + y * 32 + (lane & 31) - off - row0 : 0, last = nq - row0;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[y][4 * r + i], c, -l[r][i]));
-              if (mask) e = r * 8 + i >= seen_from ? e : 0.0f;
+              if constexpr (masked) e = r * 8 + i >= seen_from && r * 8 + i < last ? e : 0.0f;
               part[i] += e;
             }
           sum[y] += (part[0] + part[1]) + (part[2] + part[3]);
         }
       }
+    };
+    if (mask) {
+      if (!(a.causal && j0 > now + SQ - 1 + off)) add(std::true_type{});  // (else no query of the stage sees a key of the wavefront)
+    } else {
+      add(std::false_type{});
     }
     if (s + 1 < to) settle(buf ^ 1);
   }

@@ -108,6 +108,22 @@ def test_nothing_to_do(A):
     assert (out == 0).all() and (lse == -math.inf).all() and (cache.weight == 0).all()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_infinite_keys_that_nobody_attends_to_have_no_weight(A, causal):
+    """Keys at which every query's score is -inf: exactly nothing, whatever the kernels put in the place of queries that are not there."""
+    n, D = 37, 64
+    q, k = rand(1, n, 2, D), rand(2, n, 1, D)
+    q[:, :, 7] = q[:, :, 7].abs() + 0.5
+    k[[3, 20], :, 7] = -math.inf
+    c = i32([0, n])
+    out, lse = A.attn_prompt(q.cuda(), k.cuda(), rand(3, n, 1, D).cuda(), c, causal=causal)
+    w = A.attn_weights(q.cuda(), k.cuda(), lse, c, causal=causal)
+    want = ref.prompt(q, k, rand(3, n, 1, D), [0, n], [0, n], causal, 1 / 8)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert (w[0, [3, 20]] == 0).all() and torch.isfinite(w).all()
+    assert torch.allclose(w.double().cpu(), want[2], rtol=1e-4)
+
+
 def test_a_workspace_that_grows_does_not_disturb_an_earlier_call(A):
     """Larger and larger prefixes in a row, without a wait between the calls."""
     cache, k, v = filled(A, 2, 8, 2, 64, 60, [[60, 60], [7, 0]], BF16)
