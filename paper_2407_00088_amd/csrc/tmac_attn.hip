@@ -342,6 +342,9 @@ __device__ __forceinline__ f4 sum_weights(const float* scores, int64_t stride, i
   return sum;
 }
 
+// A whole cache in one chunk: at most so many slots, and the scores of at most so many rows in LDS.
+constexpr int WHOLE = 512, LDS_ROWS = 4;
+
 // Workgroups of the prefix (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys) and of the caches (one sequence
 // and key head, one chunk of its slots), the former, longer ones first (mixed, 4 rows over 2047 keys took 13.9 instead of 11.7 us).  Every one
 // leaves a part of its rows; where a row has only one, finished rows and, with accumulate, the slots' weights.
@@ -352,6 +355,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   constexpr int LDS = ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS;
   __shared__ __align__(1024) char lds[LDS];
   __shared__ float row_lse[32];
+  __shared__ __align__(16) float row_scores[LDS_ROWS * WHOLE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = a.scale * LOG2E;
   Keys keys;
@@ -409,13 +413,22 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   keys.once = a.once;
   // the group's rows of scores from this chunk on, in one range (the entry point keeps it below 2^31 bytes)
   Scores scores{};
-  if (a.scores) {
+  const bool in_lds_rows = a.whole_rows && a.G <= LDS_ROWS;
+  if (a.scores && in_lds_rows) {
+    if (exists) scores.lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)(char*)(row_scores + g * WHOLE);
+  } else if (a.scores) {
     const int64_t from = ((int64_t)b * a.Hq + h * a.G + block * 32) * a.score_stride + keys.begin;
     const int rows = min(32, a.G - block * 32);
     scores.base = a.scores + from;
     scores.range = (int)(((rows - 1) * a.score_stride + a.chunk_keys) * 4);
     scores.offset = exists ? (uint32_t)((lane & 31) * a.score_stride * 4) : 0x7fff0000u;
   }
+  // (whole rows with weights: the old ones are on their way early; a thread has four slots of at most 512)
+  const int slot0 = threadIdx.x * 4;
+  float* weight = a.whole_rows && a.scores ? a.weight + ((int64_t)b * a.Hkv + h) * a.C + slot0 : nullptr;
+  float old[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) old[j] = weight && slot0 + j < n ? weight[j] : 0.0f;
   run_streams<T, DP, true, false>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
   Target to = {};
   if (exists) {
@@ -426,18 +439,24 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     to.ml = a.ml + slot * 2;
   }
   finish<T, DP, 1>(w, to, !a.whole_rows, a.D, lds, row_lse);
-  if (!a.whole_rows || !a.scores) return;
+  if (!weight || slot0 >= n) return;
   // (the scores have been written by this workgroup: all are past the barriers of `finish`)
-  for (int at = threadIdx.x * 4; at < n; at += 1024) {
-    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G) * a.score_stride + at;
+  f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (in_lds_rows) {
+    for (int y = 0; y < a.G; ++y) {
+      const f4 x = *reinterpret_cast<const f4*>(row_scores + y * WHOLE + slot0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -row_lse[y]));
+    }
+  } else {
+    const float* s = a.scores + ((int64_t)b * a.Hq + h * a.G) * a.score_stride + slot0;
     f4 x[AHEAD];
     request_scores(s, a.score_stride, a.G, x);
-    const f4 sum = sum_weights(s, a.score_stride, a.G, x, row_lse, c);
-    float* weight = a.weight + ((int64_t)b * a.Hkv + h) * a.C + at;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (at + j < n) weight[j] += sum[j];
+    sum = sum_weights(s, a.score_stride, a.G, x, row_lse, c);
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (slot0 + j < n) weight[j] = old[j] + sum[j];
 }
 
 // --- parts of rows ------------------------------------------------------------------------------------------------------------
@@ -716,11 +735,10 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   return p;
 }
 
-#ifndef WB
-#define WB 8192
-#define WT 4
-#define WS 2
-#endif
+// Blocks of 32 keys a wavefront: two, once that leaves enough units (each key tile's stages) for the chip; the reads of q then serve twice
+// (6144 tokens, 64 heads in groups of 8: 411 us with one, 355 with two; five prompts of up to 777 tokens 19.4 and 25).  Slices of a tile's
+// stages: until there are four times the workgroups that the chip holds, because tiles weigh unlike (608 us with twice, 411 with four times, 388
+// with eight times at one block, 376, 355 and 360 at two), none shorter than two stages (19.4 us; four 22.8, one 22.8).
 struct WeightsPlan {
   int blocks, tiles, slices;
   size_t bytes;
@@ -729,10 +747,10 @@ static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) 
   WeightsPlan p;
   const int64_t stages = (int64_t)(Tq / S + 63) / 64 * (d->Hq / d->Hkv);
   auto tiles_of = [&](int per) { return (int)std::min<int64_t>(Tk / per + S, Tk); };
-  p.blocks = (int64_t)tiles_of(256) * d->Hkv * stages >= WB ? 2 : 1;
+  p.blocks = (int64_t)tiles_of(256) * d->Hkv * stages >= 8192 ? 2 : 1;
   p.tiles = tiles_of(128 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
-  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WT * WGS / wgs, stages / WS, 64}));
+  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({4 * WGS / wgs, stages / 2, 64}));
   p.bytes = p.slices > 1 ? (size_t)p.slices * d->Hkv * Tk * 4 : 0;
   return p;
 }
@@ -757,7 +775,7 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
       if (cost < best) best = cost, p.chunk_keys = keys;
     }
     // a short cache in one chunk has nothing to join, which saves a launch (about 4 us; another 128 slots cost 0.6)
-    p.whole_rows = !P && C <= 512 && p.row_blocks == 1;
+    p.whole_rows = !P && C <= WHOLE && p.row_blocks == 1;
     if (p.whole_rows) p.chunk_keys = (C + 127) / 128 * 128;
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }

@@ -365,11 +365,12 @@ struct Limits {
 };
 
 // Where a decode step keeps its scores (the weights need the whole row's sum): one row of floats per lane's row, index 0 =
-// keys.begin; rows that do not exist have an offset out of the range.
+// keys.begin, in memory (rows that do not exist have an offset out of the range) or in LDS.
 struct Scores {
-  float* base;      // null: nowhere
+  float* base;      // null: not in memory
   int range;        // bytes
   uint32_t offset;  // the lane's, in bytes
+  uint32_t lds;     // the lane's row there, 0: not there
 };
 
 template <typename T, int DP>
@@ -526,6 +527,11 @@ __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, in
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x4), rsrc, (int)(scores.offset + (uint32_t)(at - keys.begin + r * 8 + (lane >> 5) * 4) * 4u), 0, 0);
       }
       stored = true;
+    }
+    if (SCORES && scores.lds) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *in_lds<f4>(scores.lds + (at - keys.begin + r * 8 + (lane >> 5) * 4) * 4) = f4{raw[4 * r], raw[4 * r + 1], raw[4 * r + 2], raw[4 * r + 3]};
     }
     if (next >= end) break;
     at = next;
