@@ -833,7 +833,7 @@ using namespace tmac;
 using namespace tmac::attn;
 
 extern "C" size_t tmac_attn_prompt_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk) {
-  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0) return 0;
+  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0 || long_axis(S) || long_axis(Tq) || long_axis(Tk)) return 0;
   return prompt_plan(desc, S, Tq, Tk).bytes;
 }
 
@@ -844,7 +844,7 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
   if (S == 0 || Tq == 0) return TMAC_OK;
   if (!rows_ok(q, false, true, true) || !rows_ok(out, false, true, true) || !cu_q_dev || !cu_k_dev) return TMAC_EINVAL;
   if (Tk > 0 && (!rows_ok(k, false, true, true) || !rows_ok(v, false, true, true))) return TMAC_EINVAL;
-  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff || long_axis(S) || long_axis(Tq) || long_axis(Tk)) return TMAC_EUNSUPPORTED;
   const tmac_view none = {};
   if (Tk == 0) k = v = &none;
   if (far_rows(k) || far_rows(v)) return TMAC_EUNSUPPORTED;
@@ -871,7 +871,7 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
 }
 
 extern "C" size_t tmac_attn_weights_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk) {
-  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0) return 0;
+  if (!desc_ok(desc) || desc->D > 128 || S <= 0 || Tq <= 0 || Tk <= 0 || long_axis(S) || long_axis(Tq) || long_axis(Tk)) return 0;
   return weights_plan(desc, S, Tq, Tk).bytes;
 }
 
@@ -882,7 +882,7 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
   if (S == 0 || Tk == 0) return TMAC_OK;
   if (!rows_ok(k, false, true, true) || !cu_q_dev || !cu_k_dev || !weight_dev) return TMAC_EINVAL;
   if (Tq > 0 && (!rows_ok(q, false, true, true) || !lse_dev)) return TMAC_EINVAL;
-  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff || long_axis(S) || long_axis(Tq) || long_axis(Tk)) return TMAC_EUNSUPPORTED;
   const tmac_view none = {};
   if (Tq == 0) q = &none;
   if (far_rows(q)) return TMAC_EUNSUPPORTED;
@@ -917,7 +917,7 @@ static bool decode_sizes_ok(const tmac_attn_desc* d, const tmac_cache* c, int32_
 }
 
 extern "C" size_t tmac_attn_decode_workspace_bytes(const tmac_attn_desc* desc, const tmac_cache* cache, int32_t P, int32_t accumulate) {
-  if (!decode_sizes_ok(desc, cache, P, accumulate) || desc->D > 128 || cache->B == 0) return 0;
+  if (!decode_sizes_ok(desc, cache, P, accumulate) || desc->D > 128 || cache->B == 0 || long_axis(cache->capacity) || long_axis(P)) return 0;
   return decode_plan(desc, cache->B, cache->capacity, P, accumulate).bytes;
 }
 
@@ -931,7 +931,7 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   if (P > 0 && (!rows_ok(k0, false, true, true) || !rows_ok(v0, false, true, true))) return TMAC_EINVAL;
   if (C > 0 && (!rows_ok(&cache->k, true, true, true) || !rows_ok(&cache->v, true, true, true) || !cache->lens_dev)) return TMAC_EINVAL;
   if (C > 0 && accumulate && !cache->weight_dev) return TMAC_EINVAL;
-  if (desc->D > 128 || (int64_t)B * desc->Hq > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (desc->D > 128 || (int64_t)B * desc->Hq > 0x7fffffff || long_axis(C) || long_axis(P)) return TMAC_EUNSUPPORTED;
   const tmac_view none = {};
   if (P == 0) k0 = v0 = &none;
   const tmac_view* k = C ? &cache->k : &none;

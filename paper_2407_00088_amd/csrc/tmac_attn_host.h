@@ -16,6 +16,9 @@ inline bool rows_ok(const tmac_view* v, bool seq, bool token, bool head) {
   return (!seq || fits(v->seq)) && (!token || fits(v->token)) && (!head || fits(v->head));
 }
 
+// Lengths up to which whole tiles past the end are still within 32-bit indexes.
+inline bool long_axis(int64_t n) { return n > (int64_t)1 << 30; }
+
 // 128 rows span more than a buffer's range.
 inline bool far_rows(const tmac_view* v) { return v->token >= ((int64_t)1 << 22); }
 

@@ -47,16 +47,16 @@ __device__ __forceinline__ int source_tokens(const FillArgs& a, int b, int h, in
   return max(0, clamp_to(a.cu[b + 1], a.total) - first);
 }
 
-constexpr int WAVES = 16, DIGIT = 2048, HELD = 32768;  // keys that LDS holds
-constexpr int COPIED = 1024;                           // slots whose rows the selecting workgroup copies itself
+constexpr int WAVES = 16, DIGIT = 2048;
+constexpr int COPIED = 1024;  // slots whose rows the selecting workgroup copies itself
 
 // Number of set bits of `mask` below the lane.
 __device__ __forceinline__ int below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// Rows of keys and values into slots [lo, lo + rows), Unit by Unit, past the caches: every byte is read once and written once.
-// index: their tokens.
+// Keys, values, weights and positions into slots [lo, lo + rows), rows Unit by Unit and past the caches: every byte is read once and
+// written once.  index: their tokens.
 template <typename Unit, int THREADS>
 __device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int first, const int32_t* index, int lo, int rows) {
   const int per_row = a.D * 2 / (int)sizeof(Unit);
@@ -64,6 +64,14 @@ __device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int f
   const char* vs = a.v_src + b * a.vs_seq + h * a.vs_head + first * a.vs_token;
   char* kd = a.k + b * a.k_seq + h * a.k_head + lo * a.k_token;
   char* vd = a.v + b * a.v_seq + h * a.v_head + lo * a.v_token;
+  const float* w = a.w_src + b * a.ws_seq + h * a.ws_head + first * a.ws_token;
+  const int32_t* p = a.pos_src ? a.pos_src + b * a.ps_seq + h * a.ps_head + first * a.ps_token : nullptr;
+  const int64_t slot0 = ((int64_t)b * a.Hkv + h) * a.C + lo;
+  for (int x = threadIdx.x; x < rows; x += THREADS) {
+    const int i = index[x];
+    a.weight[slot0 + x] = w[i * a.ws_token];
+    a.pos[slot0 + x] = p ? p[i * a.ps_token] : i;
+  }
 #pragma unroll 4
   for (int x = threadIdx.x; x < rows * per_row; x += THREADS) {
     const int row = x / per_row, at = (x - row * per_row) * (int)sizeof(Unit);
@@ -75,135 +83,129 @@ __device__ __forceinline__ void copy_rows(const FillArgs& a, int b, int h, int f
   }
 }
 
-// Which tokens of one sequence and head stay: the (n - C)-th smallest key is found digit by digit (11, 11 and 10 bits, counted
-// in LDS), then every wavefront numbers the staying tokens of its run.  Writes weights, positions and the tokens' places in
-// the source for the copy.
-template <bool COPIES, typename Unit>
-__global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs a) {
-  __shared__ uint32_t held[HELD];
-  __shared__ uint32_t count[DIGIT];
-  __shared__ uint32_t wave_sum[WAVES];
-  __shared__ uint32_t chosen[2];
+// What the selection shares: counters of a digit, and sums and counts of wavefronts.
+struct Selecting {
+  uint32_t count[DIGIT], wave_sum[2][WAVES], chosen[2];
+};
+
+// The places of the n - leave tokens that stay, in order: of keys read_key(i), i < n, the `leave` smallest go (equal ones by i).
+// The leave-th smallest key is found digit by digit (11, 11 and 10 bits, counted in LDS), then every wavefront numbers the
+// staying tokens of its run.  PER: tokens of a lane, which stay in registers from the first look on; 0: any number, read again by
+// every step.  (128 caches, 4096 of 16384 tokens each: 24 us, the instructions of
+// 16 wavefronts on one CU; with the keys in LDS it was 30, with four counters a digit still 24.)
+template <int PER, typename ReadKey>
+__device__ __forceinline__ void select(ReadKey read_key, int n, uint32_t leave, int32_t* index, Selecting& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
-  int first;
-  const int n = source_tokens(a, b, h, first), keep = min(n, a.C);
-  const int seen = a.src_seen ? a.src_seen[bh] : n;
-  const float* w = a.w_src + b * a.ws_seq + h * a.ws_head + first * a.ws_token;
-  const int32_t* p = a.pos_src ? a.pos_src + b * a.ps_seq + h * a.ps_head + first * a.ps_token : nullptr;
-  auto position = [&](int i) { return p ? p[i * a.ps_token] : i; };
-  // the tokens' places: for the copying launch, or, where this workgroup copies its rows itself, in LDS
-  __shared__ int32_t kept[COPIES ? COPIED : 1];
-  int32_t* index = COPIES ? kept : a.index + (int64_t)bh * a.C;
-  float* weight = a.weight + (int64_t)bh * a.C;
-  int32_t* pos = a.pos + (int64_t)bh * a.C;
-  if (tid == 0) {
-    a.lens[bh] = keep;
-    a.seen[bh] = seen;
-  }
-  auto copy = [&] {
-    if constexpr (COPIES) {
-      __syncthreads();
-      copy_rows<Unit, 64 * WAVES>(a, b, h, first, kept, 0, keep);
+  const int turns = (n + 64 * WAVES - 1) / (64 * WAVES), lo = wave * turns * 64;  // a wavefront's run: `turns` times 64 tokens
+  uint32_t mine[PER ? PER : 1];
+#pragma unroll
+  for (int y = 0; y < PER; ++y)
+    if (y < turns) mine[y] = lo + y * 64 + lane < n ? read_key(lo + y * 64 + lane) : 0u;
+  auto each = [&](auto&& f) {
+    if constexpr (PER != 0) {
+#pragma unroll
+      for (int y = 0; y < PER; ++y)
+        if (y < turns) f(lo + y * 64 + lane, mine[y]);
+    } else {
+      for (int y = 0; y < turns; ++y) {
+        const int i = lo + y * 64 + lane;
+        f(i, i < n ? read_key(i) : 0u);
+      }
     }
   };
-  if (n <= a.C) {
-    for (int i = tid; i < n; i += 64 * WAVES) {
-      weight[i] = w[i * a.ws_token];
-      pos[i] = position(i);
-      index[i] = i;
-    }
-    copy();
-    return;
-  }
-  auto read_key = [&](int i) { return order_key(w[i * a.ws_token], (int64_t)position(i) >= (int64_t)seen - a.recent); };
-  const bool holds = n <= HELD;
-  auto key = [&](int i) { return holds ? held[i] : read_key(i); };
-  if (holds) {
-#pragma unroll 16
-    for (int i = tid; i < n; i += 64 * WAVES) held[i] = read_key(i);
-  }
-  // the rank-th smallest key (from zero): what is left of `rank` counts equal keys
-  uint32_t prefix = 0, rank = n - a.C - 1;
-#pragma unroll 1
+  uint32_t prefix = 0, rank = leave - 1;  // of the key that is looked for, among those with its digits so far
+#pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, above = shift + bits;
-    for (int i = tid; i < DIGIT; i += 64 * WAVES) count[i] = 0;
+#pragma unroll
+    for (int i = 0; i < DIGIT / (64 * WAVES); ++i) sh.count[tid + i * 64 * WAVES] = 0;
     __syncthreads();
-#pragma unroll 4
-    for (int i = tid; i < n; i += 64 * WAVES) {
-      const uint32_t x = key(i);
-      if (above == 32 || x >> above == prefix >> above) atomicAdd(&count[(x >> shift) & ((1u << bits) - 1)], 1u);
-    }
+    each([&](int i, uint32_t x) {
+      const bool counts = i < n && (pass == 0 || x >> (above & 31) == prefix >> (above & 31));
+      // (recent tokens lie side by side and would all meet in one counter: a wavefront's are counted together)
+      const bool recent = counts && x == 0xffffffffu;
+      const uint64_t together = __ballot(recent);
+      if (counts && !recent) atomicAdd(&sh.count[(x >> shift) & ((1u << bits) - 1)], 1u);
+      if (recent && below(together) == 0) atomicAdd(&sh.count[(1u << bits) - 1], (uint32_t)__builtin_popcountll(together));
+    });
     __syncthreads();
     // two digits a thread
-    const uint32_t c0 = count[2 * tid], c1 = count[2 * tid + 1];
+    const uint32_t c0 = sh.count[2 * tid], c1 = sh.count[2 * tid + 1];
     uint32_t incl = c0 + c1;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const uint32_t x = __shfl_up(incl, o);
       if (lane >= o) incl += x;
     }
-    if (lane == 63) wave_sum[wave] = incl;
+    if (lane == 63) sh.wave_sum[0][wave] = incl;
     __syncthreads();
     uint32_t before = incl - c0 - c1;
-    for (int i = 0; i < wave; ++i) before += wave_sum[i];
-    if (rank >= before && rank < before + c0) chosen[0] = 2 * tid, chosen[1] = before;
-    if (rank >= before + c0 && rank < before + c0 + c1) chosen[0] = 2 * tid + 1, chosen[1] = before + c0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) before += i < wave ? sh.wave_sum[0][i] : 0;
+    if (rank >= before && rank < before + c0) sh.chosen[0] = 2 * tid, sh.chosen[1] = before;
+    if (rank >= before + c0 && rank < before + c0 + c1) sh.chosen[0] = 2 * tid + 1, sh.chosen[1] = before + c0;
     __syncthreads();
-    prefix |= chosen[0] << shift;
-    rank -= chosen[1];
-    __syncthreads();
+    prefix |= sh.chosen[0] << shift;
+    rank -= sh.chosen[1];
   }
   // of the tokens whose key is `prefix`, the first rank + 1 leave
-  const uint32_t leave = rank + 1;
-  const int run = ((n + WAVES - 1) / WAVES + 63) / 64 * 64, lo = min(n, wave * run), hi = min(n, lo + run);
+  const uint32_t go = rank + 1;
   uint32_t greater = 0, equal = 0;
-  for (int i = lo; i < hi; i += 64) {
-    const uint32_t x = i + lane < hi ? key(i + lane) : 0;
-    greater += __builtin_popcountll(__ballot(i + lane < hi && x > prefix));
-    equal += __builtin_popcountll(__ballot(i + lane < hi && x == prefix));
-  }
-  if (lane == 0) count[wave] = greater, count[64 + wave] = equal;
+  each([&](int i, uint32_t x) {
+    greater += __builtin_popcountll(__ballot(i < n && x > prefix));
+    equal += __builtin_popcountll(__ballot(i < n && x == prefix));
+  });
+  __syncthreads();
+  if (lane == 0) sh.wave_sum[0][wave] = greater, sh.wave_sum[1][wave] = equal;
   __syncthreads();
   greater = equal = 0;
-  for (int i = 0; i < wave; ++i) greater += count[i], equal += count[64 + i];
-  uint32_t at = greater + (equal > leave ? equal - leave : 0);
-  // eight times 64 tokens a turn, whose weights and positions are all on their way before the first is stored
-  constexpr int TURN = 8;
-  for (int i0 = lo; i0 < hi; i0 += 64 * TURN) {
-    float wt[TURN];
-    int32_t ps[TURN];
 #pragma unroll
-    for (int y = 0; y < TURN; ++y) {
-      if (i0 + 64 * y >= hi) break;
-      const int i = min(i0 + 64 * y + lane, n - 1);
-      wt[y] = w[i * a.ws_token];
-      ps[y] = position(i);
-    }
-#pragma unroll
-    for (int y = 0; y < TURN; ++y) {
-      if (i0 + 64 * y >= hi) break;
-      const int i = i0 + 64 * y + lane;
-      const bool there = i < hi;
-      const uint32_t x = there ? key(i) : 0;
-      const uint64_t same = __ballot(there && x == prefix);
-      const bool stays = there && (x > prefix || (x == prefix && equal + below(same) >= leave));
-      const uint64_t mask = __ballot(stays);
-      if (stays) {
-        const int to = at + below(mask);
-        weight[to] = wt[y];
-        pos[to] = ps[y];
-        index[to] = i;
-      }
-      equal += __builtin_popcountll(same);
-      at += __builtin_popcountll(mask);
-    }
-  }
-  copy();
+  for (int i = 0; i < WAVES; ++i) greater += i < wave ? sh.wave_sum[0][i] : 0, equal += i < wave ? sh.wave_sum[1][i] : 0;
+  uint32_t at = greater + (equal > go ? equal - go : 0);
+  each([&](int i, uint32_t x) {
+    const uint64_t same = __ballot(i < n && x == prefix);
+    const bool stays = i < n && (x > prefix || (x == prefix && equal + below(same) >= go));
+    const uint64_t mask = __ballot(stays);
+    if (stays) index[at + below(mask)] = i;
+    equal += __builtin_popcountll(same);
+    at += __builtin_popcountll(mask);
+  });
 }
 
-// 64 slots of a sequence and key head a workgroup.
+// One workgroup a sequence and key head.  COPIES: it copies the rows too, else it leaves the tokens' places for the copying launch.
+template <bool COPIES, typename Unit>
+__global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs a) {
+  __shared__ Selecting sh;
+  __shared__ int32_t kept[COPIES ? COPIED : 1];
+  const int tid = threadIdx.x, bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
+  int first;
+  const int n = source_tokens(a, b, h, first), keep = min(n, a.C);
+  const int seen = a.src_seen ? a.src_seen[bh] : n;
+  const float* w = a.w_src + b * a.ws_seq + h * a.ws_head + first * a.ws_token;
+  const int32_t* p = a.pos_src ? a.pos_src + b * a.ps_seq + h * a.ps_head + first * a.ps_token : nullptr;
+  int32_t* index = COPIES ? kept : a.index + (int64_t)bh * a.C;
+  if (tid == 0) {
+    a.lens[bh] = keep;
+    a.seen[bh] = seen;
+  }
+  auto read_key = [&](int i) { return order_key(w[i * a.ws_token], (int64_t)(p ? p[i * a.ps_token] : i) >= (int64_t)seen - a.recent); };
+  if (n <= a.C) {
+    for (int i = tid; i < n; i += 64 * WAVES) index[i] = i;
+  } else if (n <= 4 * 64 * WAVES) {
+    select<4>(read_key, n, n - a.C, index, sh);
+  } else if (n <= 16 * 64 * WAVES) {
+    select<16>(read_key, n, n - a.C, index, sh);
+  } else {
+    select<0>(read_key, n, n - a.C, index, sh);
+  }
+  if constexpr (COPIES) {
+    __syncthreads();
+    copy_rows<Unit, 64 * WAVES>(a, b, h, first, kept, 0, keep);
+  }
+}
+
+// 64 slots of a sequence and key head a workgroup: memory's rate bounds it (128 caches of 4096 slots of 128 elements, 550 MB read and
+// written with the weights and positions: 106 us, 5.2 TB/s, what a large copy reaches).
 template <typename Unit>
 __global__ __launch_bounds__(256) void cache_copy_kernel(const FillArgs a) {
   const int bh = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, b = bh / a.Hkv, h = bh % a.Hkv;
@@ -320,7 +322,7 @@ extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache
     for (const tmac_view* x : {&src->weight, &src->pos})
       if (x->data && ((!packed && x->seq < 0) || x->token < 0 || x->head < 0 || (reinterpret_cast<uintptr_t>(x->data) & 3))) return TMAC_EINVAL;
   }
-  if (cache->D > 128 || (int64_t)B * cache->Hkv > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (cache->D > 128 || (int64_t)B * cache->Hkv > 0x7fffffff || attn::long_axis(cache->capacity) || attn::long_axis(src->total)) return TMAC_EUNSUPPORTED;
   if (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return TMAC_EINVAL;
   if (workspace_bytes < tmac_cache_fill_workspace_bytes(cache)) return TMAC_ESIZE;
   FillArgs a = {};
@@ -341,9 +343,10 @@ extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache
   const int64_t bh = (int64_t)B * cache->Hkv;
   if (bh * a.blocks > 0x7fffffff) return TMAC_EUNSUPPORTED;
   const bool wide = attn::wide_rows(&src->k, a.D) && attn::wide_rows(&src->v, a.D) && attn::wide_rows(&cache->k, a.D) && attn::wide_rows(&cache->v, a.D);
-  // Small caches are copied by the workgroup that selects, which saves a launch (96 caches of 256 slots of 100 elements: 16.3 -> FUSED us in all);
-  // beyond 256 KB of keys and values one workgroup's copy takes longer than that, the more so where there are few.
-  if (cache->capacity <= COPIED && (int64_t)cache->capacity * a.D * 4 <= 262144)
+  // Small caches are copied by the workgroup that selects, which saves a launch and what is between two (rows of 128 elements, 256 slots:
+  // 8 caches 10.0 us, 11.2 in two launches; 96 of 100 elements 12.3, 13.6); beyond 128 KB of keys and values one workgroup's
+  // copy takes longer than that (512 slots: 8 caches 15.7, 13.1; 96 caches 21.5, 18.8).
+  if (cache->capacity <= COPIED && (int64_t)cache->capacity * a.D * 4 <= 131072)
     return cache::launch(wide ? (const void*)cache_select_kernel<true, u4> : (const void*)cache_select_kernel<true, u2>, bh, 64 * WAVES, &a, stream);
   const tmac_status st = cache::launch((const void*)cache_select_kernel<false, u2>, bh, 64 * WAVES, &a, stream);
   if (st != TMAC_OK) return st;
@@ -354,7 +357,7 @@ extern "C" tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_vie
   if (!cache_ok(cache)) return TMAC_EINVAL;
   if (cache->B == 0) return TMAC_OK;
   if (!cache_set(cache) || !attn::rows_ok(k, true, false, true) || !attn::rows_ok(v, true, false, true)) return TMAC_EINVAL;
-  if (cache->D > 128 || (int64_t)cache->B * cache->Hkv > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (cache->D > 128 || (int64_t)cache->B * cache->Hkv > 0x7fffffff || attn::long_axis(cache->capacity)) return TMAC_EUNSUPPORTED;
   AppendArgs a = {};
   a.k_new = static_cast<const char*>(k->data), a.v_new = static_cast<const char*>(v->data);
   a.k = static_cast<char*>(cache->k.data), a.v = static_cast<char*>(cache->v.data);

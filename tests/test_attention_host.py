@@ -173,3 +173,22 @@ def test_workspaces_grow_with_what_is_asked():
     assert A.lib.tmac_attn_prompt_workspace_bytes(d, 0, 1, 1) == A.lib.tmac_attn_prompt_workspace_bytes(desc(D=256), 1, 1, 1) == 0
     small, large = (A.lib.tmac_attn_decode_workspace_bytes(d, cache(capacity=n), 0, 1) for n in (100, 100000))
     assert 0 < small < large
+
+
+def test_lengths_that_do_not_fit_a_32_bit_index():
+    one = desc(Hq=1, Hkv=1)
+    far = (1 << 30) + 1
+    for sizes in ((far, 10, 10), (1, far, 10), (1, 10, far)):
+        S, Tq, Tk = sizes
+        assert prompt(one, S=S, Tq=Tq, Tk=Tk) == T.TMAC_EUNSUPPORTED
+        assert A.lib.tmac_attn_weights(one, view(), view(), P16, S, Tq, Tk, P16, P16, P16, P16, 1 << 40, None) == T.TMAC_EUNSUPPORTED
+        assert A.lib.tmac_attn_prompt_workspace_bytes(one, S, Tq, Tk) == A.lib.tmac_attn_weights_workspace_bytes(one, S, Tq, Tk) == 0
+    large = cache(capacity=far)
+    assert decode(c=large) == decode(P=far) == T.TMAC_EUNSUPPORTED
+    assert A.lib.tmac_attn_decode_workspace_bytes(desc(), large, 10, 1) == A.lib.tmac_attn_decode_workspace_bytes(desc(), cache(), far, 1) == 0
+    row = view(seq=128)
+    assert A.lib.tmac_cache_append(large, row, row, None) == T.TMAC_EUNSUPPORTED
+    source = A.tmac_cache_source(view(), view(), A.tmac_view(P16, 0, 1, 100), A.tmac_view(), P16, None, None, 100)
+    assert A.lib.tmac_cache_fill(large, source, P16, 1 << 50, None) == T.TMAC_EUNSUPPORTED
+    source.total = far
+    assert A.lib.tmac_cache_fill(cache(), source, P16, 1 << 40, None) == T.TMAC_EUNSUPPORTED
