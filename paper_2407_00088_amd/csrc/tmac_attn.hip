@@ -219,13 +219,16 @@ __device__ __forceinline__ bool find_tile(const int32_t* cu_q, const int32_t* cu
   return false;
 }
 
-// Unit of a grid of `heads` x `units`: a head's units on one XCD, one head after the other, where the heads divide among the
-// eight (workgroups go round the XCDs by their number), so that a head's keys stay in that XCD's L2.
-__device__ __forceinline__ void head_and_unit(int id, int heads, int units, int& head, int& unit) {
+// Unit of a grid of heads and units: a head's units on one XCD where the heads divide among the eight (workgroups go round the XCDs
+// by their number), so that a head's keys stay in that XCD's L2.  Neighbouring heads, whose rows share lines of memory, are on the
+// same one, and every unit's turn comes for all of them before the next unit's, so that the heaviest units of all heads start
+// first (prompts of 860, 2003, 564, 158, 369, 68, 104, 242 and 1312 tokens, 32 heads of 100 elements: 109.8 us one head after the other,
+// 99.6 all heads in turn, 98.8 neighbours on one XCD too; one of 8192, 32 heads of 128: 567, 547, 548).
+__device__ __forceinline__ void head_and_unit(int id, int heads, int& head, int& unit) {
   if (heads % 8 == 0) {
-    const int j = id / 8;
-    head = id % 8 + 8 * (j / units);
-    unit = j % units;
+    const int j = id / 8, of_xcd = heads / 8;
+    head = id % 8 * of_xcd + j % of_xcd;
+    unit = j / of_xcd;
   } else {
     head = id % heads;
     unit = id / heads;
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a)
   __shared__ __align__(1024) char lds[Sh::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int h, unit;
-  head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
+  head_and_unit(blockIdx.x, a.Hkv, h, unit);
   const int z = unit % a.slices;
   Place p;
   if (!find_tile(a.cu_q, a.cu_k, a.S, a.Tq, a.Tk, false, a.G, 32 * BLOCKS, unit / a.slices, p)) return;
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   if (id < 0) {
     id += prefix;
     int h, unit;
-    head_and_unit(id, a.Hkv, a.prefix_tiles * a.prefix_slices, h, unit);
+    head_and_unit(id, a.Hkv, h, unit);
     const int z = unit / a.prefix_tiles;  // (a slice's tiles side by side: the same keys)
     const int rows = a.B * a.G;
     const Tile tile(unit % a.prefix_tiles, BLOCKS, wave, lane, rows);
@@ -580,7 +583,7 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   __shared__ __align__(16) float lse2[2][SQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   int h, unit;
-  head_and_unit(blockIdx.x, a.Hkv, a.tiles * a.slices, h, unit);
+  head_and_unit(blockIdx.x, a.Hkv, h, unit);
   const int z = unit % a.slices;
   Place p;
   if (!find_tile(a.cu_q, a.cu_k, a.S, a.Tq, a.Tk, true, 1, KEYS, unit / a.slices, p)) return;
