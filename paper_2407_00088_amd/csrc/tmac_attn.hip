@@ -718,8 +718,12 @@ static bool desc_ok(const tmac_attn_desc* d) {
 
 constexpr int WGS = 512;  // workgroups that the chip holds at once, two on a CU
 
-// Rows of a workgroup and slices of the keys.  Rows: 128 share each key read from LDS by four wavefronts, 32 let the
-// wavefronts share the keys instead.  Slices: as many as it takes to fill the chip, none shorter than 256 keys.
+// Rows of a workgroup: 128 share each stage of keys, 32 let the wavefronts share the keys instead, for sequences of at most 32 rows (32
+// of 8 rows after 1000 keys, 8 key heads: 24.7 us with 32, 28.6 with 128; 32 of 64 rows, 32 heads: 32.0 and 21.7) and for calls that
+// leave half of the chip idle otherwise (256 rows, 40 heads: 10.0 and 13.1; 1024 rows, 64 heads in groups of 8: 47.2 and 32.3).
+// Slices: as many as it takes to fill the chip, none shorter than 256 keys, if that saves the walk over 768 keys or more, since the
+// parts are joined by another launch (16 rows after 4096 keys: 14.1 us in 16 slices, 15.0 in 8; 1000 rows, 8 heads in groups of 4:
+// 18.2 us in two, 14.3 in one).
 struct PromptPlan {
   int blocks, tiles, slices;
   size_t part, ml, bytes;
@@ -728,10 +732,11 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   PromptPlan p;
   const int64_t G = d->Hq / d->Hkv, rows = Tq * G;
   auto tiles_of = [&](int per) { return (int)std::min<int64_t>(rows / per + S, rows); };
-  p.blocks = rows / S <= 64 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
+  p.blocks = rows / S <= 32 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
   p.tiles = tiles_of(32 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
   p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WGS / wgs, (Tk / S) / 256, 64}));
+  if (Tk / S - Tk / S / p.slices < 768) p.slices = 1;
   p.part = p.slices > 1 ? (size_t)p.slices * Tq * d->Hq * d->D * 4 : 0;
   p.ml = p.slices > 1 ? (size_t)p.slices * Tq * d->Hq * 8 : 0;
   p.bytes = p.part + p.ml;

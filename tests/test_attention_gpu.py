@@ -386,3 +386,56 @@ def test_a_long_cache_beyond_32_bit_offsets(A):
     s = 64.0 * 8.0 / math.sqrt(D)
     assert (out == 2.0).all() and abs(float(lse) - (s + math.log(2.0))) < 1e-4
     assert torch.allclose(cache.weight[0, 0, -2:].cpu(), torch.tensor([0.5, 0.5]), atol=1e-5)
+
+
+LARGE_PROMPTS = [  # enough rows and heads for workgroups of 128 rows, or enough pairs for two blocks of keys a wavefront
+    ([700, 3, 128, 129], [700, 3, 128, 129], 32, 32, 128, F16, True),
+    ([40] * 9, [40] * 8 + [1040], 32, 32, 100, BF16, True),
+    ([33] * 70 + [200], [33] * 70 + [231], 8, 8, 64, BF16, True),    # more sequences than lanes
+    ([512], [700], 64, 8, 100, BF16, True),
+    ([1000, 333], [1000, 64], 64, 8, 36, F16, True),                 # fewer keys than queries: rows that see nothing
+    ([200, 77], [300, 0], 64, 64, 128, F16, False),                  # no keys
+    ([200, 77], [2000, 1700], 64, 64, 64, F16, True),                # slices of the keys
+    ([1531], [1531], 64, 8, 128, BF16, True),
+    ([2100], [1400], 48, 3, 60, F16, False),
+]
+
+
+@pytest.mark.parametrize("case", LARGE_PROMPTS, ids=lambda c: f"{c[0][:3]}-{c[1][:3]}-{c[2]}-{c[3]}-{c[4]}-{c[5]}-{c[6]}".replace("torch.", ""))
+def test_large_prompt_and_weights(A, case):
+    test_prompt_and_weights(A, case)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("D", [60, 128])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_large_prompt_hidden_values_do_not_show(A, dt, D, bad):
+    """The same as in small calls where four wavefronts share the stages."""
+    n, H, at = 200, 128, 103
+    q, k, v = rand(1, 2 * n, H, D, dtype=dt).cuda(), rand(2, 2 * n, H, D, dtype=dt).cuda(), rand(3, 2 * n, H, D, dtype=dt).cuda()
+    c = i32([0, n, 2 * n])
+    clean, clean_lse = A.attn_prompt(q, k, v, c)
+    for which in "kv":
+        k2, v2 = k.clone(), v.clone()
+        (k2 if which == "k" else v2)[at, :, 5] = bad
+        (k2 if which == "k" else v2)[n + n // 2, 0] = bad
+        out, lse = A.attn_prompt(q, k2, v2, c)
+        assert torch.equal(out[:at], clean[:at]) and torch.equal(lse[:, :at], clean_lse[:, :at])
+        assert torch.equal(out[n:n + n // 2], clean[n:n + n // 2]) and torch.equal(out[n:, 1:], clean[n:, 1:])
+        if which == "v":
+            assert torch.equal(lse, clean_lse)
+            other = [d for d in range(D) if d != 5]
+            assert torch.equal(out[:n, :, other], clean[:n, :, other])
+            col = out[at:n, :, 5]
+            assert torch.isnan(col).all() if math.isnan(bad) else torch.equal(col, torch.full_like(col, bad))
+        elif math.isnan(bad):
+            assert torch.isnan(out[at:n]).all() and torch.isnan(lse[:, at:n]).all()
+
+
+def test_rows_do_not_depend_on_the_sequences_beside_them(A):
+    """A sequence's rows keep their bits whatever other sequences a call of the same shape of workgroups holds."""
+    H, D = 64, 128
+    a, b, c = (rand(40 + i, 300, 3, H, D).cuda() for i in range(3))
+    alone = A.attn_prompt(*torch.cat([a, b]).unbind(1), i32([0, 300, 600]))
+    other = A.attn_prompt(*torch.cat([c, a, b, c]).unbind(1), i32([0, 300, 600, 900, 1200]))
+    assert torch.equal(alone[0], other[0][300:900]) and torch.equal(alone[1], other[1][:, 300:900])
