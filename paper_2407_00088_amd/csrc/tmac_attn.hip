@@ -787,7 +787,10 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
     if (p.whole_rows) p.chunk_keys = (C + 127) / 128 * 128;
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }
-  p.blocks = rows <= 32 ? 1 : 4;
+  // Rows of the prefix's workgroups: 32, whose wavefronts share the keys, while that makes no more than 768 keys for each of the
+  // workgroups that the chip holds, else 128 (8 key heads, 128 rows over 4000 keys: 15.7 us with 32, 19.2 with 128; over 16000 28.2 both; 512
+  // rows over 16000 76.9 and 59.0; 32 key heads, 64 rows over 4000 23.7 and 27.9, over 16000 57.4 and 54.7).
+  p.blocks = rows <= 32 || (rows + 31) / 32 * d->Hkv * P <= WGS * 768 ? 1 : 4;
   if (P) {
     p.tiles = (int)((rows + 32 * p.blocks - 1) / (32 * p.blocks));
     // Slices until the prefix fills the chip, or beside caches half of it (64 rows over 16384 keys, 8 key heads of 128 elements, 64 caches

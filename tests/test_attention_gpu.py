@@ -439,3 +439,16 @@ def test_rows_do_not_depend_on_the_sequences_beside_them(A):
     alone = A.attn_prompt(*torch.cat([a, b]).unbind(1), i32([0, 300, 600]))
     other = A.attn_prompt(*torch.cat([c, a, b, c]).unbind(1), i32([0, 300, 600, 900, 1200]))
     assert torch.equal(alone[0], other[0][300:900]) and torch.equal(alone[1], other[1][:, 300:900])
+
+
+LARGE_DECODES = [  # enough rows over a long prefix for workgroups of 128 rows
+    (64, 32, 8, 128, 33, 6200, F16),
+    (33, 64, 4, 100, 70, 8001, BF16),
+    (130, 16, 16, 64, 5, 6000, F16),     # the last tile has two rows
+]
+
+
+@pytest.mark.parametrize("case", LARGE_DECODES, ids=str)
+@pytest.mark.parametrize("weigh", [False, True])
+def test_large_decode(A, case, weigh):
+    test_decode(A, case, weigh)
