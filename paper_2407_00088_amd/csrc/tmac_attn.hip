@@ -247,7 +247,11 @@ struct Tile {
   }
 };
 
-// One workgroup: 32 BLOCKS rows of one sequence and key head over the keys they see, or one slice of those.
+// One workgroup: 32 BLOCKS rows of one sequence and key head over the keys they see, or one slice of those; queries are read once,
+// keys once a tile, from the XCD's L2.  Long sequences are bound by power: 8192 tokens, 64 heads in groups of 8 of 128 elements take 1.11 ms, 0.99
+// PFLOP/s of the pairs that rows see (a large matrix product reaches 1.37), at 1.7 of 2.4 GHz with the matrix units busy for 52 % of the
+// cycles and the vector ALUs, mostly with exponentials, for 47 %; LDS has no bank conflicts.  Short ones are bound by latency: 33 tokens, 32
+// heads 6.1 us, one wavefront's chain of loads, products and exchanges.
 template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
   typedef Shape<DP, BLOCKS> Sh;
@@ -348,9 +352,12 @@ __device__ __forceinline__ f4 sum_weights(const float* scores, int64_t stride, i
 // A whole cache in one chunk: at most so many slots, and the scores of at most so many rows in LDS.
 constexpr int WHOLE = 512, LDS_ROWS = 4;
 
-// Workgroups of the prefix (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys) and of the caches (one sequence
+// One decode step.  Workgroups of the prefix (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys) and of the caches (one sequence
 // and key head, one chunk of its slots), the former, longer ones first (mixed, 4 rows over 2047 keys took 13.9 instead of 11.7 us).  Every one
-// leaves a part of its rows; where a row has only one, finished rows and, with accumulate, the slots' weights.
+// leaves a part of its rows; where a row has only one, finished rows and, with accumulate, the slots' weights.  A tile of 32 rows is
+// mostly empty for a group of 8 heads, but caches are bound by memory (24 of 4095 slots, 8 key heads of 128 elements, 403 MB: 78 us,
+// 5.1 TB/s, what a large copy reaches), and a prefix fills its tiles (64 rows of 64 heads in groups of 8 over 16384 keys: 46 us, 750 TFLOP/s
+// before the parts are joined; a row alone would read 67 MB for itself).
 template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<DP, BLOCKS> ShP;
@@ -504,6 +511,7 @@ __device__ __forceinline__ void join_row(const float* part, const float* ml, int
   if (lane == 0 && lse) *lse = j.sum == 0.0f ? -INFINITY : (j.top + __builtin_log2f(j.sum)) * LN2;
 }
 
+// One wavefront a row: about 4 us, what a launch with a chain of two loads takes (128 rows after 8192 keys, 32 heads).
 template <typename T>
 __global__ __launch_bounds__(256) void join_prompt_kernel(const PromptArgs a) {
   const int64_t rows = (int64_t)a.Tq * a.Hq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -514,7 +522,8 @@ __global__ __launch_bounds__(256) void join_prompt_kernel(const PromptArgs a) {
 }
 
 // Rows, then (where weights are wanted) 1024 slots of a sequence and key head a workgroup: the scores that the decode kernel
-// left become weights now that the rows' sums are known.
+// left become weights now that the rows' sums are known.  (24 caches of 4095 slots, 64 heads: 25 MB of scores, 6 MB of parts and 3 MB of
+// weights 10 us, of which the first 4 are what a launch with a chain of loads takes.)
 template <typename T>
 __global__ __launch_bounds__(256) void join_decode_kernel(const DecodeArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -575,7 +584,9 @@ struct WeightArgs {
 // One workgroup: 128 KB keys of one sequence and key head, 32 KB a wavefront, which stay in registers as the second operand of
 // S = Q K^T; a lane owns a key (of each 32) and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
 // The exponentials bind (16 a lane for 8 products of 32 x 32 x 16), so the rest is kept away from the vector ALUs: with two blocks of keys
-// a wavefront the reads of q and of lse serve twice.
+// a wavefront the reads of q and of lse serve twice.  6144 tokens, 64 heads in groups of 8 of 128 elements: 322 us, 0.95 PFLOP/s of the pairs that
+// are seen, matrix units 48 % busy and vector ALUs 61 %.  Nothing is added up atomically: a unit's sums go to memory once, those of its slices
+// to a part each.
 template <typename T, int DP, int KB>
 __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
   constexpr int SQ = 64, TILE = Layout<DP>::k_bytes(SQ), NT = DP / 16, KEYS = 128 * KB;
@@ -701,6 +712,7 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a
   }
 }
 
+// Slices' parts, in their order (4 us, a launch with one chain of loads).
 __global__ __launch_bounds__(256) void sum_weights_kernel(const float* part, float* weight, int64_t n, int slices) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
