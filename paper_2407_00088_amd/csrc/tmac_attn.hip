@@ -756,9 +756,9 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
 }
 
 // Blocks of 32 keys a wavefront: two, once that leaves enough units (each key tile's stages) for the chip; the reads of q then serve twice
-// (6144 tokens, 64 heads in groups of 8: 411 us with one, 355 with two; five prompts of up to 777 tokens 19.4 and 25).  Slices of a tile's
-// stages: until there are four times the workgroups that the chip holds, because tiles weigh unlike (608 us with twice, 411 with four times, 388
-// with eight times at one block, 376, 355 and 360 at two), none shorter than two stages (19.4 us; four 22.8, one 22.8).
+// (6144 tokens, 64 heads in groups of 8: 379 us with one, 337 with two; five prompts of up to 777 tokens 17.5 and 20.2).  Slices of a tile's
+// stages: until there are four times the workgroups that the chip holds, because tiles weigh unlike (the former 605 us at one time, 351 at
+// two, 331 at four, 332 at eight), none shorter than two stages (the latter 17.5 us; four 21.6, one 20.2).
 struct WeightsPlan {
   int blocks, tiles, slices;
   size_t bytes;
