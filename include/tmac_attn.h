@@ -12,6 +12,7 @@
  *   s_ij  = scale q_i . k_j for the keys j that row i may see
  *   lse_i = log sum_j exp s_ij           (natural logarithm; -inf for a row that sees no key, or none above -inf)
  *   o_i   = sum_j exp(s_ij - lse_i) v_j  (zeros for such a row)
+ * Results overlap neither each other's rows nor what a call reads (a cache's own weights apart, which a step adds to).
  * Elements that a row may not see do not touch its result, whatever they hold (NaN and infinities too).  Scores, exponentials,
  * sums and lse are 32-bit; the exponentials are rounded to the inputs' type before they are multiplied with v (an error of
  * the size of the result's own rounding), o_i is rounded once.

@@ -89,6 +89,23 @@ def _rows(name: str, t) -> None:
         raise ValueError(f"the elements of a row of {name} lie side by side: got strides {tuple(t.stride())}")
 
 
+def _apart(name: str, t) -> None:
+    """No two rows of a result share an element."""
+    end = t.shape[-1]
+    for stride, n in sorted(zip(t.stride()[:-1], t.shape[:-1])):
+        if n > 1:
+            if stride < end:
+                raise ValueError(f"the rows of {name} do not overlap: got strides {tuple(t.stride())} for {tuple(t.shape)}")
+            end += stride * (n - 1)
+
+
+def _counted(**sizes) -> None:
+    """The C ABI counts in 32 bits."""
+    for name, n in sizes.items():
+        if n >= 1 << 31:
+            raise ValueError(f"{name} ({n}) does not fit 32 bits")
+
+
 def _plain(name: str, t, shape, dtype) -> None:
     _dims(name, t, ", ".join(str(n) for n in shape), shape, dtype)
     if not t.is_contiguous():
@@ -131,6 +148,7 @@ def _packed(q, k, cu_q, cu_k):
     S = cu_q.numel() - 1
     _plain("cu_q", cu_q, (S + 1,), torch.int32)
     _plain("cu_k", cu_k, (S + 1,), torch.int32)
+    _counted(S=S, Tq=Tq, Tk=Tk, Hq=Hq, D=D)
     if Hkv == 0 or Hq % Hkv:
         raise ValueError(f"the query heads ({Hq}) are a multiple of the key heads ({Hkv})")
     return S, Tq, Tk, Hq, Hkv, D
@@ -156,7 +174,7 @@ def attn_prompt(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optional[f
             lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
         ws = _workspace(n, q.device) if n else None
     _dims("out", out, "Tq, Hq, D", (Tq, Hq, D), q.dtype)
-    _rows("out", out)
+    _rows("out", out), _apart("out", out)
     _plain("lse", lse, (Hq, Tq), torch.float32)
     _same_device(q, k, v, cu_q, cu_k, out, lse)
     B._check(lib.tmac_attn_prompt(desc, _view(q, None, 0, 1), _view(k, None, 0, 1), _view(v, None, 0, 1), S, Tq, Tk, cu_q.data_ptr(),
@@ -216,15 +234,17 @@ class KVCache:
                                 self.lens.data_ptr(), self.seen.data_ptr(), batch, Hkv, D, capacity, recent, _ELEM[dtype])
         self.fill_ws = None
         self.attend_ws = None
+        self.outgrown = []
 
     def _grown(self, ws, n: int, stream):
-        """A workspace of n bytes at least.  (One that is too small may still be in use by an earlier call: its memory is not handed out
-        again before that stream gets there.)"""
+        """A workspace of n bytes at least.  (One that is too small is kept: an earlier call may still run on it, or a graph that was
+        captured with it be replayed.  Sizes at least double, so that what is kept stays below what is used.)"""
         if ws is not None and ws.numel() >= n:
             return ws
+        if ws is not None:
+            self.outgrown.append(ws)
+            n = max(n, 2 * ws.numel())
         with _on(stream):
-            if ws is not None:
-                ws.record_stream(torch.cuda.current_stream())
             return _workspace(n, self.k.device)
 
     def _fill(self, source: tmac_cache_source, stream) -> None:
@@ -237,6 +257,7 @@ class KVCache:
         if stream is None and self.fill_ws is not None and calls.cache_fill(self.cache, self.k, k, v, weight, cu, self.fill_ws):
             return
         T = k.shape[0]
+        _counted(T=T)
         _dims("k", k, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
         _dims("v", v, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
         _rows("k", k), _rows("v", v)
@@ -279,6 +300,7 @@ class KVCache:
             raise ValueError("a prefix has keys and values")
         if prefix_k is not None:
             P = prefix_k.shape[0]
+            _counted(P=P)
             for name, t in (("prefix_k", prefix_k), ("prefix_v", prefix_v)):
                 _dims(name, t, "P, Hkv, D", (P, self.Hkv, self.D), dt)
                 _rows(name, t)
@@ -289,7 +311,7 @@ class KVCache:
             if lse is None:
                 lse = torch.empty((self.B, self.Hq), dtype=torch.float32, device=q.device)
         _dims("out", out, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
-        _rows("out", out)
+        _rows("out", out), _apart("out", out)
         _plain("lse", lse, (self.B, self.Hq), torch.float32)
         _same_device(self.k, q, prefix_k, prefix_v, out, lse)
         n = lib.tmac_attn_decode_workspace_bytes(self.desc, self.cache, P, int(weigh))

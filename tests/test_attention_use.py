@@ -194,3 +194,43 @@ def test_decoder_example_runs(A, capsys):
     from paper_2407_00088_amd import decoder
     decoder.main(steps=2)
     assert "step 1" in capsys.readouterr().out
+
+
+def test_a_captured_step_outlives_the_growth_of_its_workspace(A):
+    """A graph keeps the workspace that it was captured with, whatever later, larger calls and other tensors take."""
+    cache, _, _ = filled(A, 2, 8, 2, 64, 60, [[60, 60], [7, 30]], F16, garbage=0.0)
+    q, k0, v0 = rand(5, 2, 8, 64).cuda(), rand(6, 9000, 2, 64).cuda(), rand(7, 9000, 2, 64).cuda()
+    want = [x.clone() for x in cache.attend(q, k0[:700], v0[:700], weigh=False)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = cache.attend(q, k0[:700], v0[:700], weigh=False)
+    first = cache.attend_ws
+    cache.attend(q, k0, v0, weigh=False)
+    assert cache.attend_ws is not first and any(x is first for x in cache.outgrown)
+    del first
+    for turn in range(4):
+        others = [torch.full((n,), 7.0, device="cuda") for n in (2000, 30000, 300000)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert all((x == 7.0).all() for x in others)
+
+
+def test_results_whose_rows_overlap_and_sizes_beyond_32_bits_are_refused(A):
+    q, k, c = rand(1, 14, 4, 64).cuda(), rand(2, 14, 2, 64).cuda(), i32([0, 5, 14])
+    cache = A.KVCache(2, 2, 64, 8, Hq=4)
+    room = torch.zeros(14 * 4 * 64, dtype=F16, device="cuda")
+    far = k[:1].expand((1 << 31) + 5, 2, 64)
+    for bad in (lambda: A.attn_prompt(q, k, k, c, out=room[:256].view(1, 4, 64).expand(14, 4, 64)),
+                lambda: A.attn_prompt(q, k, k, c, out=room.as_strided((14, 4, 64), (252, 64, 1))),
+                lambda: cache.attend(q[:2], out=room[:64].view(1, 1, 64).expand(2, 4, 64)),
+                lambda: A.attn_prompt(q, far, far, c), lambda: cache.attend(q[:2], far, far),
+                lambda: cache.fill(far, far, torch.zeros((2, 1), device="cuda").expand(2, far.shape[0]), c)):
+        with pytest.raises(ValueError):
+            bad()
+    for ok in (room.view(4, 14, 64).transpose(0, 1), room.view(14, 4, 64)):
+        assert A.attn_prompt(q, k, k, c, out=ok)[0] is ok
