@@ -318,7 +318,6 @@ struct DecodeArgs {
   int chunks, chunk_keys, row_blocks;           // of the caches: chunks of a whole one, keys of a chunk, blocks of 32 heads of a group
   int q_wide;                                   // rows of q that are read 16 bytes at a time
   int once;                                     // the caches are more than the chip's own caches hold
-  int whole_rows;                               // no prefix, and a whole cache in one chunk: nothing is joined
   int weight_blocks;                            // of the joining kernel: blocks of 1024 slots
   float scale;
 };
@@ -349,29 +348,30 @@ __device__ __forceinline__ f4 sum_weights(const float* scores, int64_t stride, i
   return sum;
 }
 
-// A whole cache in one chunk: at most so many slots, and the scores of at most so many rows in LDS.
-constexpr int WHOLE = 512, LDS_ROWS = 4;
+// A short prefix and a whole cache in one chunk: at most so many slots, and the scores of at most so many rows in LDS.
+constexpr int SHORT = 512, LDS_ROWS = 4;
 
 // One decode step.  Workgroups of the prefix (all rows of a key head, 32 BLOCKS at a time, over one slice of its keys) and of the caches (one sequence
 // and key head, one chunk of its slots), the former, longer ones first (mixed, 4 rows over 2047 keys took 13.9 instead of 11.7 us).  Every one
-// leaves a part of its rows; where a row has only one, finished rows and, with accumulate, the slots' weights.  A tile of 32 rows is
+// leaves a part of its rows.  WHOLE: workgroups of the caches only, which take a short prefix first and leave finished rows and, with
+// accumulate, the slots' weights.  A tile of 32 rows is
 // mostly empty for a group of 8 heads, but caches are bound by memory (24 of 4095 slots, 8 key heads of 128 elements, 403 MB: 78 us,
 // 5.1 TB/s, what a large copy reaches), and a prefix fills its tiles (64 rows of 64 heads in groups of 8 over 16384 keys: 46 us, 750 TFLOP/s
 // before the parts are joined; a row alone would read 67 MB for itself).
-template <typename T, int DP, int BLOCKS>
+template <typename T, int DP, int BLOCKS, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<DP, BLOCKS> ShP;
   typedef Shape<DP, 1> ShO;
   constexpr int LDS = ShP::LDS > ShO::LDS ? ShP::LDS : ShO::LDS;
   __shared__ __align__(1024) char lds[LDS];
-  __shared__ float row_lse[32];
-  __shared__ __align__(16) float row_scores[LDS_ROWS * WHOLE];
+  __shared__ float row_lse[WHOLE ? 32 : 1];
+  __shared__ __align__(16) float row_scores[WHOLE ? LDS_ROWS * SHORT : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = a.scale * LOG2E;
   Keys keys;
-  const int prefix = a.Hkv * a.prefix_tiles * a.prefix_slices;
+  const int prefix = WHOLE ? 0 : a.Hkv * a.prefix_tiles * a.prefix_slices;
   int id = (int)blockIdx.x - prefix;
-  if (id < 0) {
+  if (!WHOLE && id < 0) {
     id += prefix;
     int h, unit;
     head_and_unit(id, a.Hkv, h, unit);
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   const int n = slots_in_use(a, b, h);
   keys.begin = chunk * a.chunk_keys;
   keys.end = min(n, keys.begin + a.chunk_keys);
-  if (keys.begin >= keys.end && !a.whole_rows) return;
+  if (!WHOLE && keys.begin >= keys.end) return;
   keys.k_stride = a.k_token;
   keys.v_stride = a.v_token;
   keys.k = a.k + b * a.k_seq + h * a.k_head;
@@ -423,9 +423,9 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   keys.once = a.once;
   // the group's rows of scores from this chunk on, in one range (the entry point keeps it below 2^31 bytes)
   Scores scores{};
-  const bool in_lds_rows = a.whole_rows && a.G <= LDS_ROWS;
+  const bool in_lds_rows = WHOLE && a.G <= LDS_ROWS;
   if (a.scores && in_lds_rows) {
-    if (exists) scores.lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)(char*)(row_scores + g * WHOLE);
+    if (exists) scores.lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)(char*)(row_scores + g * SHORT);
   } else if (a.scores) {
     const int64_t from = ((int64_t)b * a.Hq + h * a.G + block * 32) * a.score_stride + keys.begin;
     const int rows = min(32, a.G - block * 32);
@@ -435,11 +435,16 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   }
   // (whole rows with weights: the old ones are on their way early; a thread has four slots of at most 512)
   const int slot0 = threadIdx.x * 4;
-  float* weight = a.whole_rows && a.scores ? a.weight + ((int64_t)b * a.Hkv + h) * a.C + slot0 : nullptr;
+  float* weight = WHOLE && a.scores ? a.weight + ((int64_t)b * a.Hkv + h) * a.C + slot0 : nullptr;
   float old[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) old[j] = weight && slot0 + j < n ? weight[j] : 0.0f;
-  run_streams<T, DP, true, false>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
+  if constexpr (WHOLE) {
+    clear(w);
+    const Keys shared{a.k0 + h * a.k0_head, a.v0 + h * a.v0_head, a.k0_token, a.v0_token, 0, a.P, false};
+    if (a.P) run_streams<T, DP, false, false, true>(w, shared, a.D, c, Limits{a.P, a.P, a.P, a.P}, lds, Scores{});
+  }
+  run_streams<T, DP, true, false, WHOLE>(w, keys, a.D, c, Limits{keys.end, keys.end, keys.end, keys.end}, lds, scores);
   Target to = {};
   if (exists) {
     const int64_t slot = (int64_t)(a.prefix_slices + chunk) * a.B * a.Hq + row;
@@ -448,13 +453,13 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     to.part = a.part + slot * a.D;
     to.ml = a.ml + slot * 2;
   }
-  finish<T, DP, 1>(w, to, !a.whole_rows, a.D, lds, row_lse);
-  if (!weight || slot0 >= n) return;
+  finish<T, DP, 1>(w, to, !WHOLE, a.D, lds, WHOLE ? row_lse : nullptr);
+  if (!WHOLE || !weight || slot0 >= n) return;
   // (the scores have been written by this workgroup: all are past the barriers of `finish`)
   f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   if (in_lds_rows) {
     for (int y = 0; y < a.G; ++y) {
-      const f4 x = *reinterpret_cast<const f4*>(row_scores + y * WHOLE + slot0);
+      const f4 x = *reinterpret_cast<const f4*>(row_scores + y * SHORT + slot0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -row_lse[y]));
     }
@@ -794,8 +799,13 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
       const int64_t cost = (units * ((C + keys - 1) / keys) + WGS - 1) / WGS * (keys + 96);
       if (cost < best) best = cost, p.chunk_keys = keys;
     }
-    // a short cache in one chunk has nothing to join, which saves a launch (about 4 us; another 128 slots cost 0.6)
-    p.whole_rows = !P && C <= WHOLE && p.row_blocks == 1;
+    // A short cache in one chunk, after a short prefix, has nothing to join, which saves a launch (about 4 us, and what is between two).  Where
+    // caches fill half of the chip, up to 512 keys of prefix in all rounds of workgroups (64 caches of 60 and of 500 slots, 8 key heads, 100 keys:
+    // 12.0 and 20.7 us instead of 18.8 and 26.5; 512 keys 16.1 and 24.2 instead of 18.9 and 26.4; 1000 keys 21.6 and 29.2 instead of 21.0 and
+    // 26.9); elsewhere, where the chip has room to walk them side by side, up to 512 of prefix and cache (4 caches of 60 slots, 8 key heads, 100
+    // keys 10.0 instead of 12.5, 400 keys 13.4 instead of 14.5; of 500 slots, 200 keys 14.5 instead of 12.9).
+    const int64_t rounds = (units + WGS - 1) / WGS;
+    p.whole_rows = C <= SHORT && p.row_blocks == 1 && (2 * units >= WGS ? rounds * P : (int64_t)P + C) <= 512;
     if (p.whole_rows) p.chunk_keys = (C + 127) / 128 * 128;
     p.chunks = (C + p.chunk_keys - 1) / p.chunk_keys;
   }
@@ -803,7 +813,7 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
   // workgroups that the chip holds, else 128 (8 key heads, 128 rows over 4000 keys: 15.7 us with 32, 19.2 with 128; over 16000 28.2 both; 512
   // rows over 16000 76.9 and 59.0; 32 key heads, 64 rows over 4000 23.7 and 27.9, over 16000 57.4 and 54.7).
   p.blocks = rows <= 32 || (rows + 31) / 32 * d->Hkv * P <= WGS * 768 ? 1 : 4;
-  if (P) {
+  if (P && !p.whole_rows) {
     p.tiles = (int)((rows + 32 * p.blocks - 1) / (32 * p.blocks));
     // Slices until the prefix fills the chip, or beside caches half of it (64 rows over 16384 keys, 8 key heads of 128 elements, 64 caches
     // of 1024 slots: 84 us with all of it, 73 with half; without caches 50.6 and 52.7), none shorter than 256 keys.
@@ -837,8 +847,10 @@ static const void* prompt_kernel(int blocks) {
   return blocks == 4 ? (const void*)attn_prompt_kernel<T, DP, 4> : (const void*)attn_prompt_kernel<T, DP, 1>;
 }
 template <typename T, int DP>
-static const void* decode_kernel(int blocks) {
-  return blocks == 4 ? (const void*)attn_decode_kernel<T, DP, 4> : (const void*)attn_decode_kernel<T, DP, 1>;
+static const void* decode_kernel(int blocks) {  // 0: whole rows
+  return blocks == 4   ? (const void*)attn_decode_kernel<T, DP, 4, false>
+         : blocks == 1 ? (const void*)attn_decode_kernel<T, DP, 1, false>
+                       : (const void*)attn_decode_kernel<T, DP, 1, true>;
 }
 template <typename T, int DP>
 static const void* weights_kernel(int blocks) {
@@ -981,14 +993,13 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.B = B, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D, a.P = P, a.C = C;
   a.prefix_tiles = p.tiles, a.prefix_slices = p.slices, a.slice_keys = p.slice_keys;
   a.chunks = p.chunks, a.chunk_keys = std::max(1, p.chunk_keys), a.row_blocks = p.row_blocks;
-  a.whole_rows = p.whole_rows;
   a.q_wide = wide_rows(q, desc->D);
   // (24 caches of 4095 slots, 400 MB: 107 us a step where they are kept, 99.6 where they are not; a prefix of 42 MB 11.6 and 14.3)
   a.once = (int64_t)B * desc->Hkv * C * desc->D * 4 > (256 << 20);
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
-  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.blocks), grid, a, stream);
+  const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.whole_rows ? 0 : p.blocks), grid, a, stream);
   if (st != TMAC_OK || p.whole_rows) return st;
   return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
                 ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);

@@ -469,13 +469,13 @@ __device__ __forceinline__ void run_shared(Rows<T, DP>& w, const Keys& keys, int
 
 // All keys of a unit where every wavefront streams tiles of its own, 32 keys each, every fourth: a tile of K is requested as soon as
 // the one before has met q, one of V as soon as the one before has met the exponentials, and nobody waits for anybody.
-// SCORES: a cache, which keeps its scores where `scores` says.
-template <typename T, int DP, bool SCORES, bool CAREFUL>
+// SCORES: a cache, which keeps its scores where `scores` says.  ON: the rows have met other keys before.
+template <typename T, int DP, bool SCORES, bool CAREFUL, bool ON = false>
 __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, int D, float c, const Limits& lim, char* shared, const Scores& scores) {
   constexpr int KT = 32, KB = Layout<DP>::k_bytes(KT), VB = Layout<DP>::v_bytes(KT);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lds = (uint32_t)(uintptr_t)(TMAC_LDS char*)shared + wave * (KB + VB), lds_v = lds + KB;
-  clear(w);
+  if constexpr (!ON) clear(w);
   const Stage<DP, KT, 1, false> ks(keys.k_stride, D, wave, lane);
   const Stage<DP, KT, 1, true> vs(keys.v_stride, D, wave, lane);
   constexpr int LOADS = Stage<DP, KT, 1, false>::N;

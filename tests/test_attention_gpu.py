@@ -452,3 +452,37 @@ LARGE_DECODES = [  # enough rows over a long prefix for workgroups of 128 rows
 @pytest.mark.parametrize("weigh", [False, True])
 def test_large_decode(A, case, weigh):
     test_decode(A, case, weigh)
+
+
+SHORT_PREFIXES = [  # prefix and cache by one workgroup, or just not
+    (64, 8, 8, 128, 40, 500, F16),
+    (64, 8, 8, 128, 40, 513, F16),
+    (20, 128, 16, 128, 300, 512, BF16),
+    (33, 16, 8, 100, 512, 3, BF16),
+    (1, 4, 2, 68, 30, 482, F16),
+    (1, 4, 2, 68, 30, 483, F16),
+    (3, 66, 2, 36, 9, 100, F16),         # more heads in a group than rows of a tile
+]
+
+
+@pytest.mark.parametrize("case", SHORT_PREFIXES, ids=str)
+@pytest.mark.parametrize("weigh", [False, True])
+def test_decode_after_a_short_prefix(A, case, weigh):
+    test_decode(A, case, weigh)
+
+
+@pytest.mark.parametrize("P", [40, 600])
+def test_decode_strides_of_the_prefix(A, P):
+    B, Hq, Hkv, D, C = 2, 4, 2, 100, 50
+    cache, k, v = filled(A, B, Hq, Hkv, D, C, [[50, 13], [0, 1]], BF16)
+    wide = rand(8, P, 2, Hkv, D + 4, dtype=BF16).cuda()
+    qw = rand(9, B, Hq, D + 20, dtype=BF16).cuda()
+    k0, v0, q = wide[:, 0, :, :D], wide[:, 1, :, 4:], qw[..., 16:D + 16]
+    want = ref.decode(q.cpu(), k0.cpu(), v0.cpu(), k, v, cache.lens.cpu(), 0.1)
+    before = cache.weight.double().cpu()
+    cache.desc.scale = 0.1
+    out, lse = cache.attend(q, k0, v0)
+    near(out, want[0], want[3], "out")
+    near(lse, want[1], want[4], "lse")
+    total = want[2] + before
+    near(cache.weight, total, want[5] + 2.0 ** -23 * total, "weight")
