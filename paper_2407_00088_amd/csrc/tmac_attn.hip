@@ -736,8 +736,11 @@ static bool desc_ok(const tmac_attn_desc* d) {
 constexpr int WGS = 512;  // workgroups that the chip holds at once, two on a CU
 
 // Rows of a workgroup: 128 share each stage of keys, 32 let the wavefronts share the keys instead, for sequences of at most 32 rows (32
-// of 8 rows after 1000 keys, 8 key heads: 24.7 us with 32, 28.6 with 128; 32 of 64 rows, 32 heads: 32.0 and 21.7) and for calls that
-// leave half of the chip idle otherwise (256 rows, 40 heads: 10.0 and 13.1; 1024 rows, 64 heads in groups of 8: 47.2 and 32.3).
+// of 8 rows after 1000 keys, 8 key heads: 24.7 us with 32, 28.6 with 128; 32 of 64 rows, 32 heads: 32.0 and 21.7) and where the last row's
+// walk over its keys, four times as long with 128 rows, would take longer than the four times as many workgroups of 32: those take about
+// (6 + seen keys / 80) us for each 128 of 128 rows' number, the walk (5 + keys / 46) us; where half of the chip would stay idle, always (8 heads, 4096 tokens: 61.8 us with 32, 86.8 with 128, 6000
+// 120 and 134, 8192 209 and 208; 32 heads, 1024 tokens 26.8 and 27.9, 1600 50.6 and 42.8; 64 in groups of 8, 512 tokens 20.5 and 18.2; 2 key heads with
+// 3 each, 3026, 1400, 700, 300 and 90 tokens 39.2 and 62.6; 40 heads, 256 tokens 10.0 and 13.1).
 // Slices: as many as it takes to fill the chip, none shorter than 256 keys, if that saves the walk over 768 keys or more, since the
 // parts are joined by another launch (16 rows after 4096 keys: 14.1 us in 16 slices, 15.0 in 8; 1000 rows, 8 heads in groups of 4:
 // 18.2 us in two, 14.3 in one).
@@ -749,7 +752,9 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   PromptPlan p;
   const int64_t G = d->Hq / d->Hkv, rows = Tq * G;
   auto tiles_of = [&](int per) { return (int)std::min<int64_t>(rows / per + S, rows); };
-  p.blocks = rows / S <= 32 || (int64_t)tiles_of(128) * d->Hkv < WGS / 2 ? 1 : 4;
+  const int64_t keys = Tk / S, seen = d->causal ? std::max(keys / 2, keys - Tq / S / 2) : keys;
+  const int64_t wide = (int64_t)tiles_of(128) * d->Hkv;
+  p.blocks = rows / S <= 32 || wide < WGS / 2 || wide * (480 + seen) <= 51200 + 224 * keys ? 1 : 4;
   p.tiles = tiles_of(32 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
   p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({WGS / wgs, (Tk / S) / 256, 64}));
