@@ -767,8 +767,10 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
 
 // Blocks of 32 keys a wavefront: two, once that leaves enough units (each key tile's stages) for the chip; the reads of q then serve twice
 // (6144 tokens, 64 heads in groups of 8: 379 us with one, 337 with two; five prompts of up to 777 tokens 17.5 and 20.2).  Slices of a tile's
-// stages: until there are four times the workgroups that the chip holds, because tiles weigh unlike (the former 605 us at one time, 351 at
-// two, 331 at four, 332 at eight), none shorter than two stages (the latter 17.5 us; four 21.6, one 20.2).
+// stages: twice the workgroups that the chip holds, up to four times while eight stages are left to each, because tiles weigh unlike but a
+// workgroup's start costs as much as four stages or more (6144 tokens: 605 us at one time, 351 at two, 331 at four, 332 at eight; 12 of 327 tokens, 16
+// heads of one key head 27.1 at four times, 19.4 so; 2000 tokens, 32 heads in groups of 4 38.6 and 32.1; 1024 tokens, 32 heads 17.0 and 14.1; three of
+// 1000 27.6 and 28.3), none shorter than two stages (five of up to 777 17.5 us; four 21.6, one 20.2).
 struct WeightsPlan {
   int blocks, tiles, slices;
   size_t bytes;
@@ -780,7 +782,7 @@ static WeightsPlan weights_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) 
   p.blocks = (int64_t)tiles_of(256) * d->Hkv * stages >= 8192 ? 2 : 1;
   p.tiles = tiles_of(128 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
-  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({4 * WGS / wgs, stages / 2, 64}));
+  p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({4 * WGS / wgs, std::max<int64_t>(2 * WGS / wgs, stages / 8), stages / 2, 64}));
   p.bytes = p.slices > 1 ? (size_t)p.slices * d->Hkv * Tk * 4 : 0;
   return p;
 }
