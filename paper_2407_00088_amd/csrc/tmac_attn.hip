@@ -248,10 +248,10 @@ struct Tile {
 };
 
 // One workgroup: 32 BLOCKS rows of one sequence and key head over the keys they see, or one slice of those; queries are read once,
-// keys once a tile, from the XCD's L2.  Long sequences are bound by power: 8192 tokens, 64 heads in groups of 8 of 128 elements take 1.11 ms, 0.99
+// keys once a tile, from the XCD's L2.  Long sequences are bound by power: 8192 tokens, 64 heads in groups of 8 of 128 elements take 1.10 ms, 1.0
 // PFLOP/s of the pairs that rows see (a large matrix product reaches 1.37), at 1.7 of 2.4 GHz with the matrix units busy for 52 % of the
 // cycles and the vector ALUs, mostly with exponentials, for 47 %; LDS has no bank conflicts.  Short ones are bound by latency: 33 tokens, 32
-// heads 6.1 us, one wavefront's chain of loads, products and exchanges.
+// heads 6.2 us, one wavefront's chain of loads, products and exchanges.
 template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
   typedef Shape<DP, BLOCKS> Sh;
@@ -356,7 +356,7 @@ constexpr int SHORT = 512, LDS_ROWS = 4;
 // leaves a part of its rows.  WHOLE: workgroups of the caches only, which take a short prefix first and leave finished rows and, with
 // accumulate, the slots' weights.  A tile of 32 rows is
 // mostly empty for a group of 8 heads, but caches are bound by memory (24 of 4095 slots, 8 key heads of 128 elements, 403 MB: 78 us,
-// 5.1 TB/s, what a large copy reaches), and a prefix fills its tiles (64 rows of 64 heads in groups of 8 over 16384 keys: 46 us, 750 TFLOP/s
+// 5.2 TB/s, what a large copy reaches), and a prefix fills its tiles (64 rows of 64 heads in groups of 8 over 16384 keys: 46 us, 750 TFLOP/s
 // before the parts are joined; a row alone would read 67 MB for itself).
 template <typename T, int DP, int BLOCKS, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a) {
