@@ -33,7 +33,8 @@ __device__ __forceinline__ void store4(char* to, f4 x) {
   *reinterpret_cast<typename T::v4*>(to) = __builtin_convertvector(x, typename T::v4);
 }
 
-// row_lse (BLOCKS = 1 only, or null): 32 numbers in LDS beyond those that the sums meet in, the rows' lse in units of log 2.
+// row_lse (BLOCKS = 1 only, or null): 32 numbers in LDS beyond those that the sums meet in, the rows' lse in units of log 2, there for all
+// wavefronts when it returns.
 template <typename T, int DP, int BLOCKS>
 __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool parts, int D, char* lds, float* row_lse = nullptr) {
   constexpr int ND = DP / 32;
@@ -80,10 +81,11 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
       const f2 x = ml[i * 32 + (lane & 31)];
       l += x[0] == m ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - m);
     }
-    // every lane keeps its row's scale and target for the lanes that store the row
-    __syncthreads();
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    // (before the last barrier: the caller's wavefronts read it without another)
     if (row_lse && half == 0 && wave == 0) row_lse[lane] = l == 0.0f ? INFINITY : m + __builtin_log2f(l);
+    __syncthreads();
+    // every lane keeps its row's scale and target for the lanes that store the row
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (to.out && half == 0 && wave == 0) {
       if (parts) *reinterpret_cast<f2*>(to.ml) = f2{m, l};
       else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * LN2;
@@ -455,7 +457,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
   }
   finish<T, DP, 1>(w, to, !WHOLE, a.D, lds, WHOLE ? row_lse : nullptr);
   if (!WHOLE || !weight || slot0 >= n) return;
-  // (the scores have been written by this workgroup: all are past the barriers of `finish`)
+  // (the scores and row_lse have been written by this workgroup, before the last barrier of `finish`)
   f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   if (in_lds_rows) {
     for (int y = 0; y < a.G; ++y) {

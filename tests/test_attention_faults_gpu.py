@@ -1,0 +1,31 @@
+"""Faults of the attention operators that have been mended, on the GPU: each case is one that came out wrong, or could have."""
+import math
+
+import pytest
+import torch
+
+import attn_reference as ref
+from test_attention_gpu import A, BF16, F16, cu, filled, i32, near, rand  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("G", [1, 4, 5, 32])
+@pytest.mark.parametrize("C,P", [(257, 0), (400, 100), (512, 0)])
+def test_weights_of_all_wavefronts_slots(A, G, C, P):
+    """Slots from the 257th on are weighed by other wavefronts than the one that has the rows' sums: the formula's weights, and the same
+    bits every time."""
+    B, Hkv, D = 16, 8, 64
+    cache, k, v = filled(A, B, Hkv * G, Hkv, D, C, [[C - (b + h) % 3 for h in range(Hkv)] for b in range(B)], F16)
+    q, before = rand(5, B, Hkv * G, D).cuda(), cache.weight.clone()
+    k0, v0 = (rand(6, P, Hkv, D), rand(7, P, Hkv, D)) if P else (None, None)
+    prefix = [x.cuda() for x in (k0, v0)] if P else []
+    want = ref.decode(q.cpu(), k0, v0, k, v, cache.lens.cpu(), 1 / 8)
+    total = want[2] + before.double().cpu()
+    first = None
+    for _ in range(20):
+        cache.weight.copy_(before)
+        cache.attend(q, *prefix)
+        first = cache.weight.clone() if first is None else first
+        assert torch.equal(cache.weight, first)
+    near(first, total, want[5] + 2.0 ** -23 * total, "weight")
