@@ -74,8 +74,8 @@ struct Layout {
   static constexpr int CH = DP / 8, RPI = 64 / CH;  // chunks of a row, rows of a load
   static constexpr int k_bytes(int rows) { return rows / RPI * 1088; }
   static constexpr int v_bytes(int rows) { return rows * DP * 2; }
-  static __device__ __forceinline__ int k_swizzle(int row) { return (DP == 128 ? row : row >> 1) & 3; }
-  static __device__ __forceinline__ int v_swizzle(int row) { return (DP == 128 ? row & 3 : row >> 1 & 1) << 2; }
+  static __host__ __device__ __forceinline__ int k_swizzle(int row) { return (DP == 128 ? row : row >> 1) & 3; }
+  static __host__ __device__ __forceinline__ int v_swizzle(int row) { return (DP == 128 ? row & 3 : row >> 1 & 1) << 2; }
   static __device__ __forceinline__ int k_row(int row) { return row / RPI * 1088 + row % RPI * DP * 2; }
 };
 
@@ -90,8 +90,8 @@ struct Keys {
 
 // Rows of 16-bit elements on their way from memory to LDS: 1024 bytes a load of one wavefront, lane after lane, without passing
 // through registers.  Memory need only be 8-byte aligned.  Chunks of 16 bytes that lie within the row's D elements are loaded;
-// a half chunk at the row's end (D % 8 == 4) comes with its neighbour's elements, which is fine for V, whose columns from D on give
-// results that nobody reads, but not for K, where they would meet the products' sums: there the half chunk goes through a
+// a half chunk at the row's end (D % 8 == 4) comes with its neighbour's elements, or with zeros after the last row, which is fine for V,
+// whose columns from D on give results that nobody reads, but not for K, where they would meet the products' sums: there the half chunk goes through a
 // register (load_tail, store_tail).  Chunks beyond are cleared once (clear_pads).
 //
 // The load is written out: of the builtin the compiler knows only that it writes LDS, and makes every transposed read wait
@@ -122,21 +122,25 @@ struct Stage {
   uint32_t at;   // bytes from the first row to the lane's chunk in the wavefront's first load
   bool wanted;   // its elements lie within the row (K: all of them)
 
-  __device__ __forceinline__ Stage(int64_t stride, int D, int wave, int lane) {
+  __host__ __device__ __forceinline__ Stage(int64_t stride, int D, int wave, int lane) {
     const int row = lane / L::CH, chunk = (lane % L::CH) ^ (IS_V ? L::v_swizzle(row) : L::k_swizzle(row));
     at = (row + (WAVES == 1 ? 0 : wave * L::RPI)) * (uint32_t)stride + chunk * 16;
     wanted = IS_V ? chunk * 8 < D : chunk * 8 + 8 <= D;
   }
-  // Rows from `rows` on read as zeros: the descriptor's range ends there.  (What a scalar register adds to the address is not
-  // checked against the range, so it is used for whole stages only.)  Unwanted chunks stay as they are where wavefronts share a
+  // Bytes from the first row to the end of the last of n.
+  static __host__ __device__ __forceinline__ int span(int64_t stride, int n, int D) { return n > 0 ? (n - 1) * (int)stride + D * 2 : 0; }
+  // Whether scalar offsets may take the loads from row to row of a stage of which `rows` are there.  They are not checked against the
+  // range, so all rows have to be there, and for V's half chunks, which come with the eight bytes after the row, one more.
+  static __host__ __device__ __forceinline__ bool unchecked(int rows, int D) { return rows >= ROWS + (IS_V && D % 8 ? 1 : 0); }
+  // Rows from `rows` on read as zeros: the descriptor's range ends there.  Unwanted chunks stay as they are where wavefronts share a
   // stage, and become zeros where they do not: such a load is always issued, so that loads can be counted.
   __device__ __forceinline__ void load(const char* base, int64_t stride, int rows, int D, uint32_t lds, int wave, bool once = false) const {
     if (WAVES != 1 && !wanted) return;
     const uint32_t offset = wanted ? at : 0x7fffff00u;
     const int step = WAVES * L::RPI * (int)stride;
     if (WAVES != 1) lds += wave * APART;
-    if (rows >= ROWS) {
-      const u4 rsrc = buffer_of(base, (ROWS - 1) * (int)stride + D * 2);
+    if (unchecked(rows, D)) {
+      const u4 rsrc = buffer_of(base, span(stride, ROWS, D));
       if (once) {
 #pragma unroll
         for (int i = 0; i < N; ++i) load_to_lds_once(rsrc, lds + i * WAVES * APART, offset, i * step);
@@ -145,7 +149,7 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < N; ++i) load_to_lds(rsrc, lds + i * WAVES * APART, offset, i * step);
     } else {
-      const int range = rows > 0 ? (rows - 1) * (int)stride + D * 2 : 0;
+      const int range = span(stride, min(rows, ROWS), D);
 #pragma unroll
       for (int i = 0; i < N; ++i) load_to_lds(buffer_of(base + i * (int64_t)step, max(0, range - i * step)), lds + i * WAVES * APART, offset, 0);
     }

@@ -29,3 +29,22 @@ def test_weights_of_all_wavefronts_slots(A, G, C, P):
         first = cache.weight.clone() if first is None else first
         assert torch.equal(cache.weight, first)
     near(first, total, want[5] + 2.0 ** -23 * total, "weight")
+
+
+@pytest.mark.parametrize("D", [4, 60, 100])
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_half_chunks_of_rows_that_end_with_a_stage(A, D, dt):
+    """Sequences whose last row is the last of a whole stage: the half chunk at its end is not followed by another row."""
+    for nq, H in (([64, 128], 2), ([256, 128], 64)):           # workgroups of 32 and of 128 rows
+        q, k, v = (rand(i, sum(nq), H, D, dtype=dt) for i in range(3))
+        want = ref.prompt(q, k, v, cu(nq), cu(nq), True, 1 / math.sqrt(D))
+        out, lse = A.attn_prompt(q.cuda(), k.cuda(), v.cuda(), i32(cu(nq)))
+        near(out, want[0], want[3], "out")
+        near(lse, want[1], want[4], "lse")
+    cache, k, v = filled(A, 2, 4, 2, D, 256, [[256, 128], [32, 64]], dt)
+    q, k0, v0 = rand(5, 2, 4, D, dtype=dt), rand(6, 128, 2, D, dtype=dt), rand(7, 128, 2, D, dtype=dt)
+    for prefix in ((), (k0, v0)):
+        want = ref.decode(q, *(prefix or (None, None)), k, v, cache.lens.cpu(), 1 / math.sqrt(D))
+        out, lse = cache.attend(q.cuda(), *(x.cuda() for x in prefix), weigh=False)
+        near(out, want[0], want[3], "out")
+        near(lse, want[1], want[4], "lse")

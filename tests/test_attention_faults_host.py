@@ -1,7 +1,11 @@
 """Faults of the attention operators that reading or the CPU can show: what a kernel's wavefronts hand to each other, what its loads
 reach, what the entry points refuse.  No GPU needed."""
+import ctypes
 import os
 import re
+import subprocess
+
+import pytest
 
 from paper_2407_00088_amd import build
 
@@ -27,3 +31,66 @@ def test_sums_of_rows_are_handed_over_before_the_last_barrier():
     finish = body_of(src, "void finish(")
     writes = [m.start() for m in re.finditer(r"row_lse\[", finish)]
     assert writes and max(writes) < finish.rindex("__syncthreads()")
+
+
+REACH = """
+#include "tmac_attn_core.h"
+using namespace tmac::attn;
+// Bytes from the first row to the end of what the loads of a stage read, of `rows` that are there: of 16 bytes a lane, four bytes at a
+// time, those whose offset (without what a scalar register adds) is below the descriptor's range.
+template <int DP, int ROWS, int WAVES, bool IS_V>
+static long long reach(long long stride, int rows, int D) {
+  typedef Stage<DP, ROWS, WAVES, IS_V> St;
+  long long most = 0;
+  for (int wave = 0; wave < WAVES; ++wave)
+    for (int lane = 0; lane < 64; ++lane) {
+      const St st(stride, D, wave, lane);
+      if (!st.wanted) continue;
+      const bool unchecked = St::unchecked(rows, D);
+      const long long step = WAVES * Layout<DP>::RPI * stride;
+      for (int i = 0; i < St::N; ++i) {
+        const long long range = unchecked ? St::span(stride, ROWS, D) : St::span(stride, rows < ROWS ? rows : ROWS, D) - i * step;
+        for (int b = 0; b < 16; b += 4)
+          if ((long long)st.at + b < range) most = st.at + b + 4 + i * step > most ? st.at + b + 4 + i * step : most;
+      }
+    }
+  return most;
+}
+extern "C" long long reach_of(int kind, long long stride, int rows, int D) {
+  switch (kind + (D > 64 ? 8 : 0)) {
+    case 0: return reach<64, 64, 4, false>(stride, rows, D);
+    case 1: return reach<64, 64, 4, true>(stride, rows, D);
+    case 2: return reach<64, 32, 1, false>(stride, rows, D);
+    case 3: return reach<64, 32, 1, true>(stride, rows, D);
+    case 8: return reach<128, 64, 4, false>(stride, rows, D);
+    case 9: return reach<128, 64, 4, true>(stride, rows, D);
+    case 10: return reach<128, 32, 1, false>(stride, rows, D);
+    default: return reach<128, 32, 1, true>(stride, rows, D);
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def reach(tmp_path_factory):
+    out = tmp_path_factory.mktemp("reach") / "reach.so"
+    flags = [f for f in build.HIPCC_FLAGS if not f.startswith(("--offload-arch", "-O", "-amdgpu", "-mllvm"))]
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "-O1", "--offload-host-only", "-no-hip-rt", "-x", "hip", "-",
+                    "-o", str(out)], input=REACH.encode(), stderr=subprocess.DEVNULL, check=True)
+    lib = ctypes.CDLL(str(out))
+    lib.reach_of.restype, lib.reach_of.argtypes = ctypes.c_longlong, [ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+    return lib.reach_of
+
+
+@pytest.mark.parametrize("D", [4, 8, 36, 60, 64, 68, 100, 124, 128])
+def test_stages_end_with_their_last_row(reach, D):
+    """Nothing is read beyond the last element of the last row that is there, where the tensor and its memory may end, and everything
+    before it is."""
+    for kind in range(4):
+        for stride in (2 * D, 2 * D + 8, 64 * D, 0):
+            for rows in [*range(1, 70), 1000]:
+                there = min(rows, 64 if kind < 2 else 32)
+                end = reach(kind, stride, rows, D)
+                assert end <= (rows - 1) * stride + 2 * D, (kind, stride, rows)
+                # (K's last half chunk comes another way)
+                assert end >= (there - 1) * stride + 2 * (D if kind % 2 else D // 8 * 8) or D < 8, (kind, stride, rows)
