@@ -67,7 +67,7 @@ tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_view* q, con
  *   lse_dev     fp32 [Hq, Tq] as tmac_attn_prompt writes it (or that of tmac_attn_decode over one shared prefix, transposed)
  *   weight_dev  fp32 [Hkv, Tk], overwritten
  *   workspace   tmac_attn_weights_workspace_bytes(desc, S, Tq, Tk)
- * The order of the sums depends on the sizes only. */
+ * The order of the sums depends on the sizes only.  Errors: as tmac_attn_prompt's, of q and k. */
 size_t tmac_attn_weights_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk);
 tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k, const float* lse_dev, int32_t S,
                               int32_t Tq, int32_t Tk, const int32_t* cu_q_dev, const int32_t* cu_k_dev, float* weight_dev,

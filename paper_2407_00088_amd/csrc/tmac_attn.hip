@@ -931,7 +931,7 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
   if (desc->D > 128 || (int64_t)Tq * desc->Hq > 0x7fffffff || long_axis(S) || long_axis(Tq) || long_axis(Tk)) return TMAC_EUNSUPPORTED;
   const tmac_view none = {};
   if (Tq == 0) q = &none;
-  if (far_rows(q)) return TMAC_EUNSUPPORTED;
+  if (far_rows(q) || far_rows(k)) return TMAC_EUNSUPPORTED;
   const WeightsPlan p = weights_plan(desc, S, Tq, Tk);
   if (p.bytes) {
     if (!workspace_dev || !aligned16(workspace_dev)) return TMAC_EINVAL;

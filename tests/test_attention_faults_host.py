@@ -7,6 +7,7 @@ import subprocess
 
 import pytest
 
+import test_attention_host as H
 from paper_2407_00088_amd import build
 
 
@@ -94,3 +95,13 @@ def test_stages_end_with_their_last_row(reach, D):
                 assert end <= (rows - 1) * stride + 2 * D, (kind, stride, rows)
                 # (K's last half chunk comes another way)
                 assert end >= (there - 1) * stride + 2 * (D if kind % 2 else D // 8 * 8) or D < 8, (kind, stride, rows)
+
+
+def test_weights_refuse_rows_that_are_far_apart():
+    """Rows of q and of k go through descriptors of 31-bit ranges, as those of the prompts' k and v do."""
+    def weights(q=None, k=None):
+        return H.A.lib.tmac_attn_weights(H.desc(), q or H.view(), k or H.view(), H.P16, 1, 10, 10, H.P16, H.P16, H.P16, H.P16, 1 << 40, None)
+    for token in (1 << 22, 1 << 27, 1 << 39):
+        assert weights(q=H.view(token=token)) == weights(k=H.view(token=token)) == H.T.TMAC_EUNSUPPORTED
+        assert H.prompt(k=H.view(token=token)) == H.prompt(v=H.view(token=token)) == H.T.TMAC_EUNSUPPORTED
+        assert H.decode(k0=H.view(token=token)) == H.decode(c=H.cache(v=H.view(seq=2560, token=token))) == H.T.TMAC_EUNSUPPORTED
