@@ -38,14 +38,15 @@ class DecoderAttention:
         return rotated(rows[0], positions), rotated(rows[1], positions), rows[2]
 
     def share(self, x) -> None:
-        """A prefix [P, M] for all sequences, which comes before their own tokens."""
+        """A prefix [P, M] for all sequences, which comes before their own tokens: those, if there are any, end here."""
         _, k, v = self.project(x, torch.arange(x.shape[0], device=x.device))
         self.prefix, self.prefix_length = (k, v), x.shape[0]
-        self.position += x.shape[0]
+        self.cache.lens.zero_(), self.cache.seen.zero_()
+        self.position.fill_(self.prefix_length)
 
     def prompt(self, x, cu):
         """The sequences' own prompts, packed: x [T, M], cu int32 [batch + 1] on the GPU and the tokens' positions by it.  Returns [T, M]; the cache
-        keeps what it has room for."""
+        keeps what it has room for, and nothing of earlier prompts and steps."""
         n = (cu[1:] - cu[:-1]).long()
         at = torch.arange(x.shape[0], device=x.device)
         positions = at - torch.repeat_interleave(cu[:-1].long(), n) + self.prefix_length
@@ -67,7 +68,7 @@ class DecoderAttention:
         if self.prefix is not None:
             weight = weight[:, rows]
         self.cache.fill(k, v, weight, cu)
-        self.position += n
+        torch.add(n, self.prefix_length, out=self.position)
         return self.o.forward_one_call(out.view(x.shape[0], -1), out_t=B.TMAC_OUT_F16)
 
     def step(self, x):

@@ -48,3 +48,34 @@ def test_half_chunks_of_rows_that_end_with_a_stage(A, D, dt):
         out, lse = cache.attend(q.cuda(), *(x.cuda() for x in prefix), weigh=False)
         near(out, want[0], want[3], "out")
         near(lse, want[1], want[4], "lse")
+
+
+def test_decoder_layer_starts_anew(A):
+    """A second prefix and a second prompt, after prompts and steps of another conversation: the results of a fresh layer."""
+    from paper_2407_00088_amd import decoder
+    B, M = 2, 256
+    layers = [decoder.random_layer(M, 4, 2, 64, B, 24, 8, max_N=256) for _ in range(2)]
+    first, second, prompts = rand(1, 30, M).cuda(), rand(2, 50, M).cuda(), [rand(3 + i, 19, M).cuda() for i in range(2)]
+    c, steps = i32([0, 12, 19]), [rand(10 + i, B, M).cuda() for i in range(4)]
+    used, fresh = layers
+    used.share(first)
+    used.prompt(prompts[0], c)
+    for x in steps:
+        used.step(x)
+
+    def follow(layer):
+        got = [layer.prompt(prompts[1], c)] + [layer.step(x) for x in steps]
+        return got + [t.clone() for t in (layer.position, layer.cache.lens, layer.cache.seen, layer.cache.pos[:, :, :7])]
+
+    fresh.share(first)
+    for got, want in zip(follow(used), follow(fresh)):        # another prompt
+        assert torch.equal(got, want)
+    for layer in layers:
+        layer.share(second)
+    assert used.position.tolist() == [50, 50] and (used.cache.lens == 0).all()
+    for got, want in zip([used.step(x) for x in steps], [fresh.step(x) for x in steps]):   # no prompt after another prefix
+        assert torch.equal(got, want)
+    fresh = decoder.random_layer(M, 4, 2, 64, B, 24, 8, max_N=256)
+    fresh.share(second)
+    for got, want in zip(follow(used), follow(fresh)):        # another prefix and another prompt
+        assert torch.equal(got, want)
