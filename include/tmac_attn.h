@@ -15,7 +15,9 @@
  * Results overlap neither each other's rows nor what a call reads (a cache's own weights apart, which a step adds to).
  * Elements that a row may not see do not touch its result, whatever they hold (NaN and infinities too).  Scores, exponentials,
  * sums and lse are 32-bit; the exponentials are rounded to the inputs' type before they are multiplied with v (an error of
- * the size of the result's own rounding), o_i is rounded once.
+ * the size of the result's own rounding; in fp16, exponentials below 2^-20 of the row's largest are instead off by up to 2^-31 of it, so a
+ * row over n keys by up to n 2^-31 of the largest |v| more), o_i is rounded once.  Sums are 32-bit before they are divided by the
+ * row's: |v| below 2^90 stays finite whatever the scores.
  */
 #ifndef TMAC_ATTN_H_
 #define TMAC_ATTN_H_

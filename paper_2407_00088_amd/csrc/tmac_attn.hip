@@ -19,13 +19,13 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // --- epilogue ------------------------------------------------------------------------------------------------------------
 
-// Where a row's result goes: the finished row, or a part of it (sums against its own maximum, which ml holds in units of
+// Where a row's result goes: the finished row, or a part of it (sums against a number of its own, which ml holds in units of
 // log 2, with the sum of exponentials).
 struct Target {
   char* out;     // the row's D elements; null: the lane's row does not exist
   float* lse;    // or null
   float* part;   // parts: the row's D sums
-  float* ml;     // parts: maximum and sum
+  float* ml;     // parts: what the sums are taken against, and the sum
 };
 
 template <typename T>
@@ -55,7 +55,7 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
       }
     if (half != 0) return;
     if (parts) *reinterpret_cast<f2*>(to.ml) = f2{w.m, w.l};
-    else if (to.lse) *to.lse = w.l == 0.0f ? -INFINITY : (w.m + __builtin_log2f(w.l)) * LN2;
+    else if (to.lse) *to.lse = w.l == 0.0f ? -INFINITY : log2_sum<T>(w.m, w.l) * LN2;
   } else {
     // the wavefronts that share rows meet in LDS: [wave][32 rows][DP + 4] sums, then [wave][32] maximum and sum
     constexpr int KW = 4, W = DP + 4;
@@ -82,13 +82,13 @@ __device__ __forceinline__ void finish(Rows<T, DP>& w, const Target& to, bool pa
       l += x[0] == m ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - m);
     }
     // (before the last barrier: the caller's wavefronts read it without another)
-    if (row_lse && half == 0 && wave == 0) row_lse[lane] = l == 0.0f ? INFINITY : m + __builtin_log2f(l);
+    if (row_lse && half == 0 && wave == 0) row_lse[lane] = l == 0.0f ? INFINITY : log2_sum<T>(m, l);
     __syncthreads();
     // every lane keeps its row's scale and target for the lanes that store the row
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (to.out && half == 0 && wave == 0) {
       if (parts) *reinterpret_cast<f2*>(to.ml) = f2{m, l};
-      else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * LN2;
+      else if (to.lse) *to.lse = l == 0.0f ? -INFINITY : log2_sum<T>(m, l) * LN2;
     }
     // the rows, dealt over the wavefronts: 16 lanes a row where DP = 64, 32 where it is 128
     constexpr int LPR = DP / 4, RPW = 64 / LPR, N = 32 / KW / RPW;
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
 // --- parts of rows ------------------------------------------------------------------------------------------------------------
 
 struct Joined {
-  float top, sum;  // maximum of the parts in units of log 2, sum of exponentials against it
+  float top, sum;  // largest of what the parts' sums are taken against, sum of exponentials against it
 };
 
 // Of a row's n parts, one wavefront.
@@ -515,7 +515,7 @@ __device__ __forceinline__ void join_row(const float* part, const float* ml, int
     typedef typename T::elem e2 __attribute__((ext_vector_type(2)));
     *reinterpret_cast<e2*>(out + at * 2) = __builtin_convertvector(x * inv, e2);
   }
-  if (lane == 0 && lse) *lse = j.sum == 0.0f ? -INFINITY : (j.top + __builtin_log2f(j.sum)) * LN2;
+  if (lane == 0 && lse) *lse = j.sum == 0.0f ? -INFINITY : log2_sum<T>(j.top, j.sum) * LN2;
 }
 
 // One wavefront a row: about 4 us, what a launch with a chain of two loads takes (128 rows after 8192 keys, 32 heads).
@@ -566,7 +566,7 @@ __global__ __launch_bounds__(256) void join_decode_kernel(const DecodeArgs a) {
       const int64_t row = (int64_t)b * a.Hq + h * a.G + g0 + g;
       const Joined j = join(a.ml + row * 2, rows * 2, a.prefix_slices + (n + a.chunk_keys - 1) / a.chunk_keys, lane);
       // (a row without a score above -inf gives no weights)
-      if (lane == 0) row_lse[g] = j.sum == 0.0f ? INFINITY : j.top + __builtin_log2f(j.sum);
+      if (lane == 0) row_lse[g] = j.sum == 0.0f ? INFINITY : log2_sum<T>(j.top, j.sum);
     }
     __syncthreads();
     if (at < n) sum += sum_weights(s, a.score_stride, heads, x, row_lse, c);

@@ -39,7 +39,11 @@ __device__ __forceinline__ TMAC_LDS X* in_lds(uint32_t at) {
   return (TMAC_LDS X*)(uintptr_t)at;
 }
 
+// HEADROOM: the sums are taken against the row's maximum less this (in units of log 2).  Exponentials of fp16 then reach 2^7, and 2^15
+// before the maximum is moved (outgrows), and keep all their bits down to 2^-20 of the row's largest; below that they are off by at most
+// 2^-31 of it.  (Against the maximum itself a flat tail of 10^5 keys beside a heavy one lost what lay below 2^-25.)  bf16 has the range anyway.
 struct F16 {
+  static constexpr float HEADROOM = 7.0f;
   typedef _Float16 elem;
   typedef h4 v4;
   typedef h8 v8;
@@ -47,6 +51,7 @@ struct F16 {
   static __device__ __forceinline__ f16x mfma(v8 a, v8 b, f16x c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 struct BF16 {
+  static constexpr float HEADROOM = 0.0f;
   typedef __bf16 elem;
   typedef b4 v4;
   typedef b8 v8;
@@ -317,12 +322,21 @@ __device__ __forceinline__ float largest(const f16x& s) {
 }
 
 // Whether the row's sums have to be taken against a larger number.  They keep theirs until a score is 2^8 times larger:
-// exponentials up to 256 are as exact in 16 bits, and most tiles then need no rescaling.  (Row by row: a row's bits do not
-// depend on its neighbours.)  A whole number in units of log 2, so that what is rescaled keeps its bits.
-__device__ __forceinline__ bool outgrows(float mx, float c, float m) { return mx * c > m + 8.0f; }
+// exponentials 256 times as large are as exact in 16 bits, and most tiles then need no rescaling.  (Row by row: a row's bits do not
+// depend on its neighbours.)  A whole number in units of log 2, so that what is rescaled keeps its bits.  Compared is the exponent
+// itself, so that it stays within the type also where m is too large for its last digits.
+template <typename T>
+__device__ __forceinline__ bool outgrows(float mx, float c, float m) {
+  return __builtin_fmaf(mx, c, -m) > T::HEADROOM + 8.0f;
+}
+// log 2 of the sum of exp of a row's scores; l: of its exponentials against m.
+template <typename T>
+__device__ __forceinline__ float log2_sum(float m, float l) {
+  return m + T::HEADROOM + __builtin_log2f(l * __builtin_exp2f(-T::HEADROOM));
+}
 template <typename T, int DP>
 __device__ __forceinline__ void rescale(Rows<T, DP>& w, float mx, float c, bool grows) {
-  const float m = grows ? __builtin_ceilf(mx * c) : w.m;
+  const float m = grows ? __builtin_ceilf(mx * c) - T::HEADROOM : w.m;
   const float alpha = grows ? __builtin_amdgcn_exp2f(w.m - m) : 1.0f;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) w.o[d] *= alpha;
@@ -439,7 +453,7 @@ __device__ __forceinline__ void run_shared(Rows<T, DP>& w, const Keys& keys, int
 #pragma unroll
     for (int b = 1; b < KB; ++b) mx = fmaxf(mx, largest(s[b]));
     mx = max_halves(mx);
-    const bool grows = outgrows(mx, c, w.m);
+    const bool grows = outgrows<T>(mx, c, w.m);
     if (__any(grows)) rescale(w, mx, c, grows);
     const float m = base_of(w.m);
 #pragma unroll
@@ -511,7 +525,7 @@ __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, in
     const int x = lim.row - at - 4 * (lane >> 5);
     if (lim.least < at + KT) hide(s, x);
     const float mx = max_halves(largest(s));
-    const bool grows = outgrows(mx, c, w.m);
+    const bool grows = outgrows<T>(mx, c, w.m);
     if (__any(grows)) rescale(w, mx, c, grows);
     typename T::v8 p[2];
     w.l += exponentials<T>(s, c, base_of(w.m), p[0], p[1]);

@@ -79,3 +79,27 @@ def test_decoder_layer_starts_anew(A):
     fresh.share(second)
     for got, want in zip(follow(used), follow(fresh)):        # another prefix and another prompt
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("Tq,H,Tk", [(8192, 8, 1 << 17), (32, 512, 1 << 19)])
+def test_a_flat_tail_beside_a_heavy_key(A, dt, Tq, H, Tk):
+    """One key 2^25.5 times as heavy as each of the others, which all its row's sums are taken against: the others' exponentials are below
+    what 16 bits hold, if taken against that key's, and together 0.3 (1.1) % of the row.  Workgroups of 128 and of 32 rows; all rows and heads are
+    alike, the formula's result is computed once.  The bound: rounding of exponentials and result to the type (2.1 U), scores, and for each
+    key in fp16 half a unit of the subnormal numbers, 2^-25, against a largest exponential of 2^6 or more."""
+    D = 64
+    k, v = torch.zeros((Tk, 1, D), dtype=dt), (torch.rand((Tk, 1, D), generator=torch.Generator().manual_seed(1)) + 0.5).to(dt)
+    q = torch.zeros((1, 1, D), dtype=dt)
+    q[0, 0, 0], k[0, 0, 0] = 4.0, 4.40625
+    out, lse = A.attn_prompt(q.cuda().expand(Tq, H, D), k.cuda().expand(Tk, H, D), v.cuda().expand(Tk, H, D), i32([0, Tq]), i32([0, Tk]),
+                             causal=False, scale=1.0)
+    assert (out == out[0, 0]).all() and (lse == lse[0, 0]).all()
+    args = q[:, 0], k[:, 0], v[:, 0], 1.0, torch.ones((1, Tk), dtype=torch.bool)
+    want, want_lse, p = ref.rows(*args)
+    _, lse_b, _ = ref.bounds(*args, p, dt)
+    s = 4.0 * 4.40625
+    u, tail = 2.0 ** -24, Tk * 2.0 ** -31 * 1.5 if dt == F16 else 0.0
+    bound = (2.1 * ref.UNIT[dt] + 4 * ((D + 2) * u * s + 8 * u * (1 + s))) * (p @ v[:, 0].double()) + tail + u
+    near(out[0, :1], want, bound, "out")
+    near(lse[0, :1], want_lse, lse_b, "lse")
