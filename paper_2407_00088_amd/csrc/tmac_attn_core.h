@@ -388,7 +388,8 @@ struct Scores {
   float* base;      // null: not in memory
   int range;        // bytes
   uint32_t offset;  // the lane's, in bytes
-  uint32_t lds;     // the lane's row there, 0: not there
+  static constexpr uint32_t NOWHERE = ~0u;  // (0 is a place)
+  uint32_t lds = NOWHERE;                   // the lane's row there
 };
 
 template <typename T, int DP>
@@ -546,7 +547,7 @@ __device__ __forceinline__ void run_streams(Rows<T, DP>& w, const Keys& keys, in
       }
       stored = true;
     }
-    if (SCORES && scores.lds) {
+    if (SCORES && scores.lds != Scores::NOWHERE) {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         *in_lds<f4>(scores.lds + (at - keys.begin + r * 8 + (lane >> 5) * 4) * 4) = f4{raw[4 * r], raw[4 * r + 1], raw[4 * r + 2], raw[4 * r + 3]};

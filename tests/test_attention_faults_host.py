@@ -34,7 +34,7 @@ def test_sums_of_rows_are_handed_over_before_the_last_barrier():
     assert writes and max(writes) < finish.rindex("__syncthreads()")
 
 
-REACH = """
+CORE = """
 #include "tmac_attn_core.h"
 using namespace tmac::attn;
 // Bytes from the first row to the end of what the loads of a stage read, of `rows` that are there: of 16 bytes a lane, four bytes at a
@@ -57,6 +57,7 @@ static long long reach(long long stride, int rows, int D) {
     }
   return most;
 }
+extern "C" unsigned scores_in_lds() { return Scores{}.lds; }
 extern "C" long long reach_of(int kind, long long stride, int rows, int D) {
   switch (kind + (D > 64 ? 8 : 0)) {
     case 0: return reach<64, 64, 4, false>(stride, rows, D);
@@ -73,28 +74,34 @@ extern "C" long long reach_of(int kind, long long stride, int rows, int D) {
 
 
 @pytest.fixture(scope="module")
-def reach(tmp_path_factory):
+def core(tmp_path_factory):
     out = tmp_path_factory.mktemp("reach") / "reach.so"
     flags = [f for f in build.HIPCC_FLAGS if not f.startswith(("--offload-arch", "-O", "-amdgpu", "-mllvm"))]
     subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "-O1", "--offload-host-only", "-no-hip-rt", "-x", "hip", "-",
-                    "-o", str(out)], input=REACH.encode(), stderr=subprocess.DEVNULL, check=True)
+                    "-o", str(out)], input=CORE.encode(), stderr=subprocess.DEVNULL, check=True)
     lib = ctypes.CDLL(str(out))
     lib.reach_of.restype, lib.reach_of.argtypes = ctypes.c_longlong, [ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
-    return lib.reach_of
+    lib.scores_in_lds.restype = ctypes.c_uint
+    return lib
 
 
 @pytest.mark.parametrize("D", [4, 8, 36, 60, 64, 68, 100, 124, 128])
-def test_stages_end_with_their_last_row(reach, D):
+def test_stages_end_with_their_last_row(core, D):
     """Nothing is read beyond the last element of the last row that is there, where the tensor and its memory may end, and everything
     before it is."""
     for kind in range(4):
         for stride in (2 * D, 2 * D + 8, 64 * D, 0):
             for rows in [*range(1, 70), 1000]:
                 there = min(rows, 64 if kind < 2 else 32)
-                end = reach(kind, stride, rows, D)
+                end = core.reach_of(kind, stride, rows, D)
                 assert end <= (rows - 1) * stride + 2 * D, (kind, stride, rows)
                 # (K's last half chunk comes another way)
                 assert end >= (there - 1) * stride + 2 * (D if kind % 2 else D // 8 * 8) or D < 8, (kind, stride, rows)
+
+
+def test_scores_that_are_not_in_lds_have_no_place_there(core):
+    """Any offset within the 160 KB of LDS, the first too, is one that the compiler may give to the rows of scores."""
+    assert core.scores_in_lds() >= 160 * 1024
 
 
 def test_weights_refuse_rows_that_are_far_apart():
