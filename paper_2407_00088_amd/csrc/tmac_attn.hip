@@ -959,7 +959,7 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
 
 static bool decode_sizes_ok(const tmac_attn_desc* d, const tmac_cache* c, int32_t P, int32_t accumulate) {
   return desc_ok(d) && c && c->B >= 0 && c->capacity >= 0 && P >= 0 && (accumulate == 0 || accumulate == 1) && c->Hkv == d->Hkv &&
-         c->D == d->D && c->elem == d->elem;
+         c->D == d->D && c->elem == d->elem && !c->reserved[0] && !c->reserved[1];
 }
 
 extern "C" size_t tmac_attn_decode_workspace_bytes(const tmac_attn_desc* desc, const tmac_cache* cache, int32_t P, int32_t accumulate) {

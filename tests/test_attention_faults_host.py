@@ -112,3 +112,12 @@ def test_weights_refuse_rows_that_are_far_apart():
         assert weights(q=H.view(token=token)) == weights(k=H.view(token=token)) == H.T.TMAC_EUNSUPPORTED
         assert H.prompt(k=H.view(token=token)) == H.prompt(v=H.view(token=token)) == H.T.TMAC_EUNSUPPORTED
         assert H.decode(k0=H.view(token=token)) == H.decode(c=H.cache(v=H.view(seq=2560, token=token))) == H.T.TMAC_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("at", [0, 1])
+def test_reserved_fields_of_a_cache_are_zero_in_every_call(at):
+    c = H.cache()
+    c.reserved[at] = 1
+    row = H.view(seq=128)
+    assert H.A.lib.tmac_cache_append(c, row, row, None) == H.decode(c=c) == H.T.TMAC_EINVAL
+    assert H.A.lib.tmac_attn_decode_workspace_bytes(H.desc(), c, 10, 1) == H.A.lib.tmac_cache_fill_workspace_bytes(c) == 0
