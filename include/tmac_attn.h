@@ -58,7 +58,7 @@ typedef struct {
  *   lse_dev    fp32 [Hq, Tq], or NULL
  *   workspace  tmac_attn_prompt_workspace_bytes(desc, S, Tq, Tk) bytes (0: none needed), 16-byte aligned, contents arbitrary
  * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; Tq Hq beyond 2^31; S, Tq or Tk beyond 2^30; a stride of 128 rows beyond 2^30
- * bytes), TMAC_ESIZE, TMAC_EHIP. */
+ * bytes; a launch of 2^32 threads, which 2^24 short sequences, times key heads, come to), TMAC_ESIZE, TMAC_EHIP. */
 size_t tmac_attn_prompt_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk);
 tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k, const tmac_view* v, int32_t S,
                              int32_t Tq, int32_t Tk, const int32_t* cu_q_dev, const int32_t* cu_k_dev, const tmac_view* out,
@@ -114,7 +114,8 @@ typedef struct {
 /* Fills the cache: of the n tokens of each sequence and head those stay that eviction down to min(n, capacity) leaves, in the
  * order they have in the source, with their weights and positions.  lens = min(n, capacity), seen as above; slots from there on
  * keep what they hold.  The source must not overlap the cache.
- * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; capacity or total beyond 2^30), TMAC_ESIZE, TMAC_EHIP.
+ * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; capacity or total beyond 2^30; a launch of 2^32 threads, that is B Hkv of 2^22
+ * caches or 2^24 times 64 slots of theirs; of 2^24, or 2^22 of more than 1024 slots, in tmac_cache_append), TMAC_ESIZE, TMAC_EHIP.
  * workspace: tmac_cache_fill_workspace_bytes(cache) bytes.  Weight views may have any strides that are not negative. */
 size_t tmac_cache_fill_workspace_bytes(const tmac_cache* cache);
 tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache_source* source, void* workspace_dev, size_t workspace_bytes,
@@ -132,8 +133,8 @@ tmac_status tmac_cache_append(const tmac_cache* cache, const tmac_view* k, const
  *   lse_dev    fp32 [B, Hq], or NULL
  *   accumulate 1: weight[b, h, j] += sum over the group's heads of exp(s - lse) for the slots in use
  *   workspace  tmac_attn_decode_workspace_bytes(desc, cache, P, accumulate), 16-byte aligned, contents arbitrary
- * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; P or the capacity beyond 2^30; a stride of 128 rows beyond 2^30 bytes; accumulate with the lesser of the group and 32
- * times the capacity beyond 5e8), TMAC_ESIZE, TMAC_EHIP. */
+ * Errors: TMAC_EINVAL, TMAC_EUNSUPPORTED (D over 128; P or the capacity beyond 2^30; a stride of 128 rows beyond 2^30 bytes; a launch of 2^32 threads, that is B Hq of
+ * 2^26 or as many chunks of slots; accumulate with the lesser of the group and 32 times the capacity beyond 5e8), TMAC_ESIZE, TMAC_EHIP. */
 size_t tmac_attn_decode_workspace_bytes(const tmac_attn_desc* desc, const tmac_cache* cache, int32_t P, int32_t accumulate);
 tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_view* q, const tmac_view* k0, const tmac_view* v0, int32_t P,
                              const tmac_cache* cache, int32_t accumulate, const tmac_view* out, float* lse_dev, void* workspace_dev,

@@ -842,7 +842,7 @@ static DecodePlan decode_plan(const tmac_attn_desc* d, int B, int C, int P, bool
 template <typename Args>
 static tmac_status launch(const void* kernel, int64_t grid, const Args& args, void* stream) {
   if (grid <= 0) return TMAC_OK;
-  if (grid > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (!launchable(grid, 256)) return TMAC_EUNSUPPORTED;
   Args a = args;
   void* ptrs[] = {&a};
   const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3(256), ptrs, 0, static_cast<hipStream_t>(stream));
@@ -910,10 +910,11 @@ extern "C" tmac_status tmac_attn_prompt(const tmac_attn_desc* desc, const tmac_v
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
   a.q_wide = wide_rows(q, desc->D);
+  const int64_t join_grid = p.slices > 1 ? ((int64_t)Tq * desc->Hq + 3) / 4 : 0;
+  if (!launchable(join_grid, 256)) return TMAC_EUNSUPPORTED;
   const tmac_status st = launch(TMAC_PICK(prompt_kernel, desc, p.blocks), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
-  if (st != TMAC_OK || p.slices == 1) return st;
-  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>,
-                ((int64_t)Tq * desc->Hq + 3) / 4, a, stream);
+  if (st != TMAC_OK) return st;
+  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_prompt_kernel<F16> : (const void*)join_prompt_kernel<BF16>, join_grid, a, stream);
 }
 
 extern "C" size_t tmac_attn_weights_workspace_bytes(const tmac_attn_desc* desc, int32_t S, int32_t Tq, int32_t Tk) {
@@ -943,10 +944,11 @@ extern "C" tmac_status tmac_attn_weights(const tmac_attn_desc* desc, const tmac_
   a.q_token = q->token * 2, a.q_head = q->head * 2, a.k_token = k->token * 2, a.k_head = k->head * 2;
   a.S = S, a.Tq = Tq, a.Tk = Tk, a.Hq = desc->Hq, a.Hkv = desc->Hkv, a.G = desc->Hq / desc->Hkv, a.D = desc->D;
   a.causal = desc->causal, a.tiles = p.tiles, a.slices = p.slices, a.scale = desc->scale;
+  const int64_t n = (int64_t)desc->Hkv * Tk;
+  if (p.slices > 1 && !launchable((n + 255) / 256, 256)) return TMAC_EUNSUPPORTED;
   const tmac_status st =
       launch(TMAC_PICK(weights_kernel, desc, p.blocks), (int64_t)p.tiles * p.slices * desc->Hkv, a, stream);
   if (st != TMAC_OK || p.slices == 1) return st;
-  const int64_t n = (int64_t)desc->Hkv * Tk;
   int64_t n_arg = n;
   int slices = p.slices;
   void* ptrs[] = {&a.part, &a.weight, &n_arg, &slices};
@@ -1008,8 +1010,9 @@ extern "C" tmac_status tmac_attn_decode(const tmac_attn_desc* desc, const tmac_v
   a.weight_blocks = a.scores ? (C + 1023) / 1024 : 0;
   a.scale = desc->scale;
   const int64_t grid = (int64_t)p.tiles * p.slices * desc->Hkv + (int64_t)B * desc->Hkv * p.row_blocks * p.chunks;
+  const int64_t join_grid = p.whole_rows ? 0 : ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv;
+  if (!launchable(join_grid, 256)) return TMAC_EUNSUPPORTED;
   const tmac_status st = launch(TMAC_PICK(decode_kernel, desc, p.whole_rows ? 0 : p.blocks), grid, a, stream);
-  if (st != TMAC_OK || p.whole_rows) return st;
-  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>,
-                ((int64_t)B * desc->Hq + 3) / 4 + (int64_t)a.weight_blocks * B * desc->Hkv, a, stream);
+  if (st != TMAC_OK) return st;
+  return launch(desc->elem == TMAC_ELEM_F16 ? (const void*)join_decode_kernel<F16> : (const void*)join_decode_kernel<BF16>, join_grid, a, stream);
 }

@@ -19,6 +19,9 @@ inline bool rows_ok(const tmac_view* v, bool seq, bool token, bool head) {
 // Lengths up to which whole tiles past the end are still within 32-bit indexes.
 inline bool long_axis(int64_t n) { return n > (int64_t)1 << 30; }
 
+// Threads of a launch are counted in 32 bits.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= (int64_t)0xffffffff / threads; }
+
 // 128 rows span more than a buffer's range.
 inline bool far_rows(const tmac_view* v) { return v->token >= ((int64_t)1 << 22); }
 

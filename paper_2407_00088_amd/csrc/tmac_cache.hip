@@ -292,7 +292,7 @@ static bool cache_set(const tmac_cache* c) {
          c->seen_dev;
 }
 static tmac_status launch(const void* kernel, int64_t grid, int threads, void* args, void* stream) {
-  if (grid > 0x7fffffff) return TMAC_EUNSUPPORTED;
+  if (!attn::launchable(grid, threads)) return TMAC_EUNSUPPORTED;
   void* ptrs[] = {args};
   const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), ptrs, 0, static_cast<hipStream_t>(stream));
   if (e == hipSuccess) return TMAC_OK;
@@ -341,13 +341,13 @@ extern "C" tmac_status tmac_cache_fill(const tmac_cache* cache, const tmac_cache
   a.B = B, a.Hkv = cache->Hkv, a.D = cache->D, a.C = cache->capacity, a.recent = cache->recent, a.total = src->total;
   a.blocks = (cache->capacity + 63) / 64;
   const int64_t bh = (int64_t)B * cache->Hkv;
-  if (bh * a.blocks > 0x7fffffff) return TMAC_EUNSUPPORTED;
   const bool wide = attn::wide_rows(&src->k, a.D) && attn::wide_rows(&src->v, a.D) && attn::wide_rows(&cache->k, a.D) && attn::wide_rows(&cache->v, a.D);
   // Small caches are copied by the workgroup that selects, which saves a launch and what is between two (rows of 128 elements, 256 slots:
   // 8 caches 10.0 us, 11.2 in two launches; 96 of 100 elements 12.3, 13.6); beyond 128 KB of keys and values one workgroup's
   // copy takes longer than that (512 slots: 8 caches 15.7, 13.1; 96 caches 21.5, 18.8).
   if (cache->capacity <= COPIED && (int64_t)cache->capacity * a.D * 4 <= 131072)
     return cache::launch(wide ? (const void*)cache_select_kernel<true, u4> : (const void*)cache_select_kernel<true, u2>, bh, 64 * WAVES, &a, stream);
+  if (!attn::launchable(bh * a.blocks, 256)) return TMAC_EUNSUPPORTED;
   const tmac_status st = cache::launch((const void*)cache_select_kernel<false, u2>, bh, 64 * WAVES, &a, stream);
   if (st != TMAC_OK) return st;
   return cache::launch(wide ? (const void*)cache_copy_kernel<u4> : (const void*)cache_copy_kernel<u2>, bh * a.blocks, 256, &a, stream);

@@ -121,3 +121,21 @@ def test_reserved_fields_of_a_cache_are_zero_in_every_call(at):
     row = H.view(seq=128)
     assert H.A.lib.tmac_cache_append(c, row, row, None) == H.decode(c=c) == H.T.TMAC_EINVAL
     assert H.A.lib.tmac_attn_decode_workspace_bytes(H.desc(), c, 10, 1) == H.A.lib.tmac_cache_fill_workspace_bytes(c) == 0
+
+
+def test_launches_of_too_many_threads_are_refused_before_anything_is_launched():
+    """2^32 threads or more of either launch of a call.  (Without a GPU any launch is an error of another kind.)"""
+    one, many = H.desc(Hq=1, Hkv=1), H.desc(Hq=64, Hkv=64)
+    A, P16, view, no = H.A, H.P16, H.view, H.T.TMAC_EUNSUPPORTED
+    assert H.prompt(one, S=1 << 24, Tq=1 << 24, Tk=1 << 24) == no
+    assert A.lib.tmac_attn_weights(one, view(), view(), P16, 1 << 24, 1 << 24, 1 << 24, P16, P16, P16, P16, 1 << 50, None) == no
+    none = A.tmac_cache(A.tmac_view(), A.tmac_view(), None, None, None, None, 1 << 20, 64, 64, 0, 0, 0)
+    assert H.decode(many, P=1, c=none, acc=0) == no                       # 2^26 rows: the joining launch
+    few = [H.cache(Hkv=64, B=b, capacity=c, D=4) for b, c in ((1 << 18, 100), (1 << 12, 1 << 16))]
+    for c in few:
+        assert H.decode(H.desc(Hq=64, Hkv=64, D=4), c=c) == no
+    row = view(seq=128)
+    assert A.lib.tmac_cache_append(few[0], row, row, None) == no
+    source = A.tmac_cache_source(view(), view(), A.tmac_view(P16, 0, 1, 100), A.tmac_view(), P16, None, None, 100)
+    for c in few + [H.cache(Hkv=64, B=1 << 10, capacity=1 << 20, D=4)]:
+        assert A.lib.tmac_cache_fill(c, source, P16, 1 << 60, None) == no
