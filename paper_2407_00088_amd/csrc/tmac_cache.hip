@@ -1,7 +1,8 @@
 // Caches that keep the heaviest keys (tmac_attn.h): filling one from prompts or from another cache, and taking in one token.
 //
 // Eviction orders tokens by (recent or not, weight, slot).  As whole numbers: a weight's bits, mapped so that they ascend with
-// its value (NaN as -inf), all ones for a recent token, which is above +inf; equal keys go by the slot.
+// its value (NaN as -inf), all ones for a recent token, which is above +inf; equal keys go by the slot.  Recent tokens leave only where
+// positions repeat or lie ahead of what the cache has seen; the search is then made again over their weights.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -91,10 +92,10 @@ struct Selecting {
 // The places of the n - leave tokens that stay, in order: of keys read_key(i), i < n, the `leave` smallest go (equal ones by i).
 // The leave-th smallest key is found digit by digit (11, 11 and 10 bits, counted in LDS), then every wavefront numbers the
 // staying tokens of its run.  PER: tokens of a lane, which stay in registers from the first look on; 0: any number, read again by
-// every step.  (128 caches, 4096 of 16384 tokens each: 24 us, the instructions of
+// every step.  False: the leave-th is a recent token, nothing is written.  (128 caches, 4096 of 16384 tokens each: 24 us, the instructions of
 // 16 wavefronts on one CU; with the keys in LDS it was 30, with four counters a digit still 24.)
 template <int PER, typename ReadKey>
-__device__ __forceinline__ void select(ReadKey read_key, int n, uint32_t leave, int32_t* index, Selecting& sh) {
+__device__ __forceinline__ bool select(ReadKey read_key, int n, uint32_t leave, int32_t* index, Selecting& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int turns = (n + 64 * WAVES - 1) / (64 * WAVES), lo = wave * turns * 64;  // a wavefront's run: `turns` times 64 tokens
   uint32_t mine[PER ? PER : 1];
@@ -148,6 +149,7 @@ __device__ __forceinline__ void select(ReadKey read_key, int n, uint32_t leave, 
     prefix |= sh.chosen[0] << shift;
     rank -= sh.chosen[1];
   }
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(prefix) == 0xffffffffu, 0)) return false;
   // of the tokens whose key is `prefix`, the first rank + 1 leave
   const uint32_t go = rank + 1;
   uint32_t greater = 0, equal = 0;
@@ -170,6 +172,7 @@ __device__ __forceinline__ void select(ReadKey read_key, int n, uint32_t leave, 
     equal += __builtin_popcountll(same);
     at += __builtin_popcountll(mask);
   });
+  return true;
 }
 
 // One workgroup a sequence and key head.  COPIES: it copies the rows too, else it leaves the tokens' places for the copying launch.
@@ -188,15 +191,18 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_kernel(const FillArgs
     a.lens[bh] = keep;
     a.seen[bh] = seen;
   }
-  auto read_key = [&](int i) { return order_key(w[i * a.ws_token], (int64_t)(p ? p[i * a.ps_token] : i) >= (int64_t)seen - a.recent); };
+  auto recent = [&](int i) { return (int64_t)(p ? p[i * a.ps_token] : i) >= (int64_t)seen - a.recent; };
+  auto read_key = [&](int i) { return order_key(w[i * a.ws_token], recent(i)); };
+  // (more leave than are not recent: those all, below any weight's key, then the lightest recent ones; no key is a recent token's then)
+  auto read_again = [&](int i) { return recent(i) ? order_key(w[i * a.ws_token], false) : 0u; };
   if (n <= a.C) {
     for (int i = tid; i < n; i += 64 * WAVES) index[i] = i;
   } else if (n <= 4 * 64 * WAVES) {
-    select<4>(read_key, n, n - a.C, index, sh);
+    if (__builtin_expect(!select<4>(read_key, n, n - a.C, index, sh), 0)) select<4>(read_again, n, n - a.C, index, sh);
   } else if (n <= 16 * 64 * WAVES) {
-    select<16>(read_key, n, n - a.C, index, sh);
+    if (__builtin_expect(!select<16>(read_key, n, n - a.C, index, sh), 0)) select<0>(read_again, n, n - a.C, index, sh);
   } else {
-    select<0>(read_key, n, n - a.C, index, sh);
+    if (__builtin_expect(!select<0>(read_key, n, n - a.C, index, sh), 0)) select<0>(read_again, n, n - a.C, index, sh);
   }
   if constexpr (COPIES) {
     __syncthreads();
@@ -251,24 +257,33 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
   if (n == a.C) {
     const int64_t recent_from = (int64_t)seen + 1 - a.recent;
     uint64_t best = ~0ull;
-    auto consider = [&](int i, float w, int32_t p) {
-      const uint64_t x = (uint64_t)order_key(w, p >= recent_from) << 32 | (uint32_t)i;
+    auto consider = [&](int i, float w, bool recent) {
+      const uint64_t x = (uint64_t)order_key(w, recent) << 32 | (uint32_t)i;
       best = x < best ? x : best;
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (tid + j * THREADS < n) consider(tid + j * THREADS, w4[j], p4[j]);
+      if (tid + j * THREADS < n) consider(tid + j * THREADS, w4[j], p4[j] >= recent_from);
 #pragma unroll 4
-    for (int i = tid + 4 * THREADS; i < n; i += THREADS) consider(i, weight[i], pos[i]);
+    for (int i = tid + 4 * THREADS; i < n; i += THREADS) consider(i, weight[i], pos[i] >= recent_from);
+    auto meet = [&] {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t x = __shfl_xor((unsigned long long)best, o);
-      best = x < best ? x : best;
+      for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t x = __shfl_xor((unsigned long long)best, o);
+        best = x < best ? x : best;
+      }
+      if ((tid & 63) == 0) least[tid >> 6] = best;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < THREADS / 64; ++i) best = least[i] < best ? least[i] : best;
+    };
+    meet();
+    if (best >> 32 == 0xffffffffu) {  // all are recent: by their weights
+      best = ~0ull;
+      for (int i = tid; i < n; i += THREADS) consider(i, weight[i], false);
+      __syncthreads();
+      meet();
     }
-    if ((tid & 63) == 0) least[tid >> 6] = best;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i) best = least[i] < best ? least[i] : best;
     slot = (int)(uint32_t)best;
   }
   // (every thread has read the lengths and the slots before any of them is changed)

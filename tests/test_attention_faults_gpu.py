@@ -103,3 +103,36 @@ def test_a_flat_tail_beside_a_heavy_key(A, dt, Tq, H, Tk):
     bound = (2.1 * ref.UNIT[dt] + 4 * ((D + 2) * u * s + 8 * u * (1 + s))) * (p @ v[:, 0].double()) + tail + u
     near(out[0, :1], want, bound, "out")
     near(lse[0, :1], want_lse, lse_b, "lse")
+
+
+@pytest.mark.parametrize("kind", ["spread", "odd"])
+@pytest.mark.parametrize("n,C", [(90, 40), (5000, 700), (20000, 40)])
+@pytest.mark.parametrize("seen", [0, 6])
+def test_recent_tokens_leave_by_their_weights_too(A, kind, n, C, seen):
+    """Positions ahead of what the cache has seen, and positions that repeat, make more tokens recent than the cache holds."""
+    Hkv, D, recent = 2, 8, 30
+    src, k, v = filled(A, 1, Hkv, Hkv, D, n, [[n, n]], F16)
+    gen = torch.Generator().manual_seed(n)
+    w = torch.rand((1, Hkv, n), generator=gen)
+    if kind == "odd":
+        w[..., ::5], w[..., 1::9], w[..., 2::11] = math.nan, math.inf, -math.inf
+    src.weight.copy_(w), src.seen.fill_(n + seen)
+    # head 0: all are recent; head 1: all but one in five
+    pos = torch.full((1, Hkv, n), n + seen - 1)
+    pos[0, 1, ::5] = 3
+    src.pos.copy_(pos)
+    cache = A.KVCache(1, Hkv, D, C, recent=recent)
+    cache.fill_from(src)
+    for h in range(Hkv):
+        order = ref.leaving(w[0, h], pos[0, h], n + seen, recent)
+        kept = sorted(order[n - C:])
+        assert torch.equal(cache.k[0, h].cpu(), k[0, h, kept]) and torch.equal(cache.weight[0, h].cpu().view(torch.int32), w[0, h, kept].view(torch.int32))
+        assert cache.pos[0, h].tolist() == pos[0, h, kept].tolist() and int(cache.lens[0, h]) == C
+    # one more into a cache all of whose tokens are recent, then into the same with fewer
+    for turn in range(3):
+        weight, at, new = cache.weight.cpu(), cache.pos.cpu(), rand(turn, 1, Hkv, D)
+        goes = [ref.leaving(weight[0, h], at[0, h], n + seen + turn + 1, recent)[0] for h in range(Hkv)]
+        cache.append(new.cuda(), new.cuda())
+        for h in range(Hkv):
+            assert torch.equal(cache.k[0, h, goes[h]].cpu(), new[0, h]) and int(cache.pos[0, h, goes[h]]) == n + seen + turn
+            assert float(cache.weight[0, h, goes[h]]) == 0.0
