@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
+import threading
 from typing import Optional
 
 import torch
@@ -215,6 +216,7 @@ class KVCache:
       pos     int32 [batch, Hkv, capacity]       lens, seen  int32 [batch, Hkv]
 
     The tensors may be written to, not replaced.  Calls of one cache share its workspaces: on several streams they must not overlap.
+    Calls from several threads are enqueued one after the other, each whole.
     """
 
     def __init__(self, batch: int, Hkv: int, D: int, capacity: int, recent: int = 0, dtype=torch.float16, Hq: Optional[int] = None,
@@ -232,6 +234,8 @@ class KVCache:
         self.seen = torch.zeros((batch, Hkv), dtype=torch.int32, device=device)
         self.cache = tmac_cache(_view(self.k, 0, 2, 1), _view(self.v, 0, 2, 1), self.weight.data_ptr(), self.pos.data_ptr(),
                                 self.lens.data_ptr(), self.seen.data_ptr(), batch, Hkv, D, capacity, recent, _ELEM[dtype])
+        # (a call is up to two launches that hand a workspace on, and the interpreter may change threads between them)
+        self.lock = threading.RLock()
         self.fill_ws = None
         self.attend_ws = None
         self.outgrown = []
@@ -254,68 +258,73 @@ class KVCache:
 
     def fill(self, k, v, weight, cu, stream=None) -> None:
         """From packed prompts: k, v [T, Hkv, D], weight fp32 [Hkv, T] (attn_weights), cu int32 [batch + 1]."""
-        if stream is None and self.fill_ws is not None and calls.cache_fill(self.cache, self.k, k, v, weight, cu, self.fill_ws):
-            return
-        T = k.shape[0]
-        _counted(T=T)
-        _dims("k", k, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
-        _dims("v", v, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
-        _rows("k", k), _rows("v", v)
-        _dims("weight", weight, "Hkv, T", (self.Hkv, T), torch.float32)
-        _plain("cu", cu, (self.B + 1,), torch.int32)
-        _same_device(self.k, k, v, weight, cu)
-        self._fill(tmac_cache_source(_view(k, None, 0, 1), _view(v, None, 0, 1), _view(weight, None, 1, 0), tmac_view(), cu.data_ptr(), None,
-                                     None, T), stream)
+        with self.lock:
+            if stream is None and self.fill_ws is not None and calls.cache_fill(self.cache, self.k, k, v, weight, cu, self.fill_ws):
+                return
+            T = k.shape[0]
+            _counted(T=T)
+            _dims("k", k, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
+            _dims("v", v, "T, Hkv, D", (T, self.Hkv, self.D), self.k.dtype)
+            _rows("k", k), _rows("v", v)
+            _dims("weight", weight, "Hkv, T", (self.Hkv, T), torch.float32)
+            _plain("cu", cu, (self.B + 1,), torch.int32)
+            _same_device(self.k, k, v, weight, cu)
+            self._fill(tmac_cache_source(_view(k, None, 0, 1), _view(v, None, 0, 1), _view(weight, None, 1, 0), tmac_view(), cu.data_ptr(), None,
+                                         None, T), stream)
 
     def fill_from(self, other: "KVCache", stream=None) -> None:
         """From another cache of as many sequences and heads: its heaviest and latest tokens, as many as this one holds."""
         if other is self or (other.B, other.Hkv, other.D, other.k.dtype) != (self.B, self.Hkv, self.D, self.k.dtype):
             raise ValueError("the source is another cache of the same sequences, heads and type")
         _same_device(self.k, other.k)
-        self._fill(tmac_cache_source(_view(other.k, 0, 2, 1), _view(other.v, 0, 2, 1), _view(other.weight, 0, 2, 1), _view(other.pos, 0, 2, 1),
-                                     None, other.lens.data_ptr(), other.seen.data_ptr(), other.capacity), stream)
+        first, second = sorted((self, other), key=id)   # (the same order whichever is filled from the other)
+        with first.lock, second.lock:
+            self._fill(tmac_cache_source(_view(other.k, 0, 2, 1), _view(other.v, 0, 2, 1), _view(other.weight, 0, 2, 1), _view(other.pos, 0, 2, 1),
+                                         None, other.lens.data_ptr(), other.seen.data_ptr(), other.capacity), stream)
 
     def append(self, k, v, stream=None) -> None:
         """One token for every sequence: k, v [batch, Hkv, D]."""
-        if stream is None and calls.cache_append(self.cache, self.k, k, v):
-            return
-        for name, t in (("k", k), ("v", v)):
-            _dims(name, t, "batch, Hkv, D", (self.B, self.Hkv, self.D), self.k.dtype)
-            _rows(name, t)
-        _same_device(self.k, k, v)
-        B._check(lib.tmac_cache_append(self.cache, _view(k, 0, None, 1), _view(v, 0, None, 1), B._stream_ptr(stream)), "tmac_cache_append")
+        with self.lock:
+            if stream is None and calls.cache_append(self.cache, self.k, k, v):
+                return
+            for name, t in (("k", k), ("v", v)):
+                _dims(name, t, "batch, Hkv, D", (self.B, self.Hkv, self.D), self.k.dtype)
+                _rows(name, t)
+            _same_device(self.k, k, v)
+            B._check(lib.tmac_cache_append(self.cache, _view(k, 0, None, 1), _view(v, 0, None, 1), B._stream_ptr(stream)), "tmac_cache_append")
 
     def attend(self, q, prefix_k=None, prefix_v=None, weigh: bool = True, out=None, lse=None, stream=None):
         """One decode step: q [batch, Hq, D] over the prefix (k and v [P, Hkv, D], shared by all sequences), if there is one, and the
         slots in use; `weigh` adds the step's weights to the slots'.  Returns (out [batch, Hq, D], lse fp32 [batch, Hq])."""
-        if out is None and lse is None and stream is None and self.attend_ws is not None:
-            got = calls.attend(self.cache, self.k, self.desc, q, prefix_k, prefix_v, weigh, self.attend_ws)
-            if got is not None:
-                return got
-        dt = self.k.dtype
-        _dims("q", q, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
-        _rows("q", q)
-        P, v0, v1 = 0, tmac_view(), tmac_view()
-        if (prefix_k is None) != (prefix_v is None):
-            raise ValueError("a prefix has keys and values")
-        if prefix_k is not None:
-            P = prefix_k.shape[0]
-            _counted(P=P)
-            for name, t in (("prefix_k", prefix_k), ("prefix_v", prefix_v)):
-                _dims(name, t, "P, Hkv, D", (P, self.Hkv, self.D), dt)
-                _rows(name, t)
-            v0, v1 = _view(prefix_k, None, 0, 1), _view(prefix_v, None, 0, 1)
-        with _on(stream):
-            if out is None:
-                out = torch.empty((self.B, self.Hq, self.D), dtype=dt, device=q.device)
-            if lse is None:
-                lse = torch.empty((self.B, self.Hq), dtype=torch.float32, device=q.device)
-        _dims("out", out, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
-        _rows("out", out), _apart("out", out)
-        _plain("lse", lse, (self.B, self.Hq), torch.float32)
-        _same_device(self.k, q, prefix_k, prefix_v, out, lse)
-        n = lib.tmac_attn_decode_workspace_bytes(self.desc, self.cache, P, int(weigh))
-        self.attend_ws = self._grown(self.attend_ws, n, stream)
-        B._check(lib.tmac_attn_decode(self.desc, _view(q, 0, None, 1), v0, v1, P, self.cache, int(weigh), _view(out, 0, None, 1),
-                                      lse.data_ptr(), self.attend_ws.data_ptr(), n, B._stream_ptr(stream)), "tmac_attn_decode")
-        return out, lse
+        with self.lock:
+            if out is None and lse is None and stream is None and self.attend_ws is not None:
+                got = calls.attend(self.cache, self.k, self.desc, q, prefix_k, prefix_v, weigh, self.attend_ws)
+                if got is not None:
+                    return got
+            dt = self.k.dtype
+            _dims("q", q, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
+            _rows("q", q)
+            P, v0, v1 = 0, tmac_view(), tmac_view()
+            if (prefix_k is None) != (prefix_v is None):
+                raise ValueError("a prefix has keys and values")
+            if prefix_k is not None:
+                P = prefix_k.shape[0]
+                _counted(P=P)
+                for name, t in (("prefix_k", prefix_k), ("prefix_v", prefix_v)):
+                    _dims(name, t, "P, Hkv, D", (P, self.Hkv, self.D), dt)
+                    _rows(name, t)
+                v0, v1 = _view(prefix_k, None, 0, 1), _view(prefix_v, None, 0, 1)
+            with _on(stream):
+                if out is None:
+                    out = torch.empty((self.B, self.Hq, self.D), dtype=dt, device=q.device)
+                if lse is None:
+                    lse = torch.empty((self.B, self.Hq), dtype=torch.float32, device=q.device)
+            _dims("out", out, "batch, Hq, D", (self.B, self.Hq, self.D), dt)
+            _rows("out", out), _apart("out", out)
+            _plain("lse", lse, (self.B, self.Hq), torch.float32)
+            _same_device(self.k, q, prefix_k, prefix_v, out, lse)
+            n = lib.tmac_attn_decode_workspace_bytes(self.desc, self.cache, P, int(weigh))
+            self.attend_ws = self._grown(self.attend_ws, n, stream)
+            B._check(lib.tmac_attn_decode(self.desc, _view(q, 0, None, 1), v0, v1, P, self.cache, int(weigh), _view(out, 0, None, 1),
+                                          lse.data_ptr(), self.attend_ws.data_ptr(), n, B._stream_ptr(stream)), "tmac_attn_decode")
+            return out, lse

@@ -4,8 +4,11 @@ import ctypes
 import os
 import re
 import subprocess
+import threading
+import time
 
 import pytest
+import torch
 
 import test_attention_host as H
 from paper_2407_00088_amd import build
@@ -139,3 +142,44 @@ def test_launches_of_too_many_threads_are_refused_before_anything_is_launched():
     source = A.tmac_cache_source(view(), view(), A.tmac_view(P16, 0, 1, 100), A.tmac_view(), P16, None, None, 100)
     for c in few + [H.cache(Hkv=64, B=1 << 10, capacity=1 << 20, D=4)]:
         assert A.lib.tmac_cache_fill(c, source, P16, 1 << 60, None) == no
+
+
+class OneAtATime:
+    """In place of the library and of the binding's native side: calls that last, which notes whether another began meanwhile."""
+
+    def __init__(self):
+        self.running, self.most, self.calls = 0, 0, 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            if name.endswith("_bytes"):
+                return 64
+            self.running += 1
+            self.calls += 1
+            self.most = max(self.most, self.running)
+            time.sleep(0.005)
+            self.running -= 1
+            return 0 if name.startswith("tmac_") else True
+        return call
+
+
+def test_calls_of_one_cache_from_several_threads_follow_each_other(monkeypatch):
+    """Two launches of a call hand on a workspace that belongs to the cache: another thread's must not come between them."""
+    made = OneAtATime()
+    monkeypatch.setattr(H.A, "calls", made)
+    monkeypatch.setattr(H.A, "lib", made)
+    monkeypatch.setattr(H.A, "_same_device", lambda *tensors: None)
+    monkeypatch.setattr(H.A.B, "_stream_ptr", lambda stream: None)
+    one, two = (H.A.KVCache(1, 1, 64, 8, device="cpu") for _ in range(2))
+    one.attend_ws = one.fill_ws = torch.empty(64, dtype=torch.uint8)
+    row = torch.zeros((1, 1, 64), dtype=torch.float16)
+    weight, cu = torch.zeros((1, 1)), torch.zeros(2, dtype=torch.int32)
+    turns = [lambda: one.attend(row), lambda: one.append(row, row), lambda: one.fill(row, row, weight, cu), lambda: one.fill_from(two),
+             lambda: two.fill_from(one)] * 4
+    threads = [threading.Thread(target=turn, daemon=True) for turn in turns]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(30)
+        assert not t.is_alive()
+    assert made.calls == len(turns) and made.most == 1
