@@ -215,7 +215,7 @@ class KVCache:
       k, v    [batch, Hkv, capacity, D]          weight  fp32 [batch, Hkv, capacity]
       pos     int32 [batch, Hkv, capacity]       lens, seen  int32 [batch, Hkv]
 
-    The tensors may be written to, not replaced.  Calls of one cache share its workspaces: on several streams they must not overlap.
+    The tensors may be written to, not replaced (calls go by their addresses).  Calls of one cache share its workspaces: on several streams they must not overlap.
     Calls from several threads are enqueued one after the other, each whole.
     """
 
@@ -239,6 +239,12 @@ class KVCache:
         self.fill_ws = None
         self.attend_ws = None
         self.outgrown = []
+
+    def __setattr__(self, name, value):
+        # (`cache.weight *= x` comes here too, with the tensor that is there)
+        if name in ("k", "v", "weight", "pos", "lens", "seen") and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} is written to, not replaced: {name}.copy_(...)")
+        super().__setattr__(name, value)
 
     def _grown(self, ws, n: int, stream):
         """A workspace of n bytes at least.  (One that is too small is kept: an earlier call may still run on it, or a graph that was

@@ -183,3 +183,15 @@ def test_calls_of_one_cache_from_several_threads_follow_each_other(monkeypatch):
         t.join(30)
         assert not t.is_alive()
     assert made.calls == len(turns) and made.most == 1
+
+
+@pytest.mark.parametrize("name", ["k", "v", "weight", "pos", "lens", "seen"])
+def test_tensors_of_a_cache_are_not_replaced(name):
+    """The library has their addresses: it would go on writing to a tensor that is no longer there."""
+    cache = H.A.KVCache(1, 2, 64, 8, device="cpu")
+    before = getattr(cache, name)
+    with pytest.raises(AttributeError, match=name):
+        setattr(cache, name, before * 1)
+    before += 1
+    exec(f"cache.{name} *= 3", dict(cache=cache))
+    assert getattr(cache, name) is before and (before == 3).all()
