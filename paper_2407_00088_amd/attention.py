@@ -1,5 +1,6 @@
 """Attention between the projections: thin binding of include/tmac_attn.h (argument checks and marshalling; every step runs in the
-library's HIP kernels), functions that allocate results and workspace, and a holder of one layer's cache.
+library's HIP kernels), functions that allocate results and workspace, and a holder of one layer's cache.  For inference: there is no
+backward pass, and results of inputs that require gradients carry none.
 
   attn_prompt     attention over packed prompts
   attn_weights    the attention weight that each of their keys received

@@ -250,9 +250,9 @@ struct Tile {
 };
 
 // One workgroup: 32 BLOCKS rows of one sequence and key head over the keys they see, or one slice of those; queries are read once,
-// keys once a tile, from the XCD's L2.  Long sequences are bound by power: 8192 tokens, 64 heads in groups of 8 of 128 elements take 1.10 ms, 1.0
-// PFLOP/s of the pairs that rows see (a large matrix product reaches 1.37), at 1.7 of 2.4 GHz with the matrix units busy for 52 % of the
-// cycles and the vector ALUs, mostly with exponentials, for 47 %; LDS has no bank conflicts.  Short ones are bound by latency: 33 tokens, 32
+// keys once a tile, from the XCD's L2.  Long sequences are bound by power: 8192 tokens, 64 heads in groups of 8 of 128 elements take 1.10 to 1.15 ms, 1.0
+// PFLOP/s of the pairs that rows see (a large matrix product reaches 1.37), at 1.7 of 2.4 GHz with the matrix units busy for 53 % of the
+// cycles and the vector ALUs, mostly with exponentials, for 49 %; LDS has no bank conflicts.  Short ones are bound by latency: 33 tokens, 32
 // heads 6.2 us, one wavefront's chain of loads, products and exchanges.
 template <typename T, int DP, int BLOCKS>
 __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(const PromptArgs a) {
@@ -590,9 +590,10 @@ struct WeightArgs {
 
 // One workgroup: 128 KB keys of one sequence and key head, 32 KB a wavefront, which stay in registers as the second operand of
 // S = Q K^T; a lane owns a key (of each 32) and adds up exp(s - lse) over the queries that pass through LDS, 64 of one head at a time.
-// The exponentials bind (16 a lane for 8 products of 32 x 32 x 16), so the rest is kept away from the vector ALUs: with two blocks of keys
-// a wavefront the reads of q and of lse serve twice.  6144 tokens, 64 heads in groups of 8 of 128 elements: 322 us, 0.95 PFLOP/s of the pairs that
-// are seen, matrix units 48 % busy and vector ALUs 61 %.  Nothing is added up atomically: a unit's sums go to memory once, those of its slices
+// Products and exponentials (16 a lane for 8 products of 32 x 32 x 16) take turns within a wavefront, and the two wavefronts of a SIMD overlap
+// them only in part: 6144 tokens, 64 heads in groups of 8 of 128 elements take 322 to 338 us, 0.95 PFLOP/s of the pairs that are seen, matrix
+// units 49 % busy and vector ALUs 62 % at 1.8 of 2.4 GHz.  What is not either is kept away from the vector ALUs: with two blocks of keys
+// a wavefront the reads of q and of lse serve twice.  Nothing is added up atomically: a unit's sums go to memory once, those of its slices
 // to a part each.
 template <typename T, int DP, int KB>
 __global__ __launch_bounds__(256, 2) void attn_weights_kernel(const WeightArgs a) {
@@ -756,6 +757,7 @@ static PromptPlan prompt_plan(const tmac_attn_desc* d, int S, int Tq, int Tk) {
   auto tiles_of = [&](int per) { return (int)std::min<int64_t>(rows / per + S, rows); };
   const int64_t keys = Tk / S, seen = d->causal ? std::max(keys / 2, keys - Tq / S / 2) : keys;
   const int64_t wide = (int64_t)tiles_of(128) * d->Hkv;
+  // (wide / 128 (6 + seen / 80) against 5 + keys / 46, both 128 * 80 times)
   p.blocks = rows / S <= 32 || wide < WGS / 2 || wide * (480 + seen) <= 51200 + 224 * keys ? 1 : 4;
   p.tiles = tiles_of(32 * p.blocks);
   const int64_t wgs = (int64_t)p.tiles * d->Hkv;
