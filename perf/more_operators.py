@@ -181,8 +181,8 @@ def _inputs(case, seed):
     if case["op"] == "append":
         st["k"], st["v"] = _heads(gen, dt, sum(n), Hkv, D), _heads(gen, dt, sum(n), Hkv, D)
         # the blocks that the new tokens touch, from their first token on
-        st["back_cu"] = _starts([m - o // BLOCK * BLOCK for m, o in zip(lens, old)])
-        st["most_back"] = max(m - o // BLOCK * BLOCK for m, o in zip(lens, old))
+        back = [m - o // BLOCK * BLOCK for m, o in zip(lens, old)]
+        st.update(back_cu=_starts(back), back=sum(back), most_back=max(back))
     return st
 
 
@@ -331,7 +331,7 @@ def run(st):
     cache = st["cache"]
     if op == "append":
         q = cache.append(st["k"], st["v"], st["table"], st["lens"], st["cu"], q=st["q"], most=st["most_new"])
-        return q, *cache.read(st["table"], st["lens"], st["back_cu"])
+        return q, *cache.read(st["table"], st["lens"], st["back_cu"], T=st["back"], most=st["most_back"])
     return cache.attend(st["q"], st["table"], st["lens"], st["cu"], most=st["most_new"])
 
 
