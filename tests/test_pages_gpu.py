@@ -1,0 +1,392 @@
+"""Rotation, paged cache and attention over it on the GPU against plain forms in 64 bits (tests/pages_reference.py)."""
+import math
+
+import pytest
+import torch
+
+import pages_reference as R
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def P():
+    import paper_2407_00088_amd as T
+    return T
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def close(got, ref, bound, what):
+    got, ref = got.double().cpu(), ref.double()
+    nan = ref.isnan()
+    assert torch.equal(got.isnan(), nan), f"{what}: NaN in other places"
+    inf = ref.isinf()
+    assert torch.equal(got[inf], ref[inf]), f"{what}: infinities"
+    off = torch.where(nan | inf, 0.0, (got - ref).abs() - bound)
+    assert off.numel() == 0 or off.max() <= 0, f"{what}: {(off > 0).sum()} of {off.numel()} beyond the bound, by {off.max():.3g}"
+
+
+# --- rotation ---------------------------------------------------------------------------------------------------------------------------
+
+SCALINGS = [None, ("linear", 4.0), ("base", 8.0), ("ramp", 8.0, 2048.0, 32.0, 1.0), ("bands", 8.0, 2048.0, 1.0, 4.0)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("T,H,D,rot", [(1, (32, 32), 128, 128), (7, (3,), 100, 100), (33, (5, 2), 100, 52), (5, (4, 1, 2, 3), 64, 32),
+                                       (3, (7,), 80, 6), (257, (2, 2), 128, 2), (2, (1,), 4, 4), (1, (300,), 12, 10), (4, (2,), 16, 16)])
+def test_rotate(T, H, D, rot, interleaved, dtype):
+    g = gen(T * D + rot)
+    rotary = P().Rotary(D, rot=rot, interleaved=interleaved, scaling=SCALINGS[(T + rot) % 5] if rot >= 4 else None)
+    xs = [torch.randn((T, h, D), generator=g).to(dtype) for h in H]
+    positions = torch.randint(-5000, 300000, (T,), generator=g)
+    got = rotary.rotate(positions.cuda(), *(x.cuda() for x in xs))
+    freq = rotary.freq.cpu()
+    for x, y in zip(xs, got):
+        ref = R.turned(x, positions, freq, rotary.magnitude, interleaved)
+        close(y, ref, R.turned_bound(x, freq, rotary.magnitude, interleaved) + R.rounding(ref, dtype), "rotate")
+        assert torch.equal(y[..., rot:].cpu(), x[..., rot:])
+
+
+def test_rotate_strides_in_place_and_other_stream():
+    g = gen(3)
+    rotary = P().Rotary(64, rot=48)
+    wide = torch.randn((9, 6, 200), generator=g).half().cuda()
+    x = wide[:, 1:5, 4:68]                       # rows 8 bytes aligned, not 16
+    keep = wide.clone()
+    positions = torch.arange(100, 109).cuda()
+    ref = R.turned(x.cpu(), positions.cpu(), rotary.freq.cpu(), 1.0, False)
+    bound = R.turned_bound(x.cpu(), rotary.freq.cpu(), 1.0, False) + R.rounding(ref, F16)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    y, = rotary.rotate(positions, x, stream=stream)
+    stream.synchronize()
+    close(y, ref, bound, "other stream")
+    rotary.rotate(positions, x, out=[x])
+    close(x, ref, bound, "in place")
+    keep[:, 1:5, 4:68] = x
+    assert torch.equal(keep, wide)                # nothing beside it
+
+
+def test_rotate_by_negative_positions_is_the_gradient():
+    """The rotation is linear: its gradient is the rotation by -position; checked against differences in 64 bits."""
+    g = gen(4)
+    rotary = P().Rotary(32, scaling=("ramp", 4.0, 512.0, 32.0, 1.0), interleaved=True)
+    x, dy = torch.randn((6, 2, 32), generator=g).half(), torch.randn((6, 2, 32), generator=g).half()
+    positions = torch.arange(6) * 91
+    dx, = rotary.rotate(-positions.cuda(), dy.cuda())
+    freq = rotary.freq.cpu()
+    for d in (0, 5, 31):
+        e = torch.zeros(32, dtype=torch.float64)
+        e[d] = 2.0 ** -10
+        diff = (R.turned(x.double() + e, positions, freq, rotary.magnitude, True) - R.turned(x.double() - e, positions, freq, rotary.magnitude, True)) / 2.0 ** -9
+        ref = (diff * dy.double()).sum(-1)
+        # a difference of a linear form in 64 bits: 2^-52 of values of up to ten, over 2^-9
+        close(dx[..., d], ref, R.turned_bound(dy, freq, rotary.magnitude, True)[..., d] + R.rounding(ref, F16) + 2.0 ** -35, "gradient")
+
+
+def test_rotate_values_that_are_not_finite_stay_with_their_pair():
+    rotary = P().Rotary(16)
+    x = torch.ones((2, 1, 16), dtype=F16)
+    x[0, 0, 3], x[1, 0, 10] = math.inf, math.nan
+    y, = rotary.rotate(torch.tensor([5, 6]).cuda(), x.cuda())
+    bad = ~y.cpu().isfinite()
+    want = torch.zeros((2, 1, 16), dtype=torch.bool)
+    want[0, 0, [3, 11]] = want[1, 0, [2, 10]] = True
+    assert torch.equal(bad, want)
+
+
+# --- pages -----------------------------------------------------------------------------------------------------------------------------------
+
+
+def tables(lens, page, pages, g, extra=1):
+    """Every sequence its own pages, in no order, -1 behind them."""
+    held = [-(-n // page) for n in lens]
+    order = torch.randperm(pages, generator=g).tolist()
+    t = torch.full((len(lens), max(held, default=0) + extra), -1, dtype=torch.int32)
+    for s, n in enumerate(held):
+        for i in range(n):
+            t[s, i] = order.pop()
+    return t
+
+
+def starts(n):
+    return torch.tensor([sum(n[:i]) for i in range(len(n) + 1)], dtype=torch.int32)
+
+
+def same_blocks(cache, held):
+    got = R.decoded(cache)
+    for key, (codes, scale) in held.blocks.items():
+        assert float(got.blocks[key][1]) == float(scale), (key, "scale")
+        assert torch.equal(got.blocks[key][0], codes), (key, (got.blocks[key][0] != codes).nonzero()[:4])
+
+
+APPENDS = [
+    # calls one after the other: new tokens of each sequence
+    dict(calls=[[1, 1, 1]] * 3, Hkv=2, D=128, page=32),
+    dict(calls=[[40, 0, 7], [1, 33, 25], [31, 1, 64]], Hkv=3, D=100, page=64),
+    dict(calls=[[0, 0], [5, 0], [0, 100]], Hkv=1, D=64, page=32),
+    dict(calls=[[200, 3, 31, 32, 33, 1]], Hkv=2, D=80, page=128),
+    dict(calls=[[1]] * 35, Hkv=1, D=4, page=32),
+    dict(calls=[[3] * 70, [1] * 70], Hkv=1, D=20, page=32),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("case", range(len(APPENDS)))
+def test_append_holds_what_is_defined(case, code, dtype):
+    """Without rotation codes and scales are defined to the bit; growing blocks, blocks over two calls, sizes of tokens far apart."""
+    c = APPENDS[case]
+    g = gen(case)
+    S = len(c["calls"][0])
+    total = [sum(n[s] for n in c["calls"]) for s in range(S)]
+    pages = sum(-(-n // c["page"]) for n in total) + 2
+    table = tables(total, c["page"], pages, g)
+    cache = P().PagedCache(pages, c["Hkv"], c["D"], page=c["page"], code=code, dtype=dtype)
+    cache.codes.fill_(0xFF), cache.scales.fill_(math.nan)         # what a page held before does not matter
+    held = R.Held(code, c["page"], pages, c["D"])
+    lens = [0] * S
+    for i, n in enumerate(c["calls"]):
+        lens = [a + b for a, b in zip(lens, n)]
+        k, v = (torch.randn((sum(n), c["Hkv"], c["D"]), generator=g) * 2.0 ** (i % 5 - 2 + torch.randint(-3, 4, (sum(n), 1, 1), generator=g)) for _ in range(2))
+        k, v = k.to(dtype), v.to(dtype)
+        if i == 0:
+            v[:1] = 0.0
+        cu = starts(n)
+        plain = all(x == 1 for x in n) and i % 2 == 0
+        cache.append(k.cuda(), v.cuda(), table.cuda(), ints(lens), None if plain else cu.cuda(), most=max(n) if i % 2 else None)
+        held.append(k, v, table, lens, cu)
+    same_blocks(cache, held)
+    # and reads back as that, rounded once
+    T = sum(total)
+    kv = cache.read(table.cuda(), ints(lens), starts(lens).cuda(), T=T)
+    for which, x in enumerate(kv):
+        for s in range(S):
+            for h in range(c["Hkv"]):
+                codes, scales, _ = held.values(table[s], lens[s], h, which)
+                ref = (codes.float() * scales.float()[:, None]).to(dtype)
+                assert torch.equal(x[sum(lens[:s]):sum(lens[:s + 1]), h].cpu(), ref)
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("code,dtype,D,rot,Hq,Hkv", [("i8", F16, 128, 128, 8, 2), ("e4m3", BF16, 100, 52, 3, 3), ("e4m3", F16, 64, 64, 5, 1), ("i8", BF16, 20, 6, 4, 2)])
+def test_append_turns_keys_and_queries(code, dtype, D, rot, Hq, Hkv, interleaved):
+    g = gen(D)
+    T = P()
+    rotary = T.Rotary(D, rot=rot, interleaved=interleaved, scaling=("ramp", 4.0, 64.0, 8.0, 1.0))
+    n, before = [45, 1, 0, 33], [10, 64, 5, 31]
+    lens = [a + b for a, b in zip(n, before)]
+    pages = 12
+    table = tables(lens, 32, pages, g)
+    cache = T.PagedCache(pages, Hkv, D, page=32, code=code, dtype=dtype, rotary=rotary, Hq=Hq)
+    rows = lambda m, h: torch.randn((m, h, D), generator=g).to(dtype)  # noqa: E731
+    freq = rotary.freq.cpu()
+    held = {}
+    for m, upto in ((before, before), (n, lens)):
+        q, k, v, cu = rows(sum(m), Hq), rows(sum(m), Hkv), rows(sum(m), Hkv), starts(m)
+        positions = torch.cat([torch.arange(u - x, u) for x, u in zip(m, upto)])
+        given = positions * 3 - 20 if m is n else None
+        got = cache.append(k.cuda(), v.cuda(), table.cuda(), ints(upto), cu.cuda(), q=q.cuda(), positions=None if given is None else given.cuda())
+        at = positions if given is None else given
+        ref = R.turned(q, at, freq, rotary.magnitude, interleaved)
+        close(got, ref, R.turned_bound(q, freq, rotary.magnitude, interleaved) + R.rounding(ref, dtype), "queries")
+        k64, kb = R.turned(k, at, freq, rotary.magnitude, interleaved), R.turned_bound(k, freq, rotary.magnitude, interleaved)
+        for s in range(4):
+            for i in range(m[s]):
+                held[s, upto[s] - m[s] + i] = k64[int(cu[s]) + i], kb[int(cu[s]) + i], v[int(cu[s]) + i].double()
+    got = R.decoded(cache)
+    for (s, t), (k64, kb, v64) in held.items():
+        for h in range(Hkv):
+            for which, x, b in ((0, k64[h], kb[h]), (1, v64[h], torch.zeros(D))):
+                codes, scale = got.blocks[(*got.place(table[s], t), h, which)]
+                scale = float(scale)
+                y = codes[t % 32].double() * scale
+                # half a step, once more for a block that has grown since (its old codes are rounded again, from a finer step)
+                step = scale if code == "i8" else torch.exp2(torch.floor(torch.log2((x.abs() / scale).clamp(min=2.0 ** -6))) - 3) * scale
+                assert ((y - x).abs() <= 1.01 * step + b).all(), (s, t, h, which)
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_values_that_are_not_finite_and_scales_at_their_ends(code):
+    T, D = P(), 8
+    cache = T.PagedCache(2, 1, D, page=32, code=code, dtype=BF16)
+    held = R.Held(code, 32, 2, D)
+    k = torch.randn((40, 1, D), generator=gen(1)).bfloat16()
+    v = k * 1e-30
+    k[3, 0, 1], k[5, 0, 2], k[6, 0, 0] = math.inf, -math.inf, math.nan
+    k[32:] = 0.0
+    v[33:, 0] = 3e38
+    table = torch.tensor([[1, 0]], dtype=torch.int32)
+    cache.append(k.cuda(), v.cuda(), table.cuda(), ints([40]), ints([0, 40]))
+    held.append(k, v, table, [40], [0, 40])
+    same_blocks(cache, held)
+
+
+def test_pages_that_are_not_there_are_left_alone():
+    """Numbers that are no page, tokens behind the table, more rows than the length: nothing is written, zeros are read."""
+    T, D = P(), 16
+    cache = T.PagedCache(3, 1, D, page=32, code="i8")
+    cache.codes.fill_(7), cache.scales.fill_(1.0)
+    before = cache.codes.clone()
+    k = torch.ones((200, 1, D), dtype=F16, device="cuda")
+    table = ints([[-1, 3, 1 << 30, -(1 << 31)]])
+    cache.append(k[:130], k[:130], table, ints([140]), ints([0, 130]))
+    assert torch.equal(cache.codes, before)
+    got, _ = cache.read(table, ints([140]), ints([0, 130]), T=130)
+    assert not got.any()
+    # six rows, of a sequence of four tokens
+    table = ints([[1]])
+    x = torch.arange(6, device="cuda").half()[:, None, None].expand(6, 1, D).contiguous() * 32
+    cache.append(x, x, table, ints([4]), ints([0, 6]))
+    back, _ = cache.read(table, ints([4]), ints([0, 6]), T=6)
+    assert back[:, 0, 0].tolist() == [0, 0] + (x[2:, 0, 0].float() * 127 / 160).round().mul(160 / 127).half().tolist()
+    assert torch.equal(cache.codes[0], before[0]) and torch.equal(cache.codes[2], before[2])
+    # starts and lengths that cannot be
+    for lens, cu in (([-5], [0, 6]), ([4], [3, 1]), ([4], [-7, 1 << 30]), ([1 << 30], [0, 6])):
+        cache.append(x, x, table, ints(lens), ints(cu))
+        cache.read(table, ints(lens), ints(cu), T=6)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.codes[0], before[0]) and torch.equal(cache.codes[2], before[2])
+
+
+def test_tokens_taken_back_and_written_again():
+    """Drafts that were not accepted: the length falls, later tokens take their places; a block begun anew forgets its scale."""
+    T, D, g = P(), 64, gen(9)
+    for code in ("i8", "e4m3"):
+        cache, held = T.PagedCache(4, 2, D, page=64, code=code), R.Held(code, 64, 4, D)
+        table = torch.tensor([[2, 0]], dtype=torch.int32)
+        for n, upto, gain in ((70, 70, 1.0), (5, 75, 8.0), (4, 72, 0.5), (9, 73, 1.0), (3, 67, 0.1)):
+            k, v = (torch.randn((n, 2, D), generator=g).half() * gain for _ in range(2))
+            cache.append(k.cuda(), v.cuda(), table.cuda(), ints([upto]), ints([0, n]))
+            held.append(k, v, table, [upto], [0, n])
+            same_blocks(cache, held)
+
+
+# --- attention -----------------------------------------------------------------------------------------------------------------------------------
+
+
+def filled(lens, Hkv, D, page, code, dtype, g, gain=1.0, Hq=None, extra=1):
+    pages = sum(-(-n // page) for n in lens) + 3
+    table = tables(lens, page, pages, g, extra)
+    cache = P().PagedCache(pages, Hkv, D, page=page, code=code, dtype=dtype, Hq=Hq)
+    cache.codes.fill_(0x7F), cache.scales.fill_(math.nan)
+    k, v = (torch.randn((sum(lens), Hkv, D), generator=g) * gain for _ in range(2))
+    v += torch.randn((1, Hkv, D), generator=g)
+    if sum(lens):
+        cache.append(k.to(dtype).cuda(), v.to(dtype).cuda(), table.cuda(), ints(lens), starts(lens).cuda())
+    return cache, table
+
+
+ATTENDS = [
+    # (new tokens, lengths), Hq, Hkv, D, page
+    ([1], [1], 1, 1, 4, 32),
+    ([1], [300], 32, 32, 128, 64),
+    ([1, 1, 1], [31, 32, 33], 8, 2, 100, 32),
+    ([1, 1], [5000, 2], 16, 2, 64, 128),
+    ([5, 0, 5, 1], [77, 12, 5, 0], 4, 4, 80, 32),
+    ([9, 3], [4, 700], 6, 2, 20, 64),
+    ([64, 1, 130], [200, 900, 130], 10, 2, 128, 256),
+    ([33], [1033], 40, 1, 96, 64),
+    ([2] * 70, [40 + 3 * i for i in range(70)], 2, 1, 32, 32),
+    ([300, 17], [300, 400], 8, 1, 128, 64),
+    ([100], [2000], 2, 2, 100, 64),
+]
+
+
+@pytest.mark.parametrize("code,dtype", [("i8", F16), ("e4m3", BF16), ("e4m3", F16), ("i8", BF16)])
+@pytest.mark.parametrize("case", range(len(ATTENDS)))
+def test_attend(case, code, dtype):
+    n, lens, Hq, Hkv, D, page = ATTENDS[case]
+    g = gen(100 + case)
+    cache, table = filled(lens, Hkv, D, page, code, dtype, g, Hq=Hq)
+    T = sum(n)
+    q = (torch.randn((T, Hq, D), generator=g) * 1.5).to(dtype)
+    cu = starts(n)
+    plain = all(x == 1 for x in n)
+    out, lse = cache.attend(q.cuda(), table.cuda(), ints(lens), None if plain else cu.cuda(), most=max(n) if case % 2 else None)
+    ref = R.attend(q, R.decoded(cache), table, lens, cu, 1 / math.sqrt(D), Hkv)
+    close(out, ref[0], ref[2], "out")
+    close(lse, ref[1], ref[3], "lse")
+    # the same bits again, on workspaces that hold something
+    cache.attend_ws.fill_(0xFF)
+    again = cache.attend(q.cuda(), table.cuda(), ints(lens), None if plain else cu.cuda(), most=max(n) if case % 2 else None)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_attend_views_rows_behind_the_last_and_missing_pages():
+    g = gen(7)
+    cache, table = filled([200, 90], 2, 64, 32, "i8", F16, g, Hq=4)
+    table[0, 2], table[0, 5], table[1, 0], table[1, 1] = -1, 1 << 20, -7, -1
+    wide = torch.randn((40, 6, 80), generator=g).half()
+    q = wide[4:34, 1:5, 8:72]
+    n, lens = [20, 6], [200, 66]
+    cu = starts(n)
+    big = torch.full((30, 9, 72), 3.0, dtype=F16, device="cuda")
+    out, lse = big[:, 2:6, 4:68], torch.full((4, 30), 5.0, device="cuda")
+    cache.attend(q.cuda(), table.cuda(), ints(lens), cu.cuda(), out=out, lse=lse)
+    ref = R.attend(q[:26], R.decoded(cache), table, lens, cu, 1 / 8, 2)
+    close(out[:26], ref[0], ref[2], "out")
+    close(lse[:, :26], ref[1], ref[3], "lse")
+    assert (out[26:] == 3).all() and (lse[:, 26:] == 5).all()
+    out.fill_(3.0)
+    assert (big == 3).all()
+
+
+def test_attend_of_rows_that_see_nothing():
+    g = gen(8)
+    cache, table = filled([64], 1, 32, 32, "e4m3", BF16, g, Hq=2)
+    q = torch.randn((3, 2, 32), generator=g).bfloat16().cuda()
+    for row, n in (([-1, -1, -1], 64), (table[0].tolist(), 0), ([], 64)):
+        t = torch.tensor([row], dtype=torch.int32).reshape(1, len(row)).cuda()
+        out, lse = cache.attend(q, t, ints([n]), ints([0, 3]))
+        assert not out.any() and torch.isneginf(lse).all()
+
+
+def test_attend_queries_that_are_not_finite_stay_in_their_row():
+    g = gen(11)
+    for dtype in (F16, BF16):
+        cache, table = filled([100], 1, 64, 32, "i8", dtype, g, Hq=3)
+        q = torch.randn((4, 3, 64), generator=g).to(dtype)
+        args = (table.cuda(), ints([100]), ints([0, 4]))
+        good = cache.attend(q.cuda(), *args)[0]
+        q[1, 2, 5], q[2, 0, 63] = math.nan, math.inf
+        out = cache.attend(q.cuda(), *args)[0]
+        bad = torch.zeros((4, 3), dtype=torch.bool, device="cuda")
+        bad[1, 2] = bad[2, 0] = True
+        assert out[bad].isnan().all() and torch.equal(out[~bad], good[~bad])
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+def test_attend_blocks_of_unlike_scales_and_large_scores(code, dtype):
+    """Values whose scales lie 2^24 apart, a heavy key whose values are small, scores of some hundreds; tiny and large bf16 queries."""
+    g = gen(12)
+    lens, D = [500], 128
+    pages = 20
+    table = tables(lens, 32, pages, g)
+    cache = P().PagedCache(pages, 1, D, page=32, code=code, dtype=dtype, Hq=8)
+    size = torch.exp2(torch.randint(-12, 13, (500 // 32 + 1,), generator=g).double()).repeat_interleave(32)[:500, None, None].float()
+    k, v = torch.randn((500, 1, D), generator=g), torch.randn((500, 1, D), generator=g) * size
+    k[7] *= 6
+    v[0:32] *= 2.0 ** -10
+    cache.append(k.to(dtype).cuda(), v.to(dtype).cuda(), table.cuda(), ints(lens), ints([0, 500]))
+    q = torch.randn((6, 8, D), generator=g) * 4
+    q[0] *= 2.0 ** -12
+    q[1] *= 20.0
+    if dtype == BF16:
+        q[2] *= 1e-30
+        q[3] *= 2.0 ** 20 / 4
+    q = q.to(dtype)
+    out, lse = cache.attend(q.cuda(), table.cuda(), ints(lens), ints([0, 6]))
+    ref = R.attend(q, R.decoded(cache), table, lens, [0, 6], 1 / math.sqrt(D), 1)
+    close(out, ref[0], ref[2], "out")
+    close(lse, ref[1], ref[3], "lse")
