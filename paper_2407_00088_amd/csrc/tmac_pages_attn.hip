@@ -1,11 +1,11 @@
 // Attention over pages of keys and values in 8 bits (tmac_pages.h).
 //
-// Rows of a unit of work are (query token, head of the group) of one sequence and key head.  Products run on v_mfma_f32_32x32x16 in
-// transposed form, S^T = K Q^T and O^T = V^T P^T, so that a lane owns a row (lane & 31): maximum and sum need one exchange between a
-// wavefront's halves, and the exponentials are the second product's operand as they stand.  Codes are whole numbers or e4m3 values,
+// Rows of a unit of work are (query token, head of the group) of one sequence and key head.  Products run on the matrix units in
+// transposed form, S^T = K Q^T and O^T = V^T P^T, so that a lane owns a row: maximum and sum need one or two exchanges within a
+// wavefront, and the exponentials are the second product's operand as they stand.  Codes are whole numbers or e4m3 values,
 // which fp16 holds exactly; a block's scales are the same for all its products, so they are taken out of them:
 //   x_j = s_j a + log2 sv,  a = sk scale log2 e,  p_j = 2^(x_j - m),  O += sum p_j code_j,  l += (sum p_j) / sv
-// with m against the rows' largest x, and o = O / l.
+// with m against the row's largest x, and o = O / l.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,6 @@ namespace pages {
 
 typedef float f16x __attribute__((ext_vector_type(16)));
 
-constexpr int ROWS = 32;
 // The sums are taken against the row's maximum less this (in units of log 2): exponentials then reach 2^7, and 2^15 before the maximum is
 // moved, and keep all fp16 bits down to 2^-20 of the largest.
 constexpr float HEADROOM = 7.0f, KEPT = 15.0f;
@@ -37,7 +36,9 @@ struct AttendArgs {
   int64_t* bases;  // [S + 1] units before each sequence, then the number of workgroups that have some
   float* parts;    // sums of pieces
   float c;         // scale log2 e
-  int Hq, G, bf16, workgroups, least;
+  int Hq, G, bf16;
+  int workgroups, least;  // that share the units, and how many at least each
+  int tiles;              // that a sequence may have, where every segment has a workgroup
 };
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -73,23 +74,24 @@ __device__ __forceinline__ h8 halves_of<I8>(uint32_t a, uint32_t b) {
 
 // --- which work is whose --------------------------------------------------------------------------------------------------------------
 //
-// A sequence of r rows (a key head) has tiles = ceil(r / 32), for each of them the blocks of its tokens: units (head, tile, block) in
-// this order, sequence after sequence.  The workgroups share all units evenly, in order: a segment (sequence, head, tile) that several of them
-// meet is joined afterwards.
+// A sequence of r rows (a key head) has tiles = ceil(r / ROWS), for each of them the blocks of its tokens: units (head, tile, block) in
+// this order, sequence after sequence.  A segment is one (sequence, head, tile).
 
 struct Work {
-  int rows, tiles, blocks;
+  Sequence seq;
+  int rows, tiles, blocks, held;  // held: tokens that can be seen
   int64_t units;
-  __device__ __forceinline__ Work(const AttendArgs& a, int s) {
-    const Sequence seq(a.batch, s);
-    rows = min(seq.n, a.batch.most) * a.G;
-    tiles = (rows + ROWS - 1) / ROWS;
-    const int64_t held = (int64_t)a.batch.width * BT << a.pages.shift;
-    blocks = max(1, (int)((min((int64_t)seq.len, held) + BT - 1) / BT));
-    units = (int64_t)a.pages.Hkv * tiles * blocks;
+  template <int ROWS>
+  static __device__ __forceinline__ Work of(const AttendArgs& a, const Sequence& seq) {
+    Work w{seq};
+    w.rows = min(seq.n, a.batch.most) * a.G;
+    w.tiles = (w.rows + ROWS - 1) / ROWS;
+    w.held = (int)min((int64_t)seq.len, (int64_t)a.batch.width * BT << a.pages.shift);
+    w.blocks = max(1, (w.held + BT - 1) / BT);
+    w.units = (int64_t)a.pages.Hkv * w.tiles * w.blocks;
+    return w;
   }
 };
-__device__ __forceinline__ int64_t units_of_lane(const AttendArgs& a, int s) { return s < a.batch.S ? Work(a, s).units : 0; }
 
 __device__ __forceinline__ int64_t shfl64(int64_t x, int from) {
   return (int64_t)((uint64_t)(uint32_t)__shfl((int)(x >> 32), from) << 32 | (uint32_t)__shfl((int)x, from));
@@ -103,6 +105,8 @@ __device__ __forceinline__ int64_t inclusive(int64_t x) {
   }
   return x;
 }
+__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float lane_value(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
 
 // Workgroups that have units: all, or as many as get `least` each.
 __device__ __forceinline__ int64_t sharing(const AttendArgs& a, int64_t units) {
@@ -111,86 +115,130 @@ __device__ __forceinline__ int64_t sharing(const AttendArgs& a, int64_t units) {
 __device__ __forceinline__ int64_t share_from(int64_t units, int64_t sharers, int64_t w) { return units * w / sharers; }
 __device__ __forceinline__ int64_t owner_of(int64_t units, int64_t sharers, int64_t u) { return ((u + 1) * sharers - 1) / units; }
 
-// Sums of pieces, of 32 rows: maximum and sum, then D values each.  A workgroup leaves at most two: of a segment that began before it
+// Sums of pieces: maximum and sum of every row, then W values each.  A workgroup leaves at most two: of a segment that began before it
 // (slot 0) and of one that goes on after it (slot 1).
-template <int NI>
-struct Part {
-  static constexpr int W = NI * 32, FLOATS = ROWS * (W + 2);
-};
+__host__ __device__ __forceinline__ int part_floats(int rows, int width) { return rows * (width + 2); }
 
 // --- one wavefront's rows ---------------------------------------------------------------------------------------------------------------
 
-template <typename Code, int NI>
-struct Rows {
-  h8 q[NI][2];
-  f16x o[NI];
-  float m, l, c;  // c: the row's scale log2 e
-  int sees;       // tokens before this one
+// What the two shapes have in common: queries as fp16 of a row's elements d_of(i, y) .. + 7.
+template <int NQ>
+struct Queries {
+  h8 q[NQ][2];
+  float c;   // the row's scale log2 e
+  int sees;  // tokens before this one
 
-  __device__ __forceinline__ void clear() {
+  template <typename DOf>
+  __device__ __forceinline__ void load(const AttendArgs& a, const char* at, bool valid, DOf&& d_of) {
+    u2 raw[NQ][4];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) o[i] = (f16x)(0.0f);
-    m = -INFINITY, l = 0.0f;
-  }
-
-  // Queries as fp16, the lane's half of every 32 elements.
-  __device__ __forceinline__ void load_q(const AttendArgs& a, const char* q, bool valid, int half) {
-    const int D = a.pages.D;
-    float most = 0.0f;
-    uint16_t raw[NI][16];
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int d = 32 * i + 16 * half + 4 * j;
-        const u2 x = valid && d < D ? *reinterpret_cast<const u2*>(q + d * 2) : u2{0u, 0u};
-#pragma unroll
-        for (int y = 0; y < 4; ++y) raw[i][4 * j + y] = (uint16_t)(x[y >> 1] >> (16 * (y & 1)));
+        const int d = d_of(i) + 4 * j;
+        raw[i][j] = valid && d < a.pages.D ? *reinterpret_cast<const u2*>(at + d * 2) : u2{0u, 0u};
       }
     c = a.c;
     if (!a.bf16) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
+      for (int i = 0; i < NQ; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) q_at(i, j) = __builtin_bit_cast(_Float16, raw[i][j]);
+        for (int y = 0; y < 2; ++y) q[i][y] = __builtin_bit_cast(h8, u4{raw[i][2 * y][0], raw[i][2 * y][1], raw[i][2 * y + 1][0], raw[i][2 * y + 1][1]});
       return;
     }
+    float most = 0.0f;
+    auto bf = [](const u2& x, int y) { return __builtin_bit_cast(float, y & 1 ? x[y >> 1] & 0xffff0000u : x[y >> 1] << 16); };
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float x = fabsf(to_float(raw[i][j], true));
+        const float x = fabsf(bf(raw[i][j >> 2], j & 3));
         most = fmaxf(most, x <= 3.4028235e38f ? x : 0.0f);
       }
-    most = max_halves(most);
+    // (the lanes of one row lie 16 or 32 apart; rows' maxima need not be the same in all of them: but one of the row's own)
+    most = over_row(most);
     // the largest to [2^14, 2^15)
     const int e = most > 0.0f ? (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - 14 : 0;
     c = __builtin_ldexpf(a.c, e);
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NQ; ++i)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) q_at(i, j) = (_Float16)__builtin_ldexpf(to_float(raw[i][j], true), -e);
+      for (int j = 0; j < 16; ++j) q[i][j >> 3][j & 7] = (_Float16)__builtin_ldexpf(bf(raw[i][j >> 2], j & 3), -e);
   }
-  struct At {
-    h8& v;
-    int j;
-    __device__ __forceinline__ void operator=(_Float16 x) { v[j] = x; }
-  };
-  __device__ __forceinline__ At q_at(int i, int j) { return At{q[i][j >> 3], j & 7}; }
+  int apart;
+  __device__ __forceinline__ float over_row(float x) const {
+    if (apart == 16) x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+  }
+};
 
-  __device__ __forceinline__ f16x scores(const u4 (&k)[NI]) const {
+// The running maximum.  x: the largest exponent of the block; returns whether any row's moved, and by what the row's sums are multiplied.
+__device__ __forceinline__ bool outgrown(float x, float& m, float& alpha) {
+  const bool grows = x - m > KEPT;
+  const float to = grows ? __builtin_ceilf(x) - HEADROOM : m;
+  alpha = grows ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+  m = to;
+  return __any(grows);
+}
+
+// A block's keys or values.
+struct Plane {
+  static constexpr int NOWHERE = 1 << 20;
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ Plane(const char* at, int bytes) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), (short)0, bytes, 0x00020000)) {}
+  // (read once: past the caches)
+  __device__ __forceinline__ u4 load16(int lane, int fixed) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane + fixed, 0, 2)); }
+  __device__ __forceinline__ u2 load8(int lane, int fixed) const { return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane + fixed, 0, 2)); }
+};
+
+template <typename Code, int NI, int ROWS>
+struct Rows;
+
+// 32 rows: v_mfma_f32_32x32x16, row lane & 31.
+template <typename Code, int NI>
+struct Rows<Code, NI, 32> {
+  static constexpr int NK = NI, NV = NI;
+  typedef u4 KRaw;
+  typedef u4 VRaw;
+  Queries<NI> q;
+  f16x o[NI];
+  float m, l;
+  int lane;
+
+  static __device__ __forceinline__ int row(int lane) { return lane & 31; }
+  // A block's keys or values; what lies past its end reads as zeros.  Of values: a whole run of 32 elements, or the last one of 16, past
+  // which the other half's 16 lanes have nothing
+  static __device__ __forceinline__ void load_k(u4 (&k)[NK], const Plane& p, int lane) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) k[i] = p.load16(lane * 16, i * 1024);
+  }
+  static __device__ __forceinline__ void load_v(u4 (&v)[NV], const Plane& p, int lane, bool odd) {
+    const int last = odd ? ((lane & 31) < 16 ? (lane >> 5) * 256 + (lane & 31) * 16 : Plane::NOWHERE) : lane * 16;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = p.load16(i == NV - 1 ? last : lane * 16, i * 1024);
+  }
+  __device__ __forceinline__ void begin(const AttendArgs& a, const char* at, bool valid, int sees) {
+    const int half = lane >> 5;
+    q.apart = 32, q.sees = sees;
+    q.load(a, at, valid, [&](int i) { return 32 * i + 16 * half; });
+#pragma unroll
+    for (int i = 0; i < NI; ++i) o[i] = (f16x)(0.0f);
+    m = -INFINITY, l = 0.0f;
+  }
+  typedef f16x Scores;
+  __device__ __forceinline__ f16x scores(const u4 (&k)[NK]) const {
     f16x s = (f16x)(0.0f);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(k[i][0], k[i][1]), q[i][0], s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(k[i][2], k[i][3]), q[i][1], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(k[i][0], k[i][1]), q.q[i][0], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(k[i][2], k[i][3]), q.q[i][1], s, 0, 0, 0);
     }
     return s;
   }
-  // The scores' exponentials, times the scale of the values; p[0]: tokens 0-3 and 16-19 of each half's, p[1]: 8-11 and 24-27.
-  __device__ __forceinline__ void weigh(f16x s, int begin, bool masked, float sk, float sv, int half, h8 (&p)[2]) {
+  struct Weights { h8 p[2]; };  // [0]: tokens 0-3 and 16-19 of the half's, [1]: 8-11 and 24-27
+  __device__ __forceinline__ Weights weigh(f16x s, int begin, bool masked, float sk, float sv) {
     if (masked) {
-      const int x = sees - begin - 4 * half;
+      const int x = q.sees - begin - 4 * (lane >> 5);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (r >> 2) * 8 + (r & 3) < x ? s[r] : -INFINITY;
     }
@@ -198,96 +246,198 @@ struct Rows {
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
     mx = max_halves(mx);
-    const float a = sk * c, log_sv = __builtin_amdgcn_logf(sv), x = __builtin_fmaf(mx, a, log_sv);
-    const bool grows = x - m > KEPT;
-    if (__any(grows)) {
-      const float to = grows ? __builtin_ceilf(x) - HEADROOM : m, alpha = grows ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+    const float a = sk * q.c, log_sv = __builtin_amdgcn_logf(sv);
+    float alpha;
+    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) o[i] *= alpha;
       l *= alpha;
-      m = to;
     }
-    const float base = log_sv - (m == -INFINITY ? 0.0f : m);
+    const float m0 = m == -INFINITY ? 0.0f : m, base = log_sv - m0;
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a, base));
       sum[r & 1] += s[r];
     }
-    l = __builtin_fmaf(sum[0] + sum[1], 1.0f / sv, l);
+    // (without the scale again by what the exponents really had of it: base is rounded, base + m0 is not)
+    l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-(base + m0)), l);
+    Weights w;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) p[r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)s[r];
+    for (int r = 0; r < 16; ++r) w.p[r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)s[r];
+    return w;
   }
-  __device__ __forceinline__ void multiply(const u4 (&v)[NI], const h8 (&p)[2]) {
+  __device__ __forceinline__ void multiply(const u4 (&v)[NV], const Weights& w) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][0], v[i][1]), p[0], o[i], 0, 0, 0);
-      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][2], v[i][3]), p[1], o[i], 0, 0, 0);
+      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][0], v[i][1]), w.p[0], o[i], 0, 0, 0);
+      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][2], v[i][3]), w.p[1], o[i], 0, 0, 0);
     }
+  }
+  __device__ __forceinline__ float sum() const { return add_halves(l); }
+  // f(d, four sums from there on)
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    const int half = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) f(32 * i + 8 * z + 4 * half, f4{o[i][4 * z], o[i][4 * z + 1], o[i][4 * z + 2], o[i][4 * z + 3]});
   }
 };
 
-__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-
-// Blocks [begin, end), every `step`-th from begin on, for one wavefront's rows.
+// 16 rows: v_mfma_f32_16x16x32, row lane & 15.  Half the work of 32 for what is read, and half the registers.
 template <typename Code, int NI>
-__device__ __forceinline__ void run_blocks(const AttendArgs& a, Rows<Code, NI>& w, const int32_t* table, int head, int begin, int end, int step, int least) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, chunks = a.pages.chunks;
-  // where the lane's 16 bytes of each run of 32 elements lie
-  uint32_t v_at[NI];
-  bool k_is[NI], v_is[NI];
+struct Rows<Code, NI, 16> {
+  static constexpr int NQ = (NI + 1) / 2, NK = 2 * NQ, NV = 2 * NI;
+  typedef u4 KRaw;
+  typedef u2 VRaw;
+  Queries<NQ> q;
+  f4 o[NV];
+  float m, l;
+  int lane;
+
+  static __device__ __forceinline__ int row(int lane) { return lane & 15; }
+  // (keys: tokens 0-15 and 16-31 of four chunks; values: 16 elements)
+  static __device__ __forceinline__ void load_k(u4 (&k)[NK], const Plane& p, int lane) {
+    const int at = (lane >> 4) * 512 + (lane & 15) * 16;
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int n = value_run(chunks, 32 * i);
-    k_is[i] = 2 * i + half < chunks;
-    v_is[i] = (lane & 31) < n && 2 * i < chunks;
-    v_at[i] = i * 1024 + (half * n + (lane & 31)) * 16;
+    for (int i = 0; i < NK; ++i) k[i] = p.load16(at, (i >> 1) * 2048 + (i & 1) * 256);
   }
-  u4 k[NI], v[NI];
-  for (int first = begin; first < end; first += 64 * step) {
-    // 64 blocks' places and scales, one a lane
+  static __device__ __forceinline__ void load_v(u2 (&v)[NV], const Plane& p, int lane, bool odd) {
+    const int in = (lane & 15) * 16 + (lane >> 5) * 8, at = in + (lane >> 4 & 1) * 512, last = in + (lane >> 4 & 1) * (odd ? 256 : 512);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = p.load8(i >= NV - 2 ? last : at, (i >> 1) * 1024 + (i & 1) * 256);
+  }
+  __device__ __forceinline__ void begin(const AttendArgs& a, const char* at, bool valid, int sees) {
+    const int quarter = lane >> 4;
+    q.apart = 16, q.sees = sees;
+    q.load(a, at, valid, [&](int i) { return 16 * (4 * i + quarter); });
+#pragma unroll
+    for (int i = 0; i < NV; ++i) o[i] = (f4)(0.0f);
+    m = -INFINITY, l = 0.0f;
+  }
+  struct Scores { f4 s[2]; };
+  __device__ __forceinline__ Scores scores(const u4 (&k)[NK]) const {
+    Scores s = {{(f4)(0.0f), (f4)(0.0f)}};
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s.s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<Code>(k[2 * i + t][0], k[2 * i + t][1]), q.q[i][0], s.s[t], 0, 0, 0);
+        s.s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<Code>(k[2 * i + t][2], k[2 * i + t][3]), q.q[i][1], s.s[t], 0, 0, 0);
+      }
+    return s;
+  }
+  struct Weights { h8 p; };  // tokens 0-3 of the quarter's four and 16 on
+  static __device__ __forceinline__ float over_row(float x, bool adds) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const float a = __builtin_bit_cast(float, (unsigned)r[0]), b = __builtin_bit_cast(float, (unsigned)r[1]);
+    return adds ? add_halves(a + b) : max_halves(fmaxf(a, b));
+  }
+  __device__ __forceinline__ Weights weigh(Scores x, int begin, bool masked, float sk, float sv) {
+    float s[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) s[r] = x.s[r >> 2][r & 3];
+    if (masked) {
+      const int upto = q.sees - begin - 4 * (lane >> 4);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = (r >> 2) * 16 + (r & 3) < upto ? s[r] : -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
+    mx = over_row(mx, false);
+    const float a = sk * q.c, log_sv = __builtin_amdgcn_logf(sv);
+    float alpha;
+    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) o[i] *= alpha;
+      l *= alpha;
+    }
+    const float m0 = m == -INFINITY ? 0.0f : m, base = log_sv - m0;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a, base));
+      sum[r & 1] += s[r];
+    }
+    l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-(base + m0)), l);  // (as with 32 rows)
+    Weights w;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) w.p[r] = (_Float16)s[r];
+    return w;
+  }
+  __device__ __forceinline__ void multiply(const u2 (&v)[NV], const Weights& w) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<Code>(v[i][0], v[i][1]), w.p, o[i], 0, 0, 0);
+  }
+  __device__ __forceinline__ float sum() const { return over_row(l, true); }
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    const int quarter = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f(16 * i + 4 * quarter, o[i]);
+  }
+};
+
+// Places and scales of up to 64 blocks, one a lane: blocks first, first + step, ... before end.
+struct Blocks {
+  int64_t unit;
+  float sk, sv;
+  __device__ __forceinline__ Blocks(const AttendArgs& a, const int32_t* table, int head, int first, int end, int step, int lane) : sk(0.0f), sv(0.0f) {
     const int mine = first + lane * step;
-    const int64_t unit = mine < end ? a.pages.unit_of(table, a.batch.width, mine, head) : -1;
-    float sk = 0.0f, sv = 0.0f;
+    unit = mine < end ? a.pages.unit_of(table, a.batch.width, mine, head) : -1;
+  }
+  __device__ __forceinline__ void scales(const AttendArgs& a) {
     if (unit >= 0) {
       const f2 x = *reinterpret_cast<const f2*>(a.pages.scales + unit * 2);
       sk = x[0], sv = x[1];
     }
-    uint64_t left = __ballot(unit >= 0);
+  }
+  __device__ __forceinline__ const char* at(const AttendArgs& a, int n) const {
+    return a.pages.keys((int64_t)((uint64_t)(uint32_t)lane_value((int)(unit >> 32), n) << 32 | (uint32_t)lane_value((int)unit, n)));
+  }
+};
+
+// Blocks first, first + step, ... before end for one wavefront's rows, whose queries q() loads.  least: tokens that every row sees.
+// The next block's keys are requested as soon as this one's have met the queries, its values as soon as they have met the exponentials.
+template <typename R, typename Q>
+__device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int32_t* table, int head, int first, int end, int step, int least, Q&& q) {
+  const int lane = w.lane, plane = a.pages.plane_bytes();
+  const bool odd = a.pages.chunks & 1;
+  typename R::KRaw k[R::NK];
+  typename R::VRaw v[R::NV];
+  bool loaded = false;
+  for (; first < end; first += 64 * step) {
+    Blocks blocks(a, table, head, first, end, step, lane);
+    if (!loaded) q();
+    loaded = true;
+    uint64_t left = __ballot(blocks.unit >= 0);
     if (!left) continue;
     auto take = [&] {
       const int n = __builtin_ctzll(left);
       left &= left - 1;
       return n;
     };
-    auto base_of = [&](int n) {
-      return a.pages.keys((int64_t)((uint64_t)(uint32_t)lane_value((int)(unit >> 32), n) << 32 | (uint32_t)lane_value((int)unit, n)));
-    };
-    auto load_k = [&](int n) {
-      const char* at = base_of(n);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) k[i] = k_is[i] ? __builtin_nontemporal_load(reinterpret_cast<const u4*>(at + i * 1024 + lane * 16)) : u4{0u, 0u, 0u, 0u};
-    };
-    auto load_v = [&](int n) {
-      const char* at = base_of(n) + a.pages.plane_bytes();
-#pragma unroll
-      for (int i = 0; i < NI; ++i) v[i] = v_is[i] ? __builtin_nontemporal_load(reinterpret_cast<const u4*>(at + v_at[i])) : u4{0u, 0u, 0u, 0u};
-    };
+    auto load_k = [&](int n) { R::load_k(k, Plane(blocks.at(a, n), plane), lane); };
+    auto load_v = [&](int n) { R::load_v(v, Plane(blocks.at(a, n) + plane, plane), lane, odd); };
     int n = take();
-    load_k(n), load_v(n);
+    load_k(n);
+    blocks.scales(a);
+    load_v(n);
     while (true) {
       const int next = left ? take() : -1, at = (first + n * step) * BT;
-      const f16x s = w.scores(k);
+      const typename R::Scores s = w.scores(k);
       if (next >= 0) load_k(next);
-      h8 p[2];
-      w.weigh(s, at, at + BT > least, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, sk), n)),
-              __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, sv), n)), half, p);
+      const typename R::Weights p = w.weigh(s, at, at + BT > least, lane_value(blocks.sk, n), lane_value(blocks.sv, n));
       w.multiply(v, p);
       if (next < 0) break;
       load_v(next);
       n = next;
     }
   }
+  if (!loaded) q();
 }
 
 // What becomes of a row's sums.
@@ -295,146 +445,177 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return (m + HEADROOM + __builtin_log2f(l * __builtin_exp2f(-HEADROOM))) * 0.69314718055994530942f;
 }
 
-// One workgroup's share of the units.  WAVES wavefronts take every WAVES-th block of a piece, their sums meet in LDS.
-template <typename Code, int NI, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(const AttendArgs a) {
-  typedef Part<NI> P;
-  constexpr int PITCH = P::W + 4;
-  __shared__ float shared[WAVES == 1 ? 1 : WAVES * ROWS * (PITCH + 2)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int S = a.batch.S, D = a.pages.D;
-  // all units, then the sequence of the share's first
-  int64_t units = 0;
-  for (int s = 0; s < S; s += 64) units += shfl64(inclusive(units_of_lane(a, s + lane)), 63);
-  const int64_t sharers = sharing(a, units), w = blockIdx.x;
-  if (blockIdx.x == 0 && wave == 0) {
+// A row's result: sums from d on, or its lse.
+__device__ __forceinline__ void put_out(const AttendArgs& a, int row, int hq, int d, const f4& o, float m, float l) {
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  uint16_t e[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) e[j] = from_float(o[j] * inv, a.bf16);
+  if (d < a.pages.D)
+    *reinterpret_cast<u2*>(a.out + row * a.out_token + hq * a.out_head + d * 2) = u2{e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16};
+  if (d == 0 && a.lse) a.lse[(int64_t)hq * a.batch.T + row] = log_sum(m, l);
+}
+
+// A piece of a segment: blocks [begin, stop).  WAVES wavefronts take every WAVES-th, their sums meet in LDS.  part: where the piece's sums
+// go, null: it is the whole segment, whose results go out.
+template <int NI, int ROWS, int WAVES>
+struct Meeting {
+  static constexpr int W = NI * 32, PITCH = W + 4, FLOATS = WAVES == 1 ? 4 : WAVES * ROWS * (PITCH + 2);
+};
+template <typename Code, int NI, int ROWS, int WAVES>
+__device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work, int s, int head, int tile, int begin, int stop, float* part, float* shared,
+                                          bool again) {
+  typedef Meeting<NI, ROWS, WAVES> M;
+  constexpr int W = M::W, PITCH = M::PITCH;
+  // (named anew for every piece: else what follows from it is worked out before the first and kept in 40 registers)
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Rows<Code, NI, ROWS> x;
+  x.lane = lane;
+  const Sequence& seq = work.seq;
+  // the lane's row
+  const int in = x.row(lane), r = tile * ROWS + in, i = r / a.G, row = seq.row0 + i, hq = head * a.G + r - i * a.G;
+  const bool valid = r < work.rows;
+  // (the first row of a tile sees least)
+  const int least = clamp_to(seq.first + (tile * ROWS) / a.G + 1, work.held);
+  run_blocks(a, x, a.batch.row(s), head, begin + (WAVES == 1 ? 0 : wave), stop, WAVES, least,
+             [&] { x.begin(a, a.q + row * a.q_token + hq * a.q_head, valid, valid ? clamp_to(seq.first + i + 1, work.held) : 0x7fffffff); });
+  const float l = x.sum();
+  auto put = [&](int row, int hq, int in, int d, const f4& o, float m, float l) {
+    if (!part) {
+      put_out(a, row, hq, d, o, m, l);
+    } else {
+      *reinterpret_cast<f4*>(part + 2 * ROWS + in * W + d) = o;
+      if (d == 0) part[in * 2] = m, part[in * 2 + 1] = l;
+    }
+  };
+  if constexpr (WAVES == 1) {
+    x.each([&](int d, const f4& o) {
+      if (valid) put(row, hq, in, d, o, x.m, l);
+    });
+  } else {
+    float* ml = shared + WAVES * ROWS * PITCH;
+    if (again) __syncthreads();  // (the sums before have been read)
+    if (lane < ROWS) ml[(wave * ROWS + lane) * 2] = x.m, ml[(wave * ROWS + lane) * 2 + 1] = l;
+    x.each([&](int d, const f4& o) { *reinterpret_cast<f4*>(shared + (wave * ROWS + in) * PITCH + d) = o; });
+    __syncthreads();
+    const int rows = min(ROWS, work.rows - tile * ROWS);
+    for (int k = tid; k < rows * (W / 4); k += 64 * WAVES) {
+      const int in = k / (W / 4), d = k % (W / 4) * 4;
+      float m = -INFINITY, l = 0.0f;
+      f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[(y * ROWS + in) * 2]);
+#pragma unroll
+      for (int y = 0; y < WAVES; ++y) {
+        const float my = ml[(y * ROWS + in) * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
+        l = __builtin_fmaf(ml[(y * ROWS + in) * 2 + 1], f, l);
+        o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in) * PITCH + d) * f;
+      }
+      const int r = tile * ROWS + in, i = r / a.G;
+      put(seq.row0 + i, head * a.G + r - i * a.G, in, d, o, m, l);
+    }
+  }
+}
+
+// A workgroup a segment.
+template <typename Code, int NI, int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? (WAVES == 16 ? 4 : 3) : 2) void attend_whole_kernel(const AttendArgs a) {
+  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
+  const int head = blockIdx.x % a.pages.Hkv, x = blockIdx.x / a.pages.Hkv, tile = x % a.tiles, s = x / a.tiles;
+  const Work work = Work::of<ROWS>(a, Sequence(a.batch, s));
+  if (tile >= work.tiles) return;
+  run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
+}
+
+// A workgroup an equal share of all units, in order: a segment that several of them meet is joined afterwards.
+template <typename Code, int NI, int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(const AttendArgs a) {
+  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
+  __shared__ int numbers[WAVES][3][64];  // of 64 sequences: Sequence's row0, n, len
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), S = a.batch.S;
+  auto units_of = [&](int s0, bool keep) {
+    Sequence seq;
+    if (s0 + lane < S) seq = Sequence(a.batch, s0 + lane);
+    if (keep) numbers[wave][0][lane] = seq.row0, numbers[wave][1][lane] = seq.n, numbers[wave][2][lane] = seq.len;
+    return Work::of<ROWS>(a, seq).units;
+  };
+  int64_t u, end, local;
+  int s0 = 0, at;
+  {
+    int64_t x = units_of(0, true), upto = inclusive(x), units = shfl64(upto, 63);
+    for (int i = 64; i < S; i += 64) units += shfl64(inclusive(units_of(i, false)), 63);
+    const int64_t sharers = sharing(a, units), w = blockIdx.x;
+    if (blockIdx.x == 0 && wave == 0) {
+      int64_t before = 0;
+      for (int i = 0; i < S; i += 64) {
+        const int64_t y = units_of(i, false), to = inclusive(y);
+        if (i + lane < S) a.bases[i + lane] = before + to - y;
+        before += shfl64(to, 63);
+      }
+      if (lane == 0) a.bases[S] = units, a.bases[S + 1] = sharers;
+    }
+    if (w >= sharers) return;
+    u = share_from(units, sharers, w), end = share_from(units, sharers, w + 1);
+    if (u >= end) return;
+    // the share's first sequence
     int64_t before = 0;
-    for (int s = 0; s < S; s += 64) {
-      const int64_t x = units_of_lane(a, s + lane), upto = inclusive(x);
-      if (s + lane < S) a.bases[s + lane] = before + upto - x;
+    while (u >= before + shfl64(upto, 63) && s0 + 64 < S) {
       before += shfl64(upto, 63);
+      s0 += 64;
+      x = units_of(s0, true);
+      upto = inclusive(x);
     }
-    if (lane == 0) a.bases[S] = units, a.bases[S + 1] = sharers;
+    at = __builtin_ctzll(__ballot(before + upto > u) | (uint64_t)1 << 63);
+    local = u - (before + shfl64(upto - x, at));
   }
-  if (w >= sharers) return;
-  int64_t u = share_from(units, sharers, w);
-  const int64_t end = share_from(units, sharers, w + 1);
-  if (u >= end) return;
-  int s = 0;
-  int64_t local = 0, before = 0;
-  for (int s0 = 0; s0 < S; s0 += 64) {
-    const int64_t x = units_of_lane(a, s0 + lane), upto = before + inclusive(x), last = shfl64(upto, 63);
-    if (u < last) {
-      const int at = __builtin_ctzll(__ballot(upto > u));
-      s = s0 + at;
-      local = u - shfl64(upto - x, at);
-      break;
-    }
-    before = last;
-  }
-  s = __builtin_amdgcn_readfirstlane(s);
-  bool first_piece = true;
-  while (u < end && s < S) {
-    const Work work(a, s);
+  bool again = false;
+  while (u < end && s0 + at < S) {
+    Sequence seq;
+    seq.row0 = __builtin_amdgcn_readfirstlane(numbers[wave][0][at]), seq.n = __builtin_amdgcn_readfirstlane(numbers[wave][1][at]);
+    seq.len = __builtin_amdgcn_readfirstlane(numbers[wave][2][at]), seq.first = seq.len - seq.n;
+    const Work work = Work::of<ROWS>(a, seq);
     if (local >= work.units) {
-      ++s, local = 0;
+      local = 0;
+      if (++at == 64) {
+        at = 0, s0 += 64;
+        units_of(s0, true);
+      }
       continue;
     }
-    const Sequence seq(a.batch, s);
-    const int64_t segment = local / work.blocks;
-    const int begin = (int)(local - segment * work.blocks), stop = (int)min((int64_t)work.blocks, begin + (end - u));
-    const int head = (int)(segment / work.tiles), tile = (int)(segment % work.tiles);
-    // the lane's row
-    const int r = tile * ROWS + (lane & 31), i = r / a.G, g = r - i * a.G;
-    const bool valid = r < work.rows;
-    const int row = seq.row0 + i, hq = head * a.G + g;
-    Rows<Code, NI> x;
-    const int most = (int)min((int64_t)seq.len, (int64_t)a.batch.width * BT << a.pages.shift);
-    x.sees = valid ? clamp_to(seq.first + i + 1, most) : 0x7fffffff;
-    x.clear();
-    x.load_q(a, a.q + row * a.q_token + hq * a.q_head, valid, half);
-    // (the first row of a tile sees least)
-    const int least = clamp_to(seq.first + (tile * ROWS) / a.G + 1, most);
-    const int mine = WAVES == 1 ? begin : begin + wave;
-    run_blocks<Code, NI>(a, x, a.batch.row(s), head, mine, stop, WAVES, least);
-    x.l = add_halves(x.l);
+    const int segment = (int)(local / work.blocks);
+    const int begin = (int)(local - (int64_t)segment * work.blocks), stop = (int)min((int64_t)work.blocks, begin + (end - u));
+    const int head = segment / work.tiles, tile = segment % work.tiles;
     const bool whole = begin == 0 && stop == work.blocks;
-    float* part = a.parts + (2 * w + (begin == 0)) * P::FLOATS;
-    auto put = [&](bool is, int row, int hq, int in_tile, int d, f4 o, float m, float l) {
-      if (!is) return;
-      if (whole) {
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        uint16_t e[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = from_float(o[j] * inv, a.bf16);
-        if (d < D) *reinterpret_cast<u2*>(a.out + row * a.out_token + hq * a.out_head + d * 2) = u2{e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16};
-        if (d == 0 && a.lse) a.lse[(int64_t)hq * a.batch.T + row] = log_sum(m, l);
-      } else {
-        *reinterpret_cast<f4*>(part + 2 * ROWS + in_tile * P::W + d) = o;
-        if (d == 0) part[in_tile * 2] = m, part[in_tile * 2 + 1] = l;
-      }
-    };
-    if constexpr (WAVES == 1) {
-#pragma unroll
-      for (int y = 0; y < NI; ++y)
-#pragma unroll
-        for (int z = 0; z < 4; ++z)
-          put(valid, row, hq, lane & 31, 32 * y + 8 * z + 4 * half, f4{x.o[y][4 * z], x.o[y][4 * z + 1], x.o[y][4 * z + 2], x.o[y][4 * z + 3]}, x.m, x.l);
-    } else {
-      float* ml = shared + WAVES * ROWS * PITCH;
-      if (!first_piece) __syncthreads();  // (the sums before have been read)
-      if (half == 0) ml[(wave * ROWS + lane) * 2] = x.m, ml[(wave * ROWS + lane) * 2 + 1] = x.l;
-#pragma unroll
-      for (int y = 0; y < NI; ++y)
-#pragma unroll
-        for (int z = 0; z < 4; ++z)
-          *reinterpret_cast<f4*>(shared + (wave * ROWS + (lane & 31)) * PITCH + 32 * y + 8 * z + 4 * half) =
-              f4{x.o[y][4 * z], x.o[y][4 * z + 1], x.o[y][4 * z + 2], x.o[y][4 * z + 3]};
-      __syncthreads();
-      const int rows = min(ROWS, work.rows - tile * ROWS);
-      for (int k = tid; k < rows * (P::W / 4); k += 64 * WAVES) {
-        const int in_tile = k / (P::W / 4), d = k % (P::W / 4) * 4;
-        float m = -INFINITY, l = 0.0f;
-        f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[(y * ROWS + in_tile) * 2]);
-#pragma unroll
-        for (int y = 0; y < WAVES; ++y) {
-          const float my = ml[(y * ROWS + in_tile) * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
-          l = __builtin_fmaf(ml[(y * ROWS + in_tile) * 2 + 1], f, l);
-          o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in_tile) * PITCH + d) * f;
-        }
-        const int rr = tile * ROWS + in_tile, ii = rr / a.G;
-        put(true, seq.row0 + ii, head * a.G + rr - ii * a.G, in_tile, d, o, m, l);
-      }
-    }
-    first_piece = false;
+    run_piece<Code, NI, ROWS, WAVES>(a, work, s0 + at, head, tile, begin, stop,
+                                     whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(ROWS, NI * 32), shared, again);
+    again = true;
     u += stop - begin;
     local += stop - begin;
   }
 }
 
 // Rows of segments that several workgroups met: a wavefront a row, two elements a lane.
-template <int NI>
+template <int NI, int ROWS>
 __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
-  typedef Part<NI> P;
+  constexpr int W = NI * 32;
   const int lane = threadIdx.x & 63;
   const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= (int64_t)a.batch.T * a.Hq) return;
   const int row = __builtin_amdgcn_readfirstlane((int)(id / a.Hq)), hq = __builtin_amdgcn_readfirstlane((int)(id % a.Hq));
   const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, row));
-  const Sequence seq(a.batch, s);
-  const Work work(a, s);
-  const int head = hq / a.G, r = (row - seq.row0) * a.G + hq - head * a.G;
-  if (row < seq.row0 || r >= work.rows) return;
+  const Work work = Work::of<ROWS>(a, Sequence(a.batch, s));
+  const int head = hq / a.G, r = (row - work.seq.row0) * a.G + hq - head * a.G;
+  if (row < work.seq.row0 || r >= work.rows) return;
   const int64_t units = a.bases[a.batch.S], sharers = a.bases[a.batch.S + 1];
   const int64_t from = a.bases[s] + ((int64_t)head * work.tiles + r / ROWS) * work.blocks;
   const int64_t w0 = owner_of(units, sharers, from), w1 = owner_of(units, sharers, from + work.blocks - 1);
   if (w0 == w1) return;
-  const int in_tile = r % ROWS, d = lane * 2;
-  auto part_of = [&](int64_t w) { return a.parts + (2 * w + (w == w0)) * P::FLOATS; };
+  const int in = r % ROWS, d = lane * 2;
+  auto part_of = [&](int64_t w) { return a.parts + (2 * w + (w == w0)) * part_floats(ROWS, W); };
   float m = -INFINITY;
-  for (int64_t w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, part_of(w)[in_tile * 2]);
+  for (int64_t w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, part_of(w)[in * 2]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   // (fmaxf leaves NaN aside: the sums have it)
@@ -443,10 +624,10 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
 #pragma unroll 4
   for (int64_t w = w0; w <= w1; ++w) {
     const float* p = part_of(w);
-    const float my = p[in_tile * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
-    l = __builtin_fmaf(p[in_tile * 2 + 1], f, l);
-    if (d < P::W) {
-      const f2 o = *reinterpret_cast<const f2*>(p + 2 * ROWS + in_tile * P::W + d);
+    const float my = p[in * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
+    l = __builtin_fmaf(p[in * 2 + 1], f, l);
+    if (d < W) {
+      const f2 o = *reinterpret_cast<const f2*>(p + 2 * ROWS + in * W + d);
       sum[0] = __builtin_fmaf(o[0], f, sum[0]), sum[1] = __builtin_fmaf(o[1], f, sum[1]);
     }
   }
@@ -464,34 +645,46 @@ static bool desc_ok(const tmac_attn_desc* d, const tmac_pages* p) {
 }
 
 struct Plan {
-  int workgroups, waves;
+  bool whole;  // every segment by a workgroup of its own
+  int rows, waves, workgroups, least, tiles;
   size_t bases, parts;  // bytes
 };
-static Plan plan_of(const tmac_pages* p, const tmac_pages_batch* b) {
-  Plan plan;
+static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
+  Plan plan = {};
+  const int64_t most = (int64_t)view_of(b).most * (d->Hq / d->Hkv);  // rows of a sequence and head
+  plan.rows = most <= 16 ? 16 : 32;
+  plan.tiles = (int)((most + plan.rows - 1) / plan.rows);
+  const int64_t segments = (int64_t)b->S * p->Hkv * plan.tiles, blocks = (int64_t)b->width * p->page / BT;
+  plan.whole = blocks <= 128 && segments * 64 * 16 <= 0xffffffff;
+  if (plan.whole) {
+    plan.waves = plan.rows == 32 ? 4 : segments >= 1024 ? 4 : segments >= 512 ? 8 : 16;
+    plan.workgroups = (int)segments;
+    return plan;
+  }
   plan.waves = 4;
-  plan.workgroups = 512;
+  plan.workgroups = plan.rows == 16 ? 768 : 512;
+  plan.least = 8;
   plan.bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
-  plan.parts = (size_t)plan.workgroups * 2 * ROWS * ((p->D + 31) / 32 * 32 + 2) * 4;
+  plan.parts = (size_t)plan.workgroups * 2 * part_floats(plan.rows, (p->D + 31) / 32 * 32) * 4;
   return plan;
 }
 
-template <typename Code, int WAVES>
-static const void* attend_of(int ni) {
-  switch (ni) {
-    case 1: return (const void*)attend_kernel<Code, 1, WAVES>;
-    case 2: return (const void*)attend_kernel<Code, 2, WAVES>;
-    case 3: return (const void*)attend_kernel<Code, 3, WAVES>;
-    default: return (const void*)attend_kernel<Code, 4, WAVES>;
+template <typename Code, int NI>
+static const void* attend_of(const Plan& p) {
+  if (p.whole) {
+    if (p.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
+    return p.waves == 4 ? (const void*)attend_whole_kernel<Code, NI, 16, 4>
+                        : p.waves == 8 ? (const void*)attend_whole_kernel<Code, NI, 16, 8> : (const void*)attend_whole_kernel<Code, NI, 16, 16>;
   }
+  return p.rows == 16 ? (const void*)attend_kernel<Code, NI, 16, 4> : (const void*)attend_kernel<Code, NI, 32, 4>;
 }
+template <typename Code>
+static const void* attend_of(int ni, const Plan& p) {
+  return ni == 1 ? attend_of<Code, 1>(p) : ni == 2 ? attend_of<Code, 2>(p) : ni == 3 ? attend_of<Code, 3>(p) : attend_of<Code, 4>(p);
+}
+template <int ROWS>
 static const void* join_of(int ni) {
-  switch (ni) {
-    case 1: return (const void*)join_kernel<1>;
-    case 2: return (const void*)join_kernel<2>;
-    case 3: return (const void*)join_kernel<3>;
-    default: return (const void*)join_kernel<4>;
-  }
+  return ni == 1 ? (const void*)join_kernel<1, ROWS> : ni == 2 ? (const void*)join_kernel<2, ROWS> : ni == 3 ? (const void*)join_kernel<3, ROWS> : (const void*)join_kernel<4, ROWS>;
 }
 
 }  // namespace pages
@@ -502,7 +695,7 @@ using namespace tmac::pages;
 
 extern "C" size_t tmac_pages_attend_workspace_bytes(const tmac_attn_desc* desc, const tmac_pages* p, const tmac_pages_batch* batch) {
   if (!pages_ok(p) || !batch_ok(batch) || !desc_ok(desc, p) || !supported(p, batch)) return 0;
-  const Plan plan = plan_of(p, batch);
+  const Plan plan = plan_of(desc, p, batch);
   return plan.bases + plan.parts;
 }
 
@@ -512,8 +705,8 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   if (batch->S == 0 || batch->T == 0) return TMAC_OK;
   if (!pages_set(p) || !batch_set(batch) || !attn::rows_ok(q, false, true, true) || !attn::rows_ok(out, false, true, true)) return TMAC_EINVAL;
   if (!supported(p, batch) || (int64_t)batch->T * desc->Hq > (1 << 30)) return TMAC_EUNSUPPORTED;
-  if (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return TMAC_EINVAL;
-  const Plan plan = plan_of(p, batch);
+  const Plan plan = plan_of(desc, p, batch);
+  if (!plan.whole && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15))) return TMAC_EINVAL;
   if (workspace_bytes < plan.bases + plan.parts) return TMAC_ESIZE;
   AttendArgs a = {};
   a.pages = view_of(p), a.batch = view_of(batch);
@@ -524,10 +717,9 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.bases);
   a.c = desc->scale * 1.44269504088896340736f;
   a.Hq = desc->Hq, a.G = desc->Hq / desc->Hkv, a.bf16 = desc->elem == TMAC_ELEM_BF16;
-  a.workgroups = plan.workgroups, a.least = 8;
+  a.workgroups = plan.workgroups, a.least = plan.least, a.tiles = plan.tiles;
   const int ni = (p->D + 31) / 32;
-  const void* kernel = p->code == TMAC_CODE_I8 ? attend_of<I8, 4>(ni) : attend_of<E4M3, 4>(ni);
-  const tmac_status st = launch(kernel, plan.workgroups, 64 * plan.waves, &a, stream);
-  if (st != TMAC_OK) return st;
-  return launch(join_of(ni), ((int64_t)batch->T * desc->Hq + 3) / 4, 256, &a, stream);
+  const tmac_status st = launch(p->code == TMAC_CODE_I8 ? attend_of<I8>(ni, plan) : attend_of<E4M3>(ni, plan), plan.workgroups, 64 * plan.waves, &a, stream);
+  if (st != TMAC_OK || plan.whole) return st;
+  return launch(plan.rows == 16 ? join_of<16>(ni) : join_of<32>(ni), ((int64_t)batch->T * desc->Hq + 3) / 4, 256, &a, stream);
 }

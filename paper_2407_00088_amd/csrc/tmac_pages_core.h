@@ -66,7 +66,8 @@ struct Batch {
 };
 // One sequence: rows [row0, row0 + n) are tokens [first, len), where a token below 0 is none.
 struct Sequence {
-  int row0, n, len, first;
+  int row0 = 0, n = 0, len = 0, first = 0;
+  Sequence() = default;
   __device__ __forceinline__ Sequence(const Batch& b, int s) {
     row0 = b.start(s);
     n = max(0, b.start(s + 1) - row0);
