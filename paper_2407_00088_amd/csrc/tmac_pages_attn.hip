@@ -37,8 +37,10 @@ struct AttendArgs {
   float* parts;    // sums of pieces
   float c;         // scale log2 e
   int Hq, G, bf16;
+  int rows_from, rows_to; // sequences of so many rows (a key head) are this launch's
   int workgroups, least;  // that share the units, and how many at least each
-  int tiles;              // that a sequence may have, where every segment has a workgroup
+  int spare;              // units that a segment counts more than it has
+  int tiles;              // that a sequence may have (all sequences: attend_tiles_kernel), where every segment has a workgroup
 };
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -74,8 +76,9 @@ __device__ __forceinline__ h8 halves_of<I8>(uint32_t a, uint32_t b) {
 
 // --- which work is whose --------------------------------------------------------------------------------------------------------------
 //
-// A sequence of r rows (a key head) has tiles = ceil(r / ROWS), for each of them the blocks of its tokens: units (head, tile, block) in
-// this order, sequence after sequence.  A segment is one (sequence, head, tile).
+// A sequence of r rows (a key head) has tiles = ceil(r / ROWS), for each of them the blocks of its tokens (of 32; of 64 where a tile has 128
+// rows): units (head, tile, block) in this order, sequence after sequence.  A segment is one (sequence, head, tile).  What a segment costs
+// beside its blocks (its queries, first loads, the meeting of its sums) counts as `spare` units before the first.
 
 struct Work {
   Sequence seq;
@@ -85,10 +88,12 @@ struct Work {
   static __device__ __forceinline__ Work of(const AttendArgs& a, const Sequence& seq) {
     Work w{seq};
     w.rows = min(seq.n, a.batch.most) * a.G;
+    if (w.rows < a.rows_from || w.rows > a.rows_to) w.rows = 0;
     w.tiles = (w.rows + ROWS - 1) / ROWS;
     w.held = (int)min((int64_t)seq.len, (int64_t)a.batch.width * BT << a.pages.shift);
-    w.blocks = max(1, (w.held + BT - 1) / BT);
-    w.units = (int64_t)a.pages.Hkv * w.tiles * w.blocks;
+    constexpr int TOKENS = ROWS == 128 ? 2 * BT : BT;
+    w.blocks = max(1, (w.held + TOKENS - 1) / TOKENS);
+    w.units = (int64_t)a.pages.Hkv * w.tiles * (w.blocks + a.spare);
     return w;
   }
 };
@@ -188,6 +193,8 @@ struct Plane {
   __device__ __forceinline__ Plane(const char* at, int bytes) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), (short)0, bytes, 0x00020000)) {}
   // (read once: past the caches)
   __device__ __forceinline__ u4 load16(int lane, int fixed) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane + fixed, 0, 2)); }
+  // (the others of the head's tiles read it too)
+  __device__ __forceinline__ u4 load16_kept(int lane) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, 0, 0)); }
   __device__ __forceinline__ u2 load8(int lane, int fixed) const { return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane + fixed, 0, 2)); }
 };
 
@@ -529,16 +536,15 @@ __global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? (WAVES == 16 ? 4 : 3) : 2)
   run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
 }
 
-// A workgroup an equal share of all units, in order: a segment that several of them meet is joined afterwards.
-template <typename Code, int NI, int ROWS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(const AttendArgs a) {
-  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
-  __shared__ int numbers[WAVES][3][64];  // of 64 sequences: Sequence's row0, n, len
+// A workgroup's equal share of all units, in order: piece(work, sequence, head, tile, first and last block, whether that is the whole segment, whether there
+// was a piece before).  A segment that several workgroups meet is joined afterwards.  numbers: of 64 sequences, Sequence's row0, n, len.
+template <int ROWS, typename Piece>
+__device__ __forceinline__ void walk_share(const AttendArgs& a, int (*numbers)[64], Piece&& piece) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), S = a.batch.S;
   auto units_of = [&](int s0, bool keep) {
     Sequence seq;
     if (s0 + lane < S) seq = Sequence(a.batch, s0 + lane);
-    if (keep) numbers[wave][0][lane] = seq.row0, numbers[wave][1][lane] = seq.n, numbers[wave][2][lane] = seq.len;
+    if (keep) numbers[0][lane] = seq.row0, numbers[1][lane] = seq.n, numbers[2][lane] = seq.len;
     return Work::of<ROWS>(a, seq).units;
   };
   int64_t u, end, local;
@@ -573,8 +579,8 @@ __global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(
   bool again = false;
   while (u < end && s0 + at < S) {
     Sequence seq;
-    seq.row0 = __builtin_amdgcn_readfirstlane(numbers[wave][0][at]), seq.n = __builtin_amdgcn_readfirstlane(numbers[wave][1][at]);
-    seq.len = __builtin_amdgcn_readfirstlane(numbers[wave][2][at]), seq.first = seq.len - seq.n;
+    seq.row0 = __builtin_amdgcn_readfirstlane(numbers[0][at]), seq.n = __builtin_amdgcn_readfirstlane(numbers[1][at]);
+    seq.len = __builtin_amdgcn_readfirstlane(numbers[2][at]), seq.first = seq.len - seq.n;
     const Work work = Work::of<ROWS>(a, seq);
     if (local >= work.units) {
       local = 0;
@@ -584,16 +590,203 @@ __global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(
       }
       continue;
     }
-    const int segment = (int)(local / work.blocks);
-    const int begin = (int)(local - (int64_t)segment * work.blocks), stop = (int)min((int64_t)work.blocks, begin + (end - u));
-    const int head = segment / work.tiles, tile = segment % work.tiles;
-    const bool whole = begin == 0 && stop == work.blocks;
-    run_piece<Code, NI, ROWS, WAVES>(a, work, s0 + at, head, tile, begin, stop,
-                                     whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(ROWS, NI * 32), shared, again);
-    again = true;
-    u += stop - begin;
-    local += stop - begin;
+    const int whole = work.blocks + a.spare, segment = (int)(local / whole);
+    const int from = (int)(local - (int64_t)segment * whole), to = (int)min((int64_t)whole, from + (end - u));
+    if (to > a.spare) {
+      const int begin = max(0, from - a.spare), stop = to - a.spare;
+      piece(work, s0 + at, segment / work.tiles, segment % work.tiles, begin, stop, begin == 0 && stop == work.blocks, again);
+      again = true;
+    }
+    u += to - from;
+    local += to - from;
   }
+}
+
+template <typename Code, int NI, int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(const AttendArgs a) {
+  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
+  __shared__ int numbers[WAVES][3][64];
+  walk_share<ROWS>(a, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
+    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop,
+                                     whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(ROWS, NI * 32), shared, again);
+  });
+}
+
+// --- many rows ------------------------------------------------------------------------------------------------------------------------------
+//
+// 128 rows a workgroup, 32 a wavefront: stages of 64 tokens are brought to fp16 once for all four, on their way from registers to LDS, two
+// stages there: one is multiplied while the next is made and the one after that is on its way from memory.
+
+constexpr int TILE = 128, STAGE = 64;
+
+template <int NI>
+struct Staged {
+  // Bytes: keys of a block [2 NI chunks][2][32 tokens] of 16 bytes, values [NI runs][2][2 halves][32 elements]
+  static constexpr int PLANE = NI * 2048, BLOCK = 2 * PLANE, BYTES = 2 * BLOCK;
+};
+
+template <typename Code, int NI>
+__device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, int s, int head, int tile, int begin, int stop, float* part, char* shared, bool again) {
+  typedef Staged<NI> L;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // (as in run_piece)
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  const Sequence& seq = work.seq;
+  const int in = wave * 32 + (lane & 31), r = tile * TILE + in, i = r / a.G, row = seq.row0 + i, hq = head * a.G + r - i * a.G;
+  const bool valid = r < work.rows;
+  // tokens that the wavefront's first and last rows see
+  const int first = tile * TILE + wave * 32, last = min(first + 31, work.rows - 1);
+  const int least = clamp_to(seq.first + first / a.G + 1, work.held), most = first < work.rows ? clamp_to(seq.first + last / a.G + 1, work.held) : 0;
+  const int32_t* table = a.batch.row(s);
+  const int plane = a.pages.plane_bytes(), chunks = a.pages.chunks;
+  // a stage's raw codes, 16 bytes of each plane a thread, and scales
+  u4 raw[2][2];
+  f2 scales[2], next_scales[2];
+  auto fetch = [&](int stage) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int block = stage * 2 + b;
+      const int64_t unit = block * BT < work.held ? a.pages.unit_of(table, a.batch.width, block, head) : -1;
+      const bool there = unit >= 0;
+      const char* at = a.pages.keys(there ? unit : 0);
+      raw[b][0] = Plane(at, there ? plane : 0).load16_kept(tid * 16);
+      raw[b][1] = Plane(at + plane, there ? plane : 0).load16_kept(tid * 16);
+      // (a block that is not there: no token of it is seen)
+      next_scales[b] = there ? *reinterpret_cast<const f2*>(a.pages.scales + unit * 2) : f2{1.0f, -1.0f};
+    }
+  };
+  // where this thread's 16 codes of either plane go
+  const int run = tid >> 6, n = value_run(chunks, run * 32), in_run = tid & 63;
+  const uint32_t k_to = ((tid >> 5) * 64 + (tid & 31)) * 16, v_to = (run * 128 + (in_run / n) * 32 + in_run % n) * 16;
+  const bool k_is = tid < NI * 64, v_is = tid < chunks * 32;
+  auto make = [&](int place) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      char* to = shared + place * L::BYTES + b * L::BLOCK;
+      if (k_is) {
+        *reinterpret_cast<h8*>(to + k_to) = halves_of<Code>(raw[b][0][0], raw[b][0][1]);
+        *reinterpret_cast<h8*>(to + k_to + 512) = halves_of<Code>(raw[b][0][2], raw[b][0][3]);
+      }
+      if (v_is) {
+        *reinterpret_cast<h8*>(to + L::PLANE + v_to) = halves_of<Code>(raw[b][1][0], raw[b][1][1]);
+        *reinterpret_cast<h8*>(to + L::PLANE + v_to + 1024) = halves_of<Code>(raw[b][1][2], raw[b][1][3]);
+      }
+      scales[b] = next_scales[b];
+    }
+  };
+  Rows<Code, NI, 32> x;
+  x.lane = lane;
+  fetch(begin);
+  x.begin(a, a.q + row * a.q_token + hq * a.q_head, valid, valid ? clamp_to(seq.first + i + 1, work.held) : 0x7fffffff);
+  if (again) __syncthreads();  // (the stages before have been read)
+  make(0);
+  if (begin + 1 < stop) fetch(begin + 1);
+  __syncthreads();
+  int place = 0;
+  const char* const k_from = shared + (half * 64 + (lane & 31)) * 16;
+  const char* const v_from = shared + L::PLANE + (half * 32 + (lane & 31)) * 16;
+  for (int stage = begin; stage < stop; ++stage) {
+    const int at = stage * STAGE;
+    if (at < most) {
+      const char* k = k_from + place * L::BYTES;
+      const char* v = v_from + place * L::BYTES;
+      f16x sc[2] = {(f16x)(0.0f), (f16x)(0.0f)};
+#pragma unroll
+      for (int t = 0; t < NI; ++t)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(k + b * L::BLOCK + t * 2048 + y * 512), x.q.q[t][y], sc[b], 0, 0, 0);
+      if (at + STAGE > least || scales[0][1] < 0.0f || scales[1][1] < 0.0f) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int upto = scales[b][1] < 0.0f ? -1 : x.q.sees - at - b * BT - 4 * half;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[b][r] = (r >> 2) * 8 + (r & 3) < upto ? sc[b][r] : -INFINITY;
+        }
+      }
+      float scale[2], base[2], top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        float mx = sc[b][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
+        scale[b] = scales[b][0] * x.q.c, base[b] = __builtin_amdgcn_logf(fabsf(scales[b][1]));
+        top = fmaxf(top, __builtin_fmaf(mx, scale[b], base[b]));
+      }
+      top = max_halves(top);
+      float alpha;
+      if (outgrown(top, x.m, alpha)) {
+#pragma unroll
+        for (int d = 0; d < NI; ++d) x.o[d] *= alpha;
+        x.l *= alpha;
+      }
+      const float m0 = x.m == -INFINITY ? 0.0f : x.m;
+      h8 p[2][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        base[b] -= m0;
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][r], scale[b], base[b]));
+          sum[r & 1] += e;
+          p[b][r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)e;
+        }
+        x.l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-(base[b] + m0)), x.l);
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int d = 0; d < NI; ++d)
+            x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(v + b * L::BLOCK + d * 2048 + y * 1024), p[b][y], x.o[d], 0, 0, 0);
+    }
+    if (stage + 1 < stop) {
+      place ^= 1;
+      make(place);
+      if (stage + 2 < stop) fetch(stage + 2);
+      __syncthreads();
+    }
+  }
+  const float l = x.sum();
+  x.each([&](int d, const f4& o) {
+    if (!valid) return;
+    if (!part) {
+      put_out(a, row, hq, d, o, x.m, l);
+    } else {
+      *reinterpret_cast<f4*>(part + 2 * TILE + in * (NI * 32) + d) = o;
+      if (d == 0) part[in * 2] = x.m, part[in * 2 + 1] = l;
+    }
+  });
+}
+
+// A workgroup a tile: of sequences in the order of their starts, tiles' slots from starts[s] G / 128 + s on.  Neighbouring workgroups, which
+// go to neighbouring XCDs, take different key heads, so that a head's pages are in one XCD's cache; last tiles, which see most, first.
+template <typename Code, int NI>
+__global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) char shared[2 * Staged<NI>::BYTES];
+  const int head = blockIdx.x % a.pages.Hkv, slot = a.tiles - 1 - (int)(blockIdx.x / a.pages.Hkv);
+  auto from = [&](int i) { return (int64_t)a.batch.start(i) * a.G / TILE + i; };
+  const int s = count_up_to(a.batch.S, from, slot);
+  if (s >= a.batch.S) return;
+  const int tile = slot - (int)from(s);
+  const Work work = Work::of<TILE>(a, Sequence(a.batch, s));
+  if (tile >= work.tiles || work.units == 0) return;
+  const int sees = clamp_to(work.seq.first + (min((tile + 1) * TILE, work.rows) - 1) / a.G + 1, work.held);
+  run_tile<Code, NI>(a, work, s, head, tile, 0, max(1, (sees + STAGE - 1) / STAGE), nullptr, shared, false);
+}
+
+template <typename Code, int NI>
+__global__ __launch_bounds__(256, 2) void attend_tiles_shared_kernel(const AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) char shared[2 * Staged<NI>::BYTES];
+  __shared__ int numbers[4][3][64];
+  walk_share<TILE>(a, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
+    run_tile<Code, NI>(a, work, s, head, tile, begin, stop,
+                       whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(TILE, NI * 32), shared, again);
+  });
 }
 
 // Rows of segments that several workgroups met: a wavefront a row, two elements a lane.
@@ -609,7 +802,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   const int head = hq / a.G, r = (row - work.seq.row0) * a.G + hq - head * a.G;
   if (row < work.seq.row0 || r >= work.rows) return;
   const int64_t units = a.bases[a.batch.S], sharers = a.bases[a.batch.S + 1];
-  const int64_t from = a.bases[s] + ((int64_t)head * work.tiles + r / ROWS) * work.blocks;
+  const int64_t from = a.bases[s] + ((int64_t)head * work.tiles + r / ROWS) * (work.blocks + a.spare) + a.spare;
   const int64_t w0 = owner_of(units, sharers, from), w1 = owner_of(units, sharers, from + work.blocks - 1);
   if (w0 == w1) return;
   const int in = r % ROWS, d = lane * 2;
@@ -644,47 +837,83 @@ static bool desc_ok(const tmac_attn_desc* d, const tmac_pages* p) {
          std::isfinite(d->scale) && d->scale > 0 && d->causal == 1 && !d->reserved[0] && !d->reserved[1];
 }
 
-struct Plan {
-  bool whole;  // every segment by a workgroup of its own
-  int rows, waves, workgroups, least, tiles;
+// One launch over the sequences of a kind, and the one that joins what it leaves.
+struct Side {
+  bool on, whole;  // whole: every segment by a workgroup of its own, nothing to join
+  int rows, waves, workgroups, least, spare, tiles, rows_from, rows_to;
   size_t bases, parts;  // bytes
+  size_t bytes() const { return bases + parts; }
 };
+struct Plan {
+  Side few, many;
+};
+static void share(Side& x, const tmac_pages* p, const tmac_pages_batch* b) {
+  x.bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
+  x.parts = (size_t)x.workgroups * 2 * part_floats(x.rows, (p->D + 31) / 32 * 32) * 4;
+}
 static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
   Plan plan = {};
-  const int64_t most = (int64_t)view_of(b).most * (d->Hq / d->Hkv);  // rows of a sequence and head
-  plan.rows = most <= 16 ? 16 : 32;
-  plan.tiles = (int)((most + plan.rows - 1) / plan.rows);
-  const int64_t segments = (int64_t)b->S * p->Hkv * plan.tiles, blocks = (int64_t)b->width * p->page / BT;
-  plan.whole = blocks <= 128 && segments * 64 * 16 <= 0xffffffff;
-  if (plan.whole) {
-    plan.waves = plan.rows == 32 ? 4 : segments >= 1024 ? 4 : segments >= 512 ? 8 : 16;
-    plan.workgroups = (int)segments;
-    return plan;
+  const int G = d->Hq / d->Hkv;
+  const int64_t most = (int64_t)view_of(b).most * G;  // rows of a sequence and head
+  const int64_t blocks = (int64_t)b->width * p->page / BT;
+  Side& few = plan.few;
+  few.rows = most > 16 && most <= 64 ? 32 : 16;
+  few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
+  few.on = most <= 64 || (b->S > 1 && G <= 16);
+  few.tiles = few.rows == 32 ? 2 : 1;
+  const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
+  few.whole = blocks <= 128 && segments * 64 * 16 <= 0xffffffff;
+  if (few.whole) {
+    few.waves = few.rows == 32 ? 4 : segments >= 1024 ? 4 : segments >= 512 ? 8 : 16;
+    few.workgroups = (int)segments;
+  } else {
+    few.waves = 4, few.workgroups = few.rows == 16 ? 768 : 512, few.least = 8, few.spare = 16;
+    share(few, p, b);
   }
-  plan.waves = 4;
-  plan.workgroups = plan.rows == 16 ? 768 : 512;
-  plan.least = 8;
-  plan.bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
-  plan.parts = (size_t)plan.workgroups * 2 * part_floats(plan.rows, (p->D + 31) / 32 * 32) * 4;
+  Side& many = plan.many;
+  many.on = most > 64;
+  if (many.on) {
+    many.rows = TILE, many.waves = 4;
+    many.rows_from = few.on ? 17 : 1, many.rows_to = 0x7fffffff;
+    const int64_t slots = (int64_t)b->T * G / TILE + b->S, least = std::max<int64_t>(0, ((int64_t)b->T * G - (few.on ? 16 * (int64_t)b->S : 0)) / TILE) * p->Hkv;
+    many.whole = (least >= 256 || blocks <= 32) && slots * p->Hkv * 256 <= 0xffffffff;
+    many.tiles = (int)slots;
+    many.workgroups = many.whole ? (int)(slots * p->Hkv) : 512;
+    if (!many.whole) {
+      many.least = 4, many.spare = 2;
+      share(many, p, b);
+    }
+  }
   return plan;
 }
 
 template <typename Code, int NI>
-static const void* attend_of(const Plan& p) {
-  if (p.whole) {
-    if (p.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
-    return p.waves == 4 ? (const void*)attend_whole_kernel<Code, NI, 16, 4>
-                        : p.waves == 8 ? (const void*)attend_whole_kernel<Code, NI, 16, 8> : (const void*)attend_whole_kernel<Code, NI, 16, 16>;
+static const void* attend_of(const Side& x) {
+  if (x.rows == TILE) return x.whole ? (const void*)attend_tiles_kernel<Code, NI> : (const void*)attend_tiles_shared_kernel<Code, NI>;
+  if (x.whole) {
+    if (x.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
+    return x.waves == 4 ? (const void*)attend_whole_kernel<Code, NI, 16, 4>
+                        : x.waves == 8 ? (const void*)attend_whole_kernel<Code, NI, 16, 8> : (const void*)attend_whole_kernel<Code, NI, 16, 16>;
   }
-  return p.rows == 16 ? (const void*)attend_kernel<Code, NI, 16, 4> : (const void*)attend_kernel<Code, NI, 32, 4>;
+  return x.rows == 16 ? (const void*)attend_kernel<Code, NI, 16, 4> : (const void*)attend_kernel<Code, NI, 32, 4>;
 }
 template <typename Code>
-static const void* attend_of(int ni, const Plan& p) {
-  return ni == 1 ? attend_of<Code, 1>(p) : ni == 2 ? attend_of<Code, 2>(p) : ni == 3 ? attend_of<Code, 3>(p) : attend_of<Code, 4>(p);
+static const void* attend_of(int ni, const Side& x) {
+  return ni == 1 ? attend_of<Code, 1>(x) : ni == 2 ? attend_of<Code, 2>(x) : ni == 3 ? attend_of<Code, 3>(x) : attend_of<Code, 4>(x);
 }
-template <int ROWS>
-static const void* join_of(int ni) {
-  return ni == 1 ? (const void*)join_kernel<1, ROWS> : ni == 2 ? (const void*)join_kernel<2, ROWS> : ni == 3 ? (const void*)join_kernel<3, ROWS> : (const void*)join_kernel<4, ROWS>;
+template <int NI>
+static const void* join_of(int rows) {
+  return rows == 16 ? (const void*)join_kernel<NI, 16> : rows == 32 ? (const void*)join_kernel<NI, 32> : (const void*)join_kernel<NI, TILE>;
+}
+static tmac_status run_side(AttendArgs a, const Side& x, int code, char* workspace, void* stream) {
+  a.bases = reinterpret_cast<int64_t*>(workspace);
+  a.parts = reinterpret_cast<float*>(workspace + x.bases);
+  a.rows_from = x.rows_from, a.rows_to = x.rows_to, a.workgroups = x.workgroups, a.least = x.least, a.spare = x.spare, a.tiles = x.tiles;
+  const int ni = (a.pages.D + 31) / 32;
+  const tmac_status st = launch(code == TMAC_CODE_I8 ? attend_of<I8>(ni, x) : attend_of<E4M3>(ni, x), x.workgroups, 64 * x.waves, &a, stream);
+  if (st != TMAC_OK || x.whole) return st;
+  const void* join = ni == 1 ? join_of<1>(x.rows) : ni == 2 ? join_of<2>(x.rows) : ni == 3 ? join_of<3>(x.rows) : join_of<4>(x.rows);
+  return launch(join, ((int64_t)a.batch.T * a.Hq + 3) / 4, 256, &a, stream);
 }
 
 }  // namespace pages
@@ -696,7 +925,7 @@ using namespace tmac::pages;
 extern "C" size_t tmac_pages_attend_workspace_bytes(const tmac_attn_desc* desc, const tmac_pages* p, const tmac_pages_batch* batch) {
   if (!pages_ok(p) || !batch_ok(batch) || !desc_ok(desc, p) || !supported(p, batch)) return 0;
   const Plan plan = plan_of(desc, p, batch);
-  return plan.bases + plan.parts;
+  return plan.few.bytes() + plan.many.bytes();
 }
 
 extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_pages* p, const tmac_pages_batch* batch, const tmac_view* q,
@@ -706,20 +935,20 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   if (!pages_set(p) || !batch_set(batch) || !attn::rows_ok(q, false, true, true) || !attn::rows_ok(out, false, true, true)) return TMAC_EINVAL;
   if (!supported(p, batch) || (int64_t)batch->T * desc->Hq > (1 << 30)) return TMAC_EUNSUPPORTED;
   const Plan plan = plan_of(desc, p, batch);
-  if (!plan.whole && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15))) return TMAC_EINVAL;
-  if (workspace_bytes < plan.bases + plan.parts) return TMAC_ESIZE;
+  const size_t need = plan.few.bytes() + plan.many.bytes();
+  if (need && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15))) return TMAC_EINVAL;
+  if (workspace_bytes < need) return TMAC_ESIZE;
   AttendArgs a = {};
   a.pages = view_of(p), a.batch = view_of(batch);
   a.q = static_cast<const char*>(q->data), a.out = static_cast<char*>(out->data);
   a.q_token = q->token * 2, a.q_head = q->head * 2, a.out_token = out->token * 2, a.out_head = out->head * 2;
   a.lse = lse_dev;
-  a.bases = static_cast<int64_t*>(workspace_dev);
-  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.bases);
   a.c = desc->scale * 1.44269504088896340736f;
   a.Hq = desc->Hq, a.G = desc->Hq / desc->Hkv, a.bf16 = desc->elem == TMAC_ELEM_BF16;
-  a.workgroups = plan.workgroups, a.least = plan.least, a.tiles = plan.tiles;
-  const int ni = (p->D + 31) / 32;
-  const tmac_status st = launch(p->code == TMAC_CODE_I8 ? attend_of<I8>(ni, plan) : attend_of<E4M3>(ni, plan), plan.workgroups, 64 * plan.waves, &a, stream);
-  if (st != TMAC_OK || plan.whole) return st;
-  return launch(plan.rows == 16 ? join_of<16>(ni) : join_of<32>(ni), ((int64_t)batch->T * desc->Hq + 3) / 4, 256, &a, stream);
+  char* const workspace = static_cast<char*>(workspace_dev);
+  if (plan.few.on) {
+    const tmac_status st = run_side(a, plan.few, p->code, workspace, stream);
+    if (st != TMAC_OK || !plan.many.on) return st;
+  }
+  return run_side(a, plan.many, p->code, workspace + plan.few.bytes(), stream);
 }

@@ -299,15 +299,22 @@ ATTENDS = [
     ([2] * 70, [40 + 3 * i for i in range(70)], 2, 1, 32, 32),
     ([300, 17], [300, 400], 8, 1, 128, 64),
     ([100], [2000], 2, 2, 100, 64),
+    # wide tables: shares of the work that cross segments
+    ([200], [3000], 4, 2, 128, 64, 3),
+    ([70, 1, 9, 0, 2], [1500, 2500, 33, 40, 2], 8, 4, 100, 64, 90),
+    ([1] * 67, [(i * 37) % 300 + 1 for i in range(67)], 4, 1, 64, 32, 200),
+    ([4, 2, 1], [900, 3, 700], 8, 2, 80, 32, 200),
+    ([20, 1, 18], [1000, 1, 18], 3, 3, 36, 128, 60),
+    ([1, 2], [600, 40], 71, 1, 64, 64, 100),
 ]
 
 
 @pytest.mark.parametrize("code,dtype", [("i8", F16), ("e4m3", BF16), ("e4m3", F16), ("i8", BF16)])
 @pytest.mark.parametrize("case", range(len(ATTENDS)))
 def test_attend(case, code, dtype):
-    n, lens, Hq, Hkv, D, page = ATTENDS[case]
+    n, lens, Hq, Hkv, D, page, *extra = ATTENDS[case]
     g = gen(100 + case)
-    cache, table = filled(lens, Hkv, D, page, code, dtype, g, Hq=Hq)
+    cache, table = filled(lens, Hkv, D, page, code, dtype, g, Hq=Hq, extra=(extra or [1])[0])
     T = sum(n)
     q = (torch.randn((T, Hq, D), generator=g) * 1.5).to(dtype)
     cu = starts(n)
