@@ -33,14 +33,17 @@ struct AttendArgs {
   char* out;
   int64_t q_token, q_head, out_token, out_head;  // bytes
   float* lse;
-  int64_t* bases;  // [S + 1] units before each sequence, then the number of workgroups that have some
-  float* parts;    // sums of pieces
-  float c;         // scale log2 e
+  float c;  // scale log2 e
   int Hq, G, bf16;
-  int rows_from, rows_to; // sequences of so many rows (a key head) are this launch's
-  int workgroups, least;  // that share the units, and how many at least each
-  int spare;              // units that a segment counts more than it has
-  int tiles;              // that a sequence may have (all sequences: attend_tiles_kernel), where every segment has a workgroup
+  // The sequences of one kind, and how their work is dealt out
+  struct Side {
+    int rows_from, rows_to;  // sequences of so many rows (a key head)
+    int workgroups, least;   // that share the units, and how many at least each
+    int spare;               // units that a segment counts more than it has
+    int tiles;               // that a sequence may have (many rows: all sequences), where every segment has a workgroup
+    int64_t* bases;          // [S + 1] units before each sequence, then the units of a share
+    float* parts;            // sums of pieces
+  } few, many;
 };
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -85,15 +88,15 @@ struct Work {
   int rows, tiles, blocks, held;  // held: tokens that can be seen
   int64_t units;
   template <int ROWS>
-  static __device__ __forceinline__ Work of(const AttendArgs& a, const Sequence& seq) {
+  static __device__ __forceinline__ Work of(const AttendArgs& a, const AttendArgs::Side& side, const Sequence& seq) {
     Work w{seq};
     w.rows = min(seq.n, a.batch.most) * a.G;
-    if (w.rows < a.rows_from || w.rows > a.rows_to) w.rows = 0;
+    if (w.rows < side.rows_from || w.rows > side.rows_to) w.rows = 0;
     w.tiles = (w.rows + ROWS - 1) / ROWS;
     w.held = (int)min((int64_t)seq.len, (int64_t)a.batch.width * BT << a.pages.shift);
     constexpr int TOKENS = ROWS == 128 ? 2 * BT : BT;
     w.blocks = max(1, (w.held + TOKENS - 1) / TOKENS);
-    w.units = (int64_t)a.pages.Hkv * w.tiles * (w.blocks + a.spare);
+    w.units = (int64_t)a.pages.Hkv * w.tiles * (w.blocks + side.spare);
     return w;
   }
 };
@@ -113,12 +116,10 @@ __device__ __forceinline__ int64_t inclusive(int64_t x) {
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ float lane_value(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
 
-// Workgroups that have units: all, or as many as get `least` each.
-__device__ __forceinline__ int64_t sharing(const AttendArgs& a, int64_t units) {
-  return max((int64_t)1, min((int64_t)a.workgroups, (units + a.least - 1) / a.least));
+// Workgroup w has the units from w times the share on.
+__device__ __forceinline__ int64_t share_of(const AttendArgs::Side& x, int64_t units) {
+  return max((int64_t)x.least, (units + x.workgroups - 1) / x.workgroups);
 }
-__device__ __forceinline__ int64_t share_from(int64_t units, int64_t sharers, int64_t w) { return units * w / sharers; }
-__device__ __forceinline__ int64_t owner_of(int64_t units, int64_t sharers, int64_t u) { return ((u + 1) * sharers - 1) / units; }
 
 // Sums of pieces: maximum and sum of every row, then W values each.  A workgroup leaves at most two: of a segment that began before it
 // (slot 0) and of one that goes on after it (slot 1).
@@ -204,7 +205,7 @@ struct Rows;
 // 32 rows: v_mfma_f32_32x32x16, row lane & 31.
 template <typename Code, int NI>
 struct Rows<Code, NI, 32> {
-  static constexpr int NK = NI, NV = NI;
+  static constexpr int NK = NI, NV = NI, DEPTH = 1;
   typedef u4 KRaw;
   typedef u4 VRaw;
   Queries<NI> q;
@@ -296,7 +297,7 @@ struct Rows<Code, NI, 32> {
 // 16 rows: v_mfma_f32_16x16x32, row lane & 15.  Half the work of 32 for what is read, and half the registers.
 template <typename Code, int NI>
 struct Rows<Code, NI, 16> {
-  static constexpr int NQ = (NI + 1) / 2, NK = 2 * NQ, NV = 2 * NI;
+  static constexpr int NQ = (NI + 1) / 2, NK = 2 * NQ, NV = 2 * NI, DEPTH = 2;
   typedef u4 KRaw;
   typedef u2 VRaw;
   Queries<NQ> q;
@@ -408,13 +409,14 @@ struct Blocks {
 };
 
 // Blocks first, first + step, ... before end for one wavefront's rows, whose queries q() loads.  least: tokens that every row sees.
-// The next block's keys are requested as soon as this one's have met the queries, its values as soon as they have met the exponentials.
+// R::DEPTH blocks are on their way: a block's keys are requested as soon as the ones in their registers have met the queries, its values as soon as
+// those have met the exponentials.
 template <typename R, typename Q>
 __device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int32_t* table, int head, int first, int end, int step, int least, Q&& q) {
   const int lane = w.lane, plane = a.pages.plane_bytes();
   const bool odd = a.pages.chunks & 1;
-  typename R::KRaw k[R::NK];
-  typename R::VRaw v[R::NV];
+  typename R::KRaw k[R::DEPTH][R::NK];
+  typename R::VRaw v[R::DEPTH][R::NV];
   bool loaded = false;
   for (; first < end; first += 64 * step) {
     Blocks blocks(a, table, head, first, end, step, lane);
@@ -423,25 +425,33 @@ __device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int3
     uint64_t left = __ballot(blocks.unit >= 0);
     if (!left) continue;
     auto take = [&] {
+      if (!left) return -1;
       const int n = __builtin_ctzll(left);
       left &= left - 1;
       return n;
     };
-    auto load_k = [&](int n) { R::load_k(k, Plane(blocks.at(a, n), plane), lane); };
-    auto load_v = [&](int n) { R::load_v(v, Plane(blocks.at(a, n) + plane, plane), lane, odd); };
-    int n = take();
-    load_k(n);
-    blocks.scales(a);
-    load_v(n);
-    while (true) {
-      const int next = left ? take() : -1, at = (first + n * step) * BT;
-      const typename R::Scores s = w.scores(k);
-      if (next >= 0) load_k(next);
-      const typename R::Weights p = w.weigh(s, at, at + BT > least, lane_value(blocks.sk, n), lane_value(blocks.sv, n));
-      w.multiply(v, p);
-      if (next < 0) break;
-      load_v(next);
-      n = next;
+    auto load_k = [&](int j, int n) { R::load_k(k[j], Plane(blocks.at(a, n), plane), lane); };
+    auto load_v = [&](int j, int n) { R::load_v(v[j], Plane(blocks.at(a, n) + plane, plane), lane, odd); };
+    int n[R::DEPTH];
+#pragma unroll
+    for (int j = 0; j < R::DEPTH; ++j) {
+      n[j] = take();
+      if (n[j] >= 0) load_k(j, n[j]);
+      if (j == 0) blocks.scales(a);
+      if (n[j] >= 0) load_v(j, n[j]);
+    }
+    while (n[0] >= 0) {
+#pragma unroll
+      for (int j = 0; j < R::DEPTH; ++j) {
+        if (j && n[j] < 0) break;
+        const int next = take(), at = (first + n[j] * step) * BT;
+        const typename R::Scores s = w.scores(k[j]);
+        if (next >= 0) load_k(j, next);
+        const typename R::Weights p = w.weigh(s, at, at + BT > least, lane_value(blocks.sk, n[j]), lane_value(blocks.sv, n[j]));
+        w.multiply(v[j], p);
+        if (next >= 0) load_v(j, next);
+        n[j] = next;
+      }
     }
   }
   if (!loaded) q();
@@ -528,10 +538,10 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
 
 // A workgroup a segment.
 template <typename Code, int NI, int ROWS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? (WAVES == 16 ? 4 : 3) : 2) void attend_whole_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void attend_whole_kernel(const AttendArgs a) {
   __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
-  const int head = blockIdx.x % a.pages.Hkv, x = blockIdx.x / a.pages.Hkv, tile = x % a.tiles, s = x / a.tiles;
-  const Work work = Work::of<ROWS>(a, Sequence(a.batch, s));
+  const int head = blockIdx.x % a.pages.Hkv, x = blockIdx.x / a.pages.Hkv, tile = x % a.few.tiles, s = x / a.few.tiles;
+  const Work work = Work::of<ROWS>(a, a.few, Sequence(a.batch, s));
   if (tile >= work.tiles) return;
   run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
 }
@@ -539,31 +549,30 @@ __global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? (WAVES == 16 ? 4 : 3) : 2)
 // A workgroup's equal share of all units, in order: piece(work, sequence, head, tile, first and last block, whether that is the whole segment, whether there
 // was a piece before).  A segment that several workgroups meet is joined afterwards.  numbers: of 64 sequences, Sequence's row0, n, len.
 template <int ROWS, typename Piece>
-__device__ __forceinline__ void walk_share(const AttendArgs& a, int (*numbers)[64], Piece&& piece) {
+__device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs::Side& side, int w, int (*numbers)[64], Piece&& piece) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), S = a.batch.S;
   auto units_of = [&](int s0, bool keep) {
     Sequence seq;
     if (s0 + lane < S) seq = Sequence(a.batch, s0 + lane);
     if (keep) numbers[0][lane] = seq.row0, numbers[1][lane] = seq.n, numbers[2][lane] = seq.len;
-    return Work::of<ROWS>(a, seq).units;
+    return Work::of<ROWS>(a, side, seq).units;
   };
   int64_t u, end, local;
   int s0 = 0, at;
   {
     int64_t x = units_of(0, true), upto = inclusive(x), units = shfl64(upto, 63);
     for (int i = 64; i < S; i += 64) units += shfl64(inclusive(units_of(i, false)), 63);
-    const int64_t sharers = sharing(a, units), w = blockIdx.x;
-    if (blockIdx.x == 0 && wave == 0) {
+    const int64_t share = share_of(side, units);
+    if (w == 0 && wave == 0) {
       int64_t before = 0;
       for (int i = 0; i < S; i += 64) {
         const int64_t y = units_of(i, false), to = inclusive(y);
-        if (i + lane < S) a.bases[i + lane] = before + to - y;
+        if (i + lane < S) side.bases[i + lane] = before + to - y;
         before += shfl64(to, 63);
       }
-      if (lane == 0) a.bases[S] = units, a.bases[S + 1] = sharers;
+      if (lane == 0) side.bases[S] = units, side.bases[S + 1] = share;
     }
-    if (w >= sharers) return;
-    u = share_from(units, sharers, w), end = share_from(units, sharers, w + 1);
+    u = share * w, end = min(units, u + share);
     if (u >= end) return;
     // the share's first sequence
     int64_t before = 0;
@@ -581,7 +590,7 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, int (*numbers)[6
     Sequence seq;
     seq.row0 = __builtin_amdgcn_readfirstlane(numbers[0][at]), seq.n = __builtin_amdgcn_readfirstlane(numbers[1][at]);
     seq.len = __builtin_amdgcn_readfirstlane(numbers[2][at]), seq.first = seq.len - seq.n;
-    const Work work = Work::of<ROWS>(a, seq);
+    const Work work = Work::of<ROWS>(a, side, seq);
     if (local >= work.units) {
       local = 0;
       if (++at == 64) {
@@ -590,10 +599,10 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, int (*numbers)[6
       }
       continue;
     }
-    const int whole = work.blocks + a.spare, segment = (int)(local / whole);
+    const int whole = work.blocks + side.spare, segment = (int)(local / whole);
     const int from = (int)(local - (int64_t)segment * whole), to = (int)min((int64_t)whole, from + (end - u));
-    if (to > a.spare) {
-      const int begin = max(0, from - a.spare), stop = to - a.spare;
+    if (to > side.spare) {
+      const int begin = max(0, from - side.spare), stop = to - side.spare;
       piece(work, s0 + at, segment / work.tiles, segment % work.tiles, begin, stop, begin == 0 && stop == work.blocks, again);
       again = true;
     }
@@ -602,14 +611,20 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, int (*numbers)[6
   }
 }
 
+// Where the sums of a share's piece go: slot 0 of a segment that began before the share, slot 1 of one that goes on after it.
+__device__ __forceinline__ float* part_at(const AttendArgs::Side& side, int w, int begin, int floats) { return side.parts + (2 * (int64_t)w + (begin == 0)) * floats; }
+
 template <typename Code, int NI, int ROWS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, ROWS == 16 ? 3 : 2) void attend_kernel(const AttendArgs a) {
-  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
-  __shared__ int numbers[WAVES][3][64];
-  walk_share<ROWS>(a, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
-    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop,
-                                     whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(ROWS, NI * 32), shared, again);
+__device__ __forceinline__ void run_share(const AttendArgs& a, int w, float* shared, int (*numbers)[64]) {
+  walk_share<ROWS>(a, a.few, w, numbers, [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
+    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.few, w, begin, part_floats(ROWS, NI * 32)), shared, again);
   });
+}
+template <typename Code, int NI, int ROWS>
+__global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
+  __shared__ float shared[Meeting<NI, ROWS, 4>::FLOATS];
+  __shared__ int numbers[4][3][64];
+  run_share<Code, NI, ROWS, 4>(a, blockIdx.x, shared, numbers[threadIdx.x >> 6]);
 }
 
 // --- many rows ------------------------------------------------------------------------------------------------------------------------------
@@ -639,20 +654,31 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
   const int least = clamp_to(seq.first + first / a.G + 1, work.held), most = first < work.rows ? clamp_to(seq.first + last / a.G + 1, work.held) : 0;
   const int32_t* table = a.batch.row(s);
   const int plane = a.pages.plane_bytes(), chunks = a.pages.chunks;
-  // a stage's raw codes, 16 bytes of each plane a thread, and scales
+  // places and scales of 32 stages' blocks, one a lane; a stage's raw codes, 16 bytes of each plane a thread
+  const int held_blocks = (work.held + BT - 1) / BT;
+  int placed = begin;
+  auto places = [&] {
+    Blocks x(a, table, head, placed * 2, held_blocks, 1, lane);
+    x.scales(a);
+    if (x.unit < 0) x.sk = 1.0f, x.sv = -1.0f;  // (a block that is not there: no token of it is seen)
+    return x;
+  };
+  Blocks blocks = places();
   u4 raw[2][2];
-  f2 scales[2], next_scales[2];
+  float scales[2][2], next_scales[2][2];
   auto fetch = [&](int stage) {
+    if (stage == placed + 32) {
+      placed = stage;
+      blocks = places();
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int block = stage * 2 + b;
-      const int64_t unit = block * BT < work.held ? a.pages.unit_of(table, a.batch.width, block, head) : -1;
-      const bool there = unit >= 0;
-      const char* at = a.pages.keys(there ? unit : 0);
+      const int n = (stage - placed) * 2 + b;
+      next_scales[b][0] = lane_value(blocks.sk, n), next_scales[b][1] = lane_value(blocks.sv, n);
+      const bool there = lane_value((int)(blocks.unit >> 32), n) >= 0;
+      const char* at = there ? blocks.at(a, n) : a.pages.codes;
       raw[b][0] = Plane(at, there ? plane : 0).load16_kept(tid * 16);
       raw[b][1] = Plane(at + plane, there ? plane : 0).load16_kept(tid * 16);
-      // (a block that is not there: no token of it is seen)
-      next_scales[b] = there ? *reinterpret_cast<const f2*>(a.pages.scales + unit * 2) : f2{1.0f, -1.0f};
     }
   };
   // where this thread's 16 codes of either plane go
@@ -671,7 +697,7 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
         *reinterpret_cast<h8*>(to + L::PLANE + v_to) = halves_of<Code>(raw[b][1][0], raw[b][1][1]);
         *reinterpret_cast<h8*>(to + L::PLANE + v_to + 1024) = halves_of<Code>(raw[b][1][2], raw[b][1][3]);
       }
-      scales[b] = next_scales[b];
+      scales[b][0] = next_scales[b][0], scales[b][1] = next_scales[b][1];
     }
   };
   Rows<Code, NI, 32> x;
@@ -763,71 +789,109 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
   });
 }
 
-// A workgroup a tile: of sequences in the order of their starts, tiles' slots from starts[s] G / 128 + s on.  Neighbouring workgroups, which
-// go to neighbouring XCDs, take different key heads, so that a head's pages are in one XCD's cache; last tiles, which see most, first.
-template <typename Code, int NI>
+// SHARED: equal shares of all stages.  Else a workgroup a tile: of sequences in the order of their starts, tiles' slots from
+// starts[s] G / 128 + s on; neighbouring workgroups, which go to neighbouring XCDs, take different key heads, so that a head's pages are in one XCD's
+// cache; last tiles, which see most, first.  FEW: the first workgroups deal with the sequences of few rows.
+template <typename Code, int NI, bool SHARED, bool FEW>
 __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) char shared[2 * Staged<NI>::BYTES];
-  const int head = blockIdx.x % a.pages.Hkv, slot = a.tiles - 1 - (int)(blockIdx.x / a.pages.Hkv);
-  auto from = [&](int i) { return (int64_t)a.batch.start(i) * a.G / TILE + i; };
-  const int s = count_up_to(a.batch.S, from, slot);
-  if (s >= a.batch.S) return;
-  const int tile = slot - (int)from(s);
-  const Work work = Work::of<TILE>(a, Sequence(a.batch, s));
-  if (tile >= work.tiles || work.units == 0) return;
-  const int sees = clamp_to(work.seq.first + (min((tile + 1) * TILE, work.rows) - 1) / a.G + 1, work.held);
-  run_tile<Code, NI>(a, work, s, head, tile, 0, max(1, (sees + STAGE - 1) / STAGE), nullptr, shared, false);
+  constexpr int FLOATS = Meeting<NI, 16, 4>::FLOATS, BYTES = 2 * Staged<NI>::BYTES;
+  __shared__ __attribute__((aligned(16))) char shared[FEW && FLOATS * 4 > BYTES ? FLOATS * 4 : BYTES];
+  __shared__ int numbers[SHARED || FEW ? 4 : 1][3][64];
+  int w = blockIdx.x;
+  if constexpr (FEW) {
+    if (w < a.few.workgroups) {
+      run_share<Code, NI, 16, 4>(a, w, reinterpret_cast<float*>(shared), numbers[threadIdx.x >> 6]);
+      return;
+    }
+    w -= a.few.workgroups;
+  }
+  if constexpr (SHARED) {
+    walk_share<TILE>(a, a.many, w, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
+      run_tile<Code, NI>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.many, w, begin, part_floats(TILE, NI * 32)), shared, again);
+    });
+  } else {
+    const int head = w % a.pages.Hkv, slot = a.many.tiles - 1 - w / a.pages.Hkv;
+    auto from = [&](int i) { return (int64_t)a.batch.start(i) * a.G / TILE + i; };
+    const int s = count_up_to(a.batch.S, from, slot);
+    if (s >= a.batch.S) return;
+    const int tile = slot - (int)from(s);
+    const Work work = Work::of<TILE>(a, a.many, Sequence(a.batch, s));
+    if (tile >= work.tiles) return;
+    const int sees = clamp_to(work.seq.first + (min((tile + 1) * TILE, work.rows) - 1) / a.G + 1, work.held);
+    run_tile<Code, NI>(a, work, s, head, tile, 0, max(1, (sees + STAGE - 1) / STAGE), nullptr, shared, false);
+  }
 }
 
-template <typename Code, int NI>
-__global__ __launch_bounds__(256, 2) void attend_tiles_shared_kernel(const AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) char shared[2 * Staged<NI>::BYTES];
-  __shared__ int numbers[4][3][64];
-  walk_share<TILE>(a, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
-    run_tile<Code, NI>(a, work, s, head, tile, begin, stop,
-                       whole ? nullptr : a.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(TILE, NI * 32), shared, again);
-  });
-}
-
-// Rows of segments that several workgroups met: a wavefront a row, two elements a lane.
+// --- joining ----------------------------------------------------------------------------------------------------------------------------------
+//
+// A segment that several workgroups met is joined by the workgroup of its first border: border w lies between shares w - 1 and w.  A thread has four
+// elements of a row.
+constexpr int JOINING = 1024;
 template <int NI, int ROWS>
-__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
-  constexpr int W = NI * 32;
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (int64_t)a.batch.T * a.Hq) return;
-  const int row = __builtin_amdgcn_readfirstlane((int)(id / a.Hq)), hq = __builtin_amdgcn_readfirstlane((int)(id % a.Hq));
-  const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, row));
-  const Work work = Work::of<ROWS>(a, Sequence(a.batch, s));
-  const int head = hq / a.G, r = (row - work.seq.row0) * a.G + hq - head * a.G;
-  if (row < work.seq.row0 || r >= work.rows) return;
-  const int64_t units = a.bases[a.batch.S], sharers = a.bases[a.batch.S + 1];
-  const int64_t from = a.bases[s] + ((int64_t)head * work.tiles + r / ROWS) * (work.blocks + a.spare) + a.spare;
-  const int64_t w0 = owner_of(units, sharers, from), w1 = owner_of(units, sharers, from + work.blocks - 1);
-  if (w0 == w1) return;
-  const int in = r % ROWS, d = lane * 2;
-  auto part_of = [&](int64_t w) { return a.parts + (2 * w + (w == w0)) * part_floats(ROWS, W); };
-  float m = -INFINITY;
-  for (int64_t w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, part_of(w)[in * 2]);
+__device__ __forceinline__ void join(const AttendArgs& a, const AttendArgs::Side& side, int border) {
+  constexpr int W = NI * 32, T = W / 4, AT_ONCE = JOINING / T;
+  const int S = a.batch.S;
+  const int64_t units = side.bases[S], share = side.bases[S + 1], u = share * border;
+  if (u >= units) return;
+  // the sequence and the segment that the border lies in
+  const int s = min(count_up_to(S, [&](int i) { return i < S ? side.bases[i] : units; }, u), S - 1);
+  const Work work = Work::of<ROWS>(a, side, Sequence(a.batch, s));
+  if (work.units == 0) return;
+  const int whole = work.blocks + side.spare;
+  const int64_t base = side.bases[s], segment = (u - base) / whole, from = base + segment * whole + side.spare;
+  const int w0 = (int)(from / share), w1 = (int)((from + work.blocks - 1) / share);
+  if (w0 + 1 != border || w0 == w1) return;
+  const int head = (int)segment / work.tiles, tile = (int)segment % work.tiles;
+  // all rows of the thread, and some parts, on their way at once
+  constexpr int MINE = (ROWS + AT_ONCE - 1) / AT_ONCE, PARTS = MINE >= 4 ? 2 : 8 / MINE;
+  const int d = (int)threadIdx.x % T * 4, first = (int)threadIdx.x / T, rows = min(ROWS, work.rows - tile * ROWS);
+  if (first >= min(AT_ONCE, rows)) return;
+  float m[MINE], l[MINE];
+  f4 sum[MINE];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  // (fmaxf leaves NaN aside: the sums have it)
-  float l = 0.0f;
-  f2 sum = {0.0f, 0.0f};
-#pragma unroll 4
-  for (int64_t w = w0; w <= w1; ++w) {
-    const float* p = part_of(w);
-    const float my = p[in * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
-    l = __builtin_fmaf(p[in * 2 + 1], f, l);
-    if (d < W) {
-      const f2 o = *reinterpret_cast<const f2*>(p + 2 * ROWS + in * W + d);
-      sum[0] = __builtin_fmaf(o[0], f, sum[0]), sum[1] = __builtin_fmaf(o[1], f, sum[1]);
+  for (int y = 0; y < MINE; ++y) m[y] = -INFINITY, l[y] = 0.0f, sum[y] = (f4)(0.0f);
+  for (int w = w0; w <= w1; w += PARTS) {
+    f2 ml[MINE][PARTS];
+    f4 o[MINE][PARTS];
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) {
+      const float* p = part_at(side, min(w + x, w1), w + x == w0 ? 0 : 1, part_floats(ROWS, W));
+#pragma unroll
+      for (int y = 0; y < MINE; ++y) {
+        const int in = min(first + y * AT_ONCE, rows - 1);
+        ml[y][x] = *reinterpret_cast<const f2*>(p + in * 2);
+        o[y][x] = *reinterpret_cast<const f4*>(p + 2 * ROWS + in * W + d);
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < MINE; ++y) {
+      float top = m[y];
+#pragma unroll
+      for (int x = 0; x < PARTS; ++x) top = fmaxf(top, w + x <= w1 ? ml[y][x][0] : -INFINITY);
+      const float f = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - top);
+      l[y] *= f, sum[y] *= f, m[y] = top;
+#pragma unroll
+      for (int x = 0; x < PARTS; ++x) {
+        // (a maximum that is no number leaves the others alone, its sums are none either)
+        const float f = w + x > w1 || ml[y][x][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[y][x][0] - top);
+        if (w + x > w1) continue;
+        l[y] = __builtin_fmaf(ml[y][x][1], f, l[y]);
+        sum[y] += o[y][x] * f;
+      }
     }
   }
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  if (d < a.pages.D)
-    *reinterpret_cast<uint32_t*>(a.out + row * a.out_token + hq * a.out_head + d * 2) = from_float(sum[0] * inv, a.bf16) | (uint32_t)from_float(sum[1] * inv, a.bf16) << 16;
-  if (lane == 0 && a.lse) a.lse[(int64_t)hq * a.batch.T + row] = log_sum(m, l);
+#pragma unroll
+  for (int y = 0; y < MINE; ++y) {
+    const int in = first + y * AT_ONCE, r = tile * ROWS + in, i = r / a.G;
+    if (in < rows) put_out(a, work.seq.row0 + i, head * a.G + r - i * a.G, d, sum[y], m[y], l[y]);
+  }
+}
+template <int NI>
+__global__ __launch_bounds__(JOINING) void join_kernel(const AttendArgs a, int few_rows, int few_borders) {
+  const int w = blockIdx.x;
+  if (w >= few_borders) join<NI, TILE>(a, a.many, w - few_borders + 1);
+  else if (few_rows == 16) join<NI, 16>(a, a.few, w + 1);
+  else join<NI, 32>(a, a.few, w + 1);
 }
 
 // --- host ----------------------------------------------------------------------------------------------------------------------------------
@@ -837,83 +901,75 @@ static bool desc_ok(const tmac_attn_desc* d, const tmac_pages* p) {
          std::isfinite(d->scale) && d->scale > 0 && d->causal == 1 && !d->reserved[0] && !d->reserved[1];
 }
 
-// One launch over the sequences of a kind, and the one that joins what it leaves.
+// How the sequences of few and of many rows are dealt with.
 struct Side {
   bool on, whole;  // whole: every segment by a workgroup of its own, nothing to join
   int rows, waves, workgroups, least, spare, tiles, rows_from, rows_to;
   size_t bases, parts;  // bytes
   size_t bytes() const { return bases + parts; }
+  void share(const tmac_pages* p, const tmac_pages_batch* b) {
+    bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
+    parts = (size_t)workgroups * 2 * part_floats(rows, (p->D + 31) / 32 * 32) * 4;
+  }
+  AttendArgs::Side args(char* workspace) const {
+    return {rows_from, rows_to, workgroups, least, spare, tiles, reinterpret_cast<int64_t*>(workspace), reinterpret_cast<float*>(workspace + bases)};
+  }
 };
 struct Plan {
   Side few, many;
 };
-static void share(Side& x, const tmac_pages* p, const tmac_pages_batch* b) {
-  x.bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
-  x.parts = (size_t)x.workgroups * 2 * part_floats(x.rows, (p->D + 31) / 32 * 32) * 4;
-}
+static int env(const char* n, int d) { return getenv(n) ? atoi(getenv(n)) : d; }
 static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
   Plan plan = {};
+  Side &few = plan.few, &many = plan.many;
   const int G = d->Hq / d->Hkv;
   const int64_t most = (int64_t)view_of(b).most * G;  // rows of a sequence and head
   const int64_t blocks = (int64_t)b->width * p->page / BT;
-  Side& few = plan.few;
-  few.rows = most > 16 && most <= 64 ? 32 : 16;
-  few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
-  few.on = most <= 64 || (b->S > 1 && G <= 16);
-  few.tiles = few.rows == 32 ? 2 : 1;
-  const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
-  few.whole = blocks <= 128 && segments * 64 * 16 <= 0xffffffff;
-  if (few.whole) {
-    few.waves = few.rows == 32 ? 4 : segments >= 1024 ? 4 : segments >= 512 ? 8 : 16;
-    few.workgroups = (int)segments;
-  } else {
-    few.waves = 4, few.workgroups = few.rows == 16 ? 768 : 512, few.least = 8, few.spare = 16;
-    share(few, p, b);
-  }
-  Side& many = plan.many;
   many.on = most > 64;
+  few.on = !many.on || (b->S > 1 && G <= 16);
+  if (few.on) {
+    few.rows = most > 16 && !many.on ? 32 : 16, few.waves = 4;
+    few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
+    few.tiles = few.rows == 32 ? 2 : 1;
+    const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
+    few.whole = !many.on && blocks <= env("X_BLOCKS", segments < 256 ? 48 : 128) && segments * 256 <= 0xffffffff;
+    if (few.whole) {
+      few.workgroups = (int)segments;
+    } else {
+      few.workgroups = env("X_FWG", 256), few.least = env("X_FL", 8), few.spare = env("X_SPARE", 16);
+      few.share(p, b);
+    }
+  }
   if (many.on) {
     many.rows = TILE, many.waves = 4;
     many.rows_from = few.on ? 17 : 1, many.rows_to = 0x7fffffff;
     const int64_t slots = (int64_t)b->T * G / TILE + b->S, least = std::max<int64_t>(0, ((int64_t)b->T * G - (few.on ? 16 * (int64_t)b->S : 0)) / TILE) * p->Hkv;
-    many.whole = (least >= 256 || blocks <= 32) && slots * p->Hkv * 256 <= 0xffffffff;
+    many.whole = (least >= env("X_LEAST", 448) || blocks <= 32) && (slots * p->Hkv + 1024) * 256 <= 0xffffffff;
     many.tiles = (int)slots;
-    many.workgroups = many.whole ? (int)(slots * p->Hkv) : 512;
+    many.workgroups = many.whole ? (int)(slots * p->Hkv) : env("X_MWG", 512);
     if (!many.whole) {
-      many.least = 4, many.spare = 2;
-      share(many, p, b);
+      many.least = env("X_ML", 4), many.spare = env("X_MSPARE", 2);
+      many.share(p, b);
     }
   }
   return plan;
 }
 
 template <typename Code, int NI>
-static const void* attend_of(const Side& x) {
-  if (x.rows == TILE) return x.whole ? (const void*)attend_tiles_kernel<Code, NI> : (const void*)attend_tiles_shared_kernel<Code, NI>;
-  if (x.whole) {
-    if (x.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
-    return x.waves == 4 ? (const void*)attend_whole_kernel<Code, NI, 16, 4>
-                        : x.waves == 8 ? (const void*)attend_whole_kernel<Code, NI, 16, 8> : (const void*)attend_whole_kernel<Code, NI, 16, 16>;
+static const void* attend_of(const Plan& x) {
+  if (x.many.on) {
+    if (x.many.whole) return x.few.on ? (const void*)attend_tiles_kernel<Code, NI, false, true> : (const void*)attend_tiles_kernel<Code, NI, false, false>;
+    return x.few.on ? (const void*)attend_tiles_kernel<Code, NI, true, true> : (const void*)attend_tiles_kernel<Code, NI, true, false>;
   }
-  return x.rows == 16 ? (const void*)attend_kernel<Code, NI, 16, 4> : (const void*)attend_kernel<Code, NI, 32, 4>;
+  if (x.few.whole) {
+    if (x.few.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
+    return (const void*)attend_whole_kernel<Code, NI, 16, 4>;
+  }
+  return x.few.rows == 16 ? (const void*)attend_kernel<Code, NI, 16> : (const void*)attend_kernel<Code, NI, 32>;
 }
 template <typename Code>
-static const void* attend_of(int ni, const Side& x) {
+static const void* attend_of(int ni, const Plan& x) {
   return ni == 1 ? attend_of<Code, 1>(x) : ni == 2 ? attend_of<Code, 2>(x) : ni == 3 ? attend_of<Code, 3>(x) : attend_of<Code, 4>(x);
-}
-template <int NI>
-static const void* join_of(int rows) {
-  return rows == 16 ? (const void*)join_kernel<NI, 16> : rows == 32 ? (const void*)join_kernel<NI, 32> : (const void*)join_kernel<NI, TILE>;
-}
-static tmac_status run_side(AttendArgs a, const Side& x, int code, char* workspace, void* stream) {
-  a.bases = reinterpret_cast<int64_t*>(workspace);
-  a.parts = reinterpret_cast<float*>(workspace + x.bases);
-  a.rows_from = x.rows_from, a.rows_to = x.rows_to, a.workgroups = x.workgroups, a.least = x.least, a.spare = x.spare, a.tiles = x.tiles;
-  const int ni = (a.pages.D + 31) / 32;
-  const tmac_status st = launch(code == TMAC_CODE_I8 ? attend_of<I8>(ni, x) : attend_of<E4M3>(ni, x), x.workgroups, 64 * x.waves, &a, stream);
-  if (st != TMAC_OK || x.whole) return st;
-  const void* join = ni == 1 ? join_of<1>(x.rows) : ni == 2 ? join_of<2>(x.rows) : ni == 3 ? join_of<3>(x.rows) : join_of<4>(x.rows);
-  return launch(join, ((int64_t)a.batch.T * a.Hq + 3) / 4, 256, &a, stream);
 }
 
 }  // namespace pages
@@ -946,9 +1002,13 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   a.c = desc->scale * 1.44269504088896340736f;
   a.Hq = desc->Hq, a.G = desc->Hq / desc->Hkv, a.bf16 = desc->elem == TMAC_ELEM_BF16;
   char* const workspace = static_cast<char*>(workspace_dev);
-  if (plan.few.on) {
-    const tmac_status st = run_side(a, plan.few, p->code, workspace, stream);
-    if (st != TMAC_OK || !plan.many.on) return st;
-  }
-  return run_side(a, plan.many, p->code, workspace + plan.few.bytes(), stream);
+  a.few = plan.few.args(workspace), a.many = plan.many.args(workspace + plan.few.bytes());
+  const int ni = (p->D + 31) / 32, workgroups = (plan.few.on ? plan.few.workgroups : 0) + (plan.many.on ? plan.many.workgroups : 0);
+  const tmac_status st = launch(p->code == TMAC_CODE_I8 ? attend_of<I8>(ni, plan) : attend_of<E4M3>(ni, plan), workgroups, 64 * (plan.few.on ? plan.few.waves : 4), &a, stream);
+  if (st != TMAC_OK || need == 0) return st;
+  int few_rows = plan.few.rows, few_borders = plan.few.on && !plan.few.whole ? plan.few.workgroups - 1 : 0;
+  const int many_borders = plan.many.on && !plan.many.whole ? plan.many.workgroups - 1 : 0;
+  const void* join = ni == 1 ? (const void*)join_kernel<1> : ni == 2 ? (const void*)join_kernel<2> : ni == 3 ? (const void*)join_kernel<3> : (const void*)join_kernel<4>;
+  void* args[] = {&a, &few_rows, &few_borders};
+  return launch_with(join, few_borders + many_borders, JOINING, args, stream);
 }

@@ -12,13 +12,16 @@
 namespace tmac {
 namespace pages {
 
-inline tmac_status launch(const void* kernel, int64_t grid, int threads, void* args, void* stream) {
+inline tmac_status launch_with(const void* kernel, int64_t grid, int threads, void** args, void* stream) {
   if (!attn::launchable(grid, threads)) return TMAC_EUNSUPPORTED;
-  void* ptrs[] = {args};
-  const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), ptrs, 0, static_cast<hipStream_t>(stream));
+  const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, static_cast<hipStream_t>(stream));
   if (e == hipSuccess) return TMAC_OK;
   note_hip_error((int)e);
   return TMAC_EHIP;
+}
+inline tmac_status launch(const void* kernel, int64_t grid, int threads, void* args, void* stream) {
+  void* ptrs[] = {args};
+  return launch_with(kernel, grid, threads, ptrs, stream);
 }
 
 // In place, or apart (rows of a result that overlap each other are the caller's to avoid, as in the other entry points).
