@@ -41,9 +41,14 @@ struct AttendArgs {
     int workgroups, least;   // that share the units, and how many at least each
     int spare;               // units that a segment counts more than it has
     int tiles;               // that a sequence may have (many rows: all sequences), where every segment has a workgroup
-    int64_t* bases;          // [S + 1] units before each sequence, then the units of a share
+    struct Note* notes;      // of each of the workgroups that share: the segment that goes on from the share before to this one
     float* parts;            // sums of pieces
   } few, many;
+};
+
+// A segment that shares w0 to w1 have pieces of: its rows are rows r = tile_row .. of sequence and head, `rows` in all.  w1 < w0: none.
+struct Note {
+  int w0, w1, row0, rows, tile_row, head, unused[2];
 };
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -550,30 +555,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_whole_kernel(const Atten
 // was a piece before).  A segment that several workgroups meet is joined afterwards.  numbers: of 64 sequences, Sequence's row0, n, len.
 template <int ROWS, typename Piece>
 __device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs::Side& side, int w, int (*numbers)[64], Piece&& piece) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), S = a.batch.S;
+  const int lane = threadIdx.x & 63, S = a.batch.S;
   auto units_of = [&](int s0, bool keep) {
     Sequence seq;
     if (s0 + lane < S) seq = Sequence(a.batch, s0 + lane);
     if (keep) numbers[0][lane] = seq.row0, numbers[1][lane] = seq.n, numbers[2][lane] = seq.len;
     return Work::of<ROWS>(a, side, seq).units;
   };
-  int64_t u, end, local;
+  int64_t u, end, local, length;
   int s0 = 0, at;
   {
     int64_t x = units_of(0, true), upto = inclusive(x), units = shfl64(upto, 63);
     for (int i = 64; i < S; i += 64) units += shfl64(inclusive(units_of(i, false)), 63);
     const int64_t share = share_of(side, units);
-    if (w == 0 && wave == 0) {
-      int64_t before = 0;
-      for (int i = 0; i < S; i += 64) {
-        const int64_t y = units_of(i, false), to = inclusive(y);
-        if (i + lane < S) side.bases[i + lane] = before + to - y;
-        before += shfl64(to, 63);
-      }
-      if (lane == 0) side.bases[S] = units, side.bases[S + 1] = share;
-    }
+    if (threadIdx.x == 0) side.notes[w] = Note{0, -1, 0, 0, 0, 0, {0, 0}};
     u = share * w, end = min(units, u + share);
     if (u >= end) return;
+    length = share;
     // the share's first sequence
     int64_t before = 0;
     while (u >= before + shfl64(upto, 63) && s0 + 64 < S) {
@@ -603,6 +601,12 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs
     const int from = (int)(local - (int64_t)segment * whole), to = (int)min((int64_t)whole, from + (end - u));
     if (to > side.spare) {
       const int begin = max(0, from - side.spare), stop = to - side.spare;
+      if (begin > 0) {  // (the share's first piece: the first border within the segment has the note)
+        const int64_t first = u - begin;
+        const int w0 = (int)(first / length);
+        if (w0 == w - 1 && threadIdx.x == 0)
+          side.notes[w] = Note{w0, (int)((first + work.blocks - 1) / length), work.seq.row0, work.rows, segment % work.tiles * ROWS, segment / work.tiles, {0, 0}};
+      }
       piece(work, s0 + at, segment / work.tiles, segment % work.tiles, begin, stop, begin == 0 && stop == work.blocks, again);
       again = true;
     }
@@ -824,28 +828,23 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a
 
 // --- joining ----------------------------------------------------------------------------------------------------------------------------------
 //
-// A segment that several workgroups met is joined by the workgroup of its first border: border w lies between shares w - 1 and w.  A thread has four
-// elements of a row.
-constexpr int JOINING = 1024;
+// A segment that several workgroups met is joined by the workgroups of its first border: border w lies between shares w - 1 and w.  A thread has four
+// elements of up to four rows, all of whose parts, or some of them at a time, are on their way at once.
+constexpr int JOINING = 256;
 template <int NI, int ROWS>
-__device__ __forceinline__ void join(const AttendArgs& a, const AttendArgs::Side& side, int border) {
-  constexpr int W = NI * 32, T = W / 4, AT_ONCE = JOINING / T;
-  const int S = a.batch.S;
-  const int64_t units = side.bases[S], share = side.bases[S + 1], u = share * border;
-  if (u >= units) return;
-  // the sequence and the segment that the border lies in
-  const int s = min(count_up_to(S, [&](int i) { return i < S ? side.bases[i] : units; }, u), S - 1);
-  const Work work = Work::of<ROWS>(a, side, Sequence(a.batch, s));
-  if (work.units == 0) return;
-  const int whole = work.blocks + side.spare;
-  const int64_t base = side.bases[s], segment = (u - base) / whole, from = base + segment * whole + side.spare;
-  const int w0 = (int)(from / share), w1 = (int)((from + work.blocks - 1) / share);
-  if (w0 + 1 != border || w0 == w1) return;
-  const int head = (int)segment / work.tiles, tile = (int)segment % work.tiles;
-  // all rows of the thread, and some parts, on their way at once
-  constexpr int MINE = (ROWS + AT_ONCE - 1) / AT_ONCE, PARTS = MINE >= 4 ? 2 : 8 / MINE;
-  const int d = (int)threadIdx.x % T * 4, first = (int)threadIdx.x / T, rows = min(ROWS, work.rows - tile * ROWS);
-  if (first >= min(AT_ONCE, rows)) return;
+struct Joining {
+  static constexpr int T = NI * 8, AT_ONCE = JOINING / T, MINE = (ROWS + AT_ONCE - 1) / AT_ONCE < 4 ? (ROWS + AT_ONCE - 1) / AT_ONCE : 4;
+  static constexpr int GROUPS = (ROWS + AT_ONCE * MINE - 1) / (AT_ONCE * MINE);  // workgroups of a border
+};
+template <int NI, int ROWS>
+__device__ __forceinline__ void join(const AttendArgs& a, const AttendArgs::Side& side, int border, int group) {
+  typedef Joining<NI, ROWS> J;
+  constexpr int W = NI * 32, T = J::T, AT_ONCE = J::AT_ONCE, MINE = J::MINE, PARTS = 8 / MINE;
+  const Note note = side.notes[border];
+  const int w0 = note.w0, w1 = note.w1;
+  if (w1 <= w0) return;
+  const int d = (int)threadIdx.x % T * 4, first = group * AT_ONCE * MINE + (int)threadIdx.x / T, rows = min(ROWS, note.rows - note.tile_row);
+  if ((int)threadIdx.x >= AT_ONCE * T || first >= rows) return;
   float m[MINE], l[MINE];
   f4 sum[MINE];
 #pragma unroll
@@ -882,16 +881,22 @@ __device__ __forceinline__ void join(const AttendArgs& a, const AttendArgs::Side
   }
 #pragma unroll
   for (int y = 0; y < MINE; ++y) {
-    const int in = first + y * AT_ONCE, r = tile * ROWS + in, i = r / a.G;
-    if (in < rows) put_out(a, work.seq.row0 + i, head * a.G + r - i * a.G, d, sum[y], m[y], l[y]);
+    const int in = first + y * AT_ONCE, r = note.tile_row + in, i = r / a.G;
+    if (in < rows) put_out(a, note.row0 + i, note.head * a.G + r - i * a.G, d, sum[y], m[y], l[y]);
   }
 }
 template <int NI>
 __global__ __launch_bounds__(JOINING) void join_kernel(const AttendArgs a, int few_rows, int few_borders) {
-  const int w = blockIdx.x;
-  if (w >= few_borders) join<NI, TILE>(a, a.many, w - few_borders + 1);
-  else if (few_rows == 16) join<NI, 16>(a, a.few, w + 1);
-  else join<NI, 32>(a, a.few, w + 1);
+  int w = blockIdx.x;
+  constexpr int G16 = Joining<NI, 16>::GROUPS, G32 = Joining<NI, 32>::GROUPS, G128 = Joining<NI, TILE>::GROUPS;
+  const int few = few_borders * (few_rows == 16 ? G16 : G32);
+  if (w >= few) join<NI, TILE>(a, a.many, (w - few) / G128 + 1, (w - few) % G128);
+  else if (few_rows == 16) join<NI, 16>(a, a.few, w / G16 + 1, w % G16);
+  else join<NI, 32>(a, a.few, w / G32 + 1, w % G32);
+}
+template <int NI>
+static int64_t join_groups(int few_rows, int few_borders, int many_borders) {
+  return (int64_t)few_borders * (few_rows == 16 ? Joining<NI, 16>::GROUPS : Joining<NI, 32>::GROUPS) + (int64_t)many_borders * Joining<NI, TILE>::GROUPS;
 }
 
 // --- host ----------------------------------------------------------------------------------------------------------------------------------
@@ -905,20 +910,19 @@ static bool desc_ok(const tmac_attn_desc* d, const tmac_pages* p) {
 struct Side {
   bool on, whole;  // whole: every segment by a workgroup of its own, nothing to join
   int rows, waves, workgroups, least, spare, tiles, rows_from, rows_to;
-  size_t bases, parts;  // bytes
-  size_t bytes() const { return bases + parts; }
-  void share(const tmac_pages* p, const tmac_pages_batch* b) {
-    bases = (((size_t)b->S + 2) * 8 + 15) / 16 * 16;
+  size_t notes, parts;  // bytes
+  size_t bytes() const { return notes + parts; }
+  void share(const tmac_pages* p) {
+    notes = (size_t)workgroups * sizeof(Note);
     parts = (size_t)workgroups * 2 * part_floats(rows, (p->D + 31) / 32 * 32) * 4;
   }
   AttendArgs::Side args(char* workspace) const {
-    return {rows_from, rows_to, workgroups, least, spare, tiles, reinterpret_cast<int64_t*>(workspace), reinterpret_cast<float*>(workspace + bases)};
+    return {rows_from, rows_to, workgroups, least, spare, tiles, reinterpret_cast<Note*>(workspace), reinterpret_cast<float*>(workspace + notes)};
   }
 };
 struct Plan {
   Side few, many;
 };
-static int env(const char* n, int d) { return getenv(n) ? atoi(getenv(n)) : d; }
 static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
   Plan plan = {};
   Side &few = plan.few, &many = plan.many;
@@ -932,24 +936,24 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
     few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
     few.tiles = few.rows == 32 ? 2 : 1;
     const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
-    few.whole = !many.on && blocks <= env("X_BLOCKS", segments < 256 ? 48 : 128) && segments * 256 <= 0xffffffff;
+    few.whole = !many.on && blocks <= (segments < 256 ? 48 : 128) && segments * 256 <= 0xffffffff;
     if (few.whole) {
       few.workgroups = (int)segments;
     } else {
-      few.workgroups = env("X_FWG", 256), few.least = env("X_FL", 8), few.spare = env("X_SPARE", 16);
-      few.share(p, b);
+      few.workgroups = 256, few.least = 8, few.spare = 16;
+      few.share(p);
     }
   }
   if (many.on) {
     many.rows = TILE, many.waves = 4;
     many.rows_from = few.on ? 17 : 1, many.rows_to = 0x7fffffff;
     const int64_t slots = (int64_t)b->T * G / TILE + b->S, least = std::max<int64_t>(0, ((int64_t)b->T * G - (few.on ? 16 * (int64_t)b->S : 0)) / TILE) * p->Hkv;
-    many.whole = (least >= env("X_LEAST", 448) || blocks <= 32) && (slots * p->Hkv + 1024) * 256 <= 0xffffffff;
+    many.whole = (least >= 448 || blocks <= 32) && (slots * p->Hkv + 1024) * 256 <= 0xffffffff;
     many.tiles = (int)slots;
-    many.workgroups = many.whole ? (int)(slots * p->Hkv) : env("X_MWG", 512);
+    many.workgroups = many.whole ? (int)(slots * p->Hkv) : 512;
     if (!many.whole) {
-      many.least = env("X_ML", 4), many.spare = env("X_MSPARE", 2);
-      many.share(p, b);
+      many.least = 4, many.spare = 2;
+      many.share(p);
     }
   }
   return plan;
@@ -1010,5 +1014,7 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   const int many_borders = plan.many.on && !plan.many.whole ? plan.many.workgroups - 1 : 0;
   const void* join = ni == 1 ? (const void*)join_kernel<1> : ni == 2 ? (const void*)join_kernel<2> : ni == 3 ? (const void*)join_kernel<3> : (const void*)join_kernel<4>;
   void* args[] = {&a, &few_rows, &few_borders};
-  return launch_with(join, few_borders + many_borders, JOINING, args, stream);
+  const int64_t groups = ni == 1 ? join_groups<1>(few_rows, few_borders, many_borders) : ni == 2 ? join_groups<2>(few_rows, few_borders, many_borders)
+                       : ni == 3 ? join_groups<3>(few_rows, few_borders, many_borders) : join_groups<4>(few_rows, few_borders, many_borders);
+  return launch_with(join, groups, JOINING, args, stream);
 }
