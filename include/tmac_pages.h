@@ -51,7 +51,7 @@ tmac_status tmac_rotate(const tmac_rope* rope, const tmac_rope_item* items, int3
 /* --- pages --------------------------------------------------------------------------------------------------------------------
  * Keys and values in 8 bits.  TMAC_BLOCK_TOKENS consecutive tokens of a sequence share, for each key head, one scale for their keys
  * and one for their values; an element is its code's value times the scale.
- *   TMAC_CODE_I8    whole numbers -127..127;  the scale that values up to `most` need is most / 127
+ *   TMAC_CODE_I8    whole numbers -127..127;  the scale that values up to `most` need is most (1 / 127), in 32 bits
  *   TMAC_CODE_E4M3  4 exponent and 3 mantissa bits, up to 448;  most / 448 rounded up to a power of two
  * Scales are at least 2^-60 (a block of zeros has that); code = round to nearest even of x (1 / scale).  Infinite elements are held as
  * the block's largest value of their sign, NaN as zero; neither touches the scale. */

@@ -125,6 +125,7 @@ class _NoCalls:
         return None
     forward_fused = forward = forward_one_call = multi = _refuse
     attn_prompt = attn_weights = cache_fill = cache_append = attend = bind_attention = _refuse
+    rotate = pages_append = pages_read = pages_attend = bind_pages = _refuse
 
 
 def _load_calls():

@@ -98,7 +98,7 @@ __device__ __forceinline__ int sequence_of(const Batch& b, int row) {
 
 struct I8 {
   static constexpr float MOST = 127.0f;
-  static __device__ __forceinline__ float scale_for(float most) { return fmaxf(most / MOST, LEAST_SCALE); }
+  static __device__ __forceinline__ float scale_for(float most) { return fmaxf(most * (1.0f / MOST), LEAST_SCALE); }
   // Four numbers, already multiplied by 1 / scale, as codes.
   static __device__ __forceinline__ uint32_t encode(float a, float b, float c, float d) {
     auto one = [](float x) { return (uint32_t)(int)fminf(fmaxf(__builtin_rintf(x), -MOST), MOST) & 0xffu; };

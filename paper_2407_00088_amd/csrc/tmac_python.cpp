@@ -27,6 +27,7 @@
 
 #include "tmac.h"
 #include "tmac_attn.h"
+#include "tmac_pages.h"
 
 namespace {
 
@@ -45,6 +46,12 @@ decltype(&tmac_cache_fill) g_cache_fill;
 decltype(&tmac_cache_append) g_cache_append;
 decltype(&tmac_attn_decode_workspace_bytes) g_decode_workspace_bytes;
 decltype(&tmac_attn_decode) g_attn_decode;
+decltype(&tmac_rotate) g_rotate;
+decltype(&tmac_pages_append) g_pages_append;
+decltype(&tmac_pages_read) g_pages_read;
+decltype(&tmac_pages_attend_workspace_bytes) g_pages_attend_workspace_bytes;
+decltype(&tmac_pages_attend) g_pages_attend;
+PyTypeObject *g_rope, *g_pages;  // the ctypes structures tmac_rope and tmac_pages
 PyTypeObject *g_attn_desc, *g_cache;  // the ctypes structures tmac_attn_desc and tmac_cache
 PyObject* g_error;       // TmacError
 PyTypeObject* g_wdesc;   // the ctypes structure tmac_wdesc
@@ -526,6 +533,202 @@ PyObject* bind_attention(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// --- pages (pages.py) -------------------------------------------------------------------------------------------------------
+
+bool take_count(PyObject* o, int32_t* to) {
+  if (o == Py_None) {
+    *to = 0;
+    return true;
+  }
+  if (!PyLong_CheckExact(o)) return false;
+  const long long x = PyLong_AsLongLong(o);
+  if (PyErr_Occurred() || x < 0 || x > std::numeric_limits<int32_t>::max()) return false;
+  *to = (int32_t)x;
+  return true;
+}
+
+// rotate(rope, frequencies, positions, tensors ...)
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  tmac_rope rope;
+  Device here;
+  const Py_ssize_t count = n - 3;
+  if (count < 1 || count > TMAC_ROPE_MAX || modes_active() || !take_struct(a[0], g_rope, &rope)) return ordinary_only();
+  const at::Tensor *freq = plain(a[1]), *positions = plain(a[2]);
+  if (!freq || !here.of(freq) || freq->data_ptr() != rope.freq_dev || !positions || positions->dim() != 1) return ordinary_only();
+  const int64_t T = positions->numel();
+  if (T < 1 || T > std::numeric_limits<int32_t>::max() || !here.whole(a[2], at::kLong, T)) return ordinary_only();
+  const at::ScalarType dt = rope.elem == TMAC_ELEM_BF16 ? at::kBFloat16 : at::kHalf;
+  const at::Tensor* x[TMAC_ROPE_MAX];
+  tmac_rope_item items[TMAC_ROPE_MAX] = {};
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    if (!(x[i] = here.rows(a[3 + i], dt, T, -1, rope.D)) || x[i]->numel() == 0 || x[i]->size(1) > std::numeric_limits<int32_t>::max()) return ordinary_only();
+    items[i].x = view_of(*x[i], false);
+    items[i].H = (int32_t)x[i]->size(1);
+  }
+  const int64_t* at_ptr = static_cast<const int64_t*>(positions->data_ptr());
+  const at::TensorOptions options = x[0]->options();
+  void* const stream = c10::hip::getCurrentHIPStream().stream();
+  at::Tensor out[TMAC_ROPE_MAX];
+  tmac_status st;
+  {
+    const Unlocked unlocked;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      out[i] = at::empty({T, items[i].H, rope.D}, options);
+      items[i].out = view_of(out[i], false);
+    }
+    st = g_rotate(&rope, items, (int32_t)count, at_ptr, (int32_t)T, stream);
+  }
+  if (st != TMAC_OK) return refuse(st, "tmac_rotate");
+  THPObjectPtr got(PyTuple_New(count));
+  if (!got) return nullptr;
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    PyObject* const o = THPVariable_Wrap(std::move(out[i]));
+    if (!o) return nullptr;
+    PyTuple_SET_ITEM(got.get(), i, o);
+  }
+  return got.release();
+  END_HANDLE_TH_ERRORS
+}
+
+// pages, codes, desc; table, lens, cu, most
+struct Paged {
+  Device here;
+  tmac_pages pages;
+  tmac_attn_desc desc;
+  tmac_pages_batch batch = {};
+  at::ScalarType dt;
+  bool take(PyObject* const* a) {
+    if (modes_active() || !take_struct(a[0], g_pages, &pages) || !take_struct(a[2], g_attn_desc, &desc)) return false;
+    const at::Tensor* codes = plain(a[1]);
+    if (!codes || !here.of(codes) || codes->numel() == 0 || codes->data_ptr() != pages.codes_dev) return false;
+    dt = desc.elem == TMAC_ELEM_BF16 ? at::kBFloat16 : at::kHalf;
+    return true;
+  }
+  bool take_batch(PyObject* const* a, int64_t T) {
+    constexpr int64_t max = std::numeric_limits<int32_t>::max();
+    const at::Tensor *table = plain(a[0]), *lens = plain(a[1]);
+    if (!table || !lens || table->dim() != 2 || lens->dim() != 1 || T < 1 || T > max) return false;
+    const int64_t S = table->size(0), width = table->size(1);
+    if (table->scalar_type() != at::kInt || table->get_device() != here.index || S < 1 || S > max || width < 1 || width > max) return false;
+    if (width > 1 && table->stride(1) != 1) return false;
+    const int64_t stride = S > 1 ? table->stride(0) : width;
+    if (stride < width || !here.whole(a[1], at::kInt, S) || !take_count(a[3], &batch.most)) return false;
+    if (a[2] == Py_None) {
+      if (T != S) return false;
+    } else {
+      const at::Tensor* cu = here.whole(a[2], at::kInt, S + 1);
+      if (!cu || cu->dim() != 1) return false;
+      batch.cu_dev = static_cast<const int32_t*>(cu->data_ptr());
+    }
+    batch.table_dev = static_cast<const int32_t*>(table->data_ptr()), batch.table_stride = stride;
+    batch.lens_dev = static_cast<const int32_t*>(lens->data_ptr());
+    batch.S = (int32_t)S, batch.width = (int32_t)width, batch.T = (int32_t)T;
+    return true;
+  }
+};
+
+// pages_append(pages, codes, desc, table, lens, cu, most, k, v, rope, frequencies, q, positions): the turned queries, True without any
+PyObject* pages_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Paged p;
+  if (n != 13 || !p.take(a)) return ordinary_only();
+  const at::Tensor *k = p.here.rows(a[7], p.dt, -1, p.pages.Hkv, p.pages.D), *v = nullptr, *q = nullptr, *positions = nullptr;
+  if (!k || !p.take_batch(a + 3, k->size(0)) || !(v = p.here.rows(a[8], p.dt, k->size(0), p.pages.Hkv, p.pages.D))) return ordinary_only();
+  tmac_rope rope;
+  const bool turns = a[9] != Py_None;
+  if (turns) {
+    const at::Tensor* freq = plain(a[10]);
+    if (!take_struct(a[9], g_rope, &rope) || !freq || freq->get_device() != p.here.index || freq->data_ptr() != rope.freq_dev) return ordinary_only();
+  }
+  if (a[11] != Py_None && (!turns || !(q = p.here.rows(a[11], p.dt, k->size(0), p.desc.Hq, p.pages.D)))) return ordinary_only();
+  if (a[12] != Py_None && (!turns || !(positions = p.here.whole(a[12], at::kLong, k->size(0))) || positions->dim() != 1)) return ordinary_only();
+  const tmac_view kv = view_of(*k, false), vv = view_of(*v, false), qv = q ? view_of(*q, false) : tmac_view{};
+  const int64_t* at_ptr = positions ? static_cast<const int64_t*>(positions->data_ptr()) : nullptr;
+  const at::TensorOptions options = k->options();
+  void* const stream = c10::hip::getCurrentHIPStream().stream();
+  at::Tensor out;
+  tmac_view ov = {};
+  tmac_status st;
+  {
+    const Unlocked unlocked;
+    if (q) {
+      out = at::empty({p.batch.T, p.desc.Hq, p.pages.D}, options);
+      ov = view_of(out, false);
+    }
+    st = g_pages_append(&p.pages, &p.batch, p.desc.elem, &kv, &vv, turns ? &rope : nullptr, at_ptr, q ? &qv : nullptr, q ? &ov : nullptr, p.desc.Hq, stream);
+  }
+  if (st != TMAC_OK) return refuse(st, "tmac_pages_append");
+  if (q) return THPVariable_Wrap(std::move(out));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// pages_read(pages, codes, desc, table, lens, cu, most, T)
+PyObject* pages_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Paged p;
+  int32_t T;
+  if (n != 8 || !take_count(a[7], &T) || !p.take(a) || !p.take_batch(a + 3, T)) return ordinary_only();
+  const at::TensorOptions options = THPVariable_Unpack(a[1]).options().dtype(p.dt);
+  void* const stream = c10::hip::getCurrentHIPStream().stream();
+  at::Tensor k, v;
+  tmac_status st;
+  {
+    const Unlocked unlocked;
+    k = at::empty({T, p.pages.Hkv, p.pages.D}, options);
+    v = at::empty({T, p.pages.Hkv, p.pages.D}, options);
+    const tmac_view kv = view_of(k, false), vv = view_of(v, false);
+    st = g_pages_read(&p.pages, &p.batch, p.desc.elem, &kv, &vv, stream);
+  }
+  return st == TMAC_OK ? pair(std::move(k), std::move(v)) : refuse(st, "tmac_pages_read");
+  END_HANDLE_TH_ERRORS
+}
+
+// pages_attend(pages, codes, desc, table, lens, cu, most, q, workspace)
+PyObject* pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Paged p;
+  if (n != 9 || !p.take(a)) return ordinary_only();
+  const at::Tensor *q = p.here.rows(a[7], p.dt, -1, p.desc.Hq, p.pages.D), *ws = plain(a[8]);
+  if (!q || !ws || !p.take_batch(a + 3, q->size(0))) return ordinary_only();
+  if (ws->nbytes() < g_pages_attend_workspace_bytes(&p.desc, &p.pages, &p.batch)) return ordinary_only();  // (a workspace is made there)
+  const tmac_view qv = view_of(*q, false);
+  const at::TensorOptions options = q->options();
+  void* const ws_ptr = ws->data_ptr();
+  const size_t ws_bytes = ws->nbytes();
+  void* const stream = c10::hip::getCurrentHIPStream().stream();
+  at::Tensor out, lse;
+  tmac_status st;
+  {
+    const Unlocked unlocked;
+    out = at::empty({p.batch.T, p.desc.Hq, p.pages.D}, options);
+    lse = at::empty({p.desc.Hq, p.batch.T}, options.dtype(at::kFloat));
+    const tmac_view ov = view_of(out, false);
+    st = g_pages_attend(&p.desc, &p.pages, &p.batch, &qv, &ov, static_cast<float*>(lse.data_ptr()), ws_ptr, ws_bytes, stream);
+  }
+  return st == TMAC_OK ? pair(std::move(out), std::move(lse)) : refuse(st, "tmac_pages_attend");
+  END_HANDLE_TH_ERRORS
+}
+
+// bind_pages(tmac_rope, tmac_pages, addresses of tmac_rotate, tmac_pages_append, tmac_pages_read, tmac_pages_attend_workspace_bytes,
+// tmac_pages_attend)
+PyObject* bind_pages(PyObject*, PyObject* args) {
+  PyObject *rope, *pages;
+  unsigned long long f[5];
+  if (!PyArg_ParseTuple(args, "O!O!KKKKK", &PyType_Type, &rope, &PyType_Type, &pages, &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+  Py_INCREF(rope);
+  Py_INCREF(pages);
+  g_rope = reinterpret_cast<PyTypeObject*>(rope);
+  g_pages = reinterpret_cast<PyTypeObject*>(pages);
+  g_rotate = reinterpret_cast<decltype(g_rotate)>(f[0]);
+  g_pages_append = reinterpret_cast<decltype(g_pages_append)>(f[1]);
+  g_pages_read = reinterpret_cast<decltype(g_pages_read)>(f[2]);
+  g_pages_attend_workspace_bytes = reinterpret_cast<decltype(g_pages_attend_workspace_bytes)>(f[3]);
+  g_pages_attend = reinterpret_cast<decltype(g_pages_attend)>(f[4]);
+  Py_RETURN_NONE;
+}
+
 // bind(TmacError, tmac_wdesc, addresses of tmac_mpgemv_fused, tmac_precompute_lut, tmac_mpgemm, tmac_mpgemm_fused,
 // tmac_fused_workspace_bytes, tmac_mpgemv_fused_multi)
 PyObject* bind(PyObject*, PyObject* args) {
@@ -557,6 +760,11 @@ PyMethodDef methods[] = {
     {"cache_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_fill)), METH_FASTCALL, nullptr},
     {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_append)), METH_FASTCALL, nullptr},
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend)), METH_FASTCALL, nullptr},
+    {"bind_pages", bind_pages, METH_VARARGS, nullptr},
+    {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rotate)), METH_FASTCALL, nullptr},
+    {"pages_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_append)), METH_FASTCALL, nullptr},
+    {"pages_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_read)), METH_FASTCALL, nullptr},
+    {"pages_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_attend)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tmac_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -64,6 +64,10 @@ def _declare(lib):
 
 
 lib = _declare(B.lib)
+# (the ordinary calls go through the native side of the binding, as in attention.py)
+calls = B.calls
+calls.bind_pages(tmac_rope, tmac_pages, *(C.cast(getattr(lib, f), C.c_void_p).value for f in (
+    "tmac_rotate", "tmac_pages_append", "tmac_pages_read", "tmac_pages_attend_workspace_bytes", "tmac_pages_attend")))
 
 
 def _row_view(t) -> tmac_view:
@@ -130,6 +134,11 @@ class Rotary:
     def rotate(self, positions, *tensors, out: Optional[Sequence] = None, stream=None):
         """Tensors [T, H, D] of the same T tokens (up to four, H their own) turned by positions int64 [T].  Returns a tuple of as many; `out`:
         where they go (a tensor itself: in place)."""
+        if out is None and stream is None and tensors:
+            rope = self.rope.get(tensors[0].dtype)
+            got = rope and calls.rotate(rope, self.freq, positions, *tensors)
+            if got is not None:
+                return got
         if not 1 <= len(tensors) <= ROPE_MAX:
             raise ValueError(f"one to {ROPE_MAX} tensors, got {len(tensors)}")
         if out is not None and len(out) != len(tensors):
@@ -232,6 +241,12 @@ class PagedCache:
         queries q [T, Hq, D] of the same tokens, if there are any, by positions int64 [T] (None: the tokens' places in their sequences).
         Returns the turned queries, or None.  Two sequences of a call must not write to the same page."""
         with self.lock:
+            if stream is None and q_out is None:
+                rotary = self.rotary
+                got = calls.pages_append(self.cache, self.codes, self.desc, table, lens, cu, most, k, v,
+                                         None if rotary is None else rotary.rope[self.dtype], None if rotary is None else rotary.freq, q, positions)
+                if got is not None:
+                    return None if q is None else got
             T = k.shape[0]
             for name, t in (("k", k), ("v", v)):
                 A._dims(name, t, "T, Hkv, D", (T, self.Hkv, self.D), self.dtype)
@@ -267,6 +282,10 @@ class PagedCache:
         with self.lock:
             if T is None:
                 T = k.shape[0] if k is not None else lens.shape[0] if cu is None else int(cu[-1])
+            if stream is None and k is None and v is None:
+                got = calls.pages_read(self.cache, self.codes, self.desc, table, lens, cu, most, T)
+                if got is not None:
+                    return got
             batch = self._batch(T, table, lens, cu, most)
             with A._on(stream):
                 k, v = (torch.empty((T, self.Hkv, self.D), dtype=self.dtype, device=self.codes.device) if t is None else t for t in (k, v))
@@ -283,6 +302,10 @@ class PagedCache:
         """q [T, Hq, D], the last tokens of their sequences, over all tokens up to each that are in the pages.  Returns (out [T, Hq, D],
         lse fp32 [Hq, T])."""
         with self.lock:
+            if out is None and lse is None and stream is None and self.attend_ws is not None:
+                got = calls.pages_attend(self.cache, self.codes, self.desc, table, lens, cu, most, q, self.attend_ws)
+                if got is not None:
+                    return got
             T = q.shape[0]
             A._dims("q", q, "T, Hq, D", (T, self.Hq, self.D), self.dtype)
             A._rows("q", q)

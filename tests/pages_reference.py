@@ -43,7 +43,7 @@ def rounding(ref, dtype):
 def scale_for(code, most):
     most = most.float()
     if code == "i8":
-        return (most / 127.0).clamp(min=2.0 ** -60)
+        return (most * torch.tensor(1.0 / 127.0)).clamp(min=2.0 ** -60)
     # 448 = 0.875 * 2^9: the least power of two, times which 448 reaches `most`
     out = torch.full_like(most, 2.0 ** -60)
     for i in range(most.numel()):
