@@ -145,11 +145,14 @@ struct StoreArgs {
   const double* freq;                        // null: keys as they are
   const int64_t* positions;
   float magnitude;
-  int pairs, interleaved, bf16;
-  int slots;  // blocks of a sequence that have workgroups; 0: starts[s] / 32 + 2 s on
+  int pairs, turning, vectors;               // vectors of a row of keys, those that turn
+  uint32_t by_vectors, by_pairs, by_values;  // ceil(2^32 / n); 0: n is 1
+  int slots;                                 // blocks of a sequence that have workgroups; 0: starts[s] / 32 + 2 s on
+  int heads, groups, workgroups;             // key heads of a workgroup, workgroups of a block, of all blocks; those behind turn queries
+  RopeArgs q;
 };
 
-// The sequence and the block of the j-th workgroup of a call, or false.
+// The sequence and the block of the w-th place of a call, or false.
 __device__ __forceinline__ bool block_of(const Batch& b, int slots, int w, int& s, int& j) {
   if (slots) {
     s = w / slots, j = w - s * slots;
@@ -162,102 +165,186 @@ __device__ __forceinline__ bool block_of(const Batch& b, int slots, int w, int& 
   }
   return true;
 }
+__device__ __forceinline__ int divided(int i, uint32_t by) { return by ? (int)__umulhi((uint32_t)i, by) : i; }
 
-// A block of 32 tokens of a sequence and key head that the call's tokens touch.
-template <typename Code>
+// A block of 32 tokens of a sequence that the call's tokens touch, for some key heads one after the other: rows come in vectors of N elements, the
+// next head's while this one is worked on; keys turn on their way to LDS, by cosines and sines that are worked out once; with the scales
+// known, a thread makes 16 codes of either plane.  A step's few tokens wait for memory four times (lengths, table, rows and what the block holds);
+// prompts are bound by the vector unit's work beside memory.
+template <typename Code, bool BF16, bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
-  __shared__ float rows[2][BT][132];
-  __shared__ float most[2][4];
+  typedef typename Vec<N>::type V;
+  constexpr int NV = N == 8 ? 8 : 4, KI = N == 8 ? 2 : 16 / N, VI = 32 / NV / 2, PAIRS = INTERLEAVED ? N / 2 : N;
+  typedef typename Vec<NV>::type VV;
+  __shared__ __attribute__((aligned(16))) f2 turn[BT * 64];
+  __shared__ __attribute__((aligned(16))) float keys[BT][132];
+  __shared__ __attribute__((aligned(16))) uint16_t values[BT][136];
+  __shared__ float most[2][2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int head = blockIdx.x % a.pages.Hkv;
+  if ((int)blockIdx.x >= a.workgroups) {
+    const int64_t w = (int64_t)(blockIdx.x - a.workgroups) * 4 + wave;
+    const int token = __builtin_amdgcn_readfirstlane((int)(w / a.q.slices)), slice = __builtin_amdgcn_readfirstlane((int)(w % a.q.slices));
+    if (token < a.q.T) rotate_rows<BF16, INTERLEAVED, N>(a.q, token, slice, turn + wave * 64);
+    return;
+  }
+  const int h0 = blockIdx.x % a.groups * a.heads, h1 = min(a.pages.Hkv, h0 + a.heads);
   int s, j;
-  if (!block_of(a.batch, a.slots, blockIdx.x / a.pages.Hkv, s, j)) return;
+  if (!block_of(a.batch, a.slots, blockIdx.x / a.groups, s, j)) return;
   const Sequence seq(a.batch, s);
   const int block = max(seq.first, 0) / BT + j;
   // tokens [t0, t1) of the block are the call's
-  const int t0 = max(0, seq.first - block * BT), t1 = min(BT, seq.len - block * BT);
-  if (seq.n == 0 || t1 <= t0) return;
-  const int64_t unit = a.pages.unit_of(a.batch.row(s), a.batch.width, block, head);
-  if (unit < 0) return;
-  const int D = a.pages.D, pairs = a.freq ? a.pairs : 0, plain = D - 2 * pairs;
-  const int row0 = seq.row0 + block * BT - seq.first;  // the row of the block's first token, if it were the call's
-  float mk = 0.0f, mv = 0.0f;
-  auto take = [](float& most, float x) {
-    if (fabsf(x) <= 3.402823466e38f) most = fmaxf(most, fabsf(x));
-  };
-  const char* k = a.k + head * a.k_head;
-  const char* v = a.v + head * a.v_head;
-  for (int i = tid; i < (t1 - t0) * pairs; i += 256) {
-    const int t = t0 + i / pairs, p = i % pairs;
-    const int64_t position = a.positions ? a.positions[row0 + t] : (int64_t)block * BT + t;
-    const f2 cs = cos_sin((double)position * a.freq[p]) * a.magnitude;
-    const int d0 = a.interleaved ? 2 * p : p, d1 = a.interleaved ? 2 * p + 1 : p + pairs;
-    const uint16_t* row = reinterpret_cast<const uint16_t*>(k + (row0 + t) * a.k_token);
-    const float x = to_float(row[d0], a.bf16), y = to_float(row[d1], a.bf16);
-    const float x1 = x * cs[0] - y * cs[1], y1 = x * cs[1] + y * cs[0];
-    rows[0][t][d0] = x1, rows[0][t][d1] = y1;
-    take(mk, x1), take(mk, y1);
-  }
-  for (int i = tid; i < (t1 - t0) * plain; i += 256) {
-    const int t = t0 + i / plain, d = 2 * pairs + i % plain;
-    const float x = to_float(reinterpret_cast<const uint16_t*>(k + (row0 + t) * a.k_token)[d], a.bf16);
-    rows[0][t][d] = x;
-    take(mk, x);
-  }
-  for (int i = tid; i < (t1 - t0) * D; i += 256) {
-    const int t = t0 + i / D, d = i % D;
-    const float x = to_float(reinterpret_cast<const uint16_t*>(v + (row0 + t) * a.v_token)[d], a.bf16);
-    rows[1][t][d] = x;
-    take(mv, x);
-  }
+  const int t0 = max(0, seq.first - block * BT), t1 = min(BT, seq.len - block * BT), nt = t1 - t0;
+  if (seq.n == 0 || nt <= 0) return;
+  const int D = a.pages.D, chunks = a.pages.chunks, row0 = seq.row0 + block * BT - seq.first + t0;  // the row of token t0
+  const int k_count = nt * a.vectors, v_count = nt * (D / NV);
+  V k_lo[KI], k_hi[KI];
+  VV v_in[VI];
+  auto load = [&](int head) {
+    const char* k = a.k + head * a.k_head + row0 * a.k_token;
+    const char* v = a.v + head * a.v_head + row0 * a.v_token;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mk = fmaxf(mk, __shfl_xor(mk, o)), mv = fmaxf(mv, __shfl_xor(mv, o));
-  if (lane == 0) most[0][wave] = mk, most[1][wave] = mv;
-  float* scales = a.pages.scales + unit * 2;
-  const float was[2] = {t0 ? scales[0] : 0.0f, t0 ? scales[1] : 0.0f};
-  __syncthreads();
-  float scale[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    float m = fmaxf(fmaxf(most[x][0], most[x][1]), fmaxf(most[x][2], most[x][3]));
-    scale[x] = fmaxf(was[x], Code::scale_for(m));
-  }
-  if (tid == 0) scales[0] = scale[0], scales[1] = scale[1];
-  // Sixteen codes of either plane at a time: new ones, old ones (rounded again where the scale has grown), zeros
-  auto codes_of = [&](const float (*src)[132], float was, float scale, u4* at, auto&& token_of, auto&& d_of, bool some) {
-    const float inv = 1.0f / scale, ratio = was / scale;
-    u4 old = {0u, 0u, 0u, 0u};
-    if (t0) old = *at;
-    else if (!some) { *at = old; return; }
-    u4 got;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      float y[4];
-      Code::decode(old[w], y);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int t = token_of(4 * w + b), d = d_of(4 * w + b);
-        y[b] *= ratio;
-        if (t >= t0 && t < t1 && d < D) {
-          const float x = src[t][d];
-          y[b] = x == x ? x * inv : 0.0f;
-        }
-      }
-      got[w] = Code::encode(y[0], y[1], y[2], y[3]);
+    for (int u = 0; u < KI; ++u) {
+      const int i = tid + u * 256;
+      if (i >= k_count) break;
+      const int t = divided(i, a.by_vectors), slot = i - t * a.vectors;
+      const int d = slot < a.turning ? slot * N : 2 * a.pairs + (slot - a.turning) * N;
+      const char* at = k + t * a.k_token + d * 2;
+      k_lo[u] = *reinterpret_cast<const V*>(at);
+      if (!INTERLEAVED && slot < a.turning) k_hi[u] = *reinterpret_cast<const V*>(at + a.pairs * 2);
     }
-    *at = got;
+#pragma unroll
+    for (int u = 0; u < VI; ++u) {
+      const int i = tid + u * 256;
+      if (i >= v_count) break;
+      const int t = divided(i, a.by_values);
+      v_in[u] = *reinterpret_cast<const VV*>(v + t * a.v_token + (i - t * (D / NV)) * NV * 2);
+    }
   };
-  for (int i = tid; i < a.pages.chunks * BT; i += 256) {
-    const int t = i % BT, c = i / BT;
-    const bool is_new = t >= t0 && t < t1;
-    if (t0 && !is_new && was[0] == scale[0]) continue;
-    codes_of(rows[0], was[0], scale[0], reinterpret_cast<u4*>(a.pages.keys(unit) + i * 16), [&](int) { return t; },
-             [&](int b) { return c * 16 + b; }, is_new);
+  load(h0);
+  const int64_t unit0 = a.pages.unit_of(a.batch.row(s), a.batch.width, block, h0);
+  for (int i = tid; i < nt * a.pairs; i += 256) {
+    const int t = divided(i, a.by_pairs), p = i - t * a.pairs;
+    const int64_t position = a.positions ? a.positions[row0 + t] : (int64_t)block * BT + t0 + t;
+    turn[i] = cos_sin((double)position * a.freq[p]) * a.magnitude;
   }
-  for (int i = tid; i < a.pages.chunks * BT; i += 256) {
-    const int run = i / 64, n = value_run(a.pages.chunks, run * 32), half = (i - run * 64) / n, d = run * 32 + (i - run * 64) % n;
-    codes_of(rows[1], was[1], scale[1], reinterpret_cast<u4*>(a.pages.values(unit) + i * 16), [&](int b) { return value_token(half, b); },
-             [&](int) { return d; }, true);
+  if (unit0 < 0) return;
+  const int codes = chunks * BT;  // 16 of them a thread, in either plane
+  __syncthreads();
+  for (int head = h0; head < h1; ++head) {
+    const int64_t unit = unit0 + ((int64_t)(head - h0) << a.pages.shift);
+    float* scales = a.pages.scales + unit * 2;
+    u4* const v_to = reinterpret_cast<u4*>(a.pages.values(unit)) + tid;
+    float was[2] = {0.0f, 0.0f};
+    u4 old = {0u, 0u, 0u, 0u};
+    if (t0) {
+      was[0] = scales[0], was[1] = scales[1];
+      if (tid < codes) old = *v_to;
+    }
+    float mk = 0.0f, mv = 0.0f;
+    auto take = [](float& most, float x) { most = fmaxf(most, fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.0f); };
+#pragma unroll
+    for (int u = 0; u < KI; ++u) {
+      const int i = tid + u * 256;
+      if (i >= k_count) break;
+      const int t = divided(i, a.by_vectors), slot = i - t * a.vectors;
+      float lo[N], hi[N];
+#pragma unroll
+      for (int x = 0; x < N; ++x) lo[x] = to_float(elem_of<N>(k_lo[u], x), BF16);
+      if (slot < a.turning) {
+        if (!INTERLEAVED) {
+#pragma unroll
+          for (int x = 0; x < N; ++x) hi[x] = to_float(elem_of<N>(k_hi[u], x), BF16);
+        }
+#pragma unroll
+        for (int p = 0; p < PAIRS; ++p) {
+          const f2 cs = turn[t * a.pairs + slot * PAIRS + p];
+          float& x = lo[INTERLEAVED ? 2 * p : p];
+          float& y = INTERLEAVED ? lo[2 * p + (N > 1)] : hi[p];
+          const float x1 = x * cs[0] - y * cs[1], y1 = x * cs[1] + y * cs[0];
+          x = x1, y = y1;
+          take(mk, x1), take(mk, y1);
+        }
+        if (!INTERLEAVED) {
+#pragma unroll
+          for (int x = 0; x < N; ++x) keys[t0 + t][slot * N + a.pairs + x] = hi[x];
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < N; ++x) take(mk, lo[x]);
+      }
+      const int d = slot < a.turning ? slot * N : 2 * a.pairs + (slot - a.turning) * N;
+#pragma unroll
+      for (int x = 0; x < N; ++x) keys[t0 + t][d + x] = lo[x];
+    }
+#pragma unroll
+    for (int u = 0; u < VI; ++u) {
+      const int i = tid + u * 256;
+      if (i >= v_count) break;
+      const int t = divided(i, a.by_values);
+#pragma unroll
+      for (int x = 0; x < NV; ++x) take(mv, to_float(v_in[u][x], BF16));
+      *reinterpret_cast<VV*>(&values[t0 + t][(i - t * (D / NV)) * NV]) = v_in[u];
+    }
+    if (head + 1 < h1) load(head + 1);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mk = fmaxf(mk, __shfl_xor(mk, o)), mv = fmaxf(mv, __shfl_xor(mv, o));
+    const int place = (head - h0) & 1;
+    if (lane == 0) most[place][0][wave] = mk, most[place][1][wave] = mv;
+    __syncthreads();
+    float scale[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float* m = most[place][x];
+      scale[x] = fmaxf(was[x], Code::scale_for(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+    }
+    if (tid == 0) scales[0] = scale[0], scales[1] = scale[1];
+    if (tid < codes) {
+      // keys: token t, elements 16 c ..; new codes, old ones rounded again where the scale has grown, zeros in a block that is begun
+      const int t = tid % BT, c = tid / BT;
+      u4* const k_to = reinterpret_cast<u4*>(a.pages.keys(unit)) + tid;
+      if (t >= t0 && t < t1) {
+        const float inv = 1.0f / scale[0];
+        u4 got;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int d = c * 16 + 4 * w;
+          f4 x = d < D ? *reinterpret_cast<const f4*>(&keys[t][d]) : f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int b = 0; b < 4; ++b) x[b] = x[b] == x[b] ? x[b] * inv : 0.0f;
+          got[w] = Code::encode(x[0], x[1], x[2], x[3]);
+        }
+        *k_to = got;
+      } else if (t0 == 0) {
+        *k_to = u4{0u, 0u, 0u, 0u};
+      } else if (was[0] != scale[0]) {
+        u4 x = *k_to;
+        const float ratio = was[0] / scale[0];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float y[4];
+          Code::decode(x[w], y);
+          x[w] = Code::encode(y[0] * ratio, y[1] * ratio, y[2] * ratio, y[3] * ratio);
+        }
+        *k_to = x;
+      }
+      // values: element d, 16 tokens
+      const int run = tid / 64, n = value_run(chunks, run * 32), half = (tid - run * 64) / n, d = run * 32 + (tid - run * 64) % n;
+      const float inv = 1.0f / scale[1], ratio = was[1] / scale[1];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (t0) Code::decode(old[w], y);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int t = value_token(half, 4 * w + b);
+          const float x = to_float(values[t][d], BF16);
+          y[b] = t >= t0 && t < t1 && d < D ? (x == x ? x * inv : 0.0f) : t0 ? y[b] * ratio : 0.0f;
+        }
+        old[w] = Code::encode(y[0], y[1], y[2], y[3]);
+      }
+      *v_to = old;
+    }
+    if (head + 1 < h1) __syncthreads();  // (the rows have been read)
   }
 }
 
@@ -321,25 +408,36 @@ static bool rope_ok(const tmac_rope* r) {
          std::isfinite(r->magnitude) && !r->reserved[0] && !r->reserved[1] && !r->reserved[2];
 }
 
-// The widest vectors that the rows' alignment allows, and how the rows are dealt out.
-static int rope_plan(RopeArgs& a, const tmac_rope* r, const tmac_rope_item* items, int count, int T) {
+static uint32_t by(int n) { return n == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n); }
+
+// Elements of a vector: side by side, whole pairs that end at rot; in halves, as many as end at rot / 2; eight where rows are aligned for it.
+static int vector_of(const tmac_rope* r, bool wide) {
   const int half = r->rot / 2;
-  bool wide = r->D % 8 == 0, in_place = true;
-  a.freq = r->freq_dev, a.magnitude = r->magnitude, a.pairs = half, a.D = r->D, a.T = T, a.count = count, a.rows = 0;
+  const int n = r->interleaved ? (r->rot % 8 == 0 ? 8 : r->rot % 4 == 0 ? 4 : 2) : (half % 8 == 0 ? 8 : half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1);
+  return n == 8 && !wide ? 4 : n;
+}
+static int turning_of(const tmac_rope* r, int n) { return r->interleaved ? r->rot / n : r->rot / 2 / n; }
+static bool wide_rows(const tmac_view& v, int D) { return D % 8 == 0 && (reinterpret_cast<uintptr_t>(v.data) & 15) == 0 && v.token % 8 == 0 && v.head % 8 == 0; }
+
+// How the rows are dealt out.  n: elements of a vector.  Wavefronts of a token: until the chip has some thousands, or a wavefront one vector a lane left;
+// at most 256 rows each.
+static void plan_rope(RopeArgs& a, const tmac_rope* r, const tmac_rope_item* items, int count, int T, int n) {
+  bool in_place = true;
+  a.freq = r->freq_dev, a.magnitude = r->magnitude, a.pairs = r->rot / 2, a.D = r->D, a.T = T, a.count = count, a.rows = 0;
   for (int i = 0; i < count; ++i) {
     const tmac_rope_item& it = items[i];
-    for (const tmac_view* v : {&it.x, &it.out}) wide = wide && (reinterpret_cast<uintptr_t>(v->data) & 15) == 0 && v->token % 8 == 0 && v->head % 8 == 0;
     in_place = in_place && it.x.data == it.out.data;
     a.item[i] = {static_cast<const char*>(it.x.data), static_cast<char*>(it.out.data), it.x.token * 2, it.x.head * 2, it.out.token * 2, it.out.head * 2, a.rows};
     a.rows += it.H;
   }
-  // side by side: vectors of whole pairs that end at rot; in halves: that end at rot / 2
-  int n = r->interleaved ? (r->rot % 8 == 0 ? 8 : r->rot % 4 == 0 ? 4 : 2) : (half % 8 == 0 ? 8 : half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1);
-  if (n == 8 && !wide) n = 4;
-  a.turning = r->interleaved ? r->rot / n : half / n;
+  a.turning = turning_of(r, n);
   a.slots = a.turning + (in_place ? 0 : (r->D - r->rot) / n);
-  a.by_slots = a.slots == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.slots - 1) / a.slots);
-  return n;
+  a.by_slots = by(a.slots);
+  const int64_t vectors = (int64_t)a.rows * a.slots;
+  const int64_t most = (vectors + 63) / 64, least = (a.rows + 255) / 256;
+  a.slices = (int)std::max<int64_t>(least, std::min<int64_t>(most, (8192 + T - 1) / T));
+  a.per_slice = (a.rows + a.slices - 1) / a.slices;
+  a.slices = (a.rows + a.per_slice - 1) / a.per_slice;
 }
 
 template <bool BF16, bool INTERLEAVED>
@@ -349,18 +447,17 @@ static const void* rotate_of(int n) {
   if (n == 2 || INTERLEAVED) return (const void*)rotate_kernel<BF16, INTERLEAVED, 2>;
   return (const void*)rotate_kernel<BF16, false, 1>;
 }
-
-static tmac_status rotate(RopeArgs& a, const tmac_rope* r, const tmac_rope_item* items, int count, int T, void* stream) {
-  const int n = rope_plan(a, r, items, count, T);
-  // Wavefronts of a token: until the chip has some thousands, or a wavefront one vector a lane left; at most 256 rows each
-  const int64_t vectors = (int64_t)a.rows * a.slots;
-  const int64_t most = (vectors + 63) / 64, least = (a.rows + 255) / 256;
-  a.slices = (int)std::max<int64_t>(least, std::min<int64_t>(most, (4096 + T - 1) / T));
-  a.per_slice = (a.rows + a.slices - 1) / a.slices;
-  a.slices = (a.rows + a.per_slice - 1) / a.per_slice;
-  const void* kernel = r->elem == TMAC_ELEM_BF16 ? (r->interleaved ? rotate_of<true, true>(n) : rotate_of<true, false>(n))
-                                                 : (r->interleaved ? rotate_of<false, true>(n) : rotate_of<false, false>(n));
-  return launch(kernel, ((int64_t)T * a.slices + 3) / 4, 256, &a, stream);
+template <typename Code, bool BF16, bool INTERLEAVED>
+static const void* store_of(int n) {
+  if (n == 8) return (const void*)store_kernel<Code, BF16, INTERLEAVED, 8>;
+  if (n == 4) return (const void*)store_kernel<Code, BF16, INTERLEAVED, 4>;
+  if (n == 2 || INTERLEAVED) return (const void*)store_kernel<Code, BF16, INTERLEAVED, 2>;
+  return (const void*)store_kernel<Code, BF16, false, 1>;
+}
+template <typename Code>
+static const void* store_of(bool bf16, bool interleaved, int n) {
+  return bf16 ? (interleaved ? store_of<Code, true, true>(n) : store_of<Code, true, false>(n))
+              : (interleaved ? store_of<Code, false, true>(n) : store_of<Code, false, false>(n));
 }
 
 }  // namespace pages
@@ -381,9 +478,15 @@ extern "C" tmac_status tmac_rotate(const tmac_rope* rope, const tmac_rope_item* 
     rows += it.H;
   }
   if (rope->D > 128 || rows > (1 << 24) || attn::long_axis(T)) return TMAC_EUNSUPPORTED;
+  bool wide = true;
+  for (int i = 0; i < count; ++i) wide = wide && pages::wide_rows(items[i].x, rope->D) && pages::wide_rows(items[i].out, rope->D);
+  const int n = vector_of(rope, wide);
   RopeArgs a = {};
   a.positions = positions_dev;
-  return rotate(a, rope, items, count, T, stream);
+  plan_rope(a, rope, items, count, T, n);
+  const void* kernel = rope->elem == TMAC_ELEM_BF16 ? (rope->interleaved ? rotate_of<true, true>(n) : rotate_of<true, false>(n))
+                                                    : (rope->interleaved ? rotate_of<false, true>(n) : rotate_of<false, false>(n));
+  return launch(kernel, ((int64_t)T * a.slices + 3) / 4, 256, &a, stream);
 }
 
 extern "C" size_t tmac_pages_code_bytes(const tmac_pages* p) { return pages_ok(p) && p->D <= 128 ? (size_t)units_of(p) * chunks_of(p) * 1024 : 0; }
@@ -407,18 +510,30 @@ extern "C" tmac_status tmac_pages_append(const tmac_pages* p, const tmac_pages_b
   a.pages = view_of(p), a.batch = view_of(batch);
   a.k = static_cast<const char*>(k->data), a.v = static_cast<const char*>(v->data);
   a.k_token = k->token * 2, a.k_head = k->head * 2, a.v_token = v->token * 2, a.v_head = v->head * 2;
-  if (rope) a.freq = rope->freq_dev, a.pairs = rope->rot / 2, a.interleaved = rope->interleaved, a.magnitude = rope->magnitude;
-  a.positions = positions_dev;
-  a.bf16 = elem == TMAC_ELEM_BF16;
-  const int64_t blocks = block_slots(batch, a.slots);
-  if (!attn::launchable(blocks * p->Hkv, 256)) return TMAC_EUNSUPPORTED;
-  if (q) {
-    RopeArgs r = {};
-    r.positions = positions_dev, r.batch = a.batch;
-    const tmac_status st = rotate(r, rope, &item, 1, batch->T, stream);
-    if (st != TMAC_OK) return st;
+  const int D = p->D;
+  const bool wide = pages::wide_rows(*k, D) && pages::wide_rows(*v, D) && (!q || (pages::wide_rows(*q, D) && pages::wide_rows(*q_out, D)));
+  int n = wide ? 8 : 4;
+  if (rope) {
+    n = vector_of(rope, wide);
+    a.freq = rope->freq_dev, a.pairs = rope->rot / 2, a.turning = turning_of(rope, n), a.magnitude = rope->magnitude;
   }
-  return launch(p->code == TMAC_CODE_I8 ? (const void*)store_kernel<I8> : (const void*)store_kernel<E4M3>, blocks * p->Hkv, 256, &a, stream);
+  a.positions = positions_dev;
+  a.vectors = a.turning + (D - 2 * a.pairs) / n;
+  a.by_vectors = by(a.vectors), a.by_pairs = by(std::max(1, a.pairs)), a.by_values = by(D / (n == 8 ? 8 : 4));
+  const int64_t blocks = block_slots(batch, a.slots);
+  // Key heads of a workgroup: as many as leave the chip four workgroups a CU
+  a.heads = (int)std::max<int64_t>(1, std::min<int64_t>(p->Hkv, blocks * p->Hkv / 1024));
+  a.groups = (p->Hkv + a.heads - 1) / a.heads;
+  int64_t workgroups = blocks * a.groups;
+  if (!attn::launchable(workgroups, 256)) return TMAC_EUNSUPPORTED;
+  a.workgroups = (int)workgroups;
+  if (q) {
+    a.q.positions = positions_dev, a.q.batch = a.batch;
+    plan_rope(a.q, rope, &item, 1, batch->T, n);
+    workgroups += ((int64_t)batch->T * a.q.slices + 3) / 4;
+  }
+  const bool bf16 = elem == TMAC_ELEM_BF16, interleaved = rope && rope->interleaved;
+  return launch(p->code == TMAC_CODE_I8 ? store_of<I8>(bf16, interleaved, n) : store_of<E4M3>(bf16, interleaved, n), workgroups, 256, &a, stream);
 }
 
 extern "C" tmac_status tmac_pages_read(const tmac_pages* p, const tmac_pages_batch* batch, int32_t elem, const tmac_view* k, const tmac_view* v,
