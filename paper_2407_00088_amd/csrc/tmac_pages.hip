@@ -33,14 +33,14 @@ struct RopeArgs {
     const char* x;
     char* out;
     int64_t x_token, x_head, out_token, out_head;  // bytes
-    int row;                                       // the first of its heads among all items' heads
+    int slice, H;                                  // its first slice, its heads
   } item[TMAC_ROPE_MAX];
   const double* freq;
   const int64_t* positions;  // null: from the batch
   Batch batch;
   float magnitude;
-  int pairs, D, T, count, rows;            // rows: heads of all items
-  int slots, turning, slices, per_slice;   // vectors of a row, those that turn; wavefronts of a token, rows of one
+  int pairs, D, T, count;
+  int slots, turning, slices, per_slice;   // vectors of a row, those that turn; wavefronts of a token, rows (heads of one item) of each
   uint32_t by_slots;                       // ceil(2^32 / slots), exact for what a slice has; 0: one slot
 };
 
@@ -68,9 +68,15 @@ __device__ __forceinline__ void rotate_rows(const RopeArgs& a, int token, int sl
   constexpr int PAIRS = INTERLEAVED ? N / 2 : N, AT_ONCE = 4;
   const int lane = threadIdx.x & 63;
   const int64_t position = position_of(a.positions, a.batch, token);
-  if (lane < a.pairs) turn[lane] = cos_sin((double)position * a.freq[lane]) * a.magnitude;
-  __builtin_amdgcn_wave_barrier();
-  const int row0 = slice * a.per_slice, n = (min(a.rows, row0 + a.per_slice) - row0) * a.slots;
+  const double freq = lane < a.pairs ? a.freq[lane] : 0.0;
+  int k = 0;
+#pragma unroll
+  for (int j = 1; j < TMAC_ROPE_MAX; ++j) k += j < a.count && slice >= a.item[j].slice;
+  const RopeArgs::Item& it = a.item[k];
+  const int row0 = (slice - it.slice) * a.per_slice, n = (min(it.H, row0 + a.per_slice) - row0) * a.slots;
+  const int64_t x_head = it.x_head, out_head = it.out_head;
+  const char* const x0 = it.x + token * it.x_token + row0 * x_head;
+  char* const out0 = it.out + token * it.out_token + row0 * out_head;
   for (int i0 = 0; i0 < n; i0 += 64 * AT_ONCE) {
     V first[AT_ONCE], second[AT_ONCE];
     char* to[AT_ONCE];
@@ -80,18 +86,19 @@ __device__ __forceinline__ void rotate_rows(const RopeArgs& a, int token, int sl
       const int i = i0 + u * 64 + lane;
       slot[u] = -1;
       if (i >= n) continue;
-      const int r = a.by_slots ? (int)__umulhi((uint32_t)i, a.by_slots) : i, row = row0 + r;
-      slot[u] = i - r * a.slots;
-      int k = 0;
-#pragma unroll
-      for (int j = 1; j < TMAC_ROPE_MAX; ++j) k += j < a.count && row >= a.item[j].row;
-      const RopeArgs::Item& it = a.item[k];
+      const int row = a.by_slots ? (int)__umulhi((uint32_t)i, a.by_slots) : i;
+      slot[u] = i - row * a.slots;
       // a vector that turns, or one of those after the pairs
       const int d = slot[u] < a.turning ? slot[u] * N : 2 * a.pairs + (slot[u] - a.turning) * N;
-      const char* x = it.x + token * it.x_token + (row - it.row) * it.x_head + d * 2;
-      to[u] = it.out + token * it.out_token + (row - it.row) * it.out_head + d * 2;
+      const char* x = x0 + row * x_head + d * 2;
+      to[u] = out0 + row * out_head + d * 2;
       first[u] = *reinterpret_cast<const V*>(x);
       if (!INTERLEAVED && slot[u] < a.turning) second[u] = *reinterpret_cast<const V*>(x + a.pairs * 2);
+    }
+    if (i0 == 0) {
+      // (the first rows are on their way)
+      if (lane < a.pairs) turn[lane] = cos_sin((double)position * freq) * a.magnitude;
+      __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
@@ -420,24 +427,26 @@ static int turning_of(const tmac_rope* r, int n) { return r->interleaved ? r->ro
 static bool wide_rows(const tmac_view& v, int D) { return D % 8 == 0 && (reinterpret_cast<uintptr_t>(v.data) & 15) == 0 && v.token % 8 == 0 && v.head % 8 == 0; }
 
 // How the rows are dealt out.  n: elements of a vector.  Wavefronts of a token: until the chip has some thousands, or a wavefront one vector a lane left;
-// at most 256 rows each.
+// of one item and at most 256 rows each.
 static void plan_rope(RopeArgs& a, const tmac_rope* r, const tmac_rope_item* items, int count, int T, int n) {
   bool in_place = true;
-  a.freq = r->freq_dev, a.magnitude = r->magnitude, a.pairs = r->rot / 2, a.D = r->D, a.T = T, a.count = count, a.rows = 0;
+  a.freq = r->freq_dev, a.magnitude = r->magnitude, a.pairs = r->rot / 2, a.D = r->D, a.T = T, a.count = count;
+  int64_t rows = 0;
   for (int i = 0; i < count; ++i) {
-    const tmac_rope_item& it = items[i];
-    in_place = in_place && it.x.data == it.out.data;
-    a.item[i] = {static_cast<const char*>(it.x.data), static_cast<char*>(it.out.data), it.x.token * 2, it.x.head * 2, it.out.token * 2, it.out.head * 2, a.rows};
-    a.rows += it.H;
+    in_place = in_place && items[i].x.data == items[i].out.data;
+    rows += items[i].H;
   }
   a.turning = turning_of(r, n);
   a.slots = a.turning + (in_place ? 0 : (r->D - r->rot) / n);
   a.by_slots = by(a.slots);
-  const int64_t vectors = (int64_t)a.rows * a.slots;
-  const int64_t most = (vectors + 63) / 64, least = (a.rows + 255) / 256;
-  a.slices = (int)std::max<int64_t>(least, std::min<int64_t>(most, (8192 + T - 1) / T));
-  a.per_slice = (a.rows + a.slices - 1) / a.slices;
-  a.slices = (a.rows + a.per_slice - 1) / a.per_slice;
+  const int64_t slices = std::max<int64_t>(1, std::min((rows * a.slots + 63) / 64, ((int64_t)8192 + T - 1) / T));
+  a.per_slice = (int)std::min<int64_t>(256, (rows + slices - 1) / slices);
+  a.slices = 0;
+  for (int i = 0; i < count; ++i) {
+    const tmac_rope_item& it = items[i];
+    a.item[i] = {static_cast<const char*>(it.x.data), static_cast<char*>(it.out.data), it.x.token * 2, it.x.head * 2, it.out.token * 2, it.out.head * 2, a.slices, it.H};
+    a.slices += (it.H + a.per_slice - 1) / a.per_slice;
+  }
 }
 
 template <bool BF16, bool INTERLEAVED>
