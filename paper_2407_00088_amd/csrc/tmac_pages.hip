@@ -530,8 +530,8 @@ extern "C" tmac_status tmac_pages_append(const tmac_pages* p, const tmac_pages_b
   a.vectors = a.turning + (D - 2 * a.pairs) / n;
   a.by_vectors = by(a.vectors), a.by_pairs = by(std::max(1, a.pairs)), a.by_values = by(D / (n == 8 ? 8 : 4));
   const int64_t blocks = block_slots(batch, a.slots);
-  // Key heads of a workgroup: as many as leave the chip four workgroups a CU
-  a.heads = (int)std::max<int64_t>(1, std::min<int64_t>(p->Hkv, blocks * p->Hkv / 1024));
+  // Key heads of a workgroup: as many as leave the chip two workgroups a CU (8192 tokens of 32 heads of 100: see there)
+  a.heads = (int)std::max<int64_t>(1, std::min<int64_t>(p->Hkv, blocks * p->Hkv / 512));
   a.groups = (p->Hkv + a.heads - 1) / a.heads;
   int64_t workgroups = blocks * a.groups;
   if (!attn::launchable(workgroups, 256)) return TMAC_EUNSUPPORTED;
