@@ -9,4 +9,4 @@ from .runner import LinearLUT  # noqa: F401
 from . import attention  # noqa: F401
 from .attention import KVCache, attn_prompt, attn_weights  # noqa: F401
 from . import pages  # noqa: F401
-from .pages import PagedCache, Rotary  # noqa: F401
+from .pages import PagedCache, PageTable, Rotary  # noqa: F401

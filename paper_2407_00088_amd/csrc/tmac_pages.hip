@@ -198,6 +198,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   int s, j;
   if (!block_of(a.batch, a.slots, blockIdx.x / a.groups, s, j)) return;
   const Sequence seq(a.batch, s);
+  if (j > (seq.n + BT - 2) / BT) return;  // (so that what follows stays below 2^31)
   const int block = max(seq.first, 0) / BT + j;
   // tokens [t0, t1) of the block are the call's
   const int t0 = max(0, seq.first - block * BT), t1 = min(BT, seq.len - block * BT), nt = t1 - t0;
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
   int s, j;
   if (!block_of(a.batch, a.slots, blockIdx.x / a.pages.Hkv, s, j)) return;
   const Sequence seq(a.batch, s);
-  if (seq.n == 0) return;
+  if (seq.n == 0 || j > (seq.n + BT - 2) / BT) return;
   // (rows before the first token: blocks count from the first row's, which may be below zero)
   const int block = (seq.first >= 0 ? seq.first / BT : -((-(int64_t)seq.first + BT - 1) / BT)) + j;
   const int t0 = max(0, seq.first - block * BT), t1 = min(BT, seq.len - block * BT);

@@ -194,14 +194,13 @@ __device__ __forceinline__ bool outgrown(float x, float& m, float& alpha) {
 
 // A block's keys or values.
 struct Plane {
-  static constexpr int NOWHERE = 1 << 20;
   __amdgpu_buffer_rsrc_t rsrc;
   __device__ __forceinline__ Plane(const char* at, int bytes) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), (short)0, bytes, 0x00020000)) {}
   // (read once: past the caches)
-  __device__ __forceinline__ u4 load16(int lane, int fixed) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane + fixed, 0, 2)); }
+  __device__ __forceinline__ u4 load16(const At& at) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at.lane + at.fixed, 0, 2)); }
   // (the others of the head's tiles read it too)
   __device__ __forceinline__ u4 load16_kept(int lane) const { return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, 0, 0)); }
-  __device__ __forceinline__ u2 load8(int lane, int fixed) const { return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane + fixed, 0, 2)); }
+  __device__ __forceinline__ u2 load8(const At& at) const { return __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at.lane + at.fixed, 0, 2)); }
 };
 
 template <typename Code, int NI, int ROWS>
@@ -219,16 +218,13 @@ struct Rows<Code, NI, 32> {
   int lane;
 
   static __device__ __forceinline__ int row(int lane) { return lane & 31; }
-  // A block's keys or values; what lies past its end reads as zeros.  Of values: a whole run of 32 elements, or the last one of 16, past
-  // which the other half's 16 lanes have nothing
   static __device__ __forceinline__ void load_k(u4 (&k)[NK], const Plane& p, int lane) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[i] = p.load16(lane * 16, i * 1024);
+    for (int i = 0; i < NK; ++i) k[i] = p.load16(Reads32::k(i, lane));
   }
   static __device__ __forceinline__ void load_v(u4 (&v)[NV], const Plane& p, int lane, bool odd) {
-    const int last = odd ? ((lane & 31) < 16 ? (lane >> 5) * 256 + (lane & 31) * 16 : Plane::NOWHERE) : lane * 16;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = p.load16(i == NV - 1 ? last : lane * 16, i * 1024);
+    for (int i = 0; i < NV; ++i) v[i] = p.load16(Reads32::v(i, lane, i == NV - 1, odd));
   }
   __device__ __forceinline__ void begin(const AttendArgs& a, const char* at, bool valid, int sees) {
     const int half = lane >> 5;
@@ -311,16 +307,13 @@ struct Rows<Code, NI, 16> {
   int lane;
 
   static __device__ __forceinline__ int row(int lane) { return lane & 15; }
-  // (keys: tokens 0-15 and 16-31 of four chunks; values: 16 elements)
   static __device__ __forceinline__ void load_k(u4 (&k)[NK], const Plane& p, int lane) {
-    const int at = (lane >> 4) * 512 + (lane & 15) * 16;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[i] = p.load16(at, (i >> 1) * 2048 + (i & 1) * 256);
+    for (int i = 0; i < NK; ++i) k[i] = p.load16(Reads16::k(i, lane));
   }
   static __device__ __forceinline__ void load_v(u2 (&v)[NV], const Plane& p, int lane, bool odd) {
-    const int in = (lane & 15) * 16 + (lane >> 5) * 8, at = in + (lane >> 4 & 1) * 512, last = in + (lane >> 4 & 1) * (odd ? 256 : 512);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = p.load8(i >= NV - 2 ? last : at, (i >> 1) * 1024 + (i & 1) * 256);
+    for (int i = 0; i < NV; ++i) v[i] = p.load8(Reads16::v(i, lane, i >= NV - 2, odd));
   }
   __device__ __forceinline__ void begin(const AttendArgs& a, const char* at, bool valid, int sees) {
     const int quarter = lane >> 4;
@@ -398,9 +391,14 @@ struct Rows<Code, NI, 16> {
 struct Blocks {
   int64_t unit;
   float sk, sv;
-  __device__ __forceinline__ Blocks(const AttendArgs& a, const int32_t* table, int head, int first, int end, int step, int lane) : sk(0.0f), sv(0.0f) {
+  // The page of the lane's block (which may be asked for before it is known where the blocks end).
+  static __device__ __forceinline__ int page_of(const AttendArgs& a, const int32_t* table, int first, int step, int lane) {
+    const int at = (first + lane * step) >> a.pages.shift;
+    return at < a.batch.width ? table[at] : -1;
+  }
+  __device__ __forceinline__ Blocks(const AttendArgs& a, int page, int head, int first, int end, int step, int lane) : sk(0.0f), sv(0.0f) {
     const int mine = first + lane * step;
-    unit = mine < end ? a.pages.unit_of(table, a.batch.width, mine, head) : -1;
+    unit = mine < end && (unsigned)page < (unsigned)a.pages.pages ? a.pages.unit(page, mine & ((1 << a.pages.shift) - 1), head) : -1;
   }
   __device__ __forceinline__ void scales(const AttendArgs& a) {
     if (unit >= 0) {
@@ -414,17 +412,18 @@ struct Blocks {
 };
 
 // Blocks first, first + step, ... before end for one wavefront's rows, whose queries q() loads.  least: tokens that every row sees.
-// R::DEPTH blocks are on their way: a block's keys are requested as soon as the ones in their registers have met the queries, its values as soon as
+// page: of the lane's first block.  R::DEPTH blocks are on their way: a block's keys are requested as soon as the ones in their registers have met the queries, its values as soon as
 // those have met the exponentials.
 template <typename R, typename Q>
-__device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int32_t* table, int head, int first, int end, int step, int least, Q&& q) {
+__device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int32_t* table, int page, int head, int first, int end, int step, int least, Q&& q) {
   const int lane = w.lane, plane = a.pages.plane_bytes();
   const bool odd = a.pages.chunks & 1;
   typename R::KRaw k[R::DEPTH][R::NK];
   typename R::VRaw v[R::DEPTH][R::NV];
   bool loaded = false;
   for (; first < end; first += 64 * step) {
-    Blocks blocks(a, table, head, first, end, step, lane);
+    if (loaded) page = Blocks::page_of(a, table, first, step, lane);
+    Blocks blocks(a, page, head, first, end, step, lane);
     if (!loaded) q();
     loaded = true;
     uint64_t left = __ballot(blocks.unit >= 0);
@@ -486,7 +485,7 @@ struct Meeting {
 };
 template <typename Code, int NI, int ROWS, int WAVES>
 __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work, int s, int head, int tile, int begin, int stop, float* part, float* shared,
-                                          bool again) {
+                                          bool again, int page) {
   typedef Meeting<NI, ROWS, WAVES> M;
   constexpr int W = M::W, PITCH = M::PITCH;
   // (named anew for every piece: else what follows from it is worked out before the first and kept in 40 registers)
@@ -501,7 +500,7 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
   const bool valid = r < work.rows;
   // (the first row of a tile sees least)
   const int least = clamp_to(seq.first + (tile * ROWS) / a.G + 1, work.held);
-  run_blocks(a, x, a.batch.row(s), head, begin + (WAVES == 1 ? 0 : wave), stop, WAVES, least,
+  run_blocks(a, x, a.batch.row(s), page, head, begin + (WAVES == 1 ? 0 : wave), stop, WAVES, least,
              [&] { x.begin(a, a.q + row * a.q_token + hq * a.q_head, valid, valid ? clamp_to(seq.first + i + 1, work.held) : 0x7fffffff); });
   const float l = x.sum();
   auto put = [&](int row, int hq, int in, int d, const f4& o, float m, float l) {
@@ -546,9 +545,10 @@ template <typename Code, int NI, int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_whole_kernel(const AttendArgs a) {
   __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
   const int head = blockIdx.x % a.pages.Hkv, x = blockIdx.x / a.pages.Hkv, tile = x % a.few.tiles, s = x / a.few.tiles;
+  const int page = Blocks::page_of(a, a.batch.row(s), threadIdx.x >> 6, WAVES, threadIdx.x & 63);  // (beside the lengths)
   const Work work = Work::of<ROWS>(a, a.few, Sequence(a.batch, s));
   if (tile >= work.tiles) return;
-  run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
+  run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false, page);
 }
 
 // A workgroup's equal share of all units, in order: piece(work, sequence, head, tile, first and last block, whether that is the whole segment, whether there
@@ -621,7 +621,8 @@ __device__ __forceinline__ float* part_at(const AttendArgs::Side& side, int w, i
 template <typename Code, int NI, int ROWS, int WAVES>
 __device__ __forceinline__ void run_share(const AttendArgs& a, int w, float* shared, int (*numbers)[64]) {
   walk_share<ROWS>(a, a.few, w, numbers, [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
-    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.few, w, begin, part_floats(ROWS, NI * 32)), shared, again);
+    const int page = Blocks::page_of(a, a.batch.row(s), begin + (int)(threadIdx.x >> 6), WAVES, threadIdx.x & 63);
+    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.few, w, begin, part_floats(ROWS, NI * 32)), shared, again, page);
   });
 }
 template <typename Code, int NI, int ROWS>
@@ -662,7 +663,7 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
   const int held_blocks = (work.held + BT - 1) / BT;
   int placed = begin;
   auto places = [&] {
-    Blocks x(a, table, head, placed * 2, held_blocks, 1, lane);
+    Blocks x(a, Blocks::page_of(a, table, placed * 2, 1, lane), head, placed * 2, held_blocks, 1, lane);
     x.scales(a);
     if (x.unit < 0) x.sk = 1.0f, x.sv = -1.0f;  // (a block that is not there: no token of it is seen)
     return x;
@@ -934,7 +935,7 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
   if (few.on) {
     few.rows = most > 16 && !many.on ? 32 : 16, few.waves = 4;
     few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
-    few.tiles = few.rows == 32 ? 2 : 1;
+    few.tiles = few.rows == 32 ? (int)((most + 31) / 32) : 1;
     const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
     few.whole = !many.on && blocks <= (segments < 256 ? 48 : 128) && segments * 256 <= 0xffffffff;
     if (few.whole) {

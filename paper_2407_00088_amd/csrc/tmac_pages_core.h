@@ -54,6 +54,27 @@ __host__ __device__ __forceinline__ int value_at(int chunks, int token, int d) {
 // The token of byte j of a half's 16.
 __host__ __device__ __forceinline__ int value_token(int half, int j) { return (j >> 3) * 8 + (j >> 2 & 1) * 16 + half * 4 + (j & 3); }
 
+// What a lane reads of a block's keys and values as operands of 32 or 16 rows (tmac_pages_attn.hip): bytes, of which `fixed` are the
+// same for all lanes.  Chunks and runs that are not there lie past the plane's end or NOWHERE, and read as zeros.
+struct At {
+  int lane, fixed;
+};
+constexpr int NOWHERE = 1 << 20;
+struct Reads32 {  // v_mfma_f32_32x32x16: load i has 32 elements; keys: token lane & 31, 16 elements; values: element lane & 31, a half's 16 tokens
+  static __host__ __device__ __forceinline__ At k(int i, int lane) { return {lane * 16, i * 1024}; }
+  // last: of a row's runs of 32; odd: that has 16 elements only
+  static __host__ __device__ __forceinline__ At v(int i, int lane, bool last, bool odd) {
+    const int half = lane >> 5, d = lane & 31;
+    return {last && odd ? (d < 16 ? half * 256 + d * 16 : NOWHERE) : lane * 16, i * 1024};
+  }
+};
+struct Reads16 {  // v_mfma_f32_16x16x32: keys: load i has tokens 0-15 or 16-31 of 64 elements, a quarter's 16; values: 16 elements, a quarter's 8 tokens
+  static __host__ __device__ __forceinline__ At k(int i, int lane) { return {(lane >> 4) * 512 + (lane & 15) * 16, (i >> 1) * 2048 + (i & 1) * 256}; }
+  static __host__ __device__ __forceinline__ At v(int i, int lane, bool last, bool odd) {
+    return {(lane & 15) * 16 + (lane >> 5) * 8 + (lane >> 4 & 1) * (last && odd ? 256 : 512), (i >> 1) * 1024 + (i & 1) * 256};
+  }
+};
+
 // --- sequences of a call -----------------------------------------------------------------------------------------------------
 
 struct Batch {
@@ -71,7 +92,7 @@ struct Sequence {
   __device__ __forceinline__ Sequence(const Batch& b, int s) {
     row0 = b.start(s);
     n = max(0, b.start(s + 1) - row0);
-    len = max(0, b.lens[s]);
+    len = clamp_to(b.lens[s], 1 << 30);
     first = len - n;
   }
 };

@@ -1,7 +1,10 @@
-"""The attention half of a decoder layer with low-bit projections: q, k, v and o through runner.LinearLUT, positions by rotation
-(plain torch), attention over prompts, a cache that keeps the heaviest keys, and decode steps of a batch that may share a prefix.
+"""The attention half of a decoder layer with low-bit projections: q, k, v and o through runner.LinearLUT, positions by rotation.
 
-  python -m paper_2407_00088_amd.decoder      # prompts, then a few decode steps, of a small random layer
+  DecoderAttention       attention over prompts, a cache that keeps the heaviest keys, and decode steps of a batch that may share a prefix
+                         (rotation in plain torch)
+  PagedDecoderAttention  all tokens in pages of 8 bits, rotated on their way in: prompts, chunks, drafts and steps by one call
+
+  python -m paper_2407_00088_amd.decoder      # prompts, then a few decode steps, of small random layers
 """
 from __future__ import annotations
 
@@ -9,6 +12,7 @@ import torch
 
 from . import binding as B
 from .attention import KVCache, attn_prompt, attn_weights
+from .pages import PagedCache, PageTable, Rotary
 
 
 def rotated(x, positions, base: float = 10000.0):
@@ -80,6 +84,35 @@ class DecoderAttention:
         return self.o.forward_one_call(out.view(x.shape[0], -1), out_t=B.TMAC_OUT_F16)
 
 
+class PagedDecoderAttention:
+    """q, k, v, o: as for DecoderAttention.  `pages` pages of `page` tokens for all `batch` sequences, at most `width` for each."""
+
+    def __init__(self, q, k, v, o, Hq: int, Hkv: int, batch: int, pages: int, width: int, page: int = 64, code: str = "e4m3", scaling=None):
+        self.q, self.k, self.v, self.o, self.Hq, self.Hkv = q, k, v, o, Hq, Hkv
+        self.D = q.M // Hq
+        self.table = PageTable(batch, width, pages, page)
+        self.cache = PagedCache(pages, Hkv, self.D, page, code, Hq=Hq, rotary=Rotary(self.D, scaling=scaling))
+
+    def forward(self, x, counts):
+        """counts[s] more tokens of every sequence (a prompt, a chunk of it, drafts, one token, none), packed: x [T, M] (fp16).  Returns [T, M]."""
+        if x.shape[0] != sum(counts):
+            raise ValueError(f"{x.shape[0]} rows for {sum(counts)} tokens")
+        cu, most = self.table.extend(counts)
+        where = (self.table.table, self.table.lens, cu)
+        q, k, v = (lin.forward_one_call(x, out_t=B.TMAC_OUT_F16).view(x.shape[0], -1, self.D) for lin in (self.q, self.k, self.v))
+        q = self.cache.append(k, v, *where, q=q, most=most)
+        out, _ = self.cache.attend(q, *where, most=most)
+        return self.o.forward_one_call(out.view(x.shape[0], -1), out_t=B.TMAC_OUT_F16)
+
+    def step(self, x):
+        """One token of every sequence: x [batch, M].  Returns [batch, M]."""
+        return self.forward(x, [1] * self.table.batch)
+
+    def take_back(self, counts) -> None:
+        """The last counts[s] tokens of every sequence leave: drafts that were not accepted, or all of a sequence that has ended."""
+        self.table.take_back(counts)
+
+
 def random_layer(M: int, Hq: int, Hkv: int, D: int, batch: int, capacity: int, recent: int, max_N: int, bits: int = 4, group: int = 64,
                  seed: int = 0) -> DecoderAttention:
     """A layer of random weights, scaled so that unit inputs give projections of about one."""
@@ -94,6 +127,11 @@ def random_layer(M: int, Hq: int, Hkv: int, D: int, batch: int, capacity: int, r
         return LinearLUT(rows, cols, bits, group, q, s, max_N=max_N, layout=B.TMAC_LAYOUT_R64K32)
 
     return DecoderAttention(linear(Hq * D, M), linear(Hkv * D, M), linear(Hkv * D, M), linear(M, Hq * D), Hq, Hkv, batch, capacity, recent)
+
+
+def paged(layer: DecoderAttention, pages: int, width: int, page: int = 64, code: str = "e4m3") -> PagedDecoderAttention:
+    """The same projections on pages of 8 bits."""
+    return PagedDecoderAttention(layer.q, layer.k, layer.v, layer.o, layer.Hq, layer.Hkv, layer.cache.B, pages, width, page, code)
 
 
 def main(steps: int = 8) -> None:
@@ -111,6 +149,12 @@ def main(steps: int = 8) -> None:
         y = layer.step(x(batch))
         print(f"step {t}: rms {float(y.float().square().mean().sqrt()):.3f}, slots in use {layer.cache.lens[:, 0].tolist()}, "
               f"tokens seen {layer.cache.seen[:, 0].tolist()}")
+    pages = paged(layer, pages=24, width=8, page=32)
+    y = pages.forward(x(sum(lengths)), lengths)
+    print(f"the same lengths in pages of 8 bits: rms {float(y.float().square().mean().sqrt()):.3f}, pages in use {[len(o) for o in pages.table.owned]}")
+    for t in range(steps):
+        y = pages.step(x(batch))
+        print(f"step {t}: rms {float(y.float().square().mean().sqrt()):.3f}, tokens {pages.table.length}")
 
 
 if __name__ == "__main__":

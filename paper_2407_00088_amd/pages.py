@@ -210,11 +210,16 @@ class PagedCache:
             raise ValueError(f"rotary turns heads of {value.D} elements, the cache has {self.D}")
         super().__setattr__(name, value)
 
-    _grown = A.KVCache._grown
-
-    @property
-    def k(self):
-        return self.codes  # (_grown asks it for the device)
+    def _grown(self, n: int, stream):
+        """A workspace of n bytes at least; one that is too small is kept, as KVCache does."""
+        ws = self.attend_ws
+        if ws is None or ws.numel() < n:
+            if ws is not None:
+                self.outgrown.append(ws)
+                n = max(n, 2 * ws.numel())
+            with A._on(stream):
+                self.attend_ws = A._workspace(n, self.codes.device)
+        return self.attend_ws
 
     def _batch(self, T: int, table, lens, cu, most) -> tmac_pages_batch:
         S = lens.shape[0] if isinstance(lens, torch.Tensor) and lens.dim() else 0
@@ -321,7 +326,62 @@ class PagedCache:
             A._same_device(self.codes, q, out, lse, table, lens, cu)
             if T:
                 n = lib.tmac_pages_attend_workspace_bytes(self.desc, self.cache, batch)
-                self.attend_ws = self._grown(self.attend_ws, n, stream)
-                B._check(lib.tmac_pages_attend(self.desc, self.cache, batch, _row_view(q), _row_view(out), lse.data_ptr(), self.attend_ws.data_ptr(), n,
-                                               B._stream_ptr(stream)), "tmac_pages_attend")
+                B._check(lib.tmac_pages_attend(self.desc, self.cache, batch, _row_view(q), _row_view(out), lse.data_ptr(), self._grown(n, stream).data_ptr(),
+                                               n, B._stream_ptr(stream)), "tmac_pages_attend")
             return out, lse
+
+
+class PageTable:
+    """Which pages belong to which of `batch` sequences, and how many tokens these have, on the host and on the GPU:
+
+      table  int32 [batch, width]  pages of each sequence, -1 behind them       lens  int32 [batch]
+
+    The tensors keep their place (a captured graph that was given them sees what extend() and the others put there since).
+    """
+
+    def __init__(self, batch: int, width: int, pages: int, page: int = 64, device: str = "cuda"):
+        if min(batch, width, pages, page) < 1:
+            raise ValueError(f"batch ({batch}), width ({width}), pages ({pages}) and page ({page}) are above zero")
+        self.batch, self.width, self.page = batch, width, page
+        self.free = list(range(pages - 1, -1, -1))
+        self.owned = [[] for _ in range(batch)]
+        self.length = [0] * batch
+        self.table = torch.full((batch, width), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
+
+    def _write(self, table: bool) -> None:
+        self.lens.copy_(torch.tensor(self.length, dtype=torch.int32))
+        if table:
+            self.table.copy_(torch.tensor([own + [-1] * (self.width - len(own)) for own in self.owned], dtype=torch.int32))
+
+    def extend(self, counts: Sequence[int]):
+        """Room for so many more tokens of each sequence.  Returns (cu int32 [batch + 1], the most of one sequence) for the calls that are
+        about these tokens.  Without room for all of them nothing changes."""
+        if len(counts) != self.batch or min(counts) < 0:
+            raise ValueError(f"a count for each of {self.batch} sequences, got {list(counts)}")
+        need = [-(-(n + c) // self.page) - len(own) for n, c, own in zip(self.length, counts, self.owned)]
+        if any(len(own) + n > self.width for own, n in zip(self.owned, need)):
+            raise ValueError(f"a sequence has at most {self.width} pages of {self.page} tokens")
+        if sum(need) > len(self.free):
+            raise MemoryError(f"{sum(need)} pages are needed, {len(self.free)} are free")
+        for s, n in enumerate(need):
+            self.owned[s] += [self.free.pop() for _ in range(n)]
+            self.length[s] += counts[s]
+        self._write(any(need))
+        cu = torch.zeros(self.batch + 1, dtype=torch.int32)
+        torch.cumsum(torch.tensor(counts, dtype=torch.int32), 0, out=cu[1:])
+        return cu.to(self.lens.device), max(counts)
+
+    def take_back(self, counts: Sequence[int]) -> None:
+        """The last tokens of each sequence leave (drafts that were not accepted, or all of a sequence that has ended); pages that hold none any
+        more are free again."""
+        if len(counts) != self.batch or any(not 0 <= c <= n for c, n in zip(counts, self.length)):
+            raise ValueError(f"of each sequence at most as many as it has ({self.length}), got {list(counts)}")
+        freed = False
+        for s, c in enumerate(counts):
+            self.length[s] -= c
+            keep = -(-self.length[s] // self.page)
+            freed |= len(self.owned[s]) > keep
+            self.free += reversed(self.owned[s][keep:])
+            del self.owned[s][keep:]
+        self._write(freed)
