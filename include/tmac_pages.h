@@ -20,17 +20,17 @@ extern "C" {
  * A pair (a, b) of a head's elements at position p turns by p f_i:
  *   a' = a c - b s,  b' = a s + b c,  c = magnitude cos(p f_i),  s = magnitude sin(p f_i)
  * Pair i is elements (i, i + rot / 2), or (2 i, 2 i + 1) where interleaved; elements from rot on stay as they are.  Positions may be
- * negative (the turn back: with -p and 1 / magnitude the rotation's inverse, with -p and magnitude its gradient).  Angles are taken in
- * 64 bits, cosines, sines and products in 32, results are rounded once.
+ * negative (the turn back: with -p and 1 / magnitude the rotation's inverse, with -p and magnitude its gradient).  Angles,
+ * cosines and sines are taken in 64 bits and rounded to 32, products are 32-bit, results are rounded once.
  *   freq_dev  fp64 [rot / 2], radians a position, 8-byte aligned
  *   D         a multiple of 4, at most 128; rot even, 2 <= rot <= D; magnitude finite */
 typedef struct {
   const double* freq_dev;
+  double  magnitude;
   int32_t D, rot;
   int32_t interleaved;  /* 0 or 1 */
   int32_t elem;         /* tmac_elem_t */
-  float   magnitude;
-  int32_t reserved[3];  /* must be 0 */
+  int32_t reserved[2];  /* must be 0 */
 } tmac_rope;
 
 /* One tensor [T, H, D] by strides (token, head) and where its result goes: x itself (the same data and strides) or memory that does
@@ -115,8 +115,8 @@ tmac_status tmac_pages_read(const tmac_pages* pages, const tmac_pages_batch* bat
 /* Attention of the call's tokens over what is in the pages: row i of sequence s's n rows sees the tokens j <= lens[s] - n + i that are on
  * a page.  Notation and rules of values as in tmac_attn.h; desc->causal is 1.  Products are of the queries in fp16 (a bf16 row is first scaled by
  * a power of two to its range, which is exact down to 2^-38 of its largest element) with codes, which fp16 holds exactly; scores, exponentials,
- * sums and lse are 32-bit, exponentials times the scale of the values' block are rounded to fp16 for the second product: below 2^-20 of the row's
- * largest such product they are off by up to 2^-31 of it.
+ * sums and lse are 32-bit, exponentials times the scale of the values' block are fp16 in the second product, as the sum of two such numbers in tiles of 16 rows and
+ * as one in larger ones: off by 2^-22 or 2^-11 of themselves, and below 2^-20 of the row's largest by up to 2^-31 of that.
  *   q, out    [T, Hq, D] (token, head strides);  lse_dev  fp32 [Hq, T], or NULL
  *   workspace tmac_pages_attend_workspace_bytes(desc, pages, batch), 16-byte aligned, contents arbitrary
  * The order of the sums depends on sizes and lengths only.  Rows from cu[S] on stay as they are.

@@ -15,16 +15,17 @@ namespace pages {
 
 // --- rotation -----------------------------------------------------------------------------------------------------------------------
 
-// Cosine and sine of an angle.  The quarter turns are taken off in 64 bits (a position of 2^20 leaves 2^-35 of a turn), what is left,
-// |x| <= pi / 4, has Taylor's polynomials up to x^9 and x^10: off by at most 2e-9, below the last digit of 32 bits.
-__device__ __forceinline__ f2 cos_sin(double angle) {
+// Cosine and sine of an angle, times magnitude, rounded to 32 bits once.  The quarter turns are taken off (a position of 2^20 leaves 2^-35 of a turn), what
+// is left, |x| <= pi / 4, has Taylor's polynomials up to x^13 and x^14, off by at most 2e-14.  All in 64 bits, whose products are as fast here: in 32 the last
+// digit was off by one or two, and keys near the middle between two codes took the other one more often.
+__device__ __forceinline__ f2 cos_sin(double angle, double magnitude) {
   const double quarters = angle * 0.63661977236758134308;  // 2 / pi
   const double whole = __builtin_rint(quarters);
-  const float x = (float)(quarters - whole) * 1.57079632679489661923f, y = x * x;
-  const float s = x * (1.0f + y * (-1.0f / 6 + y * (1.0f / 120 + y * (-1.0f / 5040 + y * (1.0f / 362880)))));
-  const float c = 1.0f + y * (-0.5f + y * (1.0f / 24 + y * (-1.0f / 720 + y * (1.0f / 40320 + y * (-1.0f / 3628800)))));
+  const double x = (quarters - whole) * 1.57079632679489661923, y = x * x;
+  const double s = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 + y * (-1.0 / 39916800 + y * (1.0 / 6227020800.0)))))));
+  const double c = 1.0 + y * (-0.5 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800 + y * (1.0 / 479001600 + y * (-1.0 / 87178291200.0)))))));
   const int turn = (int)(whole - 4.0 * __builtin_floor(whole * 0.25));
-  const float cc = turn & 1 ? s : c, ss = turn & 1 ? c : s;
+  const float cc = (float)((turn & 1 ? s : c) * magnitude), ss = (float)((turn & 1 ? c : s) * magnitude);
   return f2{turn == 1 || turn == 2 ? -cc : cc, turn >= 2 ? -ss : ss};
 }
 
@@ -38,7 +39,7 @@ struct RopeArgs {
   const double* freq;
   const int64_t* positions;  // null: from the batch
   Batch batch;
-  float magnitude;
+  double magnitude;
   int pairs, D, T, count;
   int slots, turning, slices, per_slice;   // vectors of a row, those that turn; wavefronts of a token, rows (heads of one item) of each
   uint32_t by_slots;                       // ceil(2^32 / slots), exact for what a slice has; 0: one slot
@@ -97,7 +98,7 @@ __device__ __forceinline__ void rotate_rows(const RopeArgs& a, int token, int sl
     }
     if (i0 == 0) {
       // (the first rows are on their way)
-      if (lane < a.pairs) turn[lane] = cos_sin((double)position * freq) * a.magnitude;
+      if (lane < a.pairs) turn[lane] = cos_sin((double)position * freq, a.magnitude);
       __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
@@ -151,7 +152,7 @@ struct StoreArgs {
   int64_t k_token, k_head, v_token, v_head;  // bytes
   const double* freq;                        // null: keys as they are
   const int64_t* positions;
-  float magnitude;
+  double magnitude;
   int pairs, turning, vectors;               // vectors of a row of keys, those that turn
   uint32_t by_vectors, by_pairs, by_values;  // ceil(2^32 / n); 0: n is 1
   int slots;                                 // blocks of a sequence that have workgroups; 0: starts[s] / 32 + 2 s on
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   for (int i = tid; i < nt * a.pairs; i += 256) {
     const int t = divided(i, a.by_pairs), p = i - t * a.pairs;
     const int64_t position = a.positions ? a.positions[row0 + t] : (int64_t)block * BT + t0 + t;
-    turn[i] = cos_sin((double)position * a.freq[p]) * a.magnitude;
+    turn[i] = cos_sin((double)position * a.freq[p], a.magnitude);
   }
   if (unit0 < 0) return;
   const int codes = chunks * BT;  // 16 of them a thread, in either plane
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
 static bool rope_ok(const tmac_rope* r) {
   return r && r->freq_dev && (reinterpret_cast<uintptr_t>(r->freq_dev) & 7) == 0 && r->D > 0 && r->D % 4 == 0 && r->rot >= 2 && r->rot % 2 == 0 &&
          r->rot <= r->D && (r->interleaved == 0 || r->interleaved == 1) && (r->elem == TMAC_ELEM_F16 || r->elem == TMAC_ELEM_BF16) &&
-         std::isfinite(r->magnitude) && !r->reserved[0] && !r->reserved[1] && !r->reserved[2];
+         std::isfinite(r->magnitude) && !r->reserved[0] && !r->reserved[1];
 }
 
 static uint32_t by(int n) { return n == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n); }

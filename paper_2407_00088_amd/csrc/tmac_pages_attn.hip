@@ -335,7 +335,9 @@ struct Rows<Code, NI, 16> {
       }
     return s;
   }
-  struct Weights { h8 p; };  // tokens 0-3 of the quarter's four and 16 on
+  // Tokens 0-3 of the quarter's four and 16 on.  As two fp16 numbers each, so that the result is off by its own rounding only: eight more of the short matrix
+  // instructions a block, which memory's time hides (a batch's step 46 us with and without).
+  struct Weights { h8 p, rest; };
   static __device__ __forceinline__ float over_row(float x, bool adds) {
     const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
     const float a = __builtin_bit_cast(float, (unsigned)r[0]), b = __builtin_bit_cast(float, (unsigned)r[1]);
@@ -372,11 +374,17 @@ struct Rows<Code, NI, 16> {
     Weights w;
 #pragma unroll
     for (int r = 0; r < 8; ++r) w.p[r] = (_Float16)s[r];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) w.rest[r] = (_Float16)(s[r] - (float)w.p[r]);
     return w;
   }
   __device__ __forceinline__ void multiply(const u2 (&v)[NV], const Weights& w) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<Code>(v[i][0], v[i][1]), w.p, o[i], 0, 0, 0);
+    for (int i = 0; i < NV; ++i) {
+      const h8 x = halves_of<Code>(v[i][0], v[i][1]);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w.p, o[i], 0, 0, 0);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w.rest, o[i], 0, 0, 0);
+    }
   }
   __device__ __forceinline__ float sum() const { return over_row(l, true); }
   template <typename F>

@@ -29,8 +29,8 @@ EXPORTS = ["tmac_rotate", "tmac_pages_code_bytes", "tmac_pages_scale_bytes", "tm
 
 
 class tmac_rope(C.Structure):
-    _fields_ = [("freq_dev", C.c_void_p), ("D", C.c_int32), ("rot", C.c_int32), ("interleaved", C.c_int32), ("elem", C.c_int32),
-                ("magnitude", C.c_float), ("reserved", C.c_int32 * 3)]
+    _fields_ = [("freq_dev", C.c_void_p), ("magnitude", C.c_double), ("D", C.c_int32), ("rot", C.c_int32), ("interleaved", C.c_int32),
+                ("elem", C.c_int32), ("reserved", C.c_int32 * 2)]
 
 
 class tmac_rope_item(C.Structure):
@@ -129,7 +129,7 @@ class Rotary:
         f, self.magnitude = frequencies(rot, base, scaling)
         self.D, self.rot, self.interleaved = D, rot, bool(interleaved)
         self.freq = f.to(device)
-        self.rope = {dt: tmac_rope(self.freq.data_ptr(), D, rot, int(self.interleaved), elem, self.magnitude) for dt, elem in A._ELEM.items()}
+        self.rope = {dt: tmac_rope(self.freq.data_ptr(), self.magnitude, D, rot, int(self.interleaved), elem) for dt, elem in A._ELEM.items()}
 
     def rotate(self, positions, *tensors, out: Optional[Sequence] = None, stream=None):
         """Tensors [T, H, D] of the same T tokens (up to four, H their own) turned by positions int64 [T].  Returns a tuple of as many; `out`:

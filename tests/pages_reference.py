@@ -21,13 +21,13 @@ def turned(x, positions, freq, magnitude, interleaved):
 
 
 def turned_bound(x, freq, magnitude, interleaved):
-    """How far 32-bit arithmetic may be from it before the last rounding: cosines and sines in 32 bits are off by at most 3 units (the
-    polynomial's sums and, for a magnitude, one product more), each of the two products and their sum by one of the size of what is added; the
-    angle's error in 64 bits, 2^-52 of it or 2^-30 at angles of 2^22, is far below: together at most 8 * 2^-24 (|u| + |v|) magnitude."""
+    """How far 32-bit arithmetic may be from it before the last rounding: cosines and sines are rounded once (half a unit 2^-24 of at most the
+    magnitude), each of the two products and their sum once (half a unit of the size of what is added); the angle's error in 64 bits, 2^-52 of it or
+    2^-30 at angles of 2^22, and the polynomials' are far below: together at most 1.5 * 2^-24 (|u| + |v|) magnitude, of which twice is allowed."""
     x, rot = x.double().abs(), 2 * len(freq)
     at = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
     b = torch.zeros_like(x)
-    both = (x[..., at[0]] + x[..., at[1]]) * abs(magnitude) * 8 * 2.0 ** -24
+    both = (x[..., at[0]] + x[..., at[1]]) * abs(magnitude) * 3 * 2.0 ** -24
     b[..., at[0]], b[..., at[1]] = both, both
     return b
 

@@ -42,7 +42,7 @@ BAD_VIEWS = [view(data=None), view(data=P16 + 4), view(token=130), view(head=-64
 
 
 def rope(**kw):
-    return changed(G.tmac_rope(P16, 64, 64, 0, 0, 1.0), kw)
+    return changed(G.tmac_rope(P16, 1.0, 64, 64, 0, 0), kw)
 
 
 def item(**kw):
