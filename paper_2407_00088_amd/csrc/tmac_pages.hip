@@ -231,24 +231,27 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   };
   load(h0);
   const int64_t unit0 = a.pages.unit_of(a.batch.row(s), a.batch.width, block, h0);
+  const int codes = chunks * BT;  // 16 of them a thread, in either plane
+  // what a block that was begun before holds: its scales, the thread's values
+  f2 was = {0.0f, 0.0f};
+  u4 old = {0u, 0u, 0u, 0u};
+  auto load_old = [&](int64_t unit) {
+    if (t0 == 0 || unit0 < 0) return;
+    was = *reinterpret_cast<const f2*>(a.pages.scales + unit * 2);
+    if (tid < codes) old = *(reinterpret_cast<const u4*>(a.pages.values(unit)) + tid);
+  };
+  load_old(unit0);
   for (int i = tid; i < nt * a.pairs; i += 256) {
     const int t = divided(i, a.by_pairs), p = i - t * a.pairs;
     const int64_t position = a.positions ? a.positions[row0 + t] : (int64_t)block * BT + t0 + t;
     turn[i] = cos_sin((double)position * a.freq[p], a.magnitude);
   }
   if (unit0 < 0) return;
-  const int codes = chunks * BT;  // 16 of them a thread, in either plane
   __syncthreads();
   for (int head = h0; head < h1; ++head) {
     const int64_t unit = unit0 + ((int64_t)(head - h0) << a.pages.shift);
     float* scales = a.pages.scales + unit * 2;
     u4* const v_to = reinterpret_cast<u4*>(a.pages.values(unit)) + tid;
-    float was[2] = {0.0f, 0.0f};
-    u4 old = {0u, 0u, 0u, 0u};
-    if (t0) {
-      was[0] = scales[0], was[1] = scales[1];
-      if (tid < codes) old = *v_to;
-    }
     float mk = 0.0f, mv = 0.0f;
     auto take = [](float& most, float x) { most = fmaxf(most, fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.0f); };
 #pragma unroll
@@ -353,7 +356,10 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
       }
       *v_to = old;
     }
-    if (head + 1 < h1) __syncthreads();  // (the rows have been read)
+    if (head + 1 < h1) {
+      load_old(unit + ((int64_t)1 << a.pages.shift));
+      __syncthreads();  // (the rows have been read)
+    }
   }
 }
 

@@ -667,6 +667,8 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
   const int least = clamp_to(seq.first + first / a.G + 1, work.held), most = first < work.rows ? clamp_to(seq.first + last / a.G + 1, work.held) : 0;
   const int32_t* table = a.batch.row(s);
   const int plane = a.pages.plane_bytes(), chunks = a.pages.chunks;
+  // (stages that no row of the tile sees: shares count them)
+  stop = max(begin, min(stop, (clamp_to(seq.first + (min((tile + 1) * TILE, work.rows) - 1) / a.G + 1, work.held) + STAGE - 1) / STAGE));
   // places and scales of 32 stages' blocks, one a lane; a stage's raw codes, 16 bytes of each plane a thread
   const int held_blocks = (work.held + BT - 1) / BT;
   int placed = begin;
@@ -830,8 +832,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a
     const int tile = slot - (int)from(s);
     const Work work = Work::of<TILE>(a, a.many, Sequence(a.batch, s));
     if (tile >= work.tiles) return;
-    const int sees = clamp_to(work.seq.first + (min((tile + 1) * TILE, work.rows) - 1) / a.G + 1, work.held);
-    run_tile<Code, NI>(a, work, s, head, tile, 0, max(1, (sees + STAGE - 1) / STAGE), nullptr, shared, false);
+    run_tile<Code, NI>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
   }
 }
 
