@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "tmac_attn_host.h"
 #include "tmac_internal.h"
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   __shared__ __attribute__((aligned(16))) f2 turn[BT * 64];
   __shared__ __attribute__((aligned(16))) float keys[BT][132];
   __shared__ __attribute__((aligned(16))) uint16_t values[BT][136];
-  __shared__ float most[2][2][4];
+  __shared__ float most[3][2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if ((int)blockIdx.x >= a.workgroups) {
     const int64_t w = (int64_t)(blockIdx.x - a.workgroups) * 4 + wave;
@@ -252,8 +253,9 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
     const int64_t unit = unit0 + ((int64_t)(head - h0) << a.pages.shift);
     float* scales = a.pages.scales + unit * 2;
     u4* const v_to = reinterpret_cast<u4*>(a.pages.values(unit)) + tid;
-    float mk = 0.0f, mv = 0.0f;
-    auto take = [](float& most, float x) { most = fmaxf(most, fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.0f); };
+    // the largest, and zero where all are finite
+    float mk = 0.0f, mv = 0.0f, odd_k = 0.0f, odd_v = 0.0f;
+    auto take = [](float& most, float& odd, float x) { most = fmaxf(most, fabsf(x)), odd = __builtin_fmaf(x, 0.0f, odd); };
 #pragma unroll
     for (int u = 0; u < KI; ++u) {
       const int i = tid + u * 256;
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
           float& y = INTERLEAVED ? lo[2 * p + (N > 1)] : hi[p];
           const float x1 = x * cs[0] - y * cs[1], y1 = x * cs[1] + y * cs[0];
           x = x1, y = y1;
-          take(mk, x1), take(mk, y1);
+          take(mk, odd_k, x1), take(mk, odd_k, y1);
         }
         if (!INTERLEAVED) {
 #pragma unroll
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
         }
       } else {
 #pragma unroll
-        for (int x = 0; x < N; ++x) take(mk, lo[x]);
+        for (int x = 0; x < N; ++x) take(mk, odd_k, lo[x]);
       }
       const int d = slot < a.turning ? slot * N : 2 * a.pairs + (slot - a.turning) * N;
 #pragma unroll
@@ -294,24 +296,39 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
       if (i >= v_count) break;
       const int t = divided(i, a.by_values);
 #pragma unroll
-      for (int x = 0; x < NV; ++x) take(mv, to_float(v_in[u][x], BF16));
+      for (int x = 0; x < NV; ++x) take(mv, odd_v, to_float(v_in[u][x], BF16));
       *reinterpret_cast<VV*>(&values[t0 + t][(i - t * (D / NV)) * NV]) = v_in[u];
     }
     if (head + 1 < h1) load(head + 1);
+    float m[2];
+    auto meet = [&](int place) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mk = fmaxf(mk, __shfl_xor(mk, o)), mv = fmaxf(mv, __shfl_xor(mv, o));
-    const int place = (head - h0) & 1;
-    if (lane == 0) most[place][0][wave] = mk, most[place][1][wave] = mv;
-    __syncthreads();
-    float scale[2];
+      for (int o = 32; o > 0; o >>= 1) mk = fmaxf(mk, __shfl_xor(mk, o)), mv = fmaxf(mv, __shfl_xor(mv, o));
+      if (lane == 0) most[place][0][wave] = mk, most[place][1][wave] = mv;
+      __syncthreads();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float* m = most[place][x];
-      scale[x] = fmaxf(was[x], Code::scale_for(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+      for (int x = 0; x < 2; ++x) m[x] = fmaxf(fmaxf(most[place][x][0], most[place][x][1]), fmaxf(most[place][x][2], most[place][x][3]));
+    };
+    mk = odd_k == 0.0f ? mk : INFINITY, mv = odd_v == 0.0f ? mv : INFINITY;
+    meet((head - h0) & 1);
+    const bool odd = m[0] == INFINITY || m[1] == INFINITY;
+    if (__builtin_expect(odd, 0)) {  // some are infinite or no numbers: the largest of the others
+      mk = mv = 0.0f;
+      for (int i = tid; i < nt * D; i += 256) {
+        const float x = fabsf(keys[t0 + i / D][i % D]), y = fabsf(to_float(values[t0 + i / D][i % D], BF16));
+        mk = x <= 3.402823466e38f ? fmaxf(mk, x) : mk, mv = y <= 3.402823466e38f ? fmaxf(mv, y) : mv;
+      }
+      meet(2);
     }
+    const float scale[2] = {fmaxf(was[0], Code::scale_for(m[0])), fmaxf(was[1], Code::scale_for(m[1]))};
     if (tid == 0) scales[0] = scale[0], scales[1] = scale[1];
-    if (tid < codes) {
-      // keys: token t, elements 16 c ..; new codes, old ones rounded again where the scale has grown, zeros in a block that is begun
+    // New codes, old ones rounded again where the scale has grown, zeros in a block that is begun.  careful: of any numbers
+    auto make = [&](auto careful) {
+      auto encode = [](float a, float b, float c, float d) {
+        if constexpr (decltype(careful)::value) return Code::encode(a == a ? a : 0.0f, b == b ? b : 0.0f, c == c ? c : 0.0f, d == d ? d : 0.0f);
+        else return Code::encode_within(a, b, c, d);
+      };
+      // keys: token t, elements 16 c ..
       const int t = tid % BT, c = tid / BT;
       u4* const k_to = reinterpret_cast<u4*>(a.pages.keys(unit)) + tid;
       if (t >= t0 && t < t1) {
@@ -320,10 +337,8 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const int d = c * 16 + 4 * w;
-          f4 x = d < D ? *reinterpret_cast<const f4*>(&keys[t][d]) : f4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int b = 0; b < 4; ++b) x[b] = x[b] == x[b] ? x[b] * inv : 0.0f;
-          got[w] = Code::encode(x[0], x[1], x[2], x[3]);
+          const f4 x = (d < D ? *reinterpret_cast<const f4*>(&keys[t][d]) : f4{0.0f, 0.0f, 0.0f, 0.0f}) * inv;
+          got[w] = encode(x[0], x[1], x[2], x[3]);
         }
         *k_to = got;
       } else if (t0 == 0) {
@@ -342,19 +357,28 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
       // values: element d, 16 tokens
       const int run = tid / 64, n = value_run(chunks, run * 32), half = (tid - run * 64) / n, d = run * 32 + (tid - run * 64) % n;
       const float inv = 1.0f / scale[1], ratio = was[1] / scale[1];
+      u4 got;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (t0) Code::decode(old[w], y);
+        float y[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int t = value_token(half, 4 * w + b);
-          const float x = to_float(values[t][d], BF16);
-          y[b] = t >= t0 && t < t1 && d < D ? (x == x ? x * inv : 0.0f) : t0 ? y[b] * ratio : 0.0f;
+        for (int b = 0; b < 4; ++b) y[b] = to_float(values[value_token(half, 4 * w + b)][d], BF16) * inv;
+        if (nt < BT) {
+          float before[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          if (t0) Code::decode(old[w], before);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const int t = value_token(half, 4 * w + b);
+            y[b] = t >= t0 && t < t1 ? y[b] : t0 ? before[b] * ratio : 0.0f;
+          }
         }
-        old[w] = Code::encode(y[0], y[1], y[2], y[3]);
+        got[w] = d < D ? encode(y[0], y[1], y[2], y[3]) : 0u;
       }
-      *v_to = old;
+      *v_to = got;
+    };
+    if (tid < codes) {
+      if (__builtin_expect(odd, 0)) make(std::true_type{});
+      else make(std::false_type{});
     }
     if (head + 1 < h1) {
       load_old(unit + ((int64_t)1 << a.pages.shift));

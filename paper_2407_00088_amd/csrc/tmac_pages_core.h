@@ -120,10 +120,19 @@ __device__ __forceinline__ int sequence_of(const Batch& b, int row) {
 struct I8 {
   static constexpr float MOST = 127.0f;
   static __device__ __forceinline__ float scale_for(float most) { return fmaxf(most * (1.0f / MOST), LEAST_SCALE); }
-  // Four numbers, already multiplied by 1 / scale, as codes.
+  // Four numbers, already multiplied by 1 / scale, as codes: any, or such as the scale was made for.
   static __device__ __forceinline__ uint32_t encode(float a, float b, float c, float d) {
     auto one = [](float x) { return (uint32_t)(int)fminf(fmaxf(__builtin_rintf(x), -MOST), MOST) & 0xffu; };
     return one(a) | one(b) << 8 | one(c) << 16 | one(d) << 24;
+  }
+  // Of numbers up to 127.4: 1.5 * 2^23 more, they have no places after the point, and their low byte is the code.  (Not as one operation with the
+  // product that they come from, which is rounded by itself.)
+  static __device__ __forceinline__ uint32_t encode_within(float a, float b, float c, float d) {
+    auto one = [](float x) {
+#pragma clang fp contract(off)
+      return __builtin_bit_cast(uint32_t, x + 12582912.0f);
+    };
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(one(d), one(c), 0x0c0c0400u), __builtin_amdgcn_perm(one(b), one(a), 0x0c0c0400u), 0x05040100u);
   }
   static __device__ __forceinline__ void decode(uint32_t x, float (&y)[4]) {
 #pragma unroll
@@ -142,6 +151,10 @@ struct E4M3 {
     auto in = [](float x) { return fminf(fmaxf(x, -MOST), MOST); };
     int x = __builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), x, true);
+  }
+  static __device__ __forceinline__ uint32_t encode_within(float a, float b, float c, float d) {
+    const int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
   }
   static __device__ __forceinline__ void decode(uint32_t x, float (&y)[4]) {
     const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
