@@ -244,7 +244,8 @@ struct Rows<Code, NI, 32> {
     }
     return s;
   }
-  struct Weights { h8 p[2]; };  // [0]: tokens 0-3 and 16-19 of the half's, [1]: 8-11 and 24-27
+  // [0]: tokens 0-3 and 16-19 of the half's, [1]: 8-11 and 24-27, as two fp16 numbers each: the result is off by its own rounding only
+  struct Weights { h8 p[2], rest[2]; };
   __device__ __forceinline__ Weights weigh(f16x s, int begin, bool masked, float sk, float sv) {
     if (masked) {
       const int x = q.sees - begin - 4 * (lane >> 5);
@@ -274,13 +275,19 @@ struct Rows<Code, NI, 32> {
     Weights w;
 #pragma unroll
     for (int r = 0; r < 16; ++r) w.p[r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)s[r];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w.rest[r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)(s[r] - (float)w.p[r >> 2 & 1][(r >> 3) * 4 + (r & 3)]);
     return w;
   }
   __device__ __forceinline__ void multiply(const u4 (&v)[NV], const Weights& w) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][0], v[i][1]), w.p[0], o[i], 0, 0, 0);
-      o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves_of<Code>(v[i][2], v[i][3]), w.p[1], o[i], 0, 0, 0);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const h8 x = halves_of<Code>(v[i][2 * y], v[i][2 * y + 1]);
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w.p[y], o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w.rest[y], o[i], 0, 0, 0);
+      }
     }
   }
   __device__ __forceinline__ float sum() const { return add_halves(l); }
@@ -335,8 +342,8 @@ struct Rows<Code, NI, 16> {
       }
     return s;
   }
-  // Tokens 0-3 of the quarter's four and 16 on.  As two fp16 numbers each, so that the result is off by its own rounding only: eight more of the short matrix
-  // instructions a block, which memory's time hides (a batch's step 46 us with and without).
+  // Tokens 0-3 of the quarter's four and 16 on.  As two fp16 numbers each, as above: eight more of the short matrix instructions a block, which memory's
+  // time hides (a batch's step 46 us with and without).
   struct Weights { h8 p, rest; };
   static __device__ __forceinline__ float over_row(float x, bool adds) {
     const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
@@ -933,23 +940,31 @@ struct Side {
 struct Plan {
   Side few, many;
 };
+// By the rows that a sequence and key head may have at most, the blocks that its table has room for, and the number of segments; what lengths there are is not
+// known here.  (us of one launch and its joining one.)
 static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
   Plan plan = {};
   Side &few = plan.few, &many = plan.many;
   const int G = d->Hq / d->Hkv;
-  const int64_t most = (int64_t)view_of(b).most * G;  // rows of a sequence and head
-  const int64_t blocks = (int64_t)b->width * p->page / BT;
-  many.on = most > 64;
+  const int64_t most = (int64_t)view_of(b).most * G;
+  const int64_t blocks = (int64_t)b->width * p->page / BT, heads = (int64_t)b->S * p->Hkv;
+  // Tiles of 128 rows read a block once for up to four wavefronts, tiles of 32 start sooner: 33 to 64 rows of 32 sequences of up to 16384 tokens 117 with
+  // the former, 140 with the latter; of one sequence of 7000 tokens 35 and 26; of 16 of up to 2000 tokens 55 and 51.
+  many.on = most > 64 || (most > 32 && blocks > 128 && heads >= 128);
   few.on = !many.on || (b->S > 1 && G <= 16);
   if (few.on) {
     few.rows = most > 16 && !many.on ? 32 : 16, few.waves = 4;
     few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
     few.tiles = few.rows == 32 ? (int)((most + 31) / 32) : 1;
-    const int64_t segments = (int64_t)b->S * p->Hkv * few.tiles;
+    const int64_t segments = heads * few.tiles;
+    // A workgroup a segment, without a joining launch, while that is not much longer than the others' share: 32 segments of 1000 tokens 8.3 against 12.5 in
+    // shares, of 2000 tokens 18 against 14; 256 segments of 2000 tokens 24 against 37.
     few.whole = !many.on && blocks <= (segments < 256 ? 48 : 128) && segments * 256 <= 0xffffffff;
     if (few.whole) {
       few.workgroups = (int)segments;
     } else {
+      // Shares: four wavefronts a CU with two blocks each on their way read 6.7 TB/s; twice as many gain nothing and leave twice as many pieces (32 sequences
+      // of 128 to 16384 tokens 49 with 256 workgroups, 53 with 512, 62 with 768).  A segment costs as much as 16 blocks (none counted: 83, 8: 59, 16: 49).
       few.workgroups = 256, few.least = 8, few.spare = 16;
       few.share(p);
     }
@@ -958,6 +973,8 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
     many.rows = TILE, many.waves = 4;
     many.rows_from = few.on ? 17 : 1, many.rows_to = 0x7fffffff;
     const int64_t slots = (int64_t)b->T * G / TILE + b->S, least = std::max<int64_t>(0, ((int64_t)b->T * G - (few.on ? 16 * (int64_t)b->S : 0)) / TILE) * p->Hkv;
+    // A workgroup a tile where there are nearly two a CU, or few stages; else shares of all stages (344 tiles of up to 40 stages: 66 in shares, 76 whole;
+    // 512 of 120: 371 and 319).
     many.whole = (least >= 448 || blocks <= 32) && (slots * p->Hkv + 1024) * 256 <= 0xffffffff;
     many.tiles = (int)slots;
     many.workgroups = many.whole ? (int)(slots * p->Hkv) : 512;

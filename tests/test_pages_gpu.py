@@ -306,6 +306,8 @@ ATTENDS = [
     ([4, 2, 1], [900, 3, 700], 8, 2, 80, 32, 200),
     ([20, 1, 18], [1000, 1, 18], 3, 3, 36, 128, 60),
     ([1, 2], [600, 40], 71, 1, 64, 64, 100),
+    ([8, 1, 7, 3] * 16, [(i * 53) % 190 + 8 for i in range(64)], 10, 2, 64, 32, 140),
+    ([9, 9], [400, 9], 6, 2, 128, 64, 80),
 ]
 
 
