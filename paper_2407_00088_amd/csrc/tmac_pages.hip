@@ -63,7 +63,8 @@ __device__ __forceinline__ uint16_t elem_of(const typename Vec<N>::type& x, int 
 }
 
 // The rows of one slice of one token, by one wavefront: its lanes take a pair each for the cosines and sines, then vectors of N
-// elements.  Memory bounds it (16384 tokens of 72 heads of 128 elements, 604 MB: see the launch).
+// elements, four at once.  Memory bounds it: 16384 tokens of 72 heads of 128 elements, 604 MB, 115 us = 5.2 TB/s, a copy's rate; 2003 tokens of 64 heads of
+// 100, 51 MB, 13.8 us.  (A slice is of one tensor: with rows of several, every vector chose its tensor's strides, 23 us.)
 template <bool BF16, bool INTERLEAVED, int N>
 __device__ __forceinline__ void rotate_rows(const RopeArgs& a, int token, int slice, f2* turn) {
   typedef typename Vec<N>::type V;
@@ -178,8 +179,9 @@ __device__ __forceinline__ int divided(int i, uint32_t by) { return by ? (int)__
 
 // A block of 32 tokens of a sequence that the call's tokens touch, for some key heads one after the other: rows come in vectors of N elements, the
 // next head's while this one is worked on; keys turn on their way to LDS, by cosines and sines that are worked out once; with the scales
-// known, a thread makes 16 codes of either plane.  A step's few tokens wait for memory four times (lengths, table, rows and what the block holds);
-// prompts are bound by the vector unit's work beside memory.
+// known, a thread makes 16 codes of either plane.  A step's few tokens wait for memory one time after the other (lengths, table and rows, what the block
+// holds: 24 sequences with their 64 query heads 6.6 us); prompts are bound by memory (16384 tokens, 8 key heads, 64 query heads, 637 MB: 129 us = 4.9 TB/s) or, with
+// few bytes a workgroup, by the vector ALUs beside it (1790 tokens in seven prompts, 32 + 32 heads of 100: 24 us, 58 MB).
 template <typename Code, bool BF16, bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   typedef typename Vec<N>::type V;
@@ -397,7 +399,8 @@ struct ReadArgs {
   int bf16, slots;
 };
 
-// A block of a sequence and key head.
+// A block of a sequence and key head, through LDS, since values lie by elements.  (16384 tokens of 8 heads: 28 us, 100 MB at 3.6 TB/s; who reads pages back
+// copies or looks at them, so it was left there.)
 template <typename Code>
 __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
   __shared__ uint32_t rows[2][BT][33];
@@ -562,7 +565,8 @@ extern "C" tmac_status tmac_pages_append(const tmac_pages* p, const tmac_pages_b
   a.vectors = a.turning + (D - 2 * a.pairs) / n;
   a.by_vectors = by(a.vectors), a.by_pairs = by(std::max(1, a.pairs)), a.by_values = by(D / (n == 8 ? 8 : 4));
   const int64_t blocks = block_slots(batch, a.slots);
-  // Key heads of a workgroup: as many as leave the chip two workgroups a CU (8192 tokens of 32 heads of 100: see there)
+  // Key heads of a workgroup, which share cosines and sines: as many as leave the chip two workgroups a CU (seven prompts of 32 heads: 26.7 us, 30 with four
+  // a CU, 36 with one head each)
   a.heads = (int)std::max<int64_t>(1, std::min<int64_t>(p->Hkv, blocks * p->Hkv / 512));
   a.groups = (p->Hkv + a.heads - 1) / a.heads;
   int64_t workgroups = blocks * a.groups;

@@ -166,9 +166,8 @@ struct Queries {
         const float x = fabsf(bf(raw[i][j >> 2], j & 3));
         most = fmaxf(most, x <= 3.4028235e38f ? x : 0.0f);
       }
-    // (the lanes of one row lie 16 or 32 apart; rows' maxima need not be the same in all of them: but one of the row's own)
+    // the row's largest (its lanes lie `apart`) to [2^14, 2^15): a power of two, which goes into c
     most = over_row(most);
-    // the largest to [2^14, 2^15)
     const int e = most > 0.0f ? (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - 14 : 0;
     c = __builtin_ldexpf(a.c, e);
 #pragma unroll
@@ -206,7 +205,7 @@ struct Plane {
 template <typename Code, int NI, int ROWS>
 struct Rows;
 
-// 32 rows: v_mfma_f32_32x32x16, row lane & 31.
+// 32 rows: v_mfma_f32_32x32x16, row lane & 31.  One block on its way: its registers hold no more at two wavefronts a SIMD.
 template <typename Code, int NI>
 struct Rows<Code, NI, 32> {
   static constexpr int NK = NI, NV = NI, DEPTH = 1;
@@ -302,7 +301,8 @@ struct Rows<Code, NI, 32> {
   }
 };
 
-// 16 rows: v_mfma_f32_16x16x32, row lane & 15.  Half the work of 32 for what is read, and half the registers.
+// 16 rows: v_mfma_f32_16x16x32, row lane & 15.  Half the work of 32 for what is read, and half the registers, which take a second block on its way
+// (32 sequences of 16384 tokens, 1.08 GB: 162 us = 6.7 TB/s, with one block and three wavefronts a SIMD 171).
 template <typename Code, int NI>
 struct Rows<Code, NI, 16> {
   static constexpr int NQ = (NI + 1) / 2, NK = 2 * NQ, NV = 2 * NI, DEPTH = 2;
@@ -555,7 +555,8 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
   }
 }
 
-// A workgroup a segment.
+// A workgroup a segment: for short caches, where the launch that joins pieces would cost more (32 segments of 300 tokens 5.6 us: lengths and pages, scales
+// and first keys, values, the meeting of four wavefronts, one wait after the other).
 template <typename Code, int NI, int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_whole_kernel(const AttendArgs a) {
   __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
@@ -650,7 +651,10 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
 // --- many rows ------------------------------------------------------------------------------------------------------------------------------
 //
 // 128 rows a workgroup, 32 a wavefront: stages of 64 tokens are brought to fp16 once for all four, on their way from registers to LDS, two
-// stages there: one is multiplied while the next is made and the one after that is on its way from memory.
+// stages there: one is multiplied while the next is made and the one after that is on its way from memory.  Bound by products and exponentials that mostly take
+// turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 295 us, 0.87 PFLOP/s; matrix units 38 % busy, vector ALUs 53 %, LDS without conflicts, 2.0
+// of 2.4 GHz; codes to fp16 are about a fifth of the vector instructions).  Exponentials
+// are one fp16 number each here, as in the prompts' attention: a second product would cost a quarter more.
 
 constexpr int TILE = 128, STAGE = 64;
 
