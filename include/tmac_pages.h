@@ -82,8 +82,8 @@ size_t tmac_pages_scale_bytes(const tmac_pages* pages);
  *              that is no page (-1) means that there is none: its tokens are not written, nobody sees them, they read as zeros.
  *   lens_dev   int32 [S]: tokens of each sequence, those of this call included
  *   cu_dev     int32 [S + 1]: rows [cu[s], cu[s + 1]) of the call's tensors are the last cu[s + 1] - cu[s] tokens of sequence s, in order; it
- *              starts at 0, ends at T and does not fall.  NULL: one row a sequence (T = S).  Rows before a sequence's first token (more rows than
- *              the length) are not written, see nothing and read as zeros.
+ *              starts at 0, ends at T or before (rows behind its end are left as they are) and does not fall.  NULL: one row a sequence (T = S).
+ *              Rows before a sequence's first token (more rows than the length) are not written, see nothing and read as zeros.
  *   most       most rows of a sequence, where the caller knows it (more are left out); 0: not known
  * Tokens from width * page on are as on pages that are not there. */
 typedef struct {

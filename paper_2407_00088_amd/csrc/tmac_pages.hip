@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void store_kernel(const StoreArgs a) {
   if ((int)blockIdx.x >= a.workgroups) {
     const int64_t w = (int64_t)(blockIdx.x - a.workgroups) * 4 + wave;
     const int token = __builtin_amdgcn_readfirstlane((int)(w / a.q.slices)), slice = __builtin_amdgcn_readfirstlane((int)(w % a.q.slices));
-    if (token < a.q.T) rotate_rows<BF16, INTERLEAVED, N>(a.q, token, slice, turn + wave * 64);
+    if (token < (a.batch.cu ? a.batch.start(a.batch.S) : a.q.T)) rotate_rows<BF16, INTERLEAVED, N>(a.q, token, slice, turn + wave * 64);
     return;
   }
   const int h0 = blockIdx.x % a.groups * a.heads, h1 = min(a.pages.Hkv, h0 + a.heads);

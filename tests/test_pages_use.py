@@ -306,3 +306,37 @@ def test_pages_shared_by_sequences(T):
     ref = R.attend(q, R.decoded(cache), table.cpu(), [69, 71], [0, 5, 12], 1 / 8, 1)
     close(out, ref[0], ref[2])
     close(lse, ref[1], ref[3])
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+def test_a_padded_batch(T, code):
+    """Tensors with more rows than the starts speak of, a table that is part of a wider one, a sequence without a token, queries turned in place: what is
+    behind the last sequence stays, and the rest is as without it."""
+    D, Hq, Hkv = 80, 6, 3
+    rotary = T.Rotary(D, rot=40)
+    n, lens = [37, 0, 5], [50, 9, 5]
+    rows, room = sum(n), 64
+    wide = torch.full((3, 50), 7, dtype=torch.int32, device="cuda")
+    table = wide[:, 10:14]
+    table.copy_(torch.tensor([[4, 1, -1, -1], [0, -1, -1, -1], [6, -1, -1, -1]], dtype=torch.int32))
+    q, k, v = (rand(i, room, h, D).cuda() for i, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    q[rows:], k[rows:], v[rows:] = math.nan, math.inf, math.nan
+    cu = ints([0, 37, 37, 42])
+    got = []
+    for padded in (True, False):
+        cache = T.PagedCache(7, Hkv, D, page=32, code=code, Hq=Hq, rotary=rotary)
+        m = room if padded else rows
+        x = q[:m].clone()
+        turned = cache.append(k[:m], v[:m], table, ints(lens), cu, q=x, q_out=x)
+        assert turned is x
+        out, lse = torch.full((m, Hq, D), 3.0, dtype=F16, device="cuda"), torch.full((Hq, m), 5.0, device="cuda")
+        cache.attend(turned, table, ints(lens), cu, out=out, lse=lse)
+        kk, vv = torch.full((m, Hkv, D), 3.0, dtype=F16, device="cuda"), torch.full((m, Hkv, D), 3.0, dtype=F16, device="cuda")
+        cache.read(table, ints(lens), cu, k=kk, v=vv)
+        if padded:
+            assert turned[rows:].isnan().all() and (out[rows:] == 3).all() and (lse[:, rows:] == 5).all() and (kk[rows:] == 3).all() and (vv[rows:] == 3).all()
+        got.append((cache.codes, cache.scales, turned[:rows], out[:rows], lse[:, :rows], kk[:rows], vv[:rows]))
+        assert out[:rows].isfinite().all()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert (wide[:, :10] == 7).all() and (wide[:, 14:] == 7).all()
