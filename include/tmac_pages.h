@@ -85,7 +85,8 @@ size_t tmac_pages_scale_bytes(const tmac_pages* pages);
  *              starts at 0, ends at T or before (rows behind its end are left as they are) and does not fall.  NULL: one row a sequence (T = S).
  *              Rows before a sequence's first token (more rows than the length) are not written, see nothing and read as zeros.
  *   most       most rows of a sequence, where the caller knows it (more are left out); 0: not known
- * Tokens from width * page on are as on pages that are not there. */
+ * Tokens from width * page on are as on pages that are not there.  Starts and lengths that cannot be give wrong results, within the call's
+ * rows and the table's pages. */
 typedef struct {
   const int32_t* table_dev;
   int64_t table_stride;

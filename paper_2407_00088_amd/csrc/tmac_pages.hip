@@ -172,6 +172,7 @@ __device__ __forceinline__ bool block_of(const Batch& b, int slots, int w, int& 
     s = count_up_to(b.S, from, w);
     if (s >= b.S) return false;
     j = w - (int)from(s);
+    if (j < 0) return false;  // (starts that fall, or do not begin at zero)
   }
   return true;
 }

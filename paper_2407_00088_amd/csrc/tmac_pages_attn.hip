@@ -652,7 +652,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
 //
 // 128 rows a workgroup, 32 a wavefront: stages of 64 tokens are brought to fp16 once for all four, on their way from registers to LDS, two
 // stages there: one is multiplied while the next is made and the one after that is on its way from memory.  Bound by products and exponentials that mostly take
-// turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 295 us, 0.87 PFLOP/s; matrix units 38 % busy, vector ALUs 53 %, LDS without conflicts, 2.0
+// turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 295 us, 0.87 PFLOP/s; matrix units 39 % busy, vector ALUs 55 %, LDS without conflicts, 2.0
 // of 2.4 GHz; codes to fp16 are about a fifth of the vector instructions).  Exponentials
 // are one fp16 number each here, as in the prompts' attention: a second product would cost a quarter more.
 
@@ -842,7 +842,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a
     if (s >= a.batch.S) return;
     const int tile = slot - (int)from(s);
     const Work work = Work::of<TILE>(a, a.many, Sequence(a.batch, s));
-    if (tile >= work.tiles) return;
+    if (tile < 0 || tile >= work.tiles) return;  // (below 0: starts that fall, or do not begin at zero)
     run_tile<Code, NI>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
   }
 }

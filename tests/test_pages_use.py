@@ -340,3 +340,23 @@ def test_a_padded_batch(T, code):
     for a, b in zip(*got):
         assert torch.equal(a, b)
     assert (wide[:, :10] == 7).all() and (wide[:, 14:] == 7).all()
+
+
+def test_wrong_contents_stay_within_bounds(T):
+    """Starts that fall, lengths beyond the table, numbers that are no page, in every kernel: values are wrong, other pages and rows untouched."""
+    D, Hq, Hkv = 64, 8, 2
+    cache = T.PagedCache(5, Hkv, D, page=32, Hq=Hq, rotary=T.Rotary(D))
+    cache.codes.fill_(9), cache.scales.fill_(1.0)
+    q, k = rand(1, 300, Hq, D).cuda(), rand(2, 300, Hkv, D).cuda()
+    table = ints([[1, -5, 2, 1 << 30], [3, 5, -1, -(1 << 31)]])
+    guard = torch.full((302, Hq, D), 3.0, dtype=F16, device="cuda")
+    for lens in ([1 << 30, -(1 << 31)], [(1 << 31) - 1, 70], [0, 0], [100, 128], [5, 3]):
+        for cu in ([0, 200, 300], [0, 300, 20], [-50, 1 << 30, -(1 << 31)], [250, 100, 310], [0, 0, 0], [5, 5, 300], [40, 60, 300], [96, 100, 90]):
+            for table_ in (table, torch.nn.functional.pad(table, (0, 200), value=-1)):
+                for most in (None, 1, 3, 40):
+                    cache.append(k, k, table_, ints(lens), ints(cu), q=q, q_out=guard[1:301], most=most)
+                    cache.attend(q, table_, ints(lens), ints(cu), most=most, out=guard[1:301])
+                    cache.read(table_, ints(lens), ints(cu), T=300, most=most)
+    torch.cuda.synchronize()
+    assert (guard[0] == 3).all() and (guard[301] == 3).all()
+    assert all((cache.codes[p] == 9).all() and (cache.scales[p] == 1).all() for p in (0, 4))
