@@ -95,11 +95,14 @@ class PagedDecoderAttention:
 
     def forward(self, x, counts):
         """counts[s] more tokens of every sequence (a prompt, a chunk of it, drafts, one token, none), packed: x [T, M] (fp16).  Returns [T, M]."""
-        if x.shape[0] != sum(counts):
-            raise ValueError(f"{x.shape[0]} rows for {sum(counts)} tokens")
+        if x.shape[0] != sum(counts) or len(counts) != self.table.batch:
+            raise ValueError(f"{x.shape[0]} rows for {sum(counts)} tokens of {self.table.batch} sequences: {list(counts)}")
+        if not x.shape[0]:
+            return x.new_empty((0, self.o.M), dtype=torch.float16)
+        # (the table grows when the projections have not refused the call)
+        q, k, v = (lin.forward_one_call(x, out_t=B.TMAC_OUT_F16).view(x.shape[0], -1, self.D) for lin in (self.q, self.k, self.v))
         cu, most = self.table.extend(counts)
         where = (self.table.table, self.table.lens, cu)
-        q, k, v = (lin.forward_one_call(x, out_t=B.TMAC_OUT_F16).view(x.shape[0], -1, self.D) for lin in (self.q, self.k, self.v))
         q = self.cache.append(k, v, *where, q=q, most=most)
         out, _ = self.cache.attend(q, *where, most=most)
         return self.o.forward_one_call(out.view(x.shape[0], -1), out_t=B.TMAC_OUT_F16)

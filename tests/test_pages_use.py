@@ -360,3 +360,20 @@ def test_wrong_contents_stay_within_bounds(T):
     torch.cuda.synchronize()
     assert (guard[0] == 3).all() and (guard[301] == 3).all()
     assert all((cache.codes[p] == 9).all() and (cache.scales[p] == 1).all() for p in (0, 4))
+
+
+def test_a_layer_refuses_and_stays_as_it_was(T):
+    """More tokens than the projections or the pages take, rows that are not the counts', a call without tokens: neither table nor pages change."""
+    from paper_2407_00088_amd import decoder
+    M, batch = 256, 2
+    layer = decoder.paged(decoder.random_layer(M, 4, 2, 64, batch, capacity=8, recent=4, max_N=100), pages=3, width=3, page=32)
+    layer.forward(rand(1, 40, M).cuda(), [33, 7])
+    before = [t.clone() for t in (layer.cache.codes, layer.cache.scales, layer.table.table, layer.table.lens)]
+    for rows, counts, error in ((64, [64, 0], ValueError), (57, [31, 26], MemoryError), (101, [1, 100], AssertionError), (3, [1, 1], ValueError), (3, [3], ValueError),
+                                (2, [3, -1], ValueError)):
+        with pytest.raises(error):
+            layer.forward(rand(2, rows, M).cuda(), counts)
+    assert layer.forward(rand(3, 0, M).cuda(), [0, 0]).shape == (0, M)
+    for a, b in zip(before, (layer.cache.codes, layer.cache.scales, layer.table.table, layer.table.lens)):
+        assert torch.equal(a, b)
+    assert layer.table.length == [33, 7] and layer.table.free == []
