@@ -136,8 +136,12 @@ __host__ __device__ __forceinline__ int part_floats(int rows, int width) { retur
 template <int NQ>
 struct Queries {
   h8 q[NQ][2];
-  float c;   // the row's scale log2 e
+  int e;     // they are the row's times 2^-e
   int sees;  // tokens before this one
+
+  // What products with keys of this scale, times scale log2 e, are multiplied with.  Above zero and finite: a token that is not seen has the score -infinity, and
+  // products may be zero.  (2^e by itself may be below the smallest number where the whole is not: queries of 2^-120 beside keys of 2^120.)
+  __device__ __forceinline__ float factor(float scale) const { return __builtin_amdgcn_fmed3f(__builtin_ldexpf(scale, e), 0x1p-126f, 0x1.fffffep127f); }
 
   template <typename DOf>
   __device__ __forceinline__ void load(const AttendArgs& a, const char* at, bool valid, DOf&& d_of) {
@@ -149,7 +153,7 @@ struct Queries {
         const int d = d_of(i) + 4 * j;
         raw[i][j] = valid && d < a.pages.D ? *reinterpret_cast<const u2*>(at + d * 2) : u2{0u, 0u};
       }
-    c = a.c;
+    e = 0;
     if (!a.bf16) {
 #pragma unroll
       for (int i = 0; i < NQ; ++i)
@@ -166,10 +170,9 @@ struct Queries {
         const float x = fabsf(bf(raw[i][j >> 2], j & 3));
         most = fmaxf(most, x <= 3.4028235e38f ? x : 0.0f);
       }
-    // the row's largest (its lanes lie `apart`) to [2^14, 2^15): a power of two, which goes into c
+    // the row's largest (its lanes lie `apart`) to [2^14, 2^15): a power of two, which goes into the factor
     most = over_row(most);
-    const int e = most > 0.0f ? (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - 14 : 0;
-    c = __builtin_ldexpf(a.c, e);
+    e = most > 0.0f ? (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - 14 : 0;
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
@@ -245,6 +248,7 @@ struct Rows<Code, NI, 32> {
   }
   // [0]: tokens 0-3 and 16-19 of the half's, [1]: 8-11 and 24-27, as two fp16 numbers each: the result is off by its own rounding only
   struct Weights { h8 p[2], rest[2]; };
+  // sk: of the block's keys, times scale log2 e
   __device__ __forceinline__ Weights weigh(f16x s, int begin, bool masked, float sk, float sv) {
     if (masked) {
       const int x = q.sees - begin - 4 * (lane >> 5);
@@ -255,7 +259,7 @@ struct Rows<Code, NI, 32> {
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
     mx = max_halves(mx);
-    const float a = sk * q.c, log_sv = __builtin_amdgcn_logf(sv);
+    const float a = q.factor(sk), log_sv = __builtin_amdgcn_logf(sv);
     float alpha;
     if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
 #pragma unroll
@@ -363,7 +367,7 @@ struct Rows<Code, NI, 16> {
 #pragma unroll
     for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
     mx = over_row(mx, false);
-    const float a = sk * q.c, log_sv = __builtin_amdgcn_logf(sv);
+    const float a = q.factor(sk), log_sv = __builtin_amdgcn_logf(sv);
     float alpha;
     if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
 #pragma unroll
@@ -466,7 +470,7 @@ __device__ __forceinline__ void run_blocks(const AttendArgs& a, R& w, const int3
         const int next = take(), at = (first + n[j] * step) * BT;
         const typename R::Scores s = w.scores(k[j]);
         if (next >= 0) load_k(j, next);
-        const typename R::Weights p = w.weigh(s, at, at + BT > least, lane_value(blocks.sk, n[j]), lane_value(blocks.sv, n[j]));
+        const typename R::Weights p = w.weigh(s, at, at + BT > least, lane_value(blocks.sk, n[j]) * a.c, lane_value(blocks.sv, n[j]));
         w.multiply(v[j], p);
         if (next >= 0) load_v(j, next);
         n[j] = next;
@@ -764,7 +768,7 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
         float mx = sc[b][0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
-        scale[b] = scales[b][0] * x.q.c, base[b] = __builtin_amdgcn_logf(fabsf(scales[b][1]));
+        scale[b] = x.q.factor(scales[b][0] * a.c), base[b] = __builtin_amdgcn_logf(fabsf(scales[b][1]));
         top = fmaxf(top, __builtin_fmaf(mx, scale[b], base[b]));
       }
       top = max_halves(top);

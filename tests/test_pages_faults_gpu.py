@@ -1,0 +1,79 @@
+"""Faults of the paged cache that have been mended, and paths that only long or many caches take, on the GPU: each case is one that came out wrong, or
+could have, against the forms in 64 bits of tests/pages_reference.py."""
+import math
+
+import pytest
+import torch
+
+import pages_reference as R
+from test_pages_gpu import BF16, F16, P, close, gen, ints, starts
+
+pytestmark = pytest.mark.gpu
+
+# Every way that attention goes: (new tokens of each sequence, Hq of one key head, pages of 32 tokens that the table has room for)
+WAYS = {
+    "16 rows, whole": ([1, 1], 2, 24),
+    "16 rows, shares": ([1, 1], 2, 200),
+    "32 rows, whole": ([40, 9], 1, 24),
+    "32 rows, shares": ([40, 9], 1, 200),
+    "128 rows, whole": ([150], 2, 24),
+    "128 rows, shares": ([150], 2, 200),
+    "16 and 128 rows, whole": ([2, 150, 1], 2, 24),
+    "16 and 128 rows, shares": ([2, 150, 1, 40], 2, 200),
+}
+
+
+def kept(k, v, lens, width, code, Hq):
+    """A cache of bf16 keys and values [T, Hkv, D] of sequences one after the other, and its table."""
+    held = [-(-n // 32) for n in lens]
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    for s, n in enumerate(held):
+        table[s, :n] = torch.arange(sum(held[:s]), sum(held[:s]) + n)
+    cache = P().PagedCache(sum(held), k.shape[1], k.shape[2], page=32, code=code, dtype=k.dtype, Hq=Hq)
+    cache.append(k.cuda(), v.cuda(), table.cuda(), ints(lens), starts(lens).cuda())
+    return cache, table
+
+
+def check(cache, table, q, lens, n, held=None):
+    out, lse = cache.attend(q.cuda(), table.cuda(), ints(lens), starts(n).cuda(), most=max(n))
+    ref = R.attend(q, held or R.decoded(cache), table, lens, starts(n), 1 / math.sqrt(cache.D), cache.Hkv)
+    close(out, ref[0], ref[2], "out")
+    close(lse, ref[1], ref[3], "lse")
+    return out, ref
+
+
+# --- queries of bf16 far from one ----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("way", WAYS)
+def test_small_queries_beside_keys_of_zero(way, code):
+    """A row's power of two times the scale of a block of zeros is below the smallest number: tokens that are not seen stayed in the row as
+    -infinity times zero."""
+    n, Hq, width = WAYS[way]
+    g, D = gen(21), 16
+    lens = [300 + 7 * i for i in range(len(n))]
+    k, v = (torch.randn((sum(lens), 1, D), generator=g) for _ in range(2))
+    for lo in starts(lens)[1:].tolist():
+        k[lo - 90:lo] = 0.0
+    k[:lens[0]] = 0.0
+    cache, table = kept(k.bfloat16(), v.bfloat16(), lens, width, code, Hq)
+    q = torch.randn((sum(n), Hq, D), generator=g) * 2.0 ** -torch.randint(60, 134, (sum(n), 1, 1), generator=g).double()
+    out, _ = check(cache, table, q.bfloat16(), lens, n)
+    assert out.isfinite().all()
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("way", WAYS)
+def test_smallest_queries_beside_large_keys(way, code):
+    """Scores of some units from queries down to bf16's smallest and keys up to 2^125: a row's power of two is no factor of its own, which
+    would have lost places below 2^-126."""
+    n, Hq, width = WAYS[way]
+    g, D = gen(22), 16
+    lens = [300 + 7 * i for i in range(len(n))]
+    k, v = (torch.randn((sum(lens), 1, D), generator=g) for _ in range(2))
+    k = (k.clamp(-3.5, 3.5) * 2.0 ** 123).bfloat16()
+    cache, table = kept(k, v.bfloat16(), lens, width, code, Hq)
+    q = torch.randn((sum(n), Hq, D), generator=g).clamp(-3.5, 3.5).double() * 2.0 ** -torch.randint(121, 127, (sum(n), 1, 1), generator=g).double()
+    _, ref = check(cache, table, q.bfloat16(), lens, n)
+    assert ref[0].std() > 0.1
