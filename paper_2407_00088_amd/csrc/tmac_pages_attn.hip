@@ -5,7 +5,8 @@
 // wavefront, and the exponentials are the second product's operand as they stand.  Codes are whole numbers or e4m3 values,
 // which fp16 holds exactly; a block's scales are the same for all its products, so they are taken out of them:
 //   x_j = s_j a + log2 sv,  a = sk scale log2 e,  p_j = 2^(x_j - m),  O += sum p_j code_j,  l += (sum p_j) / sv
-// with m against the row's largest x, and o = O / l.
+// with m against the row's largest x, and o = O / l.  m is a whole number.  x has the values' scale, which spans 2^179 (blocks of zeros have 2^-60), so what is far from the largest x may
+// still be a part of l like any other: sums l move by whole powers of two, and blocks of small x are lifted (base_of).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -185,13 +186,23 @@ struct Queries {
   }
 };
 
-// The running maximum.  x: the largest exponent of the block; returns whether any row's moved, and by what the row's sums are multiplied.
-__device__ __forceinline__ bool outgrown(float x, float& m, float& alpha) {
+// Sums against the maximum m times this power of two are against `to`.  (Whole numbers; -infinity: nothing has been summed.  A factor 2^(m - to) would be zero from 2^-127 on, where l may
+// still be a number.)
+__device__ __forceinline__ int places(float m, float to) { return (int)fmaxf(m - to, -1000.0f); }
+
+// The running maximum.  x: the largest exponent of the block; returns whether any row's moved, and by what power of two the row's sums are multiplied.
+__device__ __forceinline__ bool outgrown(float x, float& m, int& by) {
   const bool grows = x - m > KEPT;
   const float to = grows ? __builtin_ceilf(x) - HEADROOM : m;
-  alpha = grows ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+  by = grows ? places(m, to) : 0;
   m = to;
   return __any(grows);
+}
+// What is added to a block's scores, the largest of which is `most`: log2 of the values' scale, less m0.  Where exponentials stay below 2^-30, fp16 holds none of them and the
+// products get nothing; they are then lifted to 2^-30, by what their sum is divided by again, since they could be below 2^-126, which is zero too.
+__device__ __forceinline__ float base_of(float log_sv, float m0, float most) {
+  const float base = log_sv - m0;
+  return most == -INFINITY ? base : fmaxf(base, __builtin_ceilf(-30.0f - most));
 }
 
 // A block's keys or values.
@@ -260,20 +271,20 @@ struct Rows<Code, NI, 32> {
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
     mx = max_halves(mx);
     const float a = q.factor(sk), log_sv = __builtin_amdgcn_logf(sv);
-    float alpha;
-    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
+    int by;
+    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, by)) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) o[i] *= alpha;
-      l *= alpha;
+      for (int i = 0; i < NI; ++i) o[i] *= __builtin_ldexpf(1.0f, by);
+      l = __builtin_ldexpf(l, by);
     }
-    const float m0 = m == -INFINITY ? 0.0f : m, base = log_sv - m0;
+    const float m0 = m == -INFINITY ? 0.0f : m, base = base_of(log_sv, m0, mx * a);
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a, base));
       sum[r & 1] += s[r];
     }
-    // (without the scale again by what the exponents really had of it: base is rounded, base + m0 is not)
+    // (without the scale, or what stands for it, again by what the exponents really had of it: base is rounded, base + m0 is not)
     l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-(base + m0)), l);
     Weights w;
 #pragma unroll
@@ -368,13 +379,13 @@ struct Rows<Code, NI, 16> {
     for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
     mx = over_row(mx, false);
     const float a = q.factor(sk), log_sv = __builtin_amdgcn_logf(sv);
-    float alpha;
-    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, alpha)) {
+    int by;
+    if (outgrown(__builtin_fmaf(mx, a, log_sv), m, by)) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) o[i] *= alpha;
-      l *= alpha;
+      for (int i = 0; i < NV; ++i) o[i] *= __builtin_ldexpf(1.0f, by);
+      l = __builtin_ldexpf(l, by);
     }
-    const float m0 = m == -INFINITY ? 0.0f : m, base = log_sv - m0;
+    const float m0 = m == -INFINITY ? 0.0f : m, base = base_of(log_sv, m0, mx * a);
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -549,9 +560,9 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
       for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[(y * ROWS + in) * 2]);
 #pragma unroll
       for (int y = 0; y < WAVES; ++y) {
-        const float my = ml[(y * ROWS + in) * 2], f = my == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(my - m);
-        l = __builtin_fmaf(ml[(y * ROWS + in) * 2 + 1], f, l);
-        o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in) * PITCH + d) * f;
+        const int by = places(ml[(y * ROWS + in) * 2], m);
+        l += __builtin_ldexpf(ml[(y * ROWS + in) * 2 + 1], by);
+        o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in) * PITCH + d) * __builtin_ldexpf(1.0f, by);
       }
       const int r = tile * ROWS + in, i = r / a.G;
       put(seq.row0 + i, head * a.G + r - i * a.G, in, d, o, m, l);
@@ -762,7 +773,7 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
           for (int r = 0; r < 16; ++r) sc[b][r] = (r >> 2) * 8 + (r & 3) < upto ? sc[b][r] : -INFINITY;
         }
       }
-      float scale[2], base[2], top = -INFINITY;
+      float scale[2], base[2], largest[2], top = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         float mx = sc[b][0];
@@ -770,19 +781,20 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[b][r]);
         scale[b] = x.q.factor(scales[b][0] * a.c), base[b] = __builtin_amdgcn_logf(fabsf(scales[b][1]));
         top = fmaxf(top, __builtin_fmaf(mx, scale[b], base[b]));
+        largest[b] = mx * scale[b];  // (of the lane's tokens, whose sum is its own)
       }
       top = max_halves(top);
-      float alpha;
-      if (outgrown(top, x.m, alpha)) {
+      int by;
+      if (outgrown(top, x.m, by)) {
 #pragma unroll
-        for (int d = 0; d < NI; ++d) x.o[d] *= alpha;
-        x.l *= alpha;
+        for (int d = 0; d < NI; ++d) x.o[d] *= __builtin_ldexpf(1.0f, by);
+        x.l = __builtin_ldexpf(x.l, by);
       }
       const float m0 = x.m == -INFINITY ? 0.0f : x.m;
       h8 p[2][2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        base[b] -= m0;
+        base[b] = base_of(base[b], m0, largest[b]);
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -892,15 +904,14 @@ __device__ __forceinline__ void join(const AttendArgs& a, const AttendArgs::Side
       float top = m[y];
 #pragma unroll
       for (int x = 0; x < PARTS; ++x) top = fmaxf(top, w + x <= w1 ? ml[y][x][0] : -INFINITY);
-      const float f = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - top);
-      l[y] *= f, sum[y] *= f, m[y] = top;
+      const int by = places(m[y], top);
+      l[y] = __builtin_ldexpf(l[y], by), sum[y] *= __builtin_ldexpf(1.0f, by), m[y] = top;
 #pragma unroll
       for (int x = 0; x < PARTS; ++x) {
-        // (a maximum that is no number leaves the others alone, its sums are none either)
-        const float f = w + x > w1 || ml[y][x][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[y][x][0] - top);
         if (w + x > w1) continue;
-        l[y] = __builtin_fmaf(ml[y][x][1], f, l[y]);
-        sum[y] += o[y][x] * f;
+        const int by = places(ml[y][x][0], top);
+        l[y] += __builtin_ldexpf(ml[y][x][1], by);
+        sum[y] += o[y][x] * __builtin_ldexpf(1.0f, by);
       }
     }
   }

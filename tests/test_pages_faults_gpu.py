@@ -77,3 +77,36 @@ def test_smallest_queries_beside_large_keys(way, code):
     q = torch.randn((sum(n), Hq, D), generator=g).clamp(-3.5, 3.5).double() * 2.0 ** -torch.randint(121, 127, (sum(n), 1, 1), generator=g).double()
     _, ref = check(cache, table, q.bfloat16(), lens, n)
     assert ref[0].std() > 0.1
+
+
+# --- values whose scales are far apart ---------------------------------------------------------------------------------------------------------
+
+FAR = {
+    "zeros, then large": [None, 115],
+    "large, then zeros": [115, None],
+    "large at the end": [None] * 8 + [96],
+    "large in one of four": [None, None, 73, None],
+    "small and large": [-95, 119, -40, 30, None, 80],
+}
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("far", FAR)
+@pytest.mark.parametrize("way", WAYS)
+def test_blocks_of_values_far_apart(way, far, code):
+    """Blocks of values of zero or nearly zero beside ones of up to 2^121 (all of bf16's range), in either order: each has the part of the row's sum that its
+    scores give it.  The values' scale is in the exponents, and a block's sums were lost where that lay 2^126 or more apart."""
+    n, Hq, width = WAYS[way]
+    g, D = gen(23), 16
+    lens = [290 + 7 * i for i in range(len(n))]
+    k, v = (torch.randn((sum(lens), 1, D), generator=g) for _ in range(2))
+    v = v.clamp(-3.5, 3.5)
+    for s, lo in enumerate(starts(lens)[:-1].tolist()):
+        for b in range(-(-lens[s] // 32)):
+            e = FAR[far][(b + s) % len(FAR[far])]
+            v[lo + 32 * b:min(lo + 32 * b + 32, lo + lens[s])] *= 0.0 if e is None else 2.0 ** e
+    cache, table = kept(k.bfloat16(), v.bfloat16(), lens, width, code, Hq)
+    q = torch.randn((sum(n), Hq, D), generator=g)
+    q[::3] *= 8.0
+    out, _ = check(cache, table, q.bfloat16(), lens, n)
+    assert out.isfinite().all()
