@@ -120,7 +120,7 @@ def frequencies(rot: int, base: float = 10000.0, scaling=None):
 
 class Rotary:
     """Rotary positions of heads of D elements, of which the first `rot` turn (None: all): pairs (i, i + rot / 2), or (2 i, 2 i + 1) where
-    `interleaved`.  base, scaling: see frequencies()."""
+    `interleaved`.  base, scaling: see frequencies().  What it consists of is not replaced (calls go by the address of `freq`, and by sizes that are kept beside it)."""
 
     def __init__(self, D: int, rot: Optional[int] = None, base: float = 10000.0, interleaved: bool = False, scaling=None, device: str = "cuda"):
         rot = D if rot is None else rot
@@ -130,6 +130,17 @@ class Rotary:
         self.D, self.rot, self.interleaved = D, rot, bool(interleaved)
         self.freq = f.to(device)
         self.rope = {dt: tmac_rope(self.freq.data_ptr(), self.magnitude, D, rot, int(self.interleaved), elem) for dt, elem in A._ELEM.items()}
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} is not replaced: make another Rotary")
+        super().__setattr__(name, value)
+
+    def _rope(self, dtype) -> tmac_rope:
+        rope = self.rope[dtype]
+        if self.freq.data_ptr() != rope.freq_dev:
+            raise ValueError("freq has been moved to other memory: make another Rotary")
+        return rope
 
     def rotate(self, positions, *tensors, out: Optional[Sequence] = None, stream=None):
         """Tensors [T, H, D] of the same T tokens (up to four, H their own) turned by positions int64 [T].  Returns a tuple of as many; `out`:
@@ -146,6 +157,7 @@ class Rotary:
         x = tensors[0]
         if x.dim() != 3 or x.dtype not in A._ELEM:
             raise ValueError(f"tensors are [T, H, D] of float16 or bfloat16, got {tuple(x.shape)} of {x.dtype}")
+        rope = self._rope(x.dtype)
         T = x.shape[0]
         A._counted(T=T)
         for i, t in enumerate(tensors):
@@ -162,7 +174,7 @@ class Rotary:
         pairs = [(t, o) for t, o in zip(tensors, got) if t.shape[1]]
         if T and pairs:
             items = (tmac_rope_item * len(pairs))(*(tmac_rope_item(_row_view(t), _row_view(o), t.shape[1]) for t, o in pairs))
-            B._check(lib.tmac_rotate(self.rope[x.dtype], items, len(pairs), positions.data_ptr(), T, B._stream_ptr(stream)), "tmac_rotate")
+            B._check(lib.tmac_rotate(rope, items, len(pairs), positions.data_ptr(), T, B._stream_ptr(stream)), "tmac_rotate")
         return got
 
 
@@ -257,6 +269,7 @@ class PagedCache:
                 A._dims(name, t, "T, Hkv, D", (T, self.Hkv, self.D), self.dtype)
                 A._rows(name, t)
             batch = self._batch(T, table, lens, cu, most)
+            rope = None if self.rotary is None else self.rotary._rope(self.dtype)
             if self.rotary is None and (q is not None or positions is not None):
                 raise ValueError("a cache without rotary turns no queries and needs no positions")
             if q is None and q_out is not None:
@@ -275,7 +288,6 @@ class PagedCache:
                 views = [_row_view(q), _row_view(q_out)]
             A._same_device(self.codes, k, v, table, lens, cu, q, q_out, positions, None if self.rotary is None else self.rotary.freq)
             if T:
-                rope = None if self.rotary is None else self.rotary.rope[self.dtype]
                 B._check(lib.tmac_pages_append(self.cache, batch, A._ELEM[self.dtype], _row_view(k), _row_view(v), rope,
                                                None if positions is None else positions.data_ptr(), *views, self.Hq, B._stream_ptr(stream)),
                          "tmac_pages_append")

@@ -1,0 +1,19 @@
+"""Faults of the paged cache's host side that have been mended: no GPU needed."""
+import pytest
+import torch
+
+import paper_2407_00088_amd as T
+
+
+def test_a_rotation_is_not_taken_apart():
+    """Calls go by the address and the sizes that a Rotary had when it was made: other frequencies would be read where the old ones were, after these are gone."""
+    rotary = T.Rotary(64, device="cpu")
+    for name, value in (("freq", rotary.freq * 2), ("freq", rotary.freq.float()), ("magnitude", 2.0), ("D", 32), ("rot", 32), ("interleaved", True), ("rope", {})):
+        with pytest.raises(AttributeError, match="replaced"):
+            setattr(rotary, name, value)
+    rotary.freq *= 1.0          # (written to, where it is)
+    x = torch.zeros((2, 1, 64), dtype=torch.float16)
+    rotary.freq.data = rotary.freq.clone()
+    for dtype in (torch.float16, torch.bfloat16):
+        with pytest.raises(ValueError, match="other memory"):
+            rotary.rotate(torch.arange(2), x.to(dtype))
