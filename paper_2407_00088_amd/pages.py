@@ -218,6 +218,9 @@ class PagedCache:
     def __setattr__(self, name, value):
         if name in ("codes", "scales") and self.__dict__.get(name, value) is not value:
             raise AttributeError(f"{name} is written to, not replaced: {name}.copy_(...)")
+        # (what tensors are checked against, and what the kernels go by)
+        if name in ("Hkv", "D", "page", "Hq", "dtype", "desc", "cache") and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} is not replaced: make another PagedCache")
         if name == "rotary" and value is not None and value.D != self.D:
             raise ValueError(f"rotary turns heads of {value.D} elements, the cache has {self.D}")
         super().__setattr__(name, value)
@@ -234,6 +237,8 @@ class PagedCache:
         return self.attend_ws
 
     def _batch(self, T: int, table, lens, cu, most) -> tmac_pages_batch:
+        if any(t.data_ptr() != (at or 0) for t, at in ((self.codes, self.cache.codes_dev), (self.scales, self.cache.scales_dev))):
+            raise ValueError("codes or scales have been moved to other memory: make another PagedCache")
         S = lens.shape[0] if isinstance(lens, torch.Tensor) and lens.dim() else 0
         A._plain("lens", lens, (S,), torch.int32)
         A._dims("table", table, "S, width", (S, -1), torch.int32)

@@ -17,3 +17,22 @@ def test_a_rotation_is_not_taken_apart():
     for dtype in (torch.float16, torch.bfloat16):
         with pytest.raises(ValueError, match="other memory"):
             rotary.rotate(torch.arange(2), x.to(dtype))
+
+
+def test_a_cache_is_not_taken_apart():
+    """Tensors are checked against the sizes that the object has, kernels go by the ones that it was made with; the same for where codes and scales are."""
+    cache = T.PagedCache(4, 2, 64, Hq=4, device="cpu")
+    for name, value in (("Hq", 2), ("Hkv", 1), ("D", 32), ("page", 32), ("dtype", torch.bfloat16), ("desc", None), ("cache", None)):
+        with pytest.raises(AttributeError, match="replaced"):
+            setattr(cache, name, value)
+    cache.rotary, cache.rotary = T.Rotary(64, device="cpu"), None
+    table, lens = torch.zeros((2, 3), dtype=torch.int32), torch.ones(2, dtype=torch.int32)
+    for name in ("codes", "scales"):
+        moved = T.PagedCache(4, 2, 64, Hq=4, device="cpu")
+        t = getattr(moved, name)
+        t.data = t.clone()
+        with pytest.raises(ValueError, match="other memory"):
+            moved.read(table, lens)
+    assert T.PagedCache(0, 2, 64, device="cpu").codes.numel() == 0
+    with pytest.raises(ValueError, match="GPU"):        # (pages none, which have no address)
+        T.PagedCache(0, 2, 64, device="cpu").read(table, lens)
