@@ -116,8 +116,9 @@ tmac_status tmac_pages_read(const tmac_pages* pages, const tmac_pages_batch* bat
 /* Attention of the call's tokens over what is in the pages: row i of sequence s's n rows sees the tokens j <= lens[s] - n + i that are on
  * a page.  Notation and rules of values as in tmac_attn.h; desc->causal is 1.  Products are of the queries in fp16 (a bf16 row is first scaled by
  * a power of two to its range, which is exact down to 2^-38 of its largest element) with codes, which fp16 holds exactly; scores, exponentials,
- * sums and lse are 32-bit, exponentials times the scale of the values' block are fp16 in the second product, as the sum of two such numbers where few rows (up to
- * 64 of a sequence and key head) are dealt with and as one else: off by 2^-22 or 2^-11 of themselves, and below 2^-20 of the row's largest by up to 2^-31 of that.
+ * sums and lse are 32-bit.  Exponentials times the scale of the values' block are fp16 in the second product: as the sum of two such numbers for sequences with up to 64 rows
+ * of the call a key head (its tokens times Hq / Hkv), off by at most 2^-22 of themselves or 2^-31 of the row's largest; as one for the others, off by at most 2^-11 of themselves
+ * or 2^-31 of the largest.  Blocks of values may be any distance apart in size.
  *   q, out    [T, Hq, D] (token, head strides);  lse_dev  fp32 [Hq, T], or NULL
  *   workspace tmac_pages_attend_workspace_bytes(desc, pages, batch), 16-byte aligned, contents arbitrary
  * The order of the sums depends on sizes and lengths only.  Rows from cu[S] on stay as they are.

@@ -668,10 +668,13 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
 // 128 rows a workgroup, 32 a wavefront: stages of 64 tokens are brought to fp16 once for all four, on their way from registers to LDS, two
 // stages there: one is multiplied while the next is made and the one after that is on its way from memory.  Bound by products and exponentials that mostly take
 // turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 295 us, 0.87 PFLOP/s; matrix units 39 % busy, vector ALUs 55 %, LDS without conflicts, 2.0
-// of 2.4 GHz; codes to fp16 are about a fifth of the vector instructions).  Exponentials
-// are one fp16 number each here, as in the prompts' attention: a second product would cost a quarter more.
+// of 2.4 GHz; codes to fp16 are about a fifth of the vector instructions).
+//
+// Exponentials are one fp16 number each here, as in the prompts' attention (off by 2^-11 of themselves, the size of the result's own rounding; two for all rows: 400 us).  Sequences of up to
+// EXACT_ROWS rows come here when others have more, and to smaller tiles when they are alone: they get two numbers in both, so that how exact a sequence's results are does not
+// depend on the others.
 
-constexpr int TILE = 128, STAGE = 64;
+constexpr int TILE = 128, STAGE = 64, EXACT_ROWS = 64;
 
 template <int NI>
 struct Staged {
@@ -679,7 +682,8 @@ struct Staged {
   static constexpr int PLANE = NI * 2048, BLOCK = 2 * PLANE, BYTES = 2 * BLOCK;
 };
 
-template <typename Code, int NI>
+// TWO: exponentials as two fp16 numbers
+template <typename Code, int NI, bool TWO>
 __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, int s, int head, int tile, int begin, int stop, float* part, char* shared, bool again) {
   typedef Staged<NI> L;
   int tid = threadIdx.x;
@@ -791,7 +795,7 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
         x.l = __builtin_ldexpf(x.l, by);
       }
       const float m0 = x.m == -INFINITY ? 0.0f : x.m;
-      h8 p[2][2];
+      h8 p[2][2], rest[2][2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         base[b] = base_of(base[b], m0, largest[b]);
@@ -800,7 +804,9 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
         for (int r = 0; r < 16; ++r) {
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][r], scale[b], base[b]));
           sum[r & 1] += e;
-          p[b][r >> 2 & 1][(r >> 3) * 4 + (r & 3)] = (_Float16)e;
+          const int y = r >> 2 & 1, j = (r >> 3) * 4 + (r & 3);
+          p[b][y][j] = (_Float16)e;
+          if constexpr (TWO) rest[b][y][j] = (_Float16)(e - (float)p[b][y][j]);
         }
         x.l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-(base[b] + m0)), x.l);
       }
@@ -809,8 +815,11 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int d = 0; d < NI; ++d)
-            x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(v + b * L::BLOCK + d * 2048 + y * 1024), p[b][y], x.o[d], 0, 0, 0);
+          for (int d = 0; d < NI; ++d) {
+            const h8 codes = *reinterpret_cast<const h8*>(v + b * L::BLOCK + d * 2048 + y * 1024);
+            x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, p[b][y], x.o[d], 0, 0, 0);
+            if constexpr (TWO) x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, rest[b][y], x.o[d], 0, 0, 0);
+          }
     }
     if (stage + 1 < stop) {
       place ^= 1;
@@ -849,7 +858,9 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a
   }
   if constexpr (SHARED) {
     walk_share<TILE>(a, a.many, w, numbers[threadIdx.x >> 6], [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
-      run_tile<Code, NI>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.many, w, begin, part_floats(TILE, NI * 32)), shared, again);
+      float* const part = whole ? nullptr : part_at(a.many, w, begin, part_floats(TILE, NI * 32));
+      if (work.rows <= EXACT_ROWS) run_tile<Code, NI, true>(a, work, s, head, tile, begin, stop, part, shared, again);
+      else run_tile<Code, NI, false>(a, work, s, head, tile, begin, stop, part, shared, again);
     });
   } else {
     const int head = w % a.pages.Hkv, slot = a.many.tiles - 1 - w / a.pages.Hkv;
@@ -859,7 +870,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a
     const int tile = slot - (int)from(s);
     const Work work = Work::of<TILE>(a, a.many, Sequence(a.batch, s));
     if (tile < 0 || tile >= work.tiles) return;  // (below 0: starts that fall, or do not begin at zero)
-    run_tile<Code, NI>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
+    if (work.rows <= EXACT_ROWS) run_tile<Code, NI, true>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
+    else run_tile<Code, NI, false>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false);
   }
 }
 
@@ -967,13 +979,13 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
   const int G = d->Hq / d->Hkv;
   const int64_t most = (int64_t)view_of(b).most * G;
   const int64_t blocks = (int64_t)b->width * p->page / BT, heads = (int64_t)b->S * p->Hkv;
-  // Tiles of 128 rows read a block once for up to four wavefronts, tiles of 32 start sooner: 33 to 64 rows of 32 sequences of up to 16384 tokens 117 with
-  // the former, 140 with the latter; of one sequence of 7000 tokens 35 and 26; of 16 of up to 2000 tokens 55 and 51.
-  many.on = most > 64 || (most > 32 && blocks > 128 && heads >= 128);
+  // Up to 64 rows in tiles of 32, which read a block twice, but have no wavefronts without rows: 40 rows of 32 sequences of up to 16384 tokens 107, in tiles of 128 rows 119; 64 rows 126
+  // and 121; 64 rows of 16 sequences of 4200 tokens 56 and 79; of one of 7000 26 and 35.
+  many.on = most > EXACT_ROWS;
   few.on = !many.on || (b->S > 1 && G <= 16);
   if (few.on) {
     few.rows = most > 16 && !many.on ? 32 : 16, few.waves = 4;
-    few.rows_from = 1, few.rows_to = few.rows == 32 ? 64 : 16;
+    few.rows_from = 1, few.rows_to = few.rows == 32 ? EXACT_ROWS : 16;
     few.tiles = few.rows == 32 ? (int)((most + 31) / 32) : 1;
     const int64_t segments = heads * few.tiles;
     // A workgroup a segment, without a joining launch, while that is not much longer than the others' share: 32 segments of 1000 tokens 8.3 against 12.5 in
