@@ -35,7 +35,7 @@ struct AttendArgs {
   int64_t q_token, q_head, out_token, out_head;  // bytes
   float* lse;
   float c;  // scale log2 e
-  int Hq, G, bf16;
+  int G, bf16;
   // The sequences of one kind, and how their work is dealt out
   struct Side {
     int rows_from, rows_to;  // sequences of so many rows (a key head)
@@ -49,7 +49,7 @@ struct AttendArgs {
 
 // A segment that shares w0 to w1 have pieces of: its rows are rows r = tile_row .. of sequence and head, `rows` in all.  w1 < w0: none.
 struct Note {
-  int w0, w1, row0, rows, tile_row, head, unused[2];
+  int w0, w1, row0, rows, tile_row, head;
 };
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -507,16 +507,17 @@ __device__ __forceinline__ void put_out(const AttendArgs& a, int row, int hq, in
   if (d == 0 && a.lse) a.lse[(int64_t)hq * a.batch.T + row] = log_sum(m, l);
 }
 
-// A piece of a segment: blocks [begin, stop).  WAVES wavefronts take every WAVES-th, their sums meet in LDS.  part: where the piece's sums
+// A piece of a segment: blocks [begin, stop).  Four wavefronts take every fourth, their sums meet in LDS.  part: where the piece's sums
 // go, null: it is the whole segment, whose results go out.
-template <int NI, int ROWS, int WAVES>
+constexpr int WAVES = 4;
+template <int NI, int ROWS>
 struct Meeting {
-  static constexpr int W = NI * 32, PITCH = W + 4, FLOATS = WAVES == 1 ? 4 : WAVES * ROWS * (PITCH + 2);
+  static constexpr int W = NI * 32, PITCH = W + 4, FLOATS = WAVES * ROWS * (PITCH + 2);
 };
-template <typename Code, int NI, int ROWS, int WAVES>
+template <typename Code, int NI, int ROWS>
 __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work, int s, int head, int tile, int begin, int stop, float* part, float* shared,
                                           bool again, int page) {
-  typedef Meeting<NI, ROWS, WAVES> M;
+  typedef Meeting<NI, ROWS> M;
   constexpr int W = M::W, PITCH = M::PITCH;
   // (named anew for every piece: else what follows from it is worked out before the first and kept in 40 registers)
   int tid = threadIdx.x;
@@ -530,7 +531,7 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
   const bool valid = r < work.rows;
   // (the first row of a tile sees least)
   const int least = clamp_to(seq.first + (tile * ROWS) / a.G + 1, work.held);
-  run_blocks(a, x, a.batch.row(s), page, head, begin + (WAVES == 1 ? 0 : wave), stop, WAVES, least,
+  run_blocks(a, x, a.batch.row(s), page, head, begin + wave, stop, WAVES, least,
              [&] { x.begin(a, a.q + row * a.q_token + hq * a.q_head, valid, valid ? clamp_to(seq.first + i + 1, work.held) : 0x7fffffff); });
   const float l = x.sum();
   auto put = [&](int row, int hq, int in, int d, const f4& o, float m, float l) {
@@ -541,45 +542,39 @@ __device__ __forceinline__ void run_piece(const AttendArgs& a, const Work& work,
       if (d == 0) part[in * 2] = m, part[in * 2 + 1] = l;
     }
   };
-  if constexpr (WAVES == 1) {
-    x.each([&](int d, const f4& o) {
-      if (valid) put(row, hq, in, d, o, x.m, l);
-    });
-  } else {
-    float* ml = shared + WAVES * ROWS * PITCH;
-    if (again) __syncthreads();  // (the sums before have been read)
-    if (lane < ROWS) ml[(wave * ROWS + lane) * 2] = x.m, ml[(wave * ROWS + lane) * 2 + 1] = l;
-    x.each([&](int d, const f4& o) { *reinterpret_cast<f4*>(shared + (wave * ROWS + in) * PITCH + d) = o; });
-    __syncthreads();
-    const int rows = min(ROWS, work.rows - tile * ROWS);
-    for (int k = tid; k < rows * (W / 4); k += 64 * WAVES) {
-      const int in = k / (W / 4), d = k % (W / 4) * 4;
-      float m = -INFINITY, l = 0.0f;
-      f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  float* ml = shared + WAVES * ROWS * PITCH;
+  if (again) __syncthreads();  // (the sums before have been read)
+  if (lane < ROWS) ml[(wave * ROWS + lane) * 2] = x.m, ml[(wave * ROWS + lane) * 2 + 1] = l;
+  x.each([&](int d, const f4& o) { *reinterpret_cast<f4*>(shared + (wave * ROWS + in) * PITCH + d) = o; });
+  __syncthreads();
+  const int rows = min(ROWS, work.rows - tile * ROWS);
+  for (int k = tid; k < rows * (W / 4); k += 64 * WAVES) {
+    const int in = k / (W / 4), d = k % (W / 4) * 4;
+    float m = -INFINITY, l = 0.0f;
+    f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[(y * ROWS + in) * 2]);
+    for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[(y * ROWS + in) * 2]);
 #pragma unroll
-      for (int y = 0; y < WAVES; ++y) {
-        const int by = places(ml[(y * ROWS + in) * 2], m);
-        l += __builtin_ldexpf(ml[(y * ROWS + in) * 2 + 1], by);
-        o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in) * PITCH + d) * __builtin_ldexpf(1.0f, by);
-      }
-      const int r = tile * ROWS + in, i = r / a.G;
-      put(seq.row0 + i, head * a.G + r - i * a.G, in, d, o, m, l);
+    for (int y = 0; y < WAVES; ++y) {
+      const int by = places(ml[(y * ROWS + in) * 2], m);
+      l += __builtin_ldexpf(ml[(y * ROWS + in) * 2 + 1], by);
+      o += *reinterpret_cast<const f4*>(shared + (y * ROWS + in) * PITCH + d) * __builtin_ldexpf(1.0f, by);
     }
+    const int r = tile * ROWS + in, i = r / a.G;
+    put(seq.row0 + i, head * a.G + r - i * a.G, in, d, o, m, l);
   }
 }
 
 // A workgroup a segment: for short caches, where the launch that joins pieces would cost more (32 segments of 300 tokens 5.6 us: lengths and pages, scales
 // and first keys, values, the meeting of four wavefronts, one wait after the other).
-template <typename Code, int NI, int ROWS, int WAVES>
+template <typename Code, int NI, int ROWS>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_whole_kernel(const AttendArgs a) {
-  __shared__ float shared[Meeting<NI, ROWS, WAVES>::FLOATS];
+  __shared__ float shared[Meeting<NI, ROWS>::FLOATS];
   const int head = blockIdx.x % a.pages.Hkv, x = blockIdx.x / a.pages.Hkv, tile = x % a.few.tiles, s = x / a.few.tiles;
   const int page = Blocks::page_of(a, a.batch.row(s), threadIdx.x >> 6, WAVES, threadIdx.x & 63);  // (beside the lengths)
   const Work work = Work::of<ROWS>(a, a.few, Sequence(a.batch, s));
   if (tile >= work.tiles) return;
-  run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false, page);
+  run_piece<Code, NI, ROWS>(a, work, s, head, tile, 0, work.blocks, nullptr, shared, false, page);
 }
 
 // A workgroup's equal share of all units, in order: piece(work, sequence, head, tile, first and last block, whether that is the whole segment, whether there
@@ -599,7 +594,7 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs
     int64_t x = units_of(0, true), upto = inclusive(x), units = shfl64(upto, 63);
     for (int i = 64; i < S; i += 64) units += shfl64(inclusive(units_of(i, false)), 63);
     const int64_t share = share_of(side, units);
-    if (threadIdx.x == 0) side.notes[w] = Note{0, -1, 0, 0, 0, 0, {0, 0}};
+    if (threadIdx.x == 0) side.notes[w] = Note{0, -1, 0, 0, 0, 0};
     u = share * w, end = min(units, u + share);
     if (u >= end) return;
     length = share;
@@ -636,7 +631,7 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs
         const int64_t first = u - begin;
         const int w0 = (int)(first / length);
         if (w0 == w - 1 && threadIdx.x == 0)
-          side.notes[w] = Note{w0, (int)((first + work.blocks - 1) / length), work.seq.row0, work.rows, segment % work.tiles * ROWS, segment / work.tiles, {0, 0}};
+          side.notes[w] = Note{w0, (int)((first + work.blocks - 1) / length), work.seq.row0, work.rows, segment % work.tiles * ROWS, segment / work.tiles};
       }
       piece(work, s0 + at, segment / work.tiles, segment % work.tiles, begin, stop, begin == 0 && stop == work.blocks, again);
       again = true;
@@ -649,18 +644,18 @@ __device__ __forceinline__ void walk_share(const AttendArgs& a, const AttendArgs
 // Where the sums of a share's piece go: slot 0 of a segment that began before the share, slot 1 of one that goes on after it.
 __device__ __forceinline__ float* part_at(const AttendArgs::Side& side, int w, int begin, int floats) { return side.parts + (2 * (int64_t)w + (begin == 0)) * floats; }
 
-template <typename Code, int NI, int ROWS, int WAVES>
+template <typename Code, int NI, int ROWS>
 __device__ __forceinline__ void run_share(const AttendArgs& a, int w, float* shared, int (*numbers)[64]) {
   walk_share<ROWS>(a, a.few, w, numbers, [&](const Work& work, int s, int head, int tile, int begin, int stop, bool whole, bool again) {
     const int page = Blocks::page_of(a, a.batch.row(s), begin + (int)(threadIdx.x >> 6), WAVES, threadIdx.x & 63);
-    run_piece<Code, NI, ROWS, WAVES>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.few, w, begin, part_floats(ROWS, NI * 32)), shared, again, page);
+    run_piece<Code, NI, ROWS>(a, work, s, head, tile, begin, stop, whole ? nullptr : part_at(a.few, w, begin, part_floats(ROWS, NI * 32)), shared, again, page);
   });
 }
 template <typename Code, int NI, int ROWS>
 __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
-  __shared__ float shared[Meeting<NI, ROWS, 4>::FLOATS];
+  __shared__ float shared[Meeting<NI, ROWS>::FLOATS];
   __shared__ int numbers[4][3][64];
-  run_share<Code, NI, ROWS, 4>(a, blockIdx.x, shared, numbers[threadIdx.x >> 6]);
+  run_share<Code, NI, ROWS>(a, blockIdx.x, shared, numbers[threadIdx.x >> 6]);
 }
 
 // --- many rows ------------------------------------------------------------------------------------------------------------------------------
@@ -845,13 +840,13 @@ __device__ __forceinline__ void run_tile(const AttendArgs& a, const Work& work, 
 // cache; last tiles, which see most, first.  FEW: the first workgroups deal with the sequences of few rows.
 template <typename Code, int NI, bool SHARED, bool FEW>
 __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendArgs a) {
-  constexpr int FLOATS = Meeting<NI, 16, 4>::FLOATS, BYTES = 2 * Staged<NI>::BYTES;
+  constexpr int FLOATS = Meeting<NI, 16>::FLOATS, BYTES = 2 * Staged<NI>::BYTES;
   __shared__ __attribute__((aligned(16))) char shared[FEW && FLOATS * 4 > BYTES ? FLOATS * 4 : BYTES];
   __shared__ int numbers[SHARED || FEW ? 4 : 1][3][64];
   int w = blockIdx.x;
   if constexpr (FEW) {
     if (w < a.few.workgroups) {
-      run_share<Code, NI, 16, 4>(a, w, reinterpret_cast<float*>(shared), numbers[threadIdx.x >> 6]);
+      run_share<Code, NI, 16>(a, w, reinterpret_cast<float*>(shared), numbers[threadIdx.x >> 6]);
       return;
     }
     w -= a.few.workgroups;
@@ -957,7 +952,7 @@ static bool desc_ok(const tmac_attn_desc* d, const tmac_pages* p) {
 // How the sequences of few and of many rows are dealt with.
 struct Side {
   bool on, whole;  // whole: every segment by a workgroup of its own, nothing to join
-  int rows, waves, workgroups, least, spare, tiles, rows_from, rows_to;
+  int rows, workgroups, least, spare, tiles, rows_from, rows_to;
   size_t notes, parts;  // bytes
   size_t bytes() const { return notes + parts; }
   void share(const tmac_pages* p) {
@@ -984,7 +979,7 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
   many.on = most > EXACT_ROWS;
   few.on = !many.on || (b->S > 1 && G <= 16);
   if (few.on) {
-    few.rows = most > 16 && !many.on ? 32 : 16, few.waves = 4;
+    few.rows = most > 16 && !many.on ? 32 : 16;
     few.rows_from = 1, few.rows_to = few.rows == 32 ? EXACT_ROWS : 16;
     few.tiles = few.rows == 32 ? (int)((most + 31) / 32) : 1;
     const int64_t segments = heads * few.tiles;
@@ -1001,7 +996,7 @@ static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pag
     }
   }
   if (many.on) {
-    many.rows = TILE, many.waves = 4;
+    many.rows = TILE;
     many.rows_from = few.on ? 17 : 1, many.rows_to = 0x7fffffff;
     const int64_t slots = (int64_t)b->T * G / TILE + b->S, least = std::max<int64_t>(0, ((int64_t)b->T * G - (few.on ? 16 * (int64_t)b->S : 0)) / TILE) * p->Hkv;
     // A workgroup a tile where there are nearly two a CU, or few stages; else shares of all stages (344 tiles of up to 40 stages: 66 in shares, 76 whole;
@@ -1024,8 +1019,8 @@ static const void* attend_of(const Plan& x) {
     return x.few.on ? (const void*)attend_tiles_kernel<Code, NI, true, true> : (const void*)attend_tiles_kernel<Code, NI, true, false>;
   }
   if (x.few.whole) {
-    if (x.few.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32, 4>;
-    return (const void*)attend_whole_kernel<Code, NI, 16, 4>;
+    if (x.few.rows == 32) return (const void*)attend_whole_kernel<Code, NI, 32>;
+    return (const void*)attend_whole_kernel<Code, NI, 16>;
   }
   return x.few.rows == 16 ? (const void*)attend_kernel<Code, NI, 16> : (const void*)attend_kernel<Code, NI, 32>;
 }
@@ -1062,11 +1057,11 @@ extern "C" tmac_status tmac_pages_attend(const tmac_attn_desc* desc, const tmac_
   a.q_token = q->token * 2, a.q_head = q->head * 2, a.out_token = out->token * 2, a.out_head = out->head * 2;
   a.lse = lse_dev;
   a.c = desc->scale * 1.44269504088896340736f;
-  a.Hq = desc->Hq, a.G = desc->Hq / desc->Hkv, a.bf16 = desc->elem == TMAC_ELEM_BF16;
+  a.G = desc->Hq / desc->Hkv, a.bf16 = desc->elem == TMAC_ELEM_BF16;
   char* const workspace = static_cast<char*>(workspace_dev);
   a.few = plan.few.args(workspace), a.many = plan.many.args(workspace + plan.few.bytes());
   const int ni = (p->D + 31) / 32, workgroups = (plan.few.on ? plan.few.workgroups : 0) + (plan.many.on ? plan.many.workgroups : 0);
-  const tmac_status st = launch(p->code == TMAC_CODE_I8 ? attend_of<I8>(ni, plan) : attend_of<E4M3>(ni, plan), workgroups, 64 * (plan.few.on ? plan.few.waves : 4), &a, stream);
+  const tmac_status st = launch(p->code == TMAC_CODE_I8 ? attend_of<I8>(ni, plan) : attend_of<E4M3>(ni, plan), workgroups, 64 * WAVES, &a, stream);
   if (st != TMAC_OK || need == 0) return st;
   int few_rows = plan.few.rows, few_borders = plan.few.on && !plan.few.whole ? plan.few.workgroups - 1 : 0;
   const int many_borders = plan.many.on && !plan.many.whole ? plan.many.workgroups - 1 : 0;
