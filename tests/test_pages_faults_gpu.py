@@ -151,3 +151,124 @@ def test_exponentials_of_few_rows_are_two_numbers(n, Hq, width, code, dtype):
             close(out[rows, h], ref, b + R.rounding(ref.abs() + b, dtype), f"sequence {s}")
             seen += 1
     assert seen
+
+
+# --- long caches, many sequences -----------------------------------------------------------------------------------------------------------------
+
+
+class Gathered(R.Held):
+    """What a cache holds, looked up for all tokens at once."""
+
+    def __init__(self, cache):
+        held = R.decoded(cache)
+        super().__init__(held.code, held.page, held.pages, held.D)
+        blocks = held.page // 32
+        order = [[(p, b, h, w) for p in range(held.pages) for h in range(cache.Hkv) for b in range(blocks)] for w in (0, 1)]
+        self.all = [torch.stack([held.blocks[at][0] for at in keys]).double().view(held.pages, cache.Hkv, blocks, 32, held.D) for keys in order]
+        self.scale = [torch.stack([held.blocks[at][1] for at in keys]).double().view(held.pages, cache.Hkv, blocks) for keys in order]
+
+    def values(self, table, n, h, which):
+        t = torch.arange(n)
+        page, part = table.long()[t // self.page], t % self.page // 32
+        return self.all[which][page, h, part, t % 32], self.scale[which][page, h, part], torch.ones(n, dtype=torch.bool)
+
+
+def plan(cache, n, lens, width, most):
+    """How the library deals a call out: (few, many), each None, "whole", or the units of a share (blocks of 32 tokens, stages of 64), held against the workspace it asks for."""
+    from paper_2407_00088_amd import pages as G
+    S, T, Hkv, group, W = len(n), sum(n), cache.Hkv, cache.Hq // cache.Hkv, (cache.D + 31) // 32 * 32
+    rows, blocks = min(most or T, T) * group, width * cache.page // 32
+    is_many = rows > 64
+    is_few = not is_many or (S > 1 and group <= 16)
+    tile = 32 if rows > 16 and not is_many else 16
+    tiles = -(-rows // 32) if tile == 32 else 1
+    few = many = None
+    need = 0
+    if is_few:
+        few = "whole"
+        if is_many or blocks > (48 if S * Hkv * tiles < 256 else 128):
+            mine = [(x, m) for x, m in zip(n, lens) if 0 < x * group <= (tile if tile == 16 else 64)]
+            few = max(8, -(-sum(Hkv * -(-x * group // tile) * (max(1, -(-m // 32)) + 16) for x, m in mine) // 256))
+            need += 256 * (24 + 2 * tile * (W + 2) * 4)
+    if is_many:
+        least = (T * group - (16 * S if is_few else 0)) // 128 * Hkv
+        many = "whole"
+        if least < 448 and blocks > 32:
+            mine = [(x, m) for x, m in zip(n, lens) if x * group > (16 if is_few else 0)]
+            many = max(4, -(-sum(Hkv * -(-x * group // 128) * (max(1, -(-m // 64)) + 2) for x, m in mine) // 512))
+            need += 512 * (24 + 2 * 128 * (W + 2) * 4)
+    batch = G.tmac_pages_batch(1 << 20, width, 1 << 20, 1 << 20, S, width, T, most or 0)
+    assert G.lib.tmac_pages_attend_workspace_bytes(cache.desc, cache.cache, batch) == need
+    return few, many
+
+
+def attended(cache, table, lens, n, q, most=None):
+    """Against 64 bits, and the same bits again on workspaces that hold something."""
+    cu = starts(n)
+    call = lambda: cache.attend(q.cuda(), table.cuda(), ints(lens), cu.cuda(), most=most)  # noqa: E731
+    out, lse = call()
+    ref = R.attend(q, Gathered(cache), table, lens, cu, 1 / math.sqrt(cache.D), cache.Hkv)
+    close(out, ref[0], ref[2], "out")
+    close(lse, ref[1], ref[3], "lse")
+    cache.attend_ws.fill_(0xFF)
+    for a, b in zip((out, lse), call()):
+        assert torch.equal(a, b)
+
+
+def filled(seed, lens, Hkv, D, page, code, dtype, Hq, width):
+    g = gen(seed)
+    held = [-(-m // page) for m in lens]
+    cache = P().PagedCache(sum(held), Hkv, D, page=page, code=code, dtype=dtype, Hq=Hq)
+    order, table = torch.randperm(sum(held), generator=g).int(), torch.full((len(lens), width), -1, dtype=torch.int32)
+    for s, m in enumerate(held):
+        table[s, :m] = order[sum(held[:s]):sum(held[:s]) + m]
+    k, v = (torch.randn((sum(lens), Hkv, D), generator=g) for _ in range(2))
+    v += torch.randn((1, Hkv, D), generator=g)
+    cache.append(k.to(dtype).cuda(), v.to(dtype).cuda(), table.cuda(), ints(lens), starts(lens).cuda())
+    return cache, table, g
+
+
+@pytest.mark.parametrize("code,dtype", [("i8", F16), ("e4m3", BF16)])
+@pytest.mark.parametrize("T,Hq,Hkv,length", [(512, 112, 1, 4500), (64, 880, 11, 4096)], ids=["whole tiles", "shares"])
+def test_tiles_of_128_rows_over_more_stages_than_they_have_places_of(T, Hq, Hkv, length, code, dtype):
+    """Pieces of more than 32 stages of 64 tokens: pages and scales are looked up 32 stages at a time."""
+    cache, table, g = filled(31, [length], Hkv, 32, 32, code, dtype, Hq, 150)
+    few, many = plan(cache, [T], [length], 150, None)
+    assert few is None and (many == "whole" if Hkv == 1 else many > 33)
+    attended(cache, table, [length], [T], (torch.randn((T, Hq, 32), generator=g) * 1.5).to(dtype))
+
+
+@pytest.mark.parametrize("code,dtype", [("i8", BF16), ("e4m3", F16)])
+@pytest.mark.parametrize("n,G", [(1, 2), (20, 1)], ids=["16 rows", "32 rows"])
+def test_shares_of_more_blocks_than_they_have_places_of(n, G, code, dtype):
+    """Pieces of more than 256 blocks, 64 for each of four wavefronts: sequences of 81920 tokens, whose tables name some pages again and again."""
+    S, Hkv, width = 4, 8, 20
+    cache, table, g = filled(32, [4096 * 3], Hkv, 4, 4096, code, dtype, Hkv * G, 3)
+    table = torch.randint(0, 3, (S, width), generator=g).int()
+    lens = [4096 * width - 45 * s for s in range(S)]
+    few, many = plan(cache, [n] * S, lens, width, n)
+    assert many is None and few > 256 + 16
+    attended(cache, table, lens, [n] * S, (torch.randn((S * n, Hkv * G, 4), generator=g) * 2).to(dtype), most=n)
+
+
+@pytest.mark.parametrize("code,dtype", [("i8", F16), ("e4m3", BF16)])
+@pytest.mark.parametrize("long", [0, 100], ids=["alone", "beside many rows"])
+def test_shares_of_several_short_sequences(long, code, dtype):
+    """A share has whole sequences and pieces of others: sums meet in the same memory one after the other."""
+    n = [1 + i % 4 if i % 7 else 0 for i in range(600)] + [long] * (long > 0)
+    lens = [(i * 37) % 90 + 4 for i in range(600)] + [700] * (long > 0)
+    cache, table, g = filled(33, lens, 1, 16, 32, code, dtype, 4, 200)
+    few, many = plan(cache, n, lens, 200, max(n))
+    assert few >= 35 and (many is None) == (not long)      # (a sequence has 17 to 19 units)
+    attended(cache, table, lens, n, (torch.randn((sum(n), 4, 16), generator=g) * 1.5).to(dtype), most=max(n))
+
+
+@pytest.mark.parametrize("code,dtype", [("i8", BF16), ("e4m3", F16)])
+def test_shares_of_several_sequences_of_many_rows(code, dtype):
+    """The same for tiles of 128 rows."""
+    n = [70 - i % 3 for i in range(350)]
+    lens = [x + i % 50 for i, x in enumerate(n)]
+    cache, table, g = filled(34, lens, 3, 16, 32, code, dtype, 3, 40)
+    few, many = plan(cache, n, lens, 40, None)
+    assert few == 8 and many > 2 * 4
+    attended(cache, table, lens, n, (torch.randn((sum(n), 3, 16), generator=g) * 1.5).to(dtype))
