@@ -66,7 +66,7 @@ enum { TMAC_BLOCK_TOKENS = 32 };
  *               finds the operands of its matrix instructions side by side.)  Elements from D on are zero.
  *   scales_dev  fp32 [units][2]: of keys, of values (tmac_pages_scale_bytes)
  * What is in a page before its first token is written does not matter.
- *   D a multiple of 4, at most 128 */
+ *   D a multiple of 4, at most 128; at most 2^40 units (more, and D over 128: TMAC_EUNSUPPORTED, and 0 bytes) */
 typedef struct {
   void*   codes_dev;
   float*  scales_dev;

@@ -534,8 +534,9 @@ extern "C" tmac_status tmac_rotate(const tmac_rope* rope, const tmac_rope_item* 
   return launch(kernel, ((int64_t)T * a.slices + 3) / 4, 256, &a, stream);
 }
 
-extern "C" size_t tmac_pages_code_bytes(const tmac_pages* p) { return pages_ok(p) && p->D <= 128 ? (size_t)units_of(p) * chunks_of(p) * 1024 : 0; }
-extern "C" size_t tmac_pages_scale_bytes(const tmac_pages* p) { return pages_ok(p) && p->D <= 128 ? (size_t)units_of(p) * 8 : 0; }
+static bool sized(const tmac_pages* p) { return pages_ok(p) && p->D <= 128 && units_of(p) <= MOST_UNITS; }
+extern "C" size_t tmac_pages_code_bytes(const tmac_pages* p) { return sized(p) ? (size_t)units_of(p) * chunks_of(p) * 1024 : 0; }
+extern "C" size_t tmac_pages_scale_bytes(const tmac_pages* p) { return sized(p) ? (size_t)units_of(p) * 8 : 0; }
 
 extern "C" tmac_status tmac_pages_append(const tmac_pages* p, const tmac_pages_batch* batch, int32_t elem, const tmac_view* k, const tmac_view* v,
                                          const tmac_rope* rope, const int64_t* positions_dev, const tmac_view* q, const tmac_view* q_out, int32_t Hq,

@@ -38,7 +38,12 @@ inline bool pages_set(const tmac_pages* p) {
   return p->pages == 0 || (p->codes_dev && (reinterpret_cast<uintptr_t>(p->codes_dev) & 15) == 0 && p->scales_dev &&
                            (reinterpret_cast<uintptr_t>(p->scales_dev) & 7) == 0);
 }
-inline int64_t units_of(const tmac_pages* p) { return (int64_t)p->pages * p->Hkv * (p->page / BT); }
+constexpr int64_t MOST_UNITS = (int64_t)1 << 40;
+// (more than MOST_UNITS where there are: the product of all three may pass 64 bits)
+inline int64_t units_of(const tmac_pages* p) {
+  const int64_t heads = (int64_t)p->pages * p->Hkv;
+  return heads > MOST_UNITS ? heads : heads * (p->page / BT);
+}
 inline int chunks_of(const tmac_pages* p) { return (p->D + 15) / 16; }
 
 inline bool batch_ok(const tmac_pages_batch* b) {
@@ -47,7 +52,7 @@ inline bool batch_ok(const tmac_pages_batch* b) {
 inline bool batch_set(const tmac_pages_batch* b) { return (b->table_dev || b->width == 0) && b->lens_dev; }
 inline bool supported(const tmac_pages* p, const tmac_pages_batch* b) {
   return p->D <= 128 && !attn::long_axis(b->S) && !attn::long_axis(b->T) && !attn::long_axis((int64_t)b->width * p->page) &&
-         units_of(p) <= ((int64_t)1 << 40);
+         units_of(p) <= MOST_UNITS;
 }
 
 inline Pages view_of(const tmac_pages* p) {

@@ -3,6 +3,8 @@ import pytest
 import torch
 
 import paper_2407_00088_amd as T
+from paper_2407_00088_amd import pages as G
+from test_pages_host import append, attend, batch, desc, pages, read
 
 
 def test_a_rotation_is_not_taken_apart():
@@ -36,3 +38,14 @@ def test_a_cache_is_not_taken_apart():
     assert T.PagedCache(0, 2, 64, device="cpu").codes.numel() == 0
     with pytest.raises(ValueError, match="GPU"):        # (pages none, which have no address)
         T.PagedCache(0, 2, 64, device="cpu").read(table, lens)
+
+
+def test_more_pages_than_can_be_counted_are_refused():
+    """pages * key heads * blocks of a page beyond 2^63: the number of units came out small, and so did the bytes that a caller is told to keep."""
+    most = (1 << 31) - 1
+    for p, d in ((pages(pages=most, Hkv=most, page=4096), desc(Hkv=most, Hq=most)), (pages(pages=1 << 30, Hkv=1 << 27, page=4096), desc(Hkv=1 << 27, Hq=1 << 27)),
+                 (pages(pages=1 << 30, Hkv=1 << 10, page=4096), desc(Hkv=1 << 10, Hq=1 << 10))):
+        assert G.lib.tmac_pages_code_bytes(p) == G.lib.tmac_pages_scale_bytes(p) == G.lib.tmac_pages_attend_workspace_bytes(d, p, batch()) == 0
+        assert append(p) == read(p) == attend(d, p) == T.TMAC_EUNSUPPORTED
+    p = pages(pages=1 << 30, Hkv=8, page=4096)
+    assert G.lib.tmac_pages_code_bytes(p) == (1 << 40) * 4096 and G.lib.tmac_pages_scale_bytes(p) == (1 << 40) * 8
