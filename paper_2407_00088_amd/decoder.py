@@ -95,7 +95,7 @@ class PagedDecoderAttention:
 
     def forward(self, x, counts):
         """counts[s] more tokens of every sequence (a prompt, a chunk of it, drafts, one token, none), packed: x [T, M] (fp16).  Returns [T, M]."""
-        if x.shape[0] != sum(counts) or len(counts) != self.table.batch:
+        if x.shape[0] != sum(counts) or len(counts) != self.table.batch or min(counts) < 0:
             raise ValueError(f"{x.shape[0]} rows for {sum(counts)} tokens of {self.table.batch} sequences: {list(counts)}")
         if not x.shape[0]:
             return x.new_empty((0, self.o.M), dtype=torch.float16)

@@ -49,3 +49,11 @@ def test_more_pages_than_can_be_counted_are_refused():
         assert append(p) == read(p) == attend(d, p) == T.TMAC_EUNSUPPORTED
     p = pages(pages=1 << 30, Hkv=8, page=4096)
     assert G.lib.tmac_pages_code_bytes(p) == (1 << 40) * 4096 and G.lib.tmac_pages_scale_bytes(p) == (1 << 40) * 8
+
+
+def test_a_layer_refuses_counts_below_zero_of_a_call_without_rows():
+    from paper_2407_00088_amd.decoder import PagedDecoderAttention
+    layer = object.__new__(PagedDecoderAttention)      # (refused before anything on the GPU is looked at)
+    layer.table = T.PageTable(2, 2, 4, device="cpu")
+    with pytest.raises(ValueError, match="rows"):
+        layer.forward(torch.zeros((0, 64), dtype=torch.float16), [1, -1])
