@@ -662,7 +662,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendArgs a) {
 //
 // 128 rows a workgroup, 32 a wavefront: stages of 64 tokens are brought to fp16 once for all four, on their way from registers to LDS, two
 // stages there: one is multiplied while the next is made and the one after that is on its way from memory.  Bound by products and exponentials that mostly take
-// turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 295 us, 0.87 PFLOP/s; matrix units 39 % busy, vector ALUs 55 %, LDS without conflicts, 2.0
+// turns (1024 rows after 7168 tokens, 64 heads in groups of 8: 293 to 312 us by the machine, 0.82 to 0.88 PFLOP/s; matrix units 37 % busy, vector ALUs 54 %, LDS without conflicts, 2.0
 // of 2.4 GHz; codes to fp16 are about a fifth of the vector instructions).
 //
 // Exponentials are one fp16 number each here, as in the prompts' attention (off by 2^-11 of themselves, the size of the result's own rounding; two for all rows: 400 us).  Sequences of up to
@@ -967,7 +967,7 @@ struct Plan {
   Side few, many;
 };
 // By the rows that a sequence and key head may have at most, the blocks that its table has room for, and the number of segments; what lengths there are is not
-// known here.  (us of one launch and its joining one.)
+// known here (one sequence of 300 tokens and 32 key heads: 6 where the table has room for 1536 tokens, in shares 10 to 11 where it has more).  (us of one launch and its joining one.)
 static Plan plan_of(const tmac_attn_desc* d, const tmac_pages* p, const tmac_pages_batch* b) {
   Plan plan = {};
   Side &few = plan.few, &many = plan.many;

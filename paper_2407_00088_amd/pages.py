@@ -353,7 +353,8 @@ class PageTable:
 
       table  int32 [batch, width]  pages of each sequence, -1 behind them       lens  int32 [batch]
 
-    The tensors keep their place (a captured graph that was given them sees what extend() and the others put there since).
+    The tensors keep their place (a captured graph that was given them sees what extend() and the others put there since).  These copy from the host and wait for the
+    GPU's stream: a step that is captured has them outside.
     """
 
     def __init__(self, batch: int, width: int, pages: int, page: int = 64, device: str = "cuda"):
